@@ -51,8 +51,10 @@ enum {
     RFSF_E_HIP = -7,                /* a HIP runtime call or kernel launch failed         */
     RFSF_E_BAD_TABLE = -8,          /* hash outside [0, D) or sign not +-1 (validate)     */
     RFSF_E_UNSUPPORTED = -9,        /* valid but outside what the kernels cover           */
-    RFSF_E_STATIC_SCRATCH_TOO_SMALL = -10 /* rfsf_ts_features_static: one sequence needs  */
+    RFSF_E_STATIC_SCRATCH_TOO_SMALL = -10, /* rfsf_ts_features_static: one sequence needs */
                                     /* more than the built-in scratch                     */
+    RFSF_E_BAD_SETTING = -11        /* a setting of the optimizer is not finite or out of */
+                                    /* its range                                          */
 };
 
 typedef struct {
@@ -256,6 +258,98 @@ int rfsf_trp_workspace_bytes(const rfsf_ts_shape *shape, size_t *recommended_byt
 int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W, const float *Z,
                       float lengthscale, float *out, void *workspace, size_t workspace_bytes,
                       void *hip_stream);
+
+/*
+ * Linear models on feature rows: a softmax classifier's loss with its gradients, the optimizer's step on its weights, and
+ * answers from rows held in 8-bit integers. (The paper hands its features to linear models of other packages, Sec. 3.6 and the
+ * appendix classes PrecomputedFeatureLinSVC; these are the pieces of one that stays on the GPU.) The general rules above hold;
+ * the optional timing record below has no entries for these calls.
+ */
+
+/*
+ * Softmax cross entropy of linear scores over C classes, with its gradients:
+ *   l[n, c]  = sum_k Phi[n, k] W[c, k]                (column 0 of features is constant: W[c, 0] is the class's offset)
+ *   loss[n]  = log sum_c exp l[n, c] - l[n, labels[n]]
+ *   G[n, c]  = s_n (exp(l[n, c]) / sum_c' exp l[n, c'] - [c = labels[n]])
+ *   dPhi     = G W,    dW = G^T Phi                    (gradients of sum_n s_n loss[n])
+ * with s_n = weight[n], or 1 / (number of rows that count) if weight is NULL.
+ *   Phi [N, ld_phi], W [C, ld_w], dPhi [N, ld_dphi], dW [C, ld_dw]   row-major, float32, or all four bfloat16 (bf16 != 0)
+ *   labels [N] int64 on the device. A negative label leaves its row out: loss 0, gradients 0, whatever Phi and weight hold
+ *          there. Labels >= C give NaN (they are not used as addresses).
+ *   weight [N] float32 or NULL; loss [N] float32
+ *   dPhi, dW: read only if RFSF_XENT_DPHI, RFSF_XENT_DW are set in `gradients`; columns beyond K are untouched
+ * The scores are never held whole: without gradients they stay in registers, with gradients the workspace holds them for a part of
+ * the rows. A smaller workspace means more parts.
+ * Accuracy: float32 operands enter the products with 22 significand bits down to 2^-17 of the largest number of their row, and with an
+ * error below 2^-38 of it beyond; bfloat16 operands enter whole down to 2^-30 of it. G enters the gradients' products with 22 bits (11
+ * with bfloat16 operands), or with an error of 2^-38 of the largest product that it takes part in: of the largest |G[n, c]| max_k |W[c, k]| of
+ * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. Sums are held in 32 bits. A row of Phi
+ * or W that holds an infinity or a NaN makes what is computed from it NaN (bfloat16: or what infinities give). Equal calls with workspaces
+ * of equal sizes give equal bits.
+ * Limits: K, C <= 4000000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW.
+ */
+enum { RFSF_XENT_DPHI = 1, RFSF_XENT_DW = 2 };
+typedef struct {
+    int64_t N, K, C;
+    int64_t ld_phi, ld_w, ld_dphi, ld_dw;    /* row strides in numbers, >= K; those of gradients not asked for are not looked at */
+    int32_t bf16;                            /* type of Phi, W, dPhi, dW: 0 float32, 1 bfloat16 */
+    int32_t gradients;                       /* RFSF_XENT_DPHI | RFSF_XENT_DW */
+} rfsf_xent_shape;
+int rfsf_softmax_xent_workspace_bytes(const rfsf_xent_shape *shape, size_t *recommended_bytes, size_t *minimum_bytes);
+int rfsf_softmax_xent(const rfsf_xent_shape *shape, const void *Phi, const void *W, const int64_t *labels, const float *weight,
+                      float *loss, void *dPhi, void *dW, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * One AdamW step of `count` tensors, in as few launches as their descriptions need (40 tensors each):
+ *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   param = param (1 - lr weight_decay) - (lr / (1 - beta1^step)) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in float32, each operation rounded by itself. step counts from 1.
+ *   state_bits 32: m, v are float32 [n].
+ *   state_bits 8: 256 consecutive numbers share a scale, the largest magnitude among them (m_scale, v_scale: float32
+ *     [ceil(n / 256)]). m is int8, a code c standing for scale * u|u| with u = c / 127; v is uint8, c standing for scale * u^4 with u = c / 255.
+ *     The step uses m and v before they are rounded to the nearest code; a v above zero never becomes code 0. All zero is a fresh
+ *     state. A block that meets an infinity or a NaN gets the scale NaN.
+ *   copy: bfloat16 [n] that receives the new param, rounded, or NULL.
+ * The array and its tensors' addresses are read during the call only. Tensors must not overlap. Addresses aligned to four numbers
+ * are fastest; any that fit their type are right.
+ * rfsf_adamw_moments writes the numbers that 8-bit states stand for: m_out[k], v_out[k] float32 [n]; param, grad, copy are not looked at.
+ */
+typedef struct {
+    void *param;                /* float32 [n], updated */
+    const void *grad;           /* float32 or bfloat16 [n] */
+    void *m, *v;                /* updated */
+    float *m_scale, *v_scale;   /* 8-bit states only */
+    void *copy;
+    int64_t n;                  /* >= 0 */
+} rfsf_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;  /* finite; 0 <= beta < 1, eps, lr, weight_decay >= 0 */
+    int64_t step;               /* >= 1 */
+    int32_t state_bits;         /* 8 or 32 */
+    int32_t grad_bf16;
+} rfsf_adamw_config;
+int rfsf_adamw_step(const rfsf_adamw_tensor *tensors, int64_t count, const rfsf_adamw_config *config, void *hip_stream);
+int rfsf_adamw_moments(const rfsf_adamw_tensor *tensors, int64_t count, float *const *m_out, float *const *v_out, void *hip_stream);
+
+/*
+ * Feature rows as 8-bit integers: codes[n, k] = round(X[n, k] (127 (1 / largest))), ties to even, and scales[n] = largest (1 / 127), with the
+ * row's largest magnitude, every operation rounded to float32; rows with nothing above 2^-119 get zeros. X [N, ldx] float32 or bfloat16. codes [N, ld_codes] bytes, rows a multiple of 16
+ * bytes apart, from a multiple of 16 on, with room for K rounded up to 128: what lies beyond K up to there is zeroed.
+ * A row with an infinity or a NaN gets the scale NaN.
+ */
+int rfsf_int8_quantize(const void *X, int32_t bf16, int64_t N, int64_t ldx, int64_t K, int8_t *codes, int64_t ld_codes, float *scales,
+                       void *hip_stream);
+
+/*
+ * rfsf_ts_gram against rows held in 8-bit integers (stored training features, or a classifier's weights):
+ *   out[i, j] = s_i scales[j] sum_k q[i, k] codes[j, k]
+ * where q, s are the codes and scales of X's rows, which are quantised on the way. The sums are exact.
+ *   X [Nx, ldx] float32 or bfloat16; codes [Ny, ld_codes] as rfsf_int8_quantize lays them out (all ld_codes bytes of every row exist and may be
+ *   read); out [Nx, ld_out] float32. Limits: K <= 131072, Ny <= 10^8. Nx = 0 or Ny = 0 is a no-op.
+ */
+int rfsf_int8_gram_workspace_bytes(int64_t Nx, int64_t Ny, int64_t K, size_t *recommended_bytes, size_t *minimum_bytes);
+int rfsf_int8_gram(const void *X, int32_t bf16, int64_t Nx, int64_t ldx, const int8_t *codes, const float *scales, int64_t Ny,
+                   int64_t ld_codes, int64_t K, float *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Optional per-kernel timing for benchmarks (not part of the method). While enabled, every

@@ -89,6 +89,21 @@ def load_library():
     lib.rfsf_ts_probe_peaks.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.POINTER(_Peaks), ctypes.c_void_p]
     lib.rfsf_ts_profile_read.restype = ctypes.c_int
     lib.rfsf_ts_profile_read.argtypes = [ctypes.POINTER(_Profile), ctypes.c_int]
+    pt = ctypes.POINTER
+    lib.rfsf_softmax_xent_workspace_bytes.restype = ctypes.c_int
+    lib.rfsf_softmax_xent_workspace_bytes.argtypes = [vp, pt(sz), pt(sz)]
+    lib.rfsf_softmax_xent.restype = ctypes.c_int
+    lib.rfsf_softmax_xent.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rfsf_adamw_step.restype = ctypes.c_int
+    lib.rfsf_adamw_step.argtypes = [vp, i64, vp, vp]
+    lib.rfsf_adamw_moments.restype = ctypes.c_int
+    lib.rfsf_adamw_moments.argtypes = [vp, i64, vp, vp, vp]
+    lib.rfsf_int8_quantize.restype = ctypes.c_int
+    lib.rfsf_int8_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+    lib.rfsf_int8_gram_workspace_bytes.restype = ctypes.c_int
+    lib.rfsf_int8_gram_workspace_bytes.argtypes = [i64, i64, i64, pt(sz), pt(sz)]
+    lib.rfsf_int8_gram.restype = ctypes.c_int
+    lib.rfsf_int8_gram.argtypes = [vp, i32, i64, i64, vp, vp, i64, i64, i64, vp, i64, vp, sz, vp]
     _lib = lib
     return lib
 

@@ -7,6 +7,8 @@
 
 #include <atomic>
 
+#include "../../include/rfsf_ts.h"
+
 namespace rfsf {
 
 constexpr size_t kLdsPerCu = 160 * 1024;
@@ -143,6 +145,20 @@ hipError_t launch_trp_scan(float *P, int64_t N, int64_t n_seq, int64_t L, int64_
                            hipStream_t stream);
 
 hipError_t launch_normalize(float *Phi, int64_t N, int64_t ld, int M, int D, hipStream_t stream);
+
+// Linear models on features (csrc/softmax_xent.hip, adamw.hip, int8_gram.hip); arguments are checked by csrc/linear_api.hip.
+void softmax_xent_bytes(const rfsf_xent_shape &shape, size_t *recommended, size_t *minimum);
+hipError_t launch_softmax_xent(const rfsf_xent_shape &shape, const void *Phi, const void *W, const int64_t *labels, const float *weight, float *loss,
+                               void *dPhi, void *dW, void *workspace, size_t bytes, hipStream_t stream);
+hipError_t launch_adamw(const rfsf_adamw_tensor *tensors, int64_t count, const rfsf_adamw_config &c, double correction1, double correction2,
+                        hipStream_t stream);
+hipError_t launch_adamw_moments(const rfsf_adamw_tensor *tensors, int64_t count, float *const *m_out, float *const *v_out, hipStream_t stream);
+hipError_t launch_clear_rows(void *rows, int64_t count, int64_t columns, int64_t ld, bool bf16, hipStream_t stream);
+hipError_t launch_int8_quantize(const void *X, bool bf16, int64_t N, int64_t ld, int64_t K, int8_t *codes, int64_t ld_codes, float *scales,
+                                hipStream_t stream);
+void int8_gram_bytes(int64_t Nx, int64_t K, size_t *recommended, size_t *minimum);
+hipError_t launch_int8_gram(const void *X, bool bf16, int64_t Nx, int64_t ldx, const int8_t *codes, const float *scales, int64_t Ny, int64_t ldy,
+                            int64_t K, float *out, int64_t ldk, void *workspace, size_t bytes, hipStream_t stream);
 
 // Benchmark helper (csrc/probe.hip): read, write, non-temporal write, copy GB/s over `scratch`, fp32 matrix and
 // fp32 vector TFLOP/s of issue loops, in this order; waits for the stream.

@@ -1,0 +1,503 @@
+// Softmax cross entropy of linear scores and its gradients (rfsf_softmax_xent):
+//   l[n, c] = sum_k Phi[n, k] W[c, k],   loss[n] = log sum_c exp l[n, c] - l[n, y_n],
+//   G[n, c] = s_n (exp l[n, c] / sum - [c = y_n]),   dPhi = G W,   dW = G^T Phi.
+//
+// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory. The operands are packed once for
+// the matrix instructions (plane_pack.h), W and Phi by rows for the scores, their transposes for the gradients, so that
+// all three products are of one kind (plane_product.h). The scores of a tile give their maximum and sum of exponentials per row before
+// they leave the registers; without gradients they are never written. For gradients the rows are taken in blocks, and the
+// scores of a block stay in the workspace from their product to the pass that turns them into G (both layouts), in as
+// few rows at a time as fill the GPU, so that the last-level cache holds them.
+#include "plane_pack.h"
+
+#include <algorithm>
+
+#include "../../include/rfsf_ts.h"
+
+namespace rfsf {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// Rows that count, of all blocks.
+__global__ __launch_bounds__(256) void count_kernel(const int64_t *labels, int64_t N, uint32_t *count)
+{
+    uint32_t mine = 0;
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < N; n += (int64_t)gridDim.x * 256) mine += labels[n] >= 0 ? 1 : 0;
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) mine += (uint32_t)__shfl_xor((int)mine, o);
+    if ((threadIdx.x & 63) == 0 && mine != 0) atomicAdd(count, mine);
+}
+__global__ void zero_kernel(uint32_t *p) { *p = 0; }
+
+template <typename T>
+__global__ __launch_bounds__(256) void clear_rows_kernel(T *rows, int64_t count, int64_t columns, int64_t ld)
+{
+    for (int64_t r = blockIdx.x; r < count; r += gridDim.x)
+        for (int64_t c = threadIdx.x; c < columns; c += 256) rows[r * ld + c] = 0;
+}
+
+// Of the scores of some classes: their maximum, the sum of exponentials from there, and the largest of score + exponent(the
+// class's weights) in powers of two, which bounds G[n, c] 2^exponent(W[c, :]).
+struct Partial { float top, sum, reach; };
+
+// Scores: classes along the tile's rows, sequences along its columns, so that a lane holds many classes of one sequence and
+// nearly all of the maximum and the sum is taken inside it.
+struct Scores {
+    const uint32_t *largest_w, *largest_phi;    // per class, per sequence of the block
+    int64_t C, rows;                            // classes; sequences of this launch
+    const int64_t *labels;                      // of its first sequence on
+    Partial *partial;                           // [class tiles][rows_ld]
+    int64_t rows_ld;
+    float *target;                              // the label's score
+    float *scores;                              // [rows][ld], or null
+    int64_t ld;
+
+    template <typename T>
+    __device__ __forceinline__ void operator()(T &t) const
+    {
+        constexpr int BM = T::BM, BN = T::BN;
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        float top[BN], sum[BN], reach[BN];
+        int shift_n[BN];
+        int64_t label[BN];
+#pragma unroll
+        for (int b = 0; b < BN; ++b) {
+            const int64_t n = t.j0 + 32 * b + col;
+            shift_n[b] = n < rows ? shift_of(largest_phi[n]) : 0;
+            label[b] = n < rows ? labels[n] : -1;
+            top[b] = reach[b] = -INFINITY;
+        }
+#pragma unroll
+        for (int a = 0; a < BM; ++a)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = t.i0 + 32 * a + 8 * q + 4 * half;
+                int shift[4];
+                float power[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t largest = i + e < C ? largest_w[i + e] : 0;
+                    shift[e] = shift_of(largest);
+                    power[e] = (float)exponent_of(largest);
+                }
+#pragma unroll
+                for (int b = 0; b < BN; ++b) {
+                    const int64_t n = t.j0 + 32 * b + col;
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = ldexpf(t.acc[a][b][4 * q + e], -(shift[e] + shift_n[b]));
+                        if (i + e == label[b]) target[n] = v[e];
+                        t.acc[a][b][4 * q + e] = i + e < C ? v[e] : -INFINITY;
+                        top[b] = fmaxf(top[b], t.acc[a][b][4 * q + e]);
+                        reach[b] = fmaxf(reach[b], fmaf(t.acc[a][b][4 * q + e], kLog2e, power[e]));
+                    }
+                    if (scores && n < rows && i < C)             // (ld is a multiple of four: numbers beyond C are nobody's)
+                        *reinterpret_cast<float4 *>(scores + n * ld + i) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < BN; ++b) {
+            top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
+            reach[b] = fmaxf(reach[b], __shfl_xor(reach[b], 32));
+            const float from = top[b] == -INFINITY ? 0.f : top[b];
+            float s = 0.f;
+#pragma unroll
+            for (int a = 0; a < BM; ++a)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += exp_of(t.acc[a][b][e] - from);
+            sum[b] = s + __shfl_xor(s, 32);
+        }
+        // the wavefronts that hold other classes of the same sequences
+        Partial *shared = reinterpret_cast<Partial *>(t.lds);
+        constexpr int WIDE = T::COLUMNS, ROWS = T::WAVES_I;
+        __syncthreads();
+        if (half == 0) {
+#pragma unroll
+            for (int b = 0; b < BN; ++b) shared[t.wave_i * WIDE + t.wave_j * (32 * BN) + 32 * b + col] = {top[b], sum[b], reach[b]};
+        }
+        __syncthreads();
+        const int64_t first = t.tile_j * WIDE;
+        for (int j = threadIdx.x; j < WIDE; j += blockDim.x) {
+            if (first + j >= rows) break;
+            Partial v = shared[j];
+#pragma unroll
+            for (int w = 1; w < ROWS; ++w) {
+                const Partial o = shared[w * WIDE + j];
+                const float m = fmaxf(v.top, o.top), from = m == -INFINITY ? 0.f : m;
+                v = {m, v.sum * exp_of(v.top - from) + o.sum * exp_of(o.top - from), fmaxf(v.reach, o.reach)};
+            }
+            partial[t.tile_i * rows_ld + first + j] = v;
+        }
+    }
+};
+
+// Joins the class tiles' parts: the loss, and for the gradients the maximum, 1 / sum, the row's scale and the exponent that bounds
+// G[n, c] 2^exponent(W[c, :]).
+struct __attribute__((aligned(16))) RowTerms { float top, inverse, scale; int32_t reach; };
+struct JoinJob {
+    const Partial *partial;
+    int64_t tiles, rows_ld, rows, C;
+    const int64_t *labels;
+    const float *weight;
+    const uint32_t *count, *largest_w;
+    const float *target;
+    float *loss;
+    RowTerms *terms;                // null without gradients
+};
+__global__ __launch_bounds__(256) void join_kernel(JoinJob job)
+{
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= job.rows) return;
+    float m = -INFINITY, reach = -INFINITY;
+    for (int64_t t = 0; t < job.tiles; ++t) {
+        const Partial v = job.partial[t * job.rows_ld + n];
+        m = fmaxf(m, v.top);
+        reach = fmaxf(reach, v.reach);
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+    for (int64_t t = 0; t < job.tiles; ++t) {
+        const Partial v = job.partial[t * job.rows_ld + n];
+        s += v.sum * exp_of(v.top - from);
+    }
+    const int64_t label = job.labels[n];
+    const bool known = label >= 0 && label < job.C;
+    job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (m - job.target[n]) : NAN;
+    if (!job.terms) return;
+    float bound = reach - fmaf(from, kLog2e, log2f(s));
+    if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
+    job.terms[n] = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : 1.0f / (float)*job.count,
+                    (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
+}
+
+// From the scores of `rows` sequences to G as operand, in tiles of 64 x 64. By rows, for the product with W^T, whose columns are scaled by
+// the classes' powers of two: (p - [c = y]) 2^exponent(W[c, :]), brought to 2^14 by the row's own exponent; the rows' scales
+// enter at the end of the product, so that rows of small scale lose nothing. Transposed, for the product with Phi^T: the same with
+// the rows' scales and exponents, brought to 2^14 by the largest of all.
+struct GradientJob {
+    const float *scores;
+    int64_t ld, rows, C;
+    const int64_t *labels;
+    const float *weight;
+    const RowStats *stats;
+    const RowTerms *terms;
+    const uint32_t *largest_w, *largest_phi;
+    char *by_row, *by_class;        // either may be null; by_class from the first sequence's column on
+    int64_t pitch_row, pitch_class;
+};
+template <bool TWO>
+__global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
+{
+    __shared__ float tile[64][65];
+    const int64_t c0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
+    const int at = threadIdx.x >> 3, group = threadIdx.x & 7;
+    const int shift = job.by_class ? kTopBit - ((int)job.stats->top - kTopBias) : 0;
+#pragma unroll
+    for (int u = 0; u < 64; u += 32) {
+        const int64_t n = n0 + at + u, c = c0 + 8 * group;
+        float g[8], scale = 0.f;
+        if (n < job.rows) {
+            const RowTerms t = job.terms[n];
+            const int64_t label = job.labels[n];
+            scale = ldexpf(job.weight ? t.scale : 1.0f, shift + exponent_of(job.largest_phi[n]));
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float4 f = c + 4 * q < job.C ? *reinterpret_cast<const float4 *>(job.scores + n * job.ld + c + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[4 * q] = f.x;
+                v[4 * q + 1] = f.y;
+                v[4 * q + 2] = f.z;
+                v[4 * q + 3] = f.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                g[e] = exp_of(v[e] - t.top) * t.inverse;
+                if (c + e == label) g[e] -= 1.0f;
+                if (label < 0 || c + e >= job.C) g[e] = 0.f;
+                else if (label >= job.C) g[e] = NAN;
+            }
+            if (job.by_row) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = c + e < job.C ? ldexpf(g[e], exponent_of(job.largest_w[c + e]) + kTopBit - t.reach) : 0.f;
+                plane::store_terms<TWO>(job.by_row + n * job.pitch_row, c, plane::terms_of<TWO>(x));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[at + u][8 * group + e] = g[e] == 0.f ? 0.f : g[e] * scale;
+    }
+    if (!job.by_class) return;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 64; u += 32) {
+        const int64_t c = c0 + at + u;
+        if (c >= job.C) continue;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = tile[8 * group + e][at + u];
+        plane::store_terms<TWO>(job.by_class + c * job.pitch_class, n0 + 8 * group, plane::terms_of<TWO>(x));
+    }
+}
+
+// A gradient: rows of the tile along the contiguous axis of the result.
+struct Gradient {
+    void *out;
+    int64_t ld, rows_i, cols_j;
+    bool bf16;                          // type of out
+    const RowTerms *terms;              // dPhi: the rows' scales and exponents. Null (dW):
+    const RowStats *stats;              // ... one exponent
+    const uint32_t *count;              // ... and, without weights (else null), one scale
+    const float *add;                   // [cols_j][add_ld] of the blocks before, or null
+    int64_t add_ld;
+
+    template <typename T>
+    __device__ __forceinline__ void operator()(T &t) const
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        const int all = terms ? 0 : (int)stats->top - kTopBias;
+        const float mean = count ? 1.0f / (float)max(*count, 1u) : 1.0f;
+#pragma unroll
+        for (int a = 0; a < T::BM; ++a)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = t.i0 + 32 * a + 8 * q + 4 * half;
+#pragma unroll
+                for (int b = 0; b < T::BN; ++b) {
+                    const int64_t j = t.j0 + 32 * b + col;
+                    if (j >= cols_j) continue;
+                    const float scale = terms ? terms[j].scale : mean;
+                    const int shift = (terms ? terms[j].reach : all) - 2 * kTopBit;
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = ldexpf(t.acc[a][b][4 * q + e], shift) * scale;
+                        if (add && i + e < rows_i) v[e] += add[j * add_ld + i + e];
+                    }
+                    store(j * ld + i, rows_i - i, v);
+                }
+            }
+    }
+    __device__ __forceinline__ void store(int64_t at, int64_t left, const float (&v)[4]) const
+    {
+        struct __attribute__((packed, aligned(4))) Float4u { float x, y, z, w; };
+        struct __attribute__((packed, aligned(2))) Bf16x4u { __bf16 x, y, z, w; };
+        if (bf16) {
+            __bf16 *dst = static_cast<__bf16 *>(out) + at;
+            if (left >= 4) {
+                *reinterpret_cast<Bf16x4u *>(dst) = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+            } else {
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) dst[e] = (__bf16)v[e];
+            }
+        } else {
+            float *dst = static_cast<float *>(out) + at;
+            if (left >= 4) {
+                *reinterpret_cast<Float4u *>(dst) = {v[0], v[1], v[2], v[3]};
+            } else {
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) dst[e] = v[e];
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// Workspace and order of work.
+constexpr int64_t kUnit = 64;                           // rows of a block are counted in these
+constexpr size_t kScoreBytes = (size_t)128 << 20;       // of scores in flight: half of the last-level cache
+constexpr size_t kBlockBytes = (size_t)8 << 30;         // recommended, of what grows with the rows of a block
+constexpr int64_t kMostBlockRows = 4000000 / kUnit * kUnit;
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+int64_t units(int64_t rows) { return (rows + kUnit - 1) / kUnit * kUnit; }
+
+struct Sizes {
+    bool two, d_phi, d_w;
+    int64_t N, K, C, ld_scores, class_tiles;
+    explicit Sizes(const rfsf_xent_shape &s)
+        : two(s.bf16 == 0), d_phi((s.gradients & RFSF_XENT_DPHI) != 0), d_w((s.gradients & RFSF_XENT_DW) != 0), N(s.N), K(s.K), C(s.C),
+          ld_scores((s.C + 3) / 4 * 4), class_tiles((s.C + kUnit - 1) / kUnit)
+    {
+    }
+    // of the call: W both ways, the magnitudes, the rows' statistics
+    size_t fixed() const
+    {
+        return up((size_t)C * plane_pitch(K, two)) + (d_phi ? up((size_t)K * plane_pitch(C, two)) : 0) + up(sizeof(RowStats)) + up(4) + up(4 * (size_t)C) + 256;
+    }
+    // of a block of `rows` rows (a multiple of kUnit)
+    size_t block(int64_t rows) const
+    {
+        size_t b = up((size_t)rows * plane_pitch(K, two)) + up(4 * (size_t)rows) + up(4 * (size_t)rows) + up(sizeof(RowTerms) * (size_t)rows) +
+                   up(sizeof(Partial) * (size_t)class_tiles * (size_t)rows);
+        if (d_phi) b += up((size_t)rows * plane_pitch(C, two));
+        if (d_w) b += up((size_t)C * plane_pitch(rows, two)) + up((size_t)K * plane_pitch(rows, two));
+        if (d_w && !two && rows < N) b += up(4 * (size_t)C * (size_t)K);        // sums of the blocks before
+        return b;
+    }
+    size_t scores(int64_t rows) const { return d_phi || d_w ? up(4 * (size_t)rows * (size_t)ld_scores) : 0; }
+    int64_t score_rows(int64_t rows) const
+    {
+        int64_t n = (int64_t)(kScoreBytes / (4 * (size_t)ld_scores)) / 256 * 256;
+        n = std::max<int64_t>(n, 256);
+        return std::min(n, rows);
+    }
+    int64_t recommended_rows() const
+    {
+        int64_t rows = std::min(units(std::max<int64_t>(N, 1)), kMostBlockRows);
+        while (rows > 4096 && block(rows) > kBlockBytes) rows = units(rows / 2);
+        return rows;
+    }
+};
+
+struct Plan { int64_t rows, score_rows; };
+// The largest blocks that the workspace holds.
+bool plan_of(const Sizes &z, size_t bytes, Plan *plan)
+{
+    if (bytes < z.fixed()) return false;
+    const size_t room = bytes - z.fixed();
+    int64_t rows = std::min(units(z.N), kMostBlockRows);
+    for (;; rows = units(rows / 2)) {
+        int64_t s = z.score_rows(rows);
+        for (;; s = units(s / 2)) {
+            if (z.block(rows) + z.scores(s) <= room) {
+                *plan = {rows, s};
+                return true;
+            }
+            if (s <= kUnit) break;
+        }
+        if (rows <= kUnit) return false;
+    }
+}
+
+struct Carve {
+    char *at;
+    template <typename T>
+    T *take(size_t bytes)
+    {
+        T *p = reinterpret_cast<T *>(at);
+        at += up(bytes);
+        return p;
+    }
+};
+
+}  // namespace
+
+void softmax_xent_bytes(const rfsf_xent_shape &shape, size_t *recommended, size_t *minimum)
+{
+    const Sizes z(shape);
+    const int64_t rows = z.recommended_rows();
+    *recommended = z.fixed() + z.block(rows) + z.scores(z.score_rows(rows));
+    const int64_t least = kUnit;
+    *minimum = z.fixed() + z.block(least) + z.scores(least);
+}
+
+hipError_t launch_clear_rows(void *rows, int64_t count, int64_t columns, int64_t ld, bool bf16, hipStream_t stream)
+{
+    const dim3 grid((unsigned)std::min<int64_t>(count, 65536));
+    if (bf16) clear_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<uint16_t *>(rows), count, columns, ld);
+    else clear_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<uint32_t *>(rows), count, columns, ld);
+    return hipGetLastError();
+}
+
+#define RFSF_TRY(call)                                   \
+    do {                                                 \
+        const hipError_t e_ = (call);                    \
+        if (e_ != hipSuccess) return e_;                 \
+    } while (0)
+
+template <PlaneMode MODE>
+hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void *W, const int64_t *labels, const float *weight, float *loss, void *dPhi,
+                       void *dW, void *workspace, size_t bytes, hipStream_t stream)
+{
+    const Sizes z(shape);
+    Plan plan;
+    if (!plan_of(z, bytes, &plan)) return hipErrorInvalidValue;
+    const bool bf16 = !z.two, gradients = z.d_phi || z.d_w;
+    const size_t element = bf16 ? 2 : 4;
+    const int64_t pitch_k = plane_pitch(z.K, z.two), pitch_c = plane_pitch(z.C, z.two), pitch_n = plane_pitch(plan.rows, z.two);
+    const int64_t N = z.N, K = z.K, C = z.C;
+
+    const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
+    Carve ws{static_cast<char *>(workspace) + (mis ? 256 - mis : 0)};
+    char *w_rows = ws.take<char>((size_t)C * pitch_k);
+    char *w_columns = z.d_phi ? ws.take<char>((size_t)K * pitch_c) : nullptr;
+    RowStats *stats = ws.take<RowStats>(sizeof(RowStats));
+    uint32_t *total = ws.take<uint32_t>(4);
+    uint32_t *largest_w = ws.take<uint32_t>(4 * (size_t)C);
+    uint32_t *largest_phi = ws.take<uint32_t>(4 * (size_t)plan.rows);
+    float *target = ws.take<float>(4 * (size_t)plan.rows);
+    RowTerms *terms = ws.take<RowTerms>(sizeof(RowTerms) * (size_t)plan.rows);
+    Partial *partial = ws.take<Partial>(sizeof(Partial) * (size_t)z.class_tiles * (size_t)plan.rows);
+    char *phi_rows = ws.take<char>((size_t)plan.rows * pitch_k);
+    char *g_rows = z.d_phi ? ws.take<char>((size_t)plan.rows * pitch_c) : nullptr;
+    char *g_classes = z.d_w ? ws.take<char>((size_t)C * pitch_n) : nullptr;
+    char *phi_columns = z.d_w ? ws.take<char>((size_t)K * pitch_n) : nullptr;
+    float *sums = z.d_w && bf16 && plan.rows < N ? ws.take<float>(4 * (size_t)C * (size_t)K) : nullptr;
+    float *scores = gradients ? ws.take<float>(4 * (size_t)plan.score_rows * (size_t)z.ld_scores) : nullptr;
+
+    // the scale of rows without weights is known from the rows' packing, unless they are packed in several blocks
+    const uint32_t *count = weight ? nullptr : plan.rows < N ? total : &stats->count;
+    if (gradients && count == total) {
+        zero_kernel<<<1, 1, 0, stream>>>(total);
+        count_kernel<<<dim3((unsigned)std::min<int64_t>((N + 1023) / 1024, 256)), dim3(256), 0, stream>>>(labels, N, total);
+        RFSF_TRY(hipGetLastError());
+    }
+    const PackJob pack_w = {W, C, K, shape.ld_w, nullptr, largest_w, w_rows, w_columns, pitch_k, pitch_c};
+    for (int64_t n0 = 0; n0 < N; n0 += plan.rows) {
+        const int64_t rows = std::min(plan.rows, N - n0);
+        const PackJob pack_phi = {static_cast<const char *>(Phi) + (size_t)n0 * shape.ld_phi * element, rows, K, shape.ld_phi, labels + n0, largest_phi,
+                                  phi_rows, phi_columns, pitch_k, pitch_n};
+        PackPair pair = {{pack_w, pack_phi}, gradients ? stats : nullptr, weight ? weight + n0 : nullptr};
+        if (n0 > 0) pair.job[0].R = 0;
+        RFSF_TRY(launch_largest(pair, bf16, stream));
+        RFSF_TRY(launch_pack(pair, bf16, stream));
+        const int64_t step = gradients ? plan.score_rows : rows;
+        for (int64_t m0 = 0; m0 < rows; m0 += step) {
+            const int64_t part = std::min(step, rows - m0);
+            const int edge = plane_tile(C, part);
+            const Scores epilogue = {largest_w, largest_phi + m0, C, part, labels + n0 + m0, partial, plan.rows, target, scores, z.ld_scores};
+            RFSF_TRY(launch_plane_product<MODE>(Planes{w_rows, pitch_k, C}, Planes{phi_rows + m0 * pitch_k, pitch_k, part}, plane_steps(K, z.two), edge,
+                                                epilogue, stream));
+            const JoinJob join = {partial, (C + edge - 1) / edge, plan.rows, part, C, labels + n0 + m0, weight ? weight + n0 + m0 : nullptr, count, largest_w,
+                                  target, loss + n0 + m0, gradients ? terms + m0 : nullptr};
+            join_kernel<<<dim3((unsigned)((part + 255) / 256)), dim3(256), 0, stream>>>(join);
+            RFSF_TRY(hipGetLastError());
+            if (!gradients) continue;
+            const GradientJob job = {scores, z.ld_scores, part, C, labels + n0 + m0, weight, stats, terms + m0, largest_w, largest_phi + m0, g_rows ? g_rows + m0 * pitch_c : nullptr,
+                                     g_classes ? g_classes + (m0 / 64) * (z.two ? 256 : 128) : nullptr, pitch_c, pitch_n};
+            const dim3 grid((unsigned)((C + 63) / 64), (unsigned)((part + 63) / 64));
+            gradient_kernel<MODE == kHalfTwo><<<grid, dim3(256), 0, stream>>>(job);
+            RFSF_TRY(hipGetLastError());
+        }
+        if (z.d_phi) {
+            const Gradient epilogue = {static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16, terms, nullptr, nullptr, nullptr, 0};
+            RFSF_TRY(launch_plane_product<MODE>(Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two), plane_tile(K, rows),
+                                                epilogue, stream));
+        }
+        if (z.d_w) {
+            const bool last = n0 + rows >= N;
+            const bool to_sums = sums && !last;
+            const float *add = n0 == 0 ? nullptr : sums ? sums : static_cast<const float *>(dW);
+            const Gradient epilogue = {to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr, stats, count,
+                                       add, sums ? K : shape.ld_dw};
+            RFSF_TRY(launch_plane_product<MODE>(Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two), plane_tile(K, C),
+                                                epilogue, stream));
+        }
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_softmax_xent(const rfsf_xent_shape &shape, const void *Phi, const void *W, const int64_t *labels, const float *weight, float *loss,
+                               void *dPhi, void *dW, void *workspace, size_t bytes, hipStream_t stream)
+{
+    return shape.bf16 ? xent_blocks<kHalf>(shape, Phi, W, labels, weight, loss, dPhi, dW, workspace, bytes, stream)
+                      : xent_blocks<kHalfTwo>(shape, Phi, W, labels, weight, loss, dPhi, dW, workspace, bytes, stream);
+}
+
+}  // namespace rfsf
