@@ -55,37 +55,31 @@ struct Scaled {
     {
         struct __attribute__((packed, aligned(4))) Float4u { float x, y, z, w; };
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-#pragma unroll
-        for (int a = 0; a < T::BM; ++a)
+        t.each_block([&](const auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            const int64_t j = t.j0 + 32 * b + col;
+            if (j >= cols_j) return;
+            const float sj = scale_j[j];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t i = t.i0 + 32 * a + 8 * q + 4 * half;
-                float s[4];
+                const int64_t i = first + 8 * q + 4 * half;
+                float *dst = out + j * ld + i;
+                float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[e] = i + e < rows_i ? scale_i[i + e] : 0.f;
+                for (int e = 0; e < 4; ++e) v[e] = (float)acc[4 * q + e] * (sj * (i + e < rows_i ? scale_i[i + e] : 0.f));
+                if (i + 3 < rows_i) {
+                    *reinterpret_cast<Float4u *>(dst) = {v[0], v[1], v[2], v[3]};
+                } else {
 #pragma unroll
-                for (int b = 0; b < T::BN; ++b) {
-                    const int64_t j = t.j0 + 32 * b + col;
-                    if (j >= cols_j) continue;
-                    const float sj = scale_j[j];
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (float)t.acc[a][b][4 * q + e] * (sj * s[e]);
-                    float *dst = out + j * ld + i;
-                    if (i + 3 < rows_i) {
-                        *reinterpret_cast<Float4u *>(dst) = {v[0], v[1], v[2], v[3]};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (i + e < rows_i) dst[e] = v[e];
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < rows_i) dst[e] = v[e];
                 }
             }
+        });
     }
 };
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
-int64_t code_pitch(int64_t K) { return (K + kStepBytes - 1) / kStepBytes * kStepBytes; }
+int64_t code_pitch(int64_t K) { return odd_steps(K); }
 size_t row_bytes(int64_t rows, int64_t K) { return up((size_t)rows * code_pitch(K)) + up(4 * (size_t)rows); }
 constexpr int64_t kMostRows = 1 << 20;      // quantised at a time
 
@@ -121,7 +115,7 @@ hipError_t launch_int8_gram(const void *X, bool bf16, int64_t Nx, int64_t ldx, c
         if (e != hipSuccess) return e;
         const Scaled epilogue = {out + n0 * ldk, ldk, Ny, rows, scales, sx};
         e = launch_plane_product<kInt8>(Planes{reinterpret_cast<const char *>(codes), ldy, Ny}, Planes{reinterpret_cast<const char *>(qx), code_pitch(K), rows},
-                                        code_pitch(K) / kStepBytes, plane_tile(Ny, rows), epilogue, stream);
+                                        (K + kStepBytes - 1) / kStepBytes, plane_tile(Ny, rows), epilogue, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

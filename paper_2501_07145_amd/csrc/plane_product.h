@@ -16,6 +16,8 @@
 
 #include "rfsf_internal.h"
 
+#include <type_traits>
+
 namespace rfsf {
 
 enum PlaneMode { kHalf = 0, kHalfTwo = 1, kInt8 = 2 };
@@ -60,11 +62,11 @@ __device__ __forceinline__ void direct_load16(const char *base, uint32_t off, ui
 
 // Tiles in the order that the XCDs' L2s see them: eight contiguous pieces of an order that goes through strips of kStrip tiles of A.
 constexpr int kStrip = 8;
-__device__ __forceinline__ bool tile_of_block(int64_t tiles_i, int64_t tiles_j, int64_t *ti, int64_t *tj)
+__device__ __forceinline__ bool tile_of_block(unsigned block, int64_t tiles_i, int64_t tiles_j, int64_t *ti, int64_t *tj)
 {
     const int64_t tiles = tiles_i * tiles_j, per = (tiles + 7) / 8;
-    const int64_t rank = (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
-    if ((int64_t)(blockIdx.x / 8) >= per || rank >= tiles) return false;
+    const int64_t rank = (int64_t)(block % 8) * per + block / 8;
+    if (rank >= tiles) return false;
     const int64_t strip = rank / (kStrip * tiles_j), at = rank - strip * kStrip * tiles_j;
     const int64_t left = tiles_i - strip * kStrip, width = left < kStrip ? left : kStrip;
     *tj = at / width;
@@ -75,25 +77,44 @@ inline unsigned blocks_of(int64_t tiles) { return (unsigned)((tiles + 7) / 8 * 8
 
 // What an epilogue is given: the wavefront's accumulators and where they belong. Element e of acc[a][b] of a lane is row
 // i0 + 32 a + 8 (e / 4) + 4 (lane / 32) + e % 4 and column j0 + 32 b + lane % 32.
-template <PlaneMode MODE, int TM, int TN, int WM, int WN>
+//
+// A tile of EXTRA has another 32 rows, from extra_i on: one block for each wavefront, that of its columns 32 wave_i .. + 31. Operands
+// with one more row than whole tiles (features have 1 + M*D columns) then need no further tiles for it.
+template <PlaneMode MODE, int TM, int TN, int WM, int WN, bool EXTRA>
 struct Tile {
-    static constexpr int BM = TM / WM / 32, BN = TN / WN / 32, COLUMNS = TN, WAVES_I = WM;
-    typename Acc<MODE>::type acc[BM][BN];
-    int64_t i0, j0, tile_i, tile_j;
+    static constexpr int BM = TM / WM / 32, BN = TN / WN / 32, ROWS = TM, COLUMNS = TN, WAVES_I = WM;
+    static constexpr bool HAS_EXTRA = EXTRA;
+    typename Acc<MODE>::type acc[BM][BN], extra;
+    int64_t i0, j0, tile_i, tile_j, extra_i;
     int wave_i, wave_j;
     char *lds;                  // free for the epilogue after a barrier
+    // f(block, first row, number of the block of columns), for every block
+    template <typename F>
+    __device__ __forceinline__ void each_block(const F &f)
+    {
+#pragma unroll
+        for (int a = 0; a < BM; ++a)
+#pragma unroll
+            for (int b = 0; b < BN; ++b) f(acc[a][b], i0 + 32 * a, b);
+        if constexpr (EXTRA) {
+#pragma unroll
+            for (int b = 0; b < BN; ++b)
+                if (b == wave_i) f(extra, extra_i, b);
+        }
+    }
 };
 
-template <PlaneMode MODE, int TM, int TN, int WM, int WN, typename Epilogue>
-__global__ __launch_bounds__(64 * WM * WN, 2)
-void plane_product(Planes A, Planes B, int64_t steps, int64_t tiles_i, int64_t tiles_j, Epilogue epilogue)
+template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA, typename Epilogue>
+__device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const Planes &B, int64_t steps, int64_t tile_i, int64_t tile_j, const Epilogue &epilogue)
 {
-    extern __shared__ __attribute__((aligned(1024))) char buffers[];
-    typedef Tile<MODE, TM, TN, WM, WN> T;
-    constexpr int BM = T::BM, BN = T::BN, kBuffer = (TM + TN) * kStepBytes, NL = (TM + TN) / 8 / (WM * WN);
+    typedef Tile<MODE, TM, TN, WM, WN, EXTRA> T;
+    constexpr int BM = T::BM, BN = T::BN, kRows = TM + TN + (EXTRA ? 32 : 0), kBuffer = kRows * kStepBytes, NL = (TM + TN) / 8 / (WM * WN);
     static_assert((TM + TN) % (8 * WM * WN) == 0 && TM % 8 == 0, "every wavefront loads whole groups of eight rows");
+    static_assert(!EXTRA || (WM == BN && WM * WN >= 4 && STAGES == 2), "a block for every wavefront, eight rows for each of four");
+    static_assert(STAGES >= 2 && (STAGES - 1) * NL < 64, "loads in flight can be counted");
     T t;
-    if (!tile_of_block(tiles_i, tiles_j, &t.tile_i, &t.tile_j)) return;
+    t.tile_i = tile_i;
+    t.tile_j = tile_j;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int half = lane >> 5, col = lane & 31;
     const int64_t first_i = t.tile_i * TM, first_j = t.tile_j * TN;
@@ -101,16 +122,18 @@ void plane_product(Planes A, Planes B, int64_t steps, int64_t tiles_i, int64_t t
     t.wave_j = wave % WN;
     t.i0 = first_i + t.wave_i * (TM / WM);
     t.j0 = first_j + t.wave_j * (TN / WN);
+    t.extra_i = first_i + TM;
     t.lds = buffers;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)buffers;
 
+    // LDS: the rows of A, those of B, the extra ones of A
     const char *base_a = A.data + first_i * A.pitch, *base_b = B.data + first_j * B.pitch;
-    uint32_t off[NL];           // from the tile's first row: at most 255 rows on, checked by the launcher to stay below 2^32
+    uint32_t off[NL + 1];       // from the tile's first row: at most 287 rows on, checked by the callers to stay below 2^32
 #pragma unroll
-    for (int l = 0; l < NL; ++l) {
-        const int row0 = 8 * (wave * NL + l), row = row0 + (lane >> 3);
-        const bool is_b = row0 >= TM;
-        const int64_t last = is_b ? B.rows - 1 - first_j : A.rows - 1 - first_i, r = is_b ? row - TM : row;
+    for (int l = 0; l <= NL; ++l) {
+        const int row0 = l < NL ? 8 * (wave * NL + l) : TM + TN + 8 * wave, row = row0 + (lane >> 3);
+        const bool is_b = l < NL && row0 >= TM;
+        const int64_t last = is_b ? B.rows - 1 - first_j : A.rows - 1 - first_i, r = is_b ? row - TM : l < NL ? row : row - TN;
         off[l] = (uint32_t)((r < last ? r : last) * (is_b ? B.pitch : A.pitch)) + 16u * (uint32_t)((lane & 7) ^ (lane >> 3));
     }
     auto load = [&](int64_t step, int buffer) {
@@ -119,95 +142,223 @@ void plane_product(Planes A, Planes B, int64_t steps, int64_t tiles_i, int64_t t
             const int row0 = 8 * (wave * NL + l);
             direct_load16((row0 >= TM ? base_b : base_a) + step * kStepBytes, off[l], lds + (uint32_t)(buffer * kBuffer + row0 * kStepBytes));
         }
+        if (EXTRA && wave < 4)
+            direct_load16(base_a + step * kStepBytes, off[NL], lds + (uint32_t)(buffer * kBuffer + (TM + TN + 8 * wave) * kStepBytes));
     };
 #pragma unroll
-    for (int a = 0; a < BM; ++a)
+    for (int e = 0; e < 16; ++e) {
+        t.extra[e] = 0;
 #pragma unroll
-        for (int b = 0; b < BN; ++b)
+        for (int a = 0; a < BM; ++a)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) t.acc[a][b][e] = 0;
+            for (int b = 0; b < BN; ++b) t.acc[a][b][e] = 0;
+    }
 
+    // Software pipeline. A step is cut into phases of BM x BN matrix instructions, whose operands have been read from LDS during the phase before,
+    // so that a wavefront's matrix instructions follow one another. Before the last phases of a step, when all of it has been read, the
+    // wavefront waits for its loads of the next step (those of the steps after it stay in flight) and then for everybody: the
+    // next step can be read, and this step's buffer takes the loads of the step STAGES ahead.
     const int row_a = t.wave_i * (TM / WM) + col, row_b = TM + t.wave_j * (TN / WN) + col;
-    load(0, 0);
-    for (int64_t s = 0; s < steps; ++s) {
-        // this wavefront's loads of the step have landed and its reads of the step before are done; then everybody's
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    const char *buf = buffers;
+    int slot = 0;
+    auto read_a = [&](intx4 (&f)[BM], const char *from, int c) {
+#pragma unroll
+        for (int a = 0; a < BM; ++a) f[a] = *reinterpret_cast<const intx4 *>(from + (row_a + 32 * a) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+    };
+    auto read_b = [&](intx4 (&f)[BN], const char *from, int c) {
+#pragma unroll
+        for (int b = 0; b < BN; ++b) f[b] = *reinterpret_cast<const intx4 *>(from + (row_b + 32 * b) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+    };
+    auto read_x = [&](const char *from, int c) {
+        if constexpr (!EXTRA) return intx4{0, 0, 0, 0};
+        return *reinterpret_cast<const intx4 *>(from + (TM + TN + col) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+    };
+    auto multiply = [&](const intx4 (&fa)[BM], const intx4 (&fb)[BN], const intx4 &fx) {
+#pragma unroll
+        for (int a = 0; a < BM; ++a)
+#pragma unroll
+            for (int b = 0; b < BN; ++b) t.acc[a][b] = mfma(fa[a], fb[b], t.acc[a][b]);
+        if constexpr (EXTRA) t.extra = mfma(fx, t.wave_i == 0 ? fb[0] : fb[BN - 1], t.extra);
+    };
+    // READS reads spread over the phase's matrix instructions
+    auto interleave = [&](auto reads) {
+        constexpr int R = decltype(reads)::value, PRODUCTS = BM * BN;
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            const int now = (i + 1) * R / PRODUCTS - i * R / PRODUCTS;
+            if (now == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (now == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            if (now > 2) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        }
+    };
+    // the step after s has landed, for everybody
+    auto landed = [&](int64_t s) {
+        if (STAGES > 2 && s + STAGES <= steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * NL) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 1 < steps) load(s + 1, (int)((s + 1) & 1));
-        const char *buf = buffers + (int)(s & 1) * kBuffer;
-        auto chunk = [&](int row, int c) {
-            return *reinterpret_cast<const intx4 *>(buf + row * kStepBytes + 16 * ((c + half) ^ (col & 7)));
-        };
-        if constexpr (MODE == kHalfTwo) {
+    };
+    auto next_buffer = [&] { return buffers + (slot + 1 == STAGES ? 0 : slot + 1) * kBuffer; };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        if (s < steps) load(s, s);
+    landed(-1);
+    if (STAGES - 1 < steps) load(STAGES - 1, STAGES - 1);
+    if constexpr (MODE == kHalfTwo) {
+        intx4 ah[BM], al[BM], bh[BN], bl[BN], next[BN], xh, xl = read_x(buf, 4);
+        read_a(al, buf, 4);
+        read_b(bh, buf, 0);
+        for (int64_t s = 0; s < steps; ++s) {
+            const char *other = next_buffer();
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                intx4 bh[BN], bl[BN];
-#pragma unroll
-                for (int b = 0; b < BN; ++b) {
-                    bh[b] = chunk(row_b + 32 * b, 2 * ks);
-                    bl[b] = chunk(row_b + 32 * b, 4 + 2 * ks);
+                const bool last = ks == 1;
+                read_a(ah, buf, 2 * ks);
+                xh = read_x(buf, 2 * ks);
+                read_b(bl, buf, 4 + 2 * ks);
+                multiply(al, bh, xl);
+                interleave(std::integral_constant<int, BM + BN>{});
+                if (last) {
+                    landed(s);
+                    if (s + STAGES < steps) load(s + STAGES, slot);
                 }
+                read_a(al, last ? other : buf, last ? 4 : 6);
+                xl = read_x(last ? other : buf, last ? 4 : 6);
+                multiply(ah, bl, xh);
+                interleave(std::integral_constant<int, BM>{});
+                read_b(next, last ? other : buf, last ? 0 : 2);
+                multiply(ah, bh, xh);
+                interleave(std::integral_constant<int, BN>{});
 #pragma unroll
-                for (int a = 0; a < BM; ++a) {
-                    const intx4 ah = chunk(row_a + 32 * a, 2 * ks), al = chunk(row_a + 32 * a, 4 + 2 * ks);
-#pragma unroll
-                    for (int b = 0; b < BN; ++b) t.acc[a][b] = mfma(al, bh[b], t.acc[a][b]);
-#pragma unroll
-                    for (int b = 0; b < BN; ++b) t.acc[a][b] = mfma(ah, bl[b], t.acc[a][b]);
-#pragma unroll
-                    for (int b = 0; b < BN; ++b) t.acc[a][b] = mfma(ah, bh[b], t.acc[a][b]);
-                }
+                for (int b = 0; b < BN; ++b) bh[b] = next[b];
             }
-        } else {
+            buf = other;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+    } else {
+        intx4 fa[2][BM], fb[2][BN], fx[2];
+        fx[0] = read_x(buf, 0);
+        read_a(fa[0], buf, 0);
+        read_b(fb[0], buf, 0);
+        for (int64_t s = 0; s < steps; ++s) {
+            const char *other = next_buffer();
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
-                intx4 fb[BN];
-#pragma unroll
-                for (int b = 0; b < BN; ++b) fb[b] = chunk(row_b + 32 * b, 2 * ks);
-#pragma unroll
-                for (int a = 0; a < BM; ++a) {
-                    const intx4 fa = chunk(row_a + 32 * a, 2 * ks);
-#pragma unroll
-                    for (int b = 0; b < BN; ++b) t.acc[a][b] = mfma(fa, fb[b], t.acc[a][b]);
+                const bool last = ks == 3;
+                if (last) {
+                    landed(s);
+                    if (s + STAGES < steps) load(s + STAGES, slot);
                 }
+                read_a(fa[(ks + 1) & 1], last ? other : buf, last ? 0 : 2 * ks + 2);
+                read_b(fb[(ks + 1) & 1], last ? other : buf, last ? 0 : 2 * ks + 2);
+                fx[(ks + 1) & 1] = read_x(last ? other : buf, last ? 0 : 2 * ks + 2);
+                multiply(fa[ks & 1], fb[ks & 1], fx[ks & 1]);
+                interleave(std::integral_constant<int, BM + BN>{});
             }
+            buf = other;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
     }
     epilogue(t);
 }
 
-template <PlaneMode MODE, int TM, int TN, int WM, int WN, typename Epilogue>
-hipError_t launch_tiles(const Planes &A, const Planes &B, int64_t steps, const Epilogue &epilogue, hipStream_t stream)
+}  // namespace plane
+
+// Products of one launch: the second one's tiles follow the first one's and share the GPU with their rest.
+template <typename Epilogue>
+struct Product {
+    Planes A, B;
+    int64_t steps;
+    Epilogue epilogue;
+};
+
+namespace plane {
+
+template <typename Epilogue>
+struct Products {
+    Product<Epilogue> product[2];
+    int64_t tiles_i[2], tiles_j[2];
+    unsigned blocks_of_first;
+};
+
+template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA, typename Epilogue>
+__global__ __launch_bounds__(64 * WM * WN, 2)
+void plane_product(Products<Epilogue> all)
 {
-    constexpr size_t lds = 2 * (size_t)(TM + TN) * kStepBytes;
+    extern __shared__ __attribute__((aligned(1024))) char buffers[];
+    const int which = blockIdx.x < all.blocks_of_first ? 0 : 1;
+    const Product<Epilogue> &p = all.product[which];
+    const int64_t tiles_i = all.tiles_i[which];
+    int64_t tile_i, tile_j;
+    if (!tile_of_block(blockIdx.x - (which ? all.blocks_of_first : 0), tiles_i, all.tiles_j[which], &tile_i, &tile_j)) return;
+    if (EXTRA && tile_i == tiles_i - 1 && p.A.rows > tiles_i * TM)
+        run_tile<MODE, TM, TN, WM, WN, STAGES, EXTRA>(buffers, p.A, p.B, p.steps, tile_i, tile_j, p.epilogue);
+    else
+        run_tile<MODE, TM, TN, WM, WN, STAGES, false>(buffers, p.A, p.B, p.steps, tile_i, tile_j, p.epilogue);
+}
+
+}  // namespace plane
+
+// Tiles along A, which an epilogue may number its parts by. A last tile of up to 32 rows of 256 is joined to the one before.
+inline bool plane_extra(int64_t rows_a, int tile) { return tile == 256 && rows_a > 256 && rows_a % 256 > 0 && rows_a % 256 <= 32; }
+inline int64_t plane_tiles_a(int64_t rows_a, int tile) { return plane_extra(rows_a, tile) ? rows_a / tile : (rows_a + tile - 1) / tile; }
+inline int64_t plane_tiles(int64_t rows_a, int64_t rows_b, int tile) { return plane_tiles_a(rows_a, tile) * ((rows_b + tile - 1) / tile); }
+
+// The edge of a launch's tiles, from their number at an edge. 256: eight wavefronts, one workgroup a CU; the smaller ones where
+// the larger would leave CUs without work.
+template <typename Tiles>
+int plane_tile_of(const Tiles &tiles)
+{
+    if (tiles(256) >= 192) return 256;
+    if (tiles(128) >= 192) return 128;
+    return 64;
+}
+inline int plane_tile(int64_t rows_a, int64_t rows_b)
+{
+    return plane_tile_of([&](int edge) { return plane_tiles(rows_a, rows_b, edge); });
+}
+
+namespace plane {
+
+template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA, typename Epilogue>
+hipError_t launch_tiles(const Product<Epilogue> *p, int count, hipStream_t stream)
+{
+    constexpr size_t lds = STAGES * (size_t)(TM + TN + (EXTRA ? 32 : 0)) * kStepBytes;
     static LdsLimit limit;
-    auto kernel = plane_product<MODE, TM, TN, WM, WN, Epilogue>;
+    auto kernel = plane_product<MODE, TM, TN, WM, WN, STAGES, EXTRA, Epilogue>;
     const hipError_t e = allow_lds(limit, reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
-    const int64_t tiles_i = (A.rows + TM - 1) / TM, tiles_j = (B.rows + TN - 1) / TN;
-    kernel<<<dim3(blocks_of(tiles_i * tiles_j)), dim3(64 * WM * WN), lds, stream>>>(A, B, steps, tiles_i, tiles_j, epilogue);
+    Products<Epilogue> all;
+    unsigned blocks[2] = {0, 0};
+    for (int k = 0; k < 2; ++k) {
+        all.product[k] = p[k < count ? k : 0];
+        all.tiles_i[k] = plane_tiles_a(all.product[k].A.rows, TM);
+        all.tiles_j[k] = (all.product[k].B.rows + TN - 1) / TN;
+        if (k < count) blocks[k] = blocks_of(all.tiles_i[k] * all.tiles_j[k]);
+    }
+    all.blocks_of_first = blocks[0];
+    kernel<<<dim3(blocks[0] + blocks[1]), dim3(64 * WM * WN), lds, stream>>>(all);
     return hipGetLastError();
 }
 
 }  // namespace plane
 
-// The edge of the tiles that a product of this size is cut into. 256: eight wavefronts, one workgroup a CU; the smaller ones where
-// the larger would leave CUs without work.
-inline int plane_tile(int64_t rows_a, int64_t rows_b)
+// One product, or two in one launch, in tiles of edge `tile`.
+template <PlaneMode MODE, typename Epilogue>
+hipError_t launch_plane_products(const Product<Epilogue> *p, int count, int tile, hipStream_t stream)
 {
-    auto tiles = [&](int64_t edge) { return ((rows_a + edge - 1) / edge) * ((rows_b + edge - 1) / edge); };
-    if (tiles(256) >= 192) return 256;
-    if (tiles(128) >= 192) return 128;
-    return 64;
+    if (plane_extra(p[0].A.rows, tile) || (count > 1 && plane_extra(p[1].A.rows, tile)))
+        return plane::launch_tiles<MODE, 256, 256, 2, 4, 2, true>(p, count, stream);
+    if (tile == 256) return plane::launch_tiles<MODE, 256, 256, 2, 4, 2, false>(p, count, stream);
+    if (tile == 128) return plane::launch_tiles<MODE, 128, 128, 2, 2, 4, false>(p, count, stream);
+    return plane::launch_tiles<MODE, 64, 64, 2, 2, 4, false>(p, count, stream);
 }
-
 template <PlaneMode MODE, typename Epilogue>
 hipError_t launch_plane_product(const Planes &A, const Planes &B, int64_t steps, int tile, const Epilogue &epilogue, hipStream_t stream)
 {
-    if (tile == 256) return plane::launch_tiles<MODE, 256, 256, 2, 4>(A, B, steps, epilogue, stream);
-    if (tile == 128) return plane::launch_tiles<MODE, 128, 128, 2, 2>(A, B, steps, epilogue, stream);
-    return plane::launch_tiles<MODE, 64, 64, 2, 2>(A, B, steps, epilogue, stream);
+    const Product<Epilogue> p = {A, B, steps, epilogue};
+    return launch_plane_products<MODE>(&p, 1, tile, stream);
 }
 
 }  // namespace rfsf

@@ -53,63 +53,78 @@ struct Scores {
     float *target;                              // the label's score
     float *scores;                              // [rows][ld], or null
     int64_t ld;
+    bool with_reach;
 
     template <typename T>
     __device__ __forceinline__ void operator()(T &t) const
     {
-        constexpr int BM = T::BM, BN = T::BN;
+        constexpr int BN = T::BN, CLASSES = T::ROWS + (T::HAS_EXTRA ? 32 : 0);
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-        float top[BN], sum[BN], reach[BN];
-        int shift_n[BN];
-        int64_t label[BN];
+        const int64_t c0 = t.tile_i * T::ROWS;
+        // the classes' powers of two (of a class without weights, whose scores are zero, the smallest)
+        int *powers = reinterpret_cast<int *>(t.lds);
+        __syncthreads();
+        for (int i = threadIdx.x; i < CLASSES; i += blockDim.x) powers[i] = exponent_of(c0 + i < C ? largest_w[c0 + i] : 0) - kTopBit;
+        __syncthreads();
+        float top[BN], sum[BN], reach[BN], from[BN];
+        int shift_n[BN], label[BN];                         // the label's place in this tile
 #pragma unroll
         for (int b = 0; b < BN; ++b) {
-            const int64_t n = t.j0 + 32 * b + col;
+            const int64_t n = t.j0 + 32 * b + col, y = n < rows ? labels[n] - c0 : -1;
             shift_n[b] = n < rows ? shift_of(largest_phi[n]) : 0;
-            label[b] = n < rows ? labels[n] : -1;
+            label[b] = y >= 0 && y < CLASSES ? (int)y : -1;
             top[b] = reach[b] = -INFINITY;
+            sum[b] = 0.f;
         }
-#pragma unroll
-        for (int a = 0; a < BM; ++a)
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t i = t.i0 + 32 * a + 8 * q + 4 * half;
-                int shift[4];
-                float power[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t largest = i + e < C ? largest_w[i + e] : 0;
-                    shift[e] = shift_of(largest);
-                    power[e] = (float)exponent_of(largest);
-                }
-#pragma unroll
-                for (int b = 0; b < BN; ++b) {
-                    const int64_t n = t.j0 + 32 * b + col;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = ldexpf(t.acc[a][b][4 * q + e], -(shift[e] + shift_n[b]));
-                        if (i + e == label[b]) target[n] = v[e];
-                        t.acc[a][b][4 * q + e] = i + e < C ? v[e] : -INFINITY;
-                        top[b] = fmaxf(top[b], t.acc[a][b][4 * q + e]);
-                        reach[b] = fmaxf(reach[b], fmaf(t.acc[a][b][4 * q + e], kLog2e, power[e]));
-                    }
-                    if (scores && n < rows && i < C)             // (ld is a multiple of four: numbers beyond C are nobody's)
-                        *reinterpret_cast<float4 *>(scores + n * ld + i) = make_float4(v[0], v[1], v[2], v[3]);
+                const int i = (int)(first - c0) + 8 * q + 4 * half;
+                const int4 p = *reinterpret_cast<const int4 *>(powers + i);
+                acc[4 * q] = ldexpf(acc[4 * q], p.x - shift_n[b]);
+                acc[4 * q + 1] = ldexpf(acc[4 * q + 1], p.y - shift_n[b]);
+                acc[4 * q + 2] = ldexpf(acc[4 * q + 2], p.z - shift_n[b]);
+                acc[4 * q + 3] = ldexpf(acc[4 * q + 3], p.w - shift_n[b]);
+                if (with_reach) {
+                    const float r0 = fmaxf(fmaf(acc[4 * q], kLog2e, (float)p.x), fmaf(acc[4 * q + 1], kLog2e, (float)p.y));
+                    const float r1 = fmaxf(fmaf(acc[4 * q + 2], kLog2e, (float)p.z), fmaf(acc[4 * q + 3], kLog2e, (float)p.w));
+                    reach[b] = fmaxf(reach[b], fmaxf(r0, r1) + (float)kTopBit);
                 }
             }
+        });
+        if (c0 + CLASSES > C)
+            t.each_block([&](auto &acc, int64_t first, int) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (first + 8 * (e / 4) + 4 * half + e % 4 >= C) acc[e] = -INFINITY;
+            });
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            const int64_t n = t.j0 + 32 * b + col;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int i = (int)(first - c0) + 8 * q + 4 * half, y = label[b] - i;
+                if (y >= 0 && y < 4) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (y == e) target[n] = acc[4 * q + e];
+                }
+                top[b] = fmaxf(top[b], fmaxf(fmaxf(acc[4 * q], acc[4 * q + 1]), fmaxf(acc[4 * q + 2], acc[4 * q + 3])));
+                if (scores && n < rows && c0 + i < C)             // (ld is a multiple of four: numbers beyond C are nobody's)
+                    *reinterpret_cast<float4 *>(scores + n * ld + c0 + i) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+            }
+        });
 #pragma unroll
         for (int b = 0; b < BN; ++b) {
             top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
             reach[b] = fmaxf(reach[b], __shfl_xor(reach[b], 32));
-            const float from = top[b] == -INFINITY ? 0.f : top[b];
-            float s = 0.f;
-#pragma unroll
-            for (int a = 0; a < BM; ++a)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s += exp_of(t.acc[a][b][e] - from);
-            sum[b] = s + __shfl_xor(s, 32);
+            from[b] = top[b] == -INFINITY ? 0.f : top[b] * kLog2e;
         }
+        t.each_block([&](auto &acc, int64_t, int b) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[b] += __builtin_amdgcn_exp2f(fmaf(acc[e], kLog2e, -from[b]));
+        });
+#pragma unroll
+        for (int b = 0; b < BN; ++b) sum[b] += __shfl_xor(sum[b], 32);
         // the wavefronts that hold other classes of the same sequences
         Partial *shared = reinterpret_cast<Partial *>(t.lds);
         constexpr int WIDE = T::COLUMNS, ROWS = T::WAVES_I;
@@ -147,27 +162,30 @@ struct JoinJob {
     float *loss;
     RowTerms *terms;                // null without gradients
 };
+// 16 rows a workgroup, whose 16 groups of threads share out the tiles.
+constexpr int kJoinRows = 16;
 __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
 {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= job.rows) return;
-    float m = -INFINITY, reach = -INFINITY;
-    for (int64_t t = 0; t < job.tiles; ++t) {
-        const Partial v = job.partial[t * job.rows_ld + n];
-        m = fmaxf(m, v.top);
-        reach = fmaxf(reach, v.reach);
-    }
-    const float from = m == -INFINITY ? 0.f : m;
-    float s = 0.f;
-    for (int64_t t = 0; t < job.tiles; ++t) {
-        const Partial v = job.partial[t * job.rows_ld + n];
-        s += v.sum * exp_of(v.top - from);
-    }
+    __shared__ Partial part[16][kJoinRows];
+    const int r = threadIdx.x % kJoinRows, group = threadIdx.x / kJoinRows;
+    const int64_t n = (int64_t)blockIdx.x * kJoinRows + r;
+    Partial v = {-INFINITY, 0.f, -INFINITY};
+    auto add = [](const Partial &a, const Partial &b) {
+        const float m = fmaxf(a.top, b.top), from = m == -INFINITY ? 0.f : m;
+        return Partial{m, a.sum * exp_of(a.top - from) + b.sum * exp_of(b.top - from), fmaxf(a.reach, b.reach)};
+    };
+    if (n < job.rows)
+        for (int64_t t = group; t < job.tiles; t += 16) v = add(v, job.partial[t * job.rows_ld + n]);
+    part[group][r] = v;
+    __syncthreads();
+    if (group != 0 || n >= job.rows) return;
+    for (int g = 1; g < 16; ++g) v = add(v, part[g][r]);
+    const float from = v.top == -INFINITY ? 0.f : v.top, s = v.sum;
     const int64_t label = job.labels[n];
     const bool known = label >= 0 && label < job.C;
-    job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (m - job.target[n]) : NAN;
+    job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (from - job.target[n]) : NAN;
     if (!job.terms) return;
-    float bound = reach - fmaf(from, kLog2e, log2f(s));
+    float bound = v.reach - fmaf(from, kLog2e, log2f(s));
     if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
     job.terms[n] = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : 1.0f / (float)*job.count,
                     (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
@@ -262,26 +280,23 @@ struct Gradient {
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
         const int all = terms ? 0 : (int)stats->top - kTopBias;
         const float mean = count ? 1.0f / (float)max(*count, 1u) : 1.0f;
-#pragma unroll
-        for (int a = 0; a < T::BM; ++a)
+        t.each_block([&](const auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            const int64_t j = t.j0 + 32 * b + col;
+            if (j >= cols_j) return;
+            const float scale = terms ? terms[j].scale : mean;
+            const int shift = (terms ? terms[j].reach : all) - 2 * kTopBit;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t i = t.i0 + 32 * a + 8 * q + 4 * half;
+                const int64_t i = first + 8 * q + 4 * half;
+                float v[4];
 #pragma unroll
-                for (int b = 0; b < T::BN; ++b) {
-                    const int64_t j = t.j0 + 32 * b + col;
-                    if (j >= cols_j) continue;
-                    const float scale = terms ? terms[j].scale : mean;
-                    const int shift = (terms ? terms[j].reach : all) - 2 * kTopBit;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = ldexpf(t.acc[a][b][4 * q + e], shift) * scale;
-                        if (add && i + e < rows_i) v[e] += add[j * add_ld + i + e];
-                    }
-                    store(j * ld + i, rows_i - i, v);
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = ldexpf(acc[4 * q + e], shift) * scale;
+                    if (add && i + e < rows_i) v[e] += add[j * add_ld + i + e];
                 }
+                if (i < rows_i) store(j * ld + i, rows_i - i, v);
             }
+        });
     }
     __device__ __forceinline__ void store(int64_t at, int64_t left, const float (&v)[4]) const
     {
@@ -461,12 +476,12 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
         for (int64_t m0 = 0; m0 < rows; m0 += step) {
             const int64_t part = std::min(step, rows - m0);
             const int edge = plane_tile(C, part);
-            const Scores epilogue = {largest_w, largest_phi + m0, C, part, labels + n0 + m0, partial, plan.rows, target, scores, z.ld_scores};
+            const Scores epilogue = {largest_w, largest_phi + m0, C, part, labels + n0 + m0, partial, plan.rows, target, scores, z.ld_scores, z.d_phi};
             RFSF_TRY(launch_plane_product<MODE>(Planes{w_rows, pitch_k, C}, Planes{phi_rows + m0 * pitch_k, pitch_k, part}, plane_steps(K, z.two), edge,
                                                 epilogue, stream));
-            const JoinJob join = {partial, (C + edge - 1) / edge, plan.rows, part, C, labels + n0 + m0, weight ? weight + n0 + m0 : nullptr, count, largest_w,
+            const JoinJob join = {partial, plane_tiles_a(C, edge), plan.rows, part, C, labels + n0 + m0, weight ? weight + n0 + m0 : nullptr, count, largest_w,
                                   target, loss + n0 + m0, gradients ? terms + m0 : nullptr};
-            join_kernel<<<dim3((unsigned)((part + 255) / 256)), dim3(256), 0, stream>>>(join);
+            join_kernel<<<dim3((unsigned)((part + kJoinRows - 1) / kJoinRows)), dim3(256), 0, stream>>>(join);
             RFSF_TRY(hipGetLastError());
             if (!gradients) continue;
             const GradientJob job = {scores, z.ld_scores, part, C, labels + n0 + m0, weight, stats, terms + m0, largest_w, largest_phi + m0, g_rows ? g_rows + m0 * pitch_c : nullptr,
@@ -475,20 +490,26 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
             gradient_kernel<MODE == kHalfTwo><<<grid, dim3(256), 0, stream>>>(job);
             RFSF_TRY(hipGetLastError());
         }
-        if (z.d_phi) {
-            const Gradient epilogue = {static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16, terms, nullptr, nullptr, nullptr, 0};
-            RFSF_TRY(launch_plane_product<MODE>(Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two), plane_tile(K, rows),
-                                                epilogue, stream));
-        }
+        if (!gradients) continue;
+        Product<Gradient> products[2];
+        int count_of_products = 0;
+        if (z.d_phi)
+            products[count_of_products++] = {Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two),
+                                             Gradient{static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16,
+                                                      terms, nullptr, nullptr, nullptr, 0}};
         if (z.d_w) {
-            const bool last = n0 + rows >= N;
-            const bool to_sums = sums && !last;
+            const bool to_sums = sums && n0 + rows < N;
             const float *add = n0 == 0 ? nullptr : sums ? sums : static_cast<const float *>(dW);
-            const Gradient epilogue = {to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr, stats, count,
-                                       add, sums ? K : shape.ld_dw};
-            RFSF_TRY(launch_plane_product<MODE>(Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two), plane_tile(K, C),
-                                                epilogue, stream));
+            products[count_of_products++] = {Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two),
+                                             Gradient{to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr,
+                                                      stats, count, add, sums ? K : shape.ld_dw}};
         }
+        const int edge = plane_tile_of([&](int e) {
+            int64_t tiles = 0;
+            for (int k = 0; k < count_of_products; ++k) tiles += plane_tiles(products[k].A.rows, products[k].B.rows, e);
+            return tiles;
+        });
+        RFSF_TRY(launch_plane_products<MODE>(products, count_of_products, edge, stream));
     }
     return hipSuccess;
 }
