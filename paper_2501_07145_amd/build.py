@@ -12,7 +12,7 @@ LIB = os.path.join(_HERE, "librfsf_ts.so")
 SOURCES = [f"sketch_fft_scan_d{n}.hip" for n in ["2048_order3", "2048_order2", "10_order3", "2048_order1", "10_order2",
                                                  "1000", "500", "10_order1", "9", "12", "13", "8", "100", "200", "7", "6"]] + \
     ["rff_increments.hip", "gram.hip", "dp1d.hip", "sketch_fft_scan.hip", "rfsf_ts_api.hip", "normalize.hip", "trp.hip",
-     "join_pieces.hip", "probe.hip", "softmax_xent.hip", "plane_pack.hip", "int8_gram.hip", "adamw.hip", "linear_api.hip"]
+     "join_pieces.hip", "probe.hip", "softmax_xent.hip", "xent_direct.hip", "plane_pack.hip", "int8_gram.hip", "adamw.hip", "linear_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",

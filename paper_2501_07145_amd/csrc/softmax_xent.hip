@@ -9,6 +9,7 @@
 // scores of a block stay in the workspace from their product to the pass that turns them into G (both layouts), in as
 // few rows at a time as fill the GPU, so that the last-level cache holds them.
 #include "plane_pack.h"
+#include "xent_direct.h"
 
 #include <algorithm>
 
@@ -85,11 +86,6 @@ struct Scores {
                 acc[4 * q + 1] = ldexpf(acc[4 * q + 1], p.y - shift_n[b]);
                 acc[4 * q + 2] = ldexpf(acc[4 * q + 2], p.z - shift_n[b]);
                 acc[4 * q + 3] = ldexpf(acc[4 * q + 3], p.w - shift_n[b]);
-                if (with_reach) {
-                    const float r0 = fmaxf(fmaf(acc[4 * q], kLog2e, (float)p.x), fmaf(acc[4 * q + 1], kLog2e, (float)p.y));
-                    const float r1 = fmaxf(fmaf(acc[4 * q + 2], kLog2e, (float)p.z), fmaf(acc[4 * q + 3], kLog2e, (float)p.w));
-                    reach[b] = fmaxf(reach[b], fmaxf(r0, r1) + (float)kTopBit);
-                }
             }
         });
         if (c0 + CLASSES > C)
@@ -109,6 +105,12 @@ struct Scores {
                         if (y == e) target[n] = acc[4 * q + e];
                 }
                 top[b] = fmaxf(top[b], fmaxf(fmaxf(acc[4 * q], acc[4 * q + 1]), fmaxf(acc[4 * q + 2], acc[4 * q + 3])));
+                if (with_reach) {
+                    const int4 p = *reinterpret_cast<const int4 *>(powers + i);
+                    const float r0 = fmaxf(fmaf(acc[4 * q], kLog2e, (float)p.x), fmaf(acc[4 * q + 1], kLog2e, (float)p.y));
+                    const float r1 = fmaxf(fmaf(acc[4 * q + 2], kLog2e, (float)p.z), fmaf(acc[4 * q + 3], kLog2e, (float)p.w));
+                    reach[b] = fmaxf(reach[b], fmaxf(r0, r1) + (float)kTopBit);
+                }
                 if (scores && n < rows && c0 + i < C)             // (ld is a multiple of four: numbers beyond C are nobody's)
                     *reinterpret_cast<float4 *>(scores + n * ld + c0 + i) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
             }
@@ -405,11 +407,15 @@ struct Carve {
 
 void softmax_xent_bytes(const rfsf_xent_shape &shape, size_t *recommended, size_t *minimum)
 {
+    if (xent_direct(shape)) {
+        *recommended = *minimum = xent_direct_bytes(shape);
+        return;
+    }
     const Sizes z(shape);
     const int64_t rows = z.recommended_rows();
     *recommended = z.fixed() + z.block(rows) + z.scores(z.score_rows(rows));
-    const int64_t least = kUnit;
-    *minimum = z.fixed() + z.block(least) + z.scores(least);
+    // (blocks of the fewest rows need room to add dW up, which all rows at once may not)
+    *minimum = std::min(*recommended, z.fixed() + z.block(kUnit) + z.scores(kUnit));
 }
 
 hipError_t launch_clear_rows(void *rows, int64_t count, int64_t columns, int64_t ld, bool bf16, hipStream_t stream)
@@ -517,6 +523,7 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
 hipError_t launch_softmax_xent(const rfsf_xent_shape &shape, const void *Phi, const void *W, const int64_t *labels, const float *weight, float *loss,
                                void *dPhi, void *dW, void *workspace, size_t bytes, hipStream_t stream)
 {
+    if (xent_direct(shape)) return launch_xent_direct(shape, Phi, W, labels, weight, loss, dPhi, dW, workspace, stream);
     return shape.bf16 ? xent_blocks<kHalf>(shape, Phi, W, labels, weight, loss, dPhi, dW, workspace, bytes, stream)
                       : xent_blocks<kHalfTwo>(shape, Phi, W, labels, weight, loss, dPhi, dW, workspace, bytes, stream);
 }

@@ -1,0 +1,836 @@
+// The softmax cross entropy of few rows, classes or columns, straight from the matrices as they lie in memory (softmax_xent.hip packs
+// them first, which pays where its products are large). What bounds it is reading Phi and W and writing the gradients, and the
+// number of launches: two for up to 64 classes, three for more, and one more where a gradient's sum is cut.
+//
+// Products: 32-bit numbers as three terms of bfloat16 (8 significand bits each, 24 in all, with the range of 32-bit numbers), six
+// products of pairs of terms, smallest first; bfloat16 operands as they are, G then as two terms. Sums in 32 bits. A tile's summed index is
+// shared out among the wavefronts of a workgroup and their parts are added up in LDS; operands go from memory to registers.
+// Gradients of up to 16 rows or 16 classes take no matrix instructions: one pass over the many of the two, in 32-bit multiply-adds.
+#include "xent_direct.h"
+
+#include <algorithm>
+
+namespace rfsf {
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float number(float x) { return x; }
+__device__ __forceinline__ float number(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+__device__ __forceinline__ floatx16 mfma(const bf16x8 &a, const bf16x8 &b, const floatx16 &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 mfma(const bf16x8 &a, const bf16x8 &b, const floatx4 &c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t round_pair(float a, float b)
+{
+    const floatx2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+// Eight numbers as TERMS terms. The first one is cut off rather than rounded, so that the largest numbers stay finite.
+template <int TERMS>
+struct Split { bf16x8 t[TERMS]; };
+template <int TERMS>
+__device__ __forceinline__ Split<TERMS> split(const float (&x)[8])
+{
+    uint32_t w[TERMS][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+        w[0][i] = (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xffff0000u);
+        if constexpr (TERMS > 1) {
+            a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+            b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+#pragma unroll
+            for (int t = 1; t < TERMS; ++t) {
+                w[t][i] = round_pair(a, b);
+                a -= __uint_as_float(w[t][i] << 16);
+                b -= __uint_as_float(w[t][i] & 0xffff0000u);
+            }
+        }
+    }
+    Split<TERMS> s;
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) s.t[t] = __builtin_bit_cast(bf16x8, make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]));
+    return s;
+}
+// c += a b, of all pairs of terms whose orders come to less than the larger number of terms, smallest first.
+template <int TA, int TB, typename Acc>
+__device__ __forceinline__ Acc multiply(const Split<TA> &a, const Split<TB> &b, Acc c)
+{
+    constexpr int MOST = (TA > TB ? TA : TB) - 1;
+#pragma unroll
+    for (int order = MOST; order >= 0; --order)
+#pragma unroll
+        for (int k = 0; k < TA; ++k)
+            if (order - k >= 0 && order - k < TB) c = mfma(a.t[k], b.t[order - k < 0 ? 0 : order - k < TB ? order - k : TB - 1], c);
+    return c;
+}
+
+// 16 of the 64 numbers of a row from k on: 16 bytes at a time, so that the four lanes that share a row read 64 bytes together.
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Chunk { T v[16 / sizeof(T)]; };
+template <typename T>
+__device__ __forceinline__ void load16(const T *row, int64_t k, int quarter, int64_t K, bool there, float (&x)[16])
+{
+    constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+    for (int j = 0; j < 16 / PER; ++j) {
+        const int64_t at = k + 4 * PER * j + PER * quarter;
+        if (at + PER <= K) {
+            const Chunk<T> c = *reinterpret_cast<const Chunk<T> *>(row + at);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[PER * j + e] = there ? number(c.v[e]) : 0.f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[PER * j + e] = there && at + e < K ? number(row[at + e]) : 0.f;
+        }
+    }
+}
+
+// Adds the wavefronts' parts of BM blocks up: block b is then whole in the registers of wavefront b (of its first ones).
+template <int BM, int NW, int PER, typename Acc>
+__device__ __forceinline__ Acc add_up(const Acc (&acc)[BM], float *shared, int wave, int lane)
+{
+#pragma unroll
+    for (int a = 0; a < BM; ++a)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) shared[((a * NW + wave) * PER + e) * 64 + lane] = acc[a][e];
+    __syncthreads();
+    Acc sum;
+    const int block = wave < BM ? wave : 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) s += shared[((block * NW + w) * PER + e) * 64 + lane];
+        sum[e] = s;
+    }
+    return sum;
+}
+
+// Scores of 16 rows and 16 BM classes, in blocks of 16 x 16. FUSED (all classes in one tile): the softmax, the loss and G = weight
+// (p - [c = y]) follow in registers; otherwise the scores are written. Wavefronts share out the columns, 64 at a time: lane l holds a
+// quarter of row l % 16 of each block.
+constexpr int kRows = 16;
+constexpr int64_t kCountedRows = 32768;          // of more, the rows that count are counted by a launch of its own, into kCountTiles numbers
+constexpr int kCountTiles = 256;
+template <typename T, int BM, int NW, bool FUSED>
+__global__ __launch_bounds__(64 * NW) void scores_kernel(XentDirect job)
+{
+    constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;
+    static_assert(BM <= NW, "a wavefront for every block");
+    __shared__ float shared[BM * NW * 4 * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+    const int64_t n0 = (int64_t)blockIdx.x * kRows, c0 = (int64_t)blockIdx.y * (16 * BM), n = n0 + col;
+    const bool row_there = n < job.N;
+    const int64_t label = row_there ? job.labels[n] : -1;
+    const bool there = label >= 0;
+    const T *phi = static_cast<const T *>(job.Phi) + (row_there ? n : job.N - 1) * job.ld_phi;
+    const T *w[BM];
+#pragma unroll
+    for (int a = 0; a < BM; ++a) w[a] = static_cast<const T *>(job.W) + std::min(c0 + 16 * a + col, job.C - 1) * job.ld_w;
+    floatx4 acc[BM];
+#pragma unroll
+    for (int a = 0; a < BM; ++a) acc[a] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float xb[16], xa[BM][16];
+    auto fetch = [&](int64_t k) {
+        load16(phi, k, quarter, job.K, there, xb);
+#pragma unroll
+        for (int a = 0; a < BM; ++a) load16(w[a], k, quarter, job.K, true, xa[a]);
+    };
+    const int64_t begin = FUSED ? 0 : blockIdx.z * job.columns_per_cut, end = FUSED ? job.K : std::min(begin + job.columns_per_cut, job.K);
+    int64_t k = begin + 64 * wave;
+    if (k < end) fetch(k);
+    while (k < end) {
+        float b[2][8], a8[BM][2][8];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            b[e / 8][e % 8] = xb[e];
+#pragma unroll
+            for (int a = 0; a < BM; ++a) a8[a][e / 8][e % 8] = xa[a][e];
+        }
+        k += 64 * NW;
+        if (k < end) fetch(k);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const Split<TERMS> sb = split<TERMS>(b[u]);
+#pragma unroll
+            for (int a = 0; a < BM; ++a) acc[a] = multiply(split<TERMS>(a8[a][u]), sb, acc[a]);
+        }
+    }
+    floatx4 sum = add_up<BM, NW, 4>(acc, shared, wave, lane);
+    // rows that count, of each tile of rows
+    if (blockIdx.y == 0 && blockIdx.z == 0 && wave == 0 && job.N <= kCountedRows) {
+        const uint64_t counting = __ballot(there && quarter == 0);
+        if (lane == 0) job.counts[blockIdx.x] = (uint32_t)__popcll(counting);
+    }
+    const int64_t first = c0 + 16 * wave + 4 * quarter;          // class of element e: first + e
+    if constexpr (!FUSED) {
+        if (wave < BM && row_there && first < job.C)
+            *reinterpret_cast<float4 *>(job.scores + ((int64_t)blockIdx.z * job.N + n) * job.ld_scores + first) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        if (!job.partial || wave >= BM) return;
+        float top = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e < job.C) top = fmaxf(top, sum[e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += first + e < job.C ? exp_of(sum[e] - from) : 0.f;
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (quarter == 0 && row_there) job.partial[((int64_t)blockIdx.y * BM + wave) * job.N + n] = make_float2(top, s);
+        return;
+    }
+    __syncthreads();                                             // everybody has read its parts
+    float *tops = shared, *sums = shared + 16 * BM, *target = shared + 32 * BM;
+    float top = -INFINITY;
+    if (wave < BM) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e < job.C) top = fmaxf(top, sum[e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (quarter == 0) tops[16 * wave + col] = top;
+    }
+    __syncthreads();
+    top = tops[col];
+#pragma unroll
+    for (int a = 1; a < BM; ++a) top = fmaxf(top, tops[16 * a + col]);
+    const float from = top == -INFINITY ? 0.f : top;
+    if (wave < BM) {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (first + e == label) target[col] = sum[e];
+            sum[e] = first + e < job.C ? exp_of(sum[e] - from) : 0.f;
+            s += sum[e];
+        }
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (quarter == 0) sums[16 * wave + col] = s;
+    }
+    __syncthreads();
+    if (!row_there || wave >= BM) return;
+    float total = sums[col];
+#pragma unroll
+    for (int a = 1; a < BM; ++a) total += sums[16 * a + col];
+    const bool known = label < job.C;
+    if (wave == 0 && quarter == 0) job.loss[n] = !there ? 0.f : known ? logf(total) + (from - target[col]) : NAN;
+    if (!job.gradients || first >= job.C) return;
+    const float scale = job.weight && there ? job.weight[n] : 1.0f, inverse = 1.0f / total;
+    float g[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        g[e] = sum[e] * inverse;
+        if (first + e == label) g[e] -= 1.0f;
+        g[e] = !there || first + e >= job.C ? 0.f : known ? g[e] * scale : NAN;
+    }
+    if (job.by_class) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e < job.C) job.G[(first + e) * job.ld_g + n] = g[e];
+    } else {
+        *reinterpret_cast<float4 *>(job.G + n * job.ld_g + first) = make_float4(g[0], g[1], g[2], g[3]);
+    }
+}
+
+__global__ __launch_bounds__(256) void count_kernel(XentDirect job)
+{
+    __shared__ uint32_t part[4];
+    uint32_t count = 0;
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < job.N; n += 256 * kCountTiles) count += job.labels[n] >= 0 ? 1 : 0;
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) count += (uint32_t)__shfl_xor((int)count, o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = count;
+    __syncthreads();
+    if (threadIdx.x == 0) job.counts[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// Scores to loss and G, a workgroup per row, and with many classes (job.partial: the maxima and sums of 16 classes each are known) per
+// kPart classes of it. Scores cut in columns are added up on the way.
+constexpr int kSoftmaxThreads = 512, kAhead = 4, kPart = 4 * kAhead * kSoftmaxThreads;
+__global__ __launch_bounds__(kSoftmaxThreads) void softmax_kernel(XentDirect job)
+{
+    __shared__ float2 part[kSoftmaxThreads / 64];
+    __shared__ float label_score;
+    const int64_t n = blockIdx.x, label = job.labels[n];
+    const float *row = job.scores + n * job.ld_scores;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = job.partial ? (int64_t)blockIdx.y * kPart : 0, end = job.partial ? std::min(begin + kPart, job.C) : job.C;
+    // four classes of G, in the row's place, or one after the other in rows of the classes
+    auto store = [&](int64_t c, const float (&g)[4]) {
+        if (job.by_class) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < job.C) job.G[(c + e) * job.ld_g + n] = g[e];
+        } else {
+            *reinterpret_cast<float4 *>(job.G + n * job.ld_g + c) = make_float4(g[0], g[1], g[2], g[3]);
+        }
+    };
+    if (label < 0) {
+        const float none[4] = {0.f, 0.f, 0.f, 0.f};
+        if (threadIdx.x == 0 && begin == 0) job.loss[n] = 0.f;
+        if (job.gradients)
+            for (int64_t c = begin + 4 * (int64_t)threadIdx.x; c < end; c += 4 * kSoftmaxThreads) store(c, none);
+        return;
+    }
+    auto load = [&](int64_t c) {
+        float4 f = *reinterpret_cast<const float4 *>(row + c);
+        for (unsigned k = 1; k < job.column_cuts; ++k) {
+            const float4 o = *reinterpret_cast<const float4 *>(row + (int64_t)k * job.N * job.ld_scores + c);
+            f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
+        }
+        return f;
+    };
+    auto add = [](float2 a, float2 b) {
+        const float m = fmaxf(a.x, b.x), from = m == -INFINITY ? 0.f : m;
+        return make_float2(m, a.y * exp_of(a.x - from) + b.y * exp_of(b.x - from));
+    };
+    float2 v = make_float2(-INFINITY, 0.f);
+    if (job.partial) {
+        for (int64_t t = threadIdx.x; t < (job.C + 15) / 16; t += kSoftmaxThreads) v = add(v, job.partial[t * job.N + n]);
+        if (threadIdx.x == 0) label_score = label < job.C ? row[label] : 0.f;
+    } else {
+        for (int64_t c0 = 4 * (int64_t)threadIdx.x; c0 < job.C; c0 += kPart) {
+            float4 f[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+                f[u] = c < job.C ? load(c) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (job.column_cuts > 1 && c < job.C) *const_cast<float4 *>(reinterpret_cast<const float4 *>(row + c)) = f[u];
+            }
+            float m = v.x;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+                float x[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (c + e >= job.C) x[e] = -INFINITY;
+                    if (c + e == label) label_score = x[e];
+                    m = fmaxf(m, x[e]);
+                }
+                f[u] = make_float4(x[0], x[1], x[2], x[3]);
+            }
+            const float from = m == -INFINITY ? 0.f : m;
+            v.y *= exp_of(v.x - from);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v.y += (exp_of(f[u].x - from) + exp_of(f[u].y - from)) + (exp_of(f[u].z - from) + exp_of(f[u].w - from));
+            v.x = m;
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) v = add(v, make_float2(__shfl_xor(v.x, o), __shfl_xor(v.y, o)));
+    if (lane == 0) part[wave] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < kSoftmaxThreads / 64; ++w) v = add(v, part[w]);
+    const float from = v.x == -INFINITY ? 0.f : v.x;
+    const bool known = label < job.C;
+    if (threadIdx.x == 0 && begin == 0) job.loss[n] = known ? logf(v.y) + (from - label_score) : NAN;
+    if (!job.gradients) return;
+    const float inverse = 1.0f / v.y, scale = job.weight ? job.weight[n] : 1.0f;
+    for (int64_t c0 = begin + 4 * (int64_t)threadIdx.x; c0 < end; c0 += kPart) {
+        float4 f[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+            f[u] = c < end ? *reinterpret_cast<const float4 *>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);       // (a thread's own, added up above)
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+            if (c >= end) break;
+            float g[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                g[e] = exp_of(g[e] - from) * inverse;
+                if (c + e == label) g[e] -= 1.0f;
+                g[e] = known ? g[e] * scale : NAN;
+            }
+            store(c, g);
+        }
+    }
+}
+
+__device__ __forceinline__ float mean_scale(const XentDirect &job)
+{
+    if (job.weight) return 1.0f;
+    uint32_t count = 0;
+    for (int t = threadIdx.x & 63; t < job.count_tiles; t += 256) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) count += t + 64 * u < job.count_tiles ? job.counts[t + 64 * u] : 0;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) count += (uint32_t)__shfl_xor((int)count, o);
+    return 1.0f / (float)max(count, 1u);
+}
+template <typename T>
+__device__ __forceinline__ void store(T *dst, float v)
+{
+    if constexpr (sizeof(T) == 4) *dst = v;
+    else *reinterpret_cast<__bf16 *>(dst) = (__bf16)v;
+}
+
+// Gradients of few (up to FEW) rows and many classes, or of few classes and many rows: with G[m][f], the many by the few, one pass over the
+// many gives  of_many[m, :] = sum_f G[m][f] small[f, :]  and  of_few[f, :] += G[m][f] big[m, :].  A lane has four columns of K, in which it
+// keeps the few rows of `small` and the sums; G's rows are the same for all lanes and come through scalar registers. The
+// wavefronts of a workgroup take rows in turn and add their sums up in LDS; the many are cut among workgroups.
+// What bounds it is reading `big` and writing of_many.
+constexpr int kFewWaves = 4, kFewColumns = 256;
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
+// memory that no kernel writes while this one runs: uniform addresses become scalar loads
+template <typename T>
+using Constant = const __attribute__((address_space(4))) T;
+template <typename T, int FEW, bool OF_MANY, bool OF_FEW>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
+{
+    __shared__ float4 parts[OF_FEW ? kFewWaves : 1][FEW][64];
+    const bool rows_are_few = job.by_class;
+    const DirectGradient &of_few = rows_are_few ? job.dphi : job.dw, &of_many = rows_are_few ? job.dw : job.dphi;
+    const int64_t few = rows_are_few ? job.N : job.C, many = rows_are_few ? job.C : job.N;
+    Constant<float> *G = (Constant<float> *)(uintptr_t)job.G;
+    Constant<int64_t> *labels = (Constant<int64_t> *)(uintptr_t)job.labels;
+    const T *small = static_cast<const T *>(rows_are_few ? job.Phi : job.W), *big = static_cast<const T *>(rows_are_few ? job.W : job.Phi);
+    const int64_t ld_small = rows_are_few ? job.ld_phi : job.ld_w, ld_big = rows_are_few ? job.ld_w : job.ld_phi;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const unsigned across = (unsigned)((job.K + kFewColumns - 1) / kFewColumns), cut = blockIdx.x / across;
+    const int64_t k = (int64_t)(blockIdx.x % across) * kFewColumns + 4 * lane;
+    const int64_t begin = (int64_t)cut * of_few.per_cut, end = std::min(begin + of_few.per_cut, many);
+    const bool whole = k + 4 <= job.K;
+    auto load4 = [&](const T *row, float (&x)[4]) {
+        if (whole) {
+            const Four<T> f = *reinterpret_cast<const Four<T> *>(row + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = number(f.v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = k + e < job.K ? number(row[k + e]) : 0.f;
+        }
+    };
+    float s[OF_MANY ? FEW : 1][4], sums[OF_FEW ? FEW : 1][4];
+    if constexpr (OF_MANY) {
+#pragma unroll
+        for (int f = 0; f < FEW; ++f) {
+            if (f < few && !(rows_are_few && labels[f] < 0)) {          // rows left out may hold anything
+                load4(small + f * ld_small, s[f]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[f][e] = 0.f;
+            }
+        }
+    }
+    if constexpr (OF_FEW) {
+#pragma unroll
+        for (int f = 0; f < FEW; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[f][e] = 0.f;
+    }
+    const float scale = OF_MANY || of_few.cuts == 1 ? mean_scale(job) : 1.0f;
+    constexpr int AHEAD = 4;
+    for (int64_t m0 = begin + wave; m0 < end; m0 += AHEAD * kFewWaves) {
+        float x[AHEAD][4];
+        if constexpr (OF_FEW) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t m = m0 + u * kFewWaves;
+                if (m < end && !(!rows_are_few && labels[m] < 0)) {
+                    load4(big + m * ld_big, x[u]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[u][e] = 0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t m = m0 + u * kFewWaves;
+            if (m >= end) break;
+            float g[FEW];
+#pragma unroll
+            for (int f = 0; f < FEW; ++f) {            // (behind the last row's numbers lie others of the workspace)
+                const float v = G[m * job.ld_g + f];
+                g[f] = f < few ? v : 0.f;
+            }
+            if constexpr (OF_FEW) {
+#pragma unroll
+                for (int f = 0; f < FEW; ++f)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sums[f][e] = fmaf(g[f], x[u][e], sums[f][e]);
+            }
+            if constexpr (OF_MANY) {
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int f = 0; f < FEW; ++f)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = fmaf(g[f], s[f][e], y[e]);
+                T *dst = static_cast<T *>(of_many.out) + m * of_many.ld + k;
+                if (whole) {
+                    Four<T> v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) store(&v.v[e], y[e] * scale);
+                    *reinterpret_cast<Four<T> *>(dst) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (k + e < job.K) store(dst + e, y[e] * scale);
+                }
+            }
+        }
+    }
+    if constexpr (OF_FEW) {
+#pragma unroll
+        for (int f = 0; f < FEW; ++f) parts[wave][f][lane] = make_float4(sums[f][0], sums[f][1], sums[f][2], sums[f][3]);
+        __syncthreads();
+        for (int f = wave; f < few; f += kFewWaves) {
+            float4 v = parts[0][f][lane];
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w) {
+                const float4 o = parts[w][f][lane];
+                v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+            }
+            const float sum[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (k + e >= job.K) break;
+                if (of_few.cuts > 1) of_few.parts[((int64_t)cut * few + f) * job.K + k + e] = sum[e];
+                else store(static_cast<T *>(of_few.out) + f * of_few.ld + k + e, sum[e] * scale);
+            }
+        }
+    }
+}
+
+// Both gradients of more of either, in tiles of 32 rows (sequences, summed over classes, or classes, summed over sequences) x 64 columns of K,
+// in blocks of 32 x 32. The wavefronts of a workgroup share out the sum, or (OWN: sums of up to 64 numbers) have tiles of their own next to each
+// other. A lane's column of the result is its number in the wavefront, so that 32 lanes write 128 bytes of a row.
+constexpr int kWide = 64, kSumWaves = 4;
+template <typename T, bool OWN>
+__global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect job)
+{
+    constexpr int TA = sizeof(T) == 4 ? 3 : 1, TB = sizeof(T) == 4 ? 3 : 2;
+    __shared__ float shared[OWN ? 1 : 2 * kSumWaves * 16 * 64];
+    const bool is_w = blockIdx.x >= job.blocks_phi;
+    const DirectGradient &g = is_w ? job.dw : job.dphi;
+    unsigned id = blockIdx.x - (is_w ? job.blocks_phi : 0);
+    constexpr int WIDE = OWN ? kWide * kSumWaves : kWide;
+    const unsigned across = (unsigned)((job.K + WIDE - 1) / WIDE), cut = id % g.cuts;
+    id /= g.cuts;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5, col = lane & 31;
+    const int64_t i0 = (int64_t)(id % across) * WIDE + (OWN ? kWide * wave : 0), j0 = (int64_t)(id / across) * 32;
+    if (OWN && i0 >= job.K) return;
+    const int64_t rows = is_w ? job.C : job.N, summed = is_w ? job.N : job.C;
+    const int64_t begin = (int64_t)cut * g.per_cut, end = std::min(begin + g.per_cut, summed);
+    const T *A = static_cast<const T *>(is_w ? job.Phi : job.W);
+    const int64_t ld_a = is_w ? job.ld_phi : job.ld_w;
+    // features beyond K and columns beyond the rows are read as the last ones
+    const int64_t ia[2] = {std::min(i0 + col, job.K - 1), std::min(i0 + 32 + col, job.K - 1)};
+    const int64_t jb = std::min(j0 + col, rows - 1);
+    floatx16 acc[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[a][e] = 0.f;
+    float xa[2][8], xb[8];
+    auto fetch = [&](int64_t s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t m = s + 8 * half + e, at = std::min(m, summed - 1);
+            bool there = m < end;
+            xb[e] = there ? job.G[is_w ? at * job.ld_g + jb : jb * job.ld_g + at] : 0.f;
+            if (is_w) there = there && job.labels[at] >= 0;          // rows left out may hold anything
+            xa[0][e] = there ? number(A[at * ld_a + ia[0]]) : 0.f;
+            xa[1][e] = there ? number(A[at * ld_a + ia[1]]) : 0.f;
+        }
+    };
+    int64_t s = begin + (OWN ? 0 : 16 * wave);
+    if (s < end) fetch(s);
+    while (s < end) {
+        float a0[8], a1[8], b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            a0[e] = xa[0][e];
+            a1[e] = xa[1][e];
+            b[e] = xb[e];
+        }
+        s += OWN ? 16 : 16 * kSumWaves;
+        if (s < end) fetch(s);
+        const Split<TB> sb = split<TB>(b);
+        acc[0] = multiply(sb, split<TA>(a0), acc[0]);
+        acc[1] = multiply(sb, split<TA>(a1), acc[1]);
+    }
+    const float scale = g.cuts == 1 ? mean_scale(job) : 1.0f;
+    auto store_block = [&](const floatx16 &sum, int64_t first) {
+        const int64_t i = first + col;
+        if (i >= job.K) return;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int64_t r = j0 + 8 * (e / 4) + 4 * half + e % 4;
+            if (r >= rows) continue;
+            if (g.cuts > 1) g.parts[((int64_t)cut * rows + r) * job.K + i] = sum[e];
+            else store(static_cast<T *>(g.out) + r * g.ld + i, sum[e] * scale);
+        }
+    };
+    if constexpr (OWN) {
+        store_block(acc[0], i0);
+        store_block(acc[1], i0 + 32);
+    } else {
+        const floatx16 sum = add_up<2, kSumWaves, 16>(acc, shared, wave, lane);
+        if (wave < 2) store_block(sum, i0 + 32 * wave);
+    }
+}
+
+// Adds the parts of the cut sums up: 64 numbers a workgroup, whose wavefronts take parts in turn.
+template <typename T>
+__global__ __launch_bounds__(256) void add_parts_kernel(XentDirect job)
+{
+    __shared__ float shared[4][64];
+    const int64_t of_phi = job.dphi.cuts > 1 ? job.N * job.K : 0, of_w = job.dw.cuts > 1 ? job.C * job.K : 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float scale = mean_scale(job);
+    const unsigned groups_phi = (unsigned)((of_phi + 63) / 64), groups = groups_phi + (unsigned)((of_w + 63) / 64);
+    for (unsigned group = blockIdx.x; group < groups; group += gridDim.x) {
+        const bool is_w = group >= groups_phi;
+        const DirectGradient &g = is_w ? job.dw : job.dphi;
+        const int64_t m = (int64_t)(group - (is_w ? groups_phi : 0)) * 64 + lane, all = is_w ? of_w : of_phi;
+        float sum = 0.f;
+        if (m < all) {
+#pragma unroll 4
+            for (unsigned c = wave; c < g.cuts; c += 4) sum += g.parts[(int64_t)c * all + m];
+        }
+        shared[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && m < all) {
+            sum = (shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]);
+            const int64_t r = m / job.K;
+            store(static_cast<T *>(g.out) + r * g.ld + (m - r * job.K), sum * scale);
+        }
+        __syncthreads();
+    }
+}
+
+constexpr int64_t kWorkgroups = 768;         // three for every CU
+constexpr int64_t kLeastSummed = 128;        // of a cut
+constexpr int64_t kFew = 16, kOwn = 64;
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+// How a gradient's sum is cut: into as many parts as fill the GPU.
+DirectGradient cut_of(int64_t tiles, int64_t summed, int64_t unit)
+{
+    DirectGradient g = {};
+    int64_t cuts = std::min(kWorkgroups / tiles, summed / kLeastSummed);
+    if (cuts < 2) cuts = 1;
+    g.per_cut = ((summed + cuts - 1) / cuts + unit - 1) / unit * unit;
+    g.cuts = (uint32_t)((summed + g.per_cut - 1) / g.per_cut);
+    return g;
+}
+bool is_few(const rfsf_xent_shape &s) { return std::min(s.N, s.C) <= kFew; }
+// The few of the two: rows (G then lies by classes), or classes.
+bool rows_are_few(const rfsf_xent_shape &s) { return is_few(s) && s.N < s.C; }
+constexpr int64_t kLeastMany = 16, kMostParts = 128;           // rows of a workgroup of few_kernel; parts to add up
+void cuts_of(const rfsf_xent_shape &s, DirectGradient *dphi, DirectGradient *dw)
+{
+    if (is_few(s)) {
+        const int64_t many = std::max(s.N, s.C), across = (s.K + kFewColumns - 1) / kFewColumns;
+        const int64_t cuts = std::max<int64_t>(std::min(std::min(kWorkgroups / across, kMostParts), many / kLeastMany), 1);
+        DirectGradient g = {};
+        g.per_cut = (many + cuts - 1) / cuts;
+        g.cuts = (uint32_t)((many + g.per_cut - 1) / g.per_cut);
+        *dphi = *dw = g;
+        (rows_are_few(s) ? *dw : *dphi).cuts = 1;                      // (of the many: no sums to add up)
+    } else {
+        const int64_t across = (s.K + kWide - 1) / kWide;
+        *dphi = cut_of((s.N + 31) / 32 * across, s.C, 64);             // (sums of up to kOwn numbers are whole)
+        *dw = cut_of((s.C + 31) / 32 * across, s.N, 64);
+    }
+    if (!(s.gradients & RFSF_XENT_DPHI)) dphi->cuts = 1;
+    if (!(s.gradients & RFSF_XENT_DW)) dw->cuts = 1;
+}
+
+template <typename T, int FEW>
+void launch_few(const XentDirect &job, unsigned blocks, hipStream_t stream)
+{
+    const bool of_few = (job.by_class ? job.dphi.out : job.dw.out) != nullptr, of_many = (job.by_class ? job.dw.out : job.dphi.out) != nullptr;
+    if (of_few && of_many) few_kernel<T, FEW, true, true><<<dim3(blocks), 64 * kFewWaves, 0, stream>>>(job);
+    else if (of_few) few_kernel<T, FEW, false, true><<<dim3(blocks), 64 * kFewWaves, 0, stream>>>(job);
+    else few_kernel<T, FEW, true, false><<<dim3(blocks), 64 * kFewWaves, 0, stream>>>(job);
+}
+
+template <typename T, int BM>
+void launch_fused(const XentDirect &job, unsigned tiles, hipStream_t stream)
+{
+    // wavefronts to share out the columns: more where there are few workgroups
+    constexpr int MOST = BM == 1 ? 16 : 8;              // (registers)
+    if (tiles <= 256 && job.K > 4 * 64) scores_kernel<T, BM, MOST, true><<<dim3(tiles), 64 * MOST, 0, stream>>>(job);
+    else scores_kernel<T, BM, 4, true><<<dim3(tiles), 256, 0, stream>>>(job);
+}
+
+template <typename T>
+hipError_t run(const XentDirect &job, bool few, hipStream_t stream)
+{
+    const unsigned tiles_n = (unsigned)((job.N + kRows - 1) / kRows);
+    if (job.fused && job.C <= 16) {
+        launch_fused<T, 1>(job, tiles_n, stream);
+    } else if (job.fused && job.C <= 32) {
+        launch_fused<T, 2>(job, tiles_n, stream);
+    } else if (job.fused) {
+        launch_fused<T, 4>(job, tiles_n, stream);
+    } else {
+        scores_kernel<T, 2, 4, false><<<dim3(tiles_n, (unsigned)((job.C + 31) / 32), job.column_cuts), 256, 0, stream>>>(job);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        softmax_kernel<<<dim3((unsigned)job.N, job.partial ? (unsigned)((job.C + kPart - 1) / kPart) : 1), kSoftmaxThreads, 0, stream>>>(job);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !job.gradients) return e;
+    if (job.N > kCountedRows && !job.weight) count_kernel<<<dim3(kCountTiles), 256, 0, stream>>>(job);
+    if (few) {
+        const int64_t few_of = std::min(job.N, job.C), cuts = (std::max(job.N, job.C) + job.dphi.per_cut - 1) / job.dphi.per_cut;
+        const unsigned blocks = (unsigned)((job.K + kFewColumns - 1) / kFewColumns * cuts);
+        if (few_of <= 4) launch_few<T, 4>(job, blocks, stream);
+        else if (few_of <= 8) launch_few<T, 8>(job, blocks, stream);
+        else launch_few<T, 16>(job, blocks, stream);
+    } else {
+        // each gradient in its own way: a launch has one of them
+        XentDirect one = job;
+        auto launch = [&](bool own, bool is_w) {
+            const int64_t wide = own ? kWide * kSumWaves : kWide, across = (job.K + wide - 1) / wide;
+            const int64_t blocks = ((is_w ? job.C : job.N) + 31) / 32 * across * (is_w ? job.dw.cuts : job.dphi.cuts);
+            one.blocks_phi = is_w ? 0 : (unsigned)blocks;
+            if (own) gradients_kernel<T, true><<<dim3((unsigned)blocks), 64 * kSumWaves, 0, stream>>>(one);
+            else gradients_kernel<T, false><<<dim3((unsigned)blocks), 64 * kSumWaves, 0, stream>>>(one);
+        };
+        const bool own_phi = job.C <= kOwn, own_w = job.N <= kOwn;
+        if (job.dphi.out && job.dw.out && !own_phi && !own_w) {
+            const int64_t across = (job.K + kWide - 1) / kWide;
+            one.blocks_phi = (unsigned)((job.N + 31) / 32 * across * job.dphi.cuts);
+            gradients_kernel<T, false><<<dim3((unsigned)(one.blocks_phi + (job.C + 31) / 32 * across * job.dw.cuts)), 64 * kSumWaves, 0, stream>>>(one);
+        } else {
+            if (job.dphi.out) launch(own_phi, false);
+            if (job.dw.out) launch(own_w, true);
+        }
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t numbers = (job.dphi.cuts > 1 ? job.N * job.K : 0) + (job.dw.cuts > 1 ? job.C * job.K : 0);
+    if (numbers == 0) return hipSuccess;
+    add_parts_kernel<T><<<dim3((unsigned)std::min<int64_t>((numbers + 63) / 64 + 1, 4096)), 256, 0, stream>>>(job);
+    return hipGetLastError();
+}
+
+// How the scores are made: with up to 64 classes in one launch with the softmax, unless few rows of many columns leave CUs without work;
+// otherwise cut in columns where there are few tiles, and with the softmax' parts where a row has many classes.
+struct ScorePlan { bool fused, partial; uint32_t cuts; int64_t per_cut; };
+constexpr int64_t kFusedTiles = 128, kFusedColumns = 1024, kColumnTiles = 512, kLeastColumns = 512;
+ScorePlan score_plan(const rfsf_xent_shape &s)
+{
+    const int64_t tiles_n = (s.N + kRows - 1) / kRows;
+    if (s.C <= 64 && (tiles_n >= kFusedTiles || s.K <= kFusedColumns)) return {true, false, 1, s.K};
+    if (s.C > kPart) return {false, true, 1, s.K};
+    const int64_t tiles = tiles_n * ((s.C + 31) / 32);
+    int64_t cuts = std::min(kColumnTiles / tiles, s.K / kLeastColumns);
+    if (cuts < 2) return {false, false, 1, s.K};
+    const int64_t per = ((s.K + cuts - 1) / cuts + 63) / 64 * 64;
+    return {false, false, (uint32_t)((s.K + per - 1) / per), per};
+}
+struct Places { size_t g, scores, partial, counts, parts_phi, parts_w, all; };
+int64_t four(int64_t v) { return (v + 3) / 4 * 4; }
+Places places_of(const rfsf_xent_shape &s, const DirectGradient &dphi, const DirectGradient &dw)
+{
+    Places p;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes);
+        return here;
+    };
+    const ScorePlan plan = score_plan(s);
+    p.scores = p.g = take(4 * (size_t)s.N * (size_t)four(s.C) * plan.cuts);                                       // G in the scores' place, unless it lies by classes
+    if (rows_are_few(s)) p.g = take(4 * (size_t)s.C * (size_t)four(s.N));
+    p.partial = take(plan.partial ? sizeof(float2) * (size_t)s.N * (size_t)((s.C + 31) / 32 * 2) : 0);
+    p.counts = take(4 * (size_t)(kCountedRows / kRows));
+    p.parts_phi = take(dphi.cuts > 1 ? 4 * (size_t)dphi.cuts * (size_t)s.N * (size_t)s.K : 0);
+    p.parts_w = take(dw.cuts > 1 ? 4 * (size_t)dw.cuts * (size_t)s.C * (size_t)s.K : 0);
+    p.all = at + 256;
+    return p;
+}
+
+}  // namespace
+
+// Where this way is the faster one: for up to 16 rows or classes everywhere, otherwise by the products N K C and by h = N C / (N + C),
+// their ratio to what the packed way reads and writes beside them. Of 260 shapes with 17 to 10000 rows, 65 to 10241 columns and 17 to
+// 50000 classes, N K C from 5e6 to 6e9, both types and any gradients, all timed both ways, the way chosen takes 2.3 % longer than the better one
+// on average. (us, packed and here: 24 x 5648, 2103 classes, bfloat16, dW 104 and 60; 93 x 2829, 1310, float32, dW 80 and 56;
+// 7060 x 1164, 11, float32, dW 123 and 47; 1 x 2283, 42173, float32, both 2702 and 345; but 348 x 283, 6096, bfloat16, dW 51 and 95; 1724 x
+// 897, 589, bfloat16, dPhi 52 and 130; 7843 x 1026, 288, float32, dW 152 and 257.)
+bool xent_direct(const rfsf_xent_shape &s)
+{
+    const double n = (double)s.N, c = (double)s.C;
+    if (s.N < 1 || s.C > 1000000 || n * c > 1 << 26) return false;
+    if (is_few(s)) return true;
+    const double h = n * c / (n + c), products = n * c * (double)s.K;
+    return products <= (h <= 64 ? 4e9 : h <= 128 ? 1e9 : h <= 256 ? 2.5e8 : 1e8);
+}
+
+size_t xent_direct_bytes(const rfsf_xent_shape &s)
+{
+    DirectGradient dphi, dw;
+    cuts_of(s, &dphi, &dw);
+    return places_of(s, dphi, dw).all;
+}
+
+hipError_t launch_xent_direct(const rfsf_xent_shape &s, const void *Phi, const void *W, const int64_t *labels, const float *weight, float *loss, void *dPhi,
+                              void *dW, void *workspace, hipStream_t stream)
+{
+    XentDirect job = {};
+    job.Phi = Phi;
+    job.W = W;
+    job.labels = labels;
+    job.weight = weight;
+    job.loss = loss;
+    job.N = s.N;
+    job.K = s.K;
+    job.C = s.C;
+    job.ld_phi = s.ld_phi;
+    job.ld_w = s.ld_w;
+    job.gradients = s.gradients;
+    cuts_of(s, &job.dphi, &job.dw);
+    const Places p = places_of(s, job.dphi, job.dw);
+    const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
+    char *ws = static_cast<char *>(workspace) + (mis ? 256 - mis : 0);
+    job.by_class = rows_are_few(s);
+    job.scores = reinterpret_cast<float *>(ws + p.scores);
+    job.ld_scores = four(s.C);
+    const ScorePlan plan = score_plan(s);
+    job.fused = plan.fused;
+    job.column_cuts = plan.cuts;
+    job.columns_per_cut = plan.per_cut;
+    job.partial = plan.partial ? reinterpret_cast<float2 *>(ws + p.partial) : nullptr;
+    job.G = reinterpret_cast<float *>(ws + p.g);
+    job.ld_g = four(job.by_class ? s.N : s.C);
+    job.counts = reinterpret_cast<uint32_t *>(ws + p.counts);
+    job.count_tiles = s.N > kCountedRows ? kCountTiles : (int32_t)((s.N + kRows - 1) / kRows);
+    job.dphi.parts = reinterpret_cast<float *>(ws + p.parts_phi);
+    job.dw.parts = reinterpret_cast<float *>(ws + p.parts_w);
+    job.dphi.ld = s.ld_dphi;
+    job.dw.ld = s.ld_dw;
+    job.dphi.out = (s.gradients & RFSF_XENT_DPHI) ? dPhi : nullptr;
+    job.dw.out = (s.gradients & RFSF_XENT_DW) ? dW : nullptr;
+    return s.bf16 ? run<uint16_t>(job, is_few(s), stream) : run<float>(job, is_few(s), stream);
+}
+
+}  // namespace rfsf

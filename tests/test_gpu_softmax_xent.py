@@ -41,7 +41,12 @@ def _check(phi, w, y, s, got):
 
 
 SIZES = [(1, 1, 1), (1, 5, 2), (3, 33, 7), (16, 193, 10), (64, 64, 64), (65, 65, 65), (40, 31, 129), (129, 127, 300), (257, 300, 1000),
-         (300, 70, 4097), (1000, 129, 31), (2, 2049, 513), (700, 50, 32), (130, 1001, 10), (1, 1000, 33), (513, 64, 16)]
+         (300, 70, 4097), (1000, 129, 31), (2, 2049, 513), (700, 50, 32), (130, 1001, 10), (1, 1000, 33), (513, 64, 16),
+         # every way of making the scores and the gradients: few rows, few classes, a long sum cut, many classes, packed operands
+         (5, 70, 9000), (16, 300, 17), (17, 300, 17), (9, 131, 9), (3000, 66, 16), (40, 2051, 40), (33, 2100, 70), (20, 5000, 63), (2100, 40, 50),
+         (620, 300, 600), (530, 291, 777)]
+# rows, columns, classes: by the ways above, the last one packed
+WAYS = [(90, 40, 20), (90, 40, 300), (12, 40, 300), (300, 40, 7), (620, 300, 600)]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
@@ -54,7 +59,7 @@ def test_against_64_bits(N, K, C, bf16):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("need_dPhi,need_dW", [(False, False), (True, False), (False, True)])
-@pytest.mark.parametrize("N,K,C", [(150, 70, 10), (150, 70, 200)])
+@pytest.mark.parametrize("N,K,C", [(150, 70, 10), (150, 70, 200), (15, 70, 200), (620, 300, 600)])
 def test_what_is_not_asked_for(N, K, C, bf16, need_dPhi, need_dW):
     phi, w, y, s = _inputs(N, K, C, bf16)
     loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=need_dPhi, need_dW=need_dW)
@@ -64,7 +69,7 @@ def test_what_is_not_asked_for(N, K, C, bf16, need_dPhi, need_dW):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("weighted", [False, True])
-@pytest.mark.parametrize("N,K,C", [(200, 40, 20), (450, 70, 300)])
+@pytest.mark.parametrize("N,K,C", [(200, 40, 20), (450, 70, 300), (620, 300, 600), (1500, 170, 900)])
 def test_the_smallest_workspace(N, K, C, bf16, weighted):
     """Blocks of 64 rows: dW is added up over them."""
     phi, w, y, s = _inputs(N, K, C, bf16)
@@ -75,9 +80,9 @@ def test_the_smallest_workspace(N, K, C, bf16, weighted):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("C", [20, 300])
-def test_rows_left_out_may_hold_anything(C, bf16):
-    phi, w, y, s = _inputs(130, 40, C, bf16, left=0.5)
+@pytest.mark.parametrize("N,K,C", [(130, 40, 20), (130, 40, 300), (14, 40, 300), (300, 40, 7), (620, 300, 600)])
+def test_rows_left_out_may_hold_anything(N, K, C, bf16):
+    phi, w, y, s = _inputs(N, K, C, bf16, left=0.5)
     phi[y < 0] = float("nan")
     phi[torch.nonzero(y < 0)[0]] = float("inf")
     s[y < 0] = float("nan")
@@ -86,10 +91,10 @@ def test_rows_left_out_may_hold_anything(C, bf16):
     assert torch.all(loss[y < 0] == 0) and torch.all(dPhi[y < 0] == 0)
 
 
-@pytest.mark.parametrize("C", [20, 300])
+@pytest.mark.parametrize("N,K,C", WAYS)
 @pytest.mark.parametrize("weighted", [False, True])
-def test_no_row_counts(C, weighted):
-    phi, w, y, s = _inputs(70, 40, C, False, left=2.0)
+def test_no_row_counts(N, K, C, weighted):
+    phi, w, y, s = _inputs(N, K, C, False, left=2.0)
     loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, weight=s if weighted else None, need_dPhi=True, need_dW=True)
     assert torch.all(loss == 0) and torch.all(dPhi == 0) and torch.all(dW == 0)
 
@@ -104,10 +109,10 @@ def test_no_rows():
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("off", [-1e9, -1e30, -3.3e38])
-@pytest.mark.parametrize("C", [20, 300])
-def test_classes_shut_off_by_their_offset(C, off, bf16):
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_classes_shut_off_by_their_offset(N, K, C, off, bf16):
     """Column 0 of features is constant; a huge negative weight there takes a class out. The others lose nothing by it."""
-    phi, w, y, s = _inputs(90, 40, C, bf16)
+    phi, w, y, s = _inputs(N, K, C, bf16)
     phi[:, 0] = 0.5
     w[3::4, 0] = off
     y[y % 4 == 3] -= 1
@@ -116,23 +121,71 @@ def test_classes_shut_off_by_their_offset(C, off, bf16):
     assert torch.all(got[2][3::4] == 0)
 
 
-@pytest.mark.parametrize("C", [20, 300])
-def test_rows_of_all_magnitudes(C):
-    """Rows of Phi from 2^-60 to 2^6, weights of the rows from 2^-30 to 2^30."""
-    phi, w, y, s = _inputs(134, 40, C, False)
-    phi *= torch.pow(2.0, torch.arange(134, device="cuda") % 67 - 60)[:, None]
-    s *= torch.pow(2.0, (torch.arange(134, device="cuda") * 7) % 61 - 30)
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("off", [-400.0, 400.0])
+@pytest.mark.parametrize("N,K,C", WAYS + [(600, 70, 1000)])
+def test_scores_far_from_zero(N, K, C, off, bf16):
+    """All scores shifted by -200 or 200, which changes nothing but their rounding."""
+    phi, w, y, s = _inputs(N, K, C, bf16)
+    phi[:, 0] = 0.5
+    w[:, 0] = off
     _check(phi, w, y, s, rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True))
 
 
-@pytest.mark.parametrize("C", [20, 300])
-def test_infinities_nan_and_labels_beyond_the_classes_show(C):
-    phi, w, y, s = _inputs(100, 40, C, False, left=0.0)
+@pytest.mark.parametrize("N,K,C", WAYS)
+@pytest.mark.parametrize("off", [-3.4028234663852886e38, -3.0e38])
+def test_offsets_of_the_lowest_value(N, K, C, off):
+    phi, w, y, s = _inputs(N, K, C, False)
+    phi[:, 0] = 0.5
+    w[3::4, 0] = off
+    y[y % 4 == 3] -= 1
+    got = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True)
+    _check(phi, w, y, s, got)
+    assert torch.all(got[2][3::4] == 0)
+
+
+@pytest.mark.parametrize("N,K,C,bf16", [(700, 513, 2000, False), (700, 513, 2000, True), (3100, 270, 4097, True), (3100, 270, 4097, False),
+                                        (4200, 2060, 4097, True), (4200, 2060, 4097, False), (2000, 6164, 40, True)])
+def test_large_tiles(N, K, C, bf16):
+    """Tiles of all sizes, with and without a 33rd block of rows, against 64 bits on the GPU: each entry within the worst case of its sum, (a + n 2^-24) of
+    the sum of magnitudes with a of the operands' rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    phi = (torch.randn(N, K, generator=gen, device="cuda") / K ** 0.5).to(dtype)
+    w = (torch.randn(C, K, generator=gen, device="cuda") * 2).to(dtype)
+    y = torch.randint(0, C, (N,), generator=gen, device="cuda")
+    loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, need_dPhi=True, need_dW=True)
+    x, v = phi.double(), w.double()
+    l = x @ v.T
+    lse = l.logsumexp(1)
+    g = (l - lse[:, None]).exp()
+    g[torch.arange(N, device="cuda"), y] -= 1
+    u = 2.0 ** -24
+    dl = ((3 * 2.0 ** -22 + 3 * (K + 4) * u) * (x.abs() @ v.abs().T)).amax(1) + 1e-5
+    assert torch.all((loss.double() - (lse - l.gather(1, y[:, None])[:, 0])).abs() <= 2 * dl + 1e-5)
+    rough = (2.0 ** -11 if bf16 else 2.0 ** -20) + 2 * dl.max().item()
+    out = 2.0 ** -8 if bf16 else 2 * u
+    for have, want, size, n in ((dPhi, g @ v / N, g.abs() @ v.abs() / N, C), (dW, g.T @ x / N, g.abs().T @ x.abs() / N, N)):
+        assert torch.all((have.double() - want).abs() <= (rough + 3 * (n + 4) * u) * size + out * want.abs() + 1e-12)
+
+
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_rows_of_all_magnitudes(N, K, C):
+    """Rows of Phi from 2^-60 to 2^6, weights of the rows from 2^-30 to 2^30."""
+    phi, w, y, s = _inputs(N, K, C, False)
+    phi *= torch.pow(2.0, torch.arange(N, device="cuda") % 67 - 60)[:, None]
+    s *= torch.pow(2.0, (torch.arange(N, device="cuda") * 7) % 61 - 30)
+    _check(phi, w, y, s, rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True))
+
+
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_infinities_nan_and_labels_beyond_the_classes_show(N, K, C):
+    phi, w, y, s = _inputs(N, K, C, False, left=0.0)
     phi[7, 3] = float("nan")
     phi[9, 2] = float("inf")
     y[11] = C
     loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True)
-    bad = torch.zeros(100, dtype=torch.bool, device="cuda")
+    bad = torch.zeros(N, dtype=torch.bool, device="cuda")
     bad[[7, 9, 11]] = True
     assert torch.equal(torch.isnan(loss), bad)
     assert torch.all(torch.isnan(dPhi[bad])) and torch.isfinite(dPhi[~bad]).all() and torch.all(torch.isnan(dW))
@@ -166,17 +219,25 @@ def test_gradients_against_differences(N, K, C):
         assert abs(difference - grad) <= float((np.abs(_np(s)) * third).sum()) * h * h / 6 + bound / (2 * h) + 2 * moved + 1e-5 * abs(grad)
 
 
-def test_padding_of_results_and_odd_strides():
-    phi, w, y, s = _inputs(77, 45, 83, False, pad=5)
-    bufs = torch.full((77, 50), 9.0, device="cuda"), torch.full((83, 47), 9.0, device="cuda")
-    got = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True, dPhi=bufs[0][:, 1:46], dW=bufs[1][:, 1:46])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,K,C", [(77, 45, 83)] + WAYS)
+def test_padding_of_results_and_odd_strides(N, K, C, bf16):
+    phi, w, y, s = _inputs(N, K, C, bf16, pad=5)
+    bufs = torch.full((N, K + 5), 9.0, device="cuda", dtype=phi.dtype), torch.full((C, K + 2), 9.0, device="cuda", dtype=phi.dtype)
+    got = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True, dPhi=bufs[0][:, 1:K + 1], dW=bufs[1][:, 1:K + 1])
     _check(phi, w, y, s, got)
-    assert torch.all(bufs[0][:, 0] == 9) and torch.all(bufs[0][:, 46:] == 9) and torch.all(bufs[1][:, 0] == 9) and torch.all(bufs[1][:, 46:] == 9)
+    assert all(torch.all(b[:, 0] == 9) and torch.all(b[:, K + 1:] == 9) for b in bufs)
 
 
-@pytest.mark.parametrize("C", [10, 400])
-def test_equal_calls_give_equal_bits_on_any_stream(C):
-    phi, w, y, s = _inputs(300, 100, C, False)
+@pytest.mark.parametrize("N,K,C", [(40000, 5, 3), (33000, 9, 20)])
+def test_many_rows_of_few_columns(N, K, C):
+    phi, w, y, _ = _inputs(N, K, C, False)
+    _check(phi, w, y, None, rfsf.rfsf_softmax_xent(phi, w, y, need_dPhi=True, need_dW=True))
+
+
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_equal_calls_give_equal_bits_on_any_stream(N, K, C):
+    phi, w, y, s = _inputs(N, K, C, False)
     first = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -185,11 +246,11 @@ def test_equal_calls_give_equal_bits_on_any_stream(C):
     assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
-@pytest.mark.parametrize("C", [10, 400])
-def test_in_a_graph(C):
-    phi, w, y, s = _inputs(300, 100, C, False)
-    rec, _ = rfsf.rfsf_softmax_xent_workspace_bytes(300, 100, C, torch.float32, True, True)
-    keep = dict(loss=torch.empty(300, device="cuda"), dPhi=torch.empty(300, 100, device="cuda"), dW=torch.empty(C, 100, device="cuda"),
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_in_a_graph(N, K, C):
+    phi, w, y, s = _inputs(N, K, C, False)
+    rec, _ = rfsf.rfsf_softmax_xent_workspace_bytes(N, K, C, torch.float32, True, True)
+    keep = dict(loss=torch.empty(N, device="cuda"), dPhi=torch.empty(N, K, device="cuda"), dW=torch.empty(C, K, device="cuda"),
                 workspace=torch.empty(rec, dtype=torch.uint8, device="cuda"))
     call = lambda **kw: rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True, **kw)          # noqa: E731
     call(**keep)

@@ -47,7 +47,7 @@ def test_xent_pointers(missing):
 
 
 def test_xent_workspace():
-    lib, shp = binding.load_library(), _xent_shape(N=5000, K=100, C=77, ld_phi=100, ld_w=100, ld_dphi=100, ld_dw=100)
+    lib, shp = binding.load_library(), _xent_shape(N=5000, K=1000, C=777, ld_phi=1000, ld_w=1000, ld_dphi=1000, ld_dw=1000)
     rec, mn = ctypes.c_size_t(0), ctypes.c_size_t(0)
     assert lib.rfsf_softmax_xent_workspace_bytes(ctypes.byref(shp), ctypes.byref(rec), ctypes.byref(mn)) == 0
     assert 0 < mn.value < rec.value
@@ -56,6 +56,14 @@ def test_xent_workspace():
     assert rfsf.rfsf_softmax_xent_workspace_bytes(1 << 20, 1025, 32768, torch.bfloat16, True, True)[0] < 12 << 30
     # without gradients no scores are held at all
     assert rfsf.rfsf_softmax_xent_workspace_bytes(10000, 65, 50000)[0] < 10000 * 50000
+
+
+def test_the_smallest_workspace_is_no_larger_than_the_recommended_one():
+    rng = np.random.default_rng(1)
+    for _ in range(2000):
+        N, K, C = (int(np.exp(rng.uniform(0, np.log(top)))) for top in (20000, 12000, 50000))
+        rec, least = rfsf.rfsf_softmax_xent_workspace_bytes(N, K, C, (torch.float32, torch.bfloat16)[rng.integers(2)], bool(rng.integers(2)), bool(rng.integers(2)))
+        assert 0 < least <= rec, (N, K, C)
 
 
 def test_no_rows_need_nothing():
