@@ -5,6 +5,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
+import numpy as np
 import torch
 
 from .binding import _check, _dev, _empty_on, _stream_ptr, load_library
@@ -100,9 +101,10 @@ def rfsf_softmax_xent(Phi: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, 
 class RfsfAdamW:
     """AdamW over many tensors, with states of 32 bits or of 8 (256 numbers to a scale).
 
-    params: float32 tensors, contiguous, on the device, updated in place by step(). copies: bfloat16 tensors of the same shapes that
-    receive the updated parameters. state: the states' tensors to use, a dict of lists `m`, `v` (float32, or int8 and uint8) and with
-    8 bits `m_scale`, `v_scale` (float32, ceil(n / 256) each); fresh ones if None. The same dict is kept as `self.state`."""
+    params: float32 tensors, contiguous, on the device, updated in place by step(); the optimizer keeps views of their memory, so that
+    a parameter whose `.data` is replaced later is not followed. copies: bfloat16 tensors of the same shapes that receive the updated
+    parameters. state: the states' tensors to use, a dict of lists `m`, `v` (float32, or int8 and uint8) and with 8 bits `m_scale`,
+    `v_scale` (float32, ceil(n / 256) each); fresh ones if None. `self.state` holds them in the same form."""
 
     BLOCK = 256
 
@@ -110,7 +112,7 @@ class RfsfAdamW:
                  copies: Optional[Sequence[torch.Tensor]] = None):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
-        self.params = [_dev(p, torch.float32, "params") for p in params]
+        self.params = [_dev(p, torch.float32, "params").detach() for p in params]
         self.state_bits = state_bits
         eight = state_bits == 8
         types = {"m": torch.int8 if eight else torch.float32, "v": torch.uint8 if eight else torch.float32}
@@ -136,10 +138,16 @@ class RfsfAdamW:
             for c, p in zip(copies, self.params):
                 if _dev(c, torch.bfloat16, "copies").numel() != p.numel():
                     raise ValueError("copies do not fit their parameters")
-        self.state, self.copies = state, copies
-
-    def _tensors(self):
-        return (_AdamwTensor * len(self.params))()
+        state = {k: [t.detach() for t in state[k]] for k in types}
+        self.state, self.copies = state, None if copies is None else [c.detach() for c in copies]
+        # the tensors' descriptions (rfsf_adamw_tensor: eight words each); the gradients' addresses come with each step
+        self._sizes = [p.numel() for p in self.params]
+        self._words = np.zeros((len(self.params), 8), dtype=np.int64)
+        columns = {0: self.params, 2: state["m"], 3: state["v"], 4: state.get("m_scale"), 5: state.get("v_scale"), 6: self.copies}
+        for k, tensors in columns.items():
+            if tensors:
+                self._words[:, k] = [t.data_ptr() for t in tensors]
+        self._words[:, 7] = self._sizes
 
     def step(self, grads: Sequence[torch.Tensor], step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -147,22 +155,14 @@ class RfsfAdamW:
         `grad_scale` first."""
         if len(grads) != len(self.params):
             raise ValueError("grads must hold a tensor for each parameter")
-        dtype = grads[0].dtype if grads else torch.float32
+        if not grads:
+            return
+        dtype = grads[0].dtype
         if dtype not in _BF16:
             raise ValueError("grads must be float32 or bfloat16")
-        array, state, eight, copies = self._tensors(), self.state, self.state_bits == 8, self.copies
-        for k, (p, g) in enumerate(zip(self.params, grads)):
-            n = p.numel()
-            if _dev(g, dtype, "grads").numel() != n:
-                raise ValueError("grads do not fit their parameters")
-            t = array[k]
-            t.param, t.grad, t.m, t.v, t.n = p.data_ptr(), g.data_ptr(), state["m"][k].data_ptr(), state["v"][k].data_ptr(), n
-            if eight:
-                t.m_scale, t.v_scale = state["m_scale"][k].data_ptr(), state["v_scale"][k].data_ptr()
-            if copies is not None:
-                t.copy = copies[k].data_ptr()
+        self._words[:, 1] = _addresses(grads, self._sizes, dtype, "grads")
         config = _AdamwConfig(lr, betas[0], betas[1], eps, weight_decay, grad_scale, step, self.state_bits, _BF16[dtype])
-        _check(load_library().rfsf_adamw_step(ctypes.byref(array), len(array), ctypes.byref(config), _stream_ptr(stream)))
+        _check(load_library().rfsf_adamw_step(self._words.ctypes.data, len(grads), ctypes.byref(config), _stream_ptr(stream)))
 
     def moments(self, out=None, stream: Optional[torch.cuda.Stream] = None):
         """(m, v): lists of float32 tensors, what the states hold. 32 bits: the states themselves; 8 bits: the numbers that the codes
@@ -171,21 +171,20 @@ class RfsfAdamW:
             return self.state["m"], self.state["v"]
         if out is None:
             out = tuple([_empty_on(stream, p.shape, dtype=torch.float32, device=p.device) for p in self.params] for _ in range(2))
-        n, state, array = len(self.params), self.state, self._tensors()
-        places = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)()
-        for which in range(2):
-            if len(out[which]) != n:
-                raise ValueError("out must hold a tensor for each parameter, twice")
-            for k, (t, p) in enumerate(zip(out[which], self.params)):
-                if _dev(t, torch.float32, "out").numel() != p.numel():
-                    raise ValueError("out does not fit the parameters")
-                places[which][k] = t.data_ptr()
-        for k, p in enumerate(self.params):
-            t = array[k]
-            t.m, t.v, t.n = state["m"][k].data_ptr(), state["v"][k].data_ptr(), p.numel()
-            t.m_scale, t.v_scale = state["m_scale"][k].data_ptr(), state["v_scale"][k].data_ptr()
-        _check(load_library().rfsf_adamw_moments(ctypes.byref(array), n, ctypes.byref(places[0]), ctypes.byref(places[1]), _stream_ptr(stream)))
+        if any(len(tensors) != len(self.params) for tensors in out):
+            raise ValueError("out must hold a tensor for each parameter, twice")
+        places = [np.array(_addresses(tensors, self._sizes, torch.float32, "out"), dtype=np.int64) for tensors in out]
+        _check(load_library().rfsf_adamw_moments(self._words.ctypes.data, len(self.params), places[0].ctypes.data, places[1].ctypes.data,
+                                                 _stream_ptr(stream)))
         return out
+
+
+def _addresses(tensors, sizes, dtype, name):
+    """Addresses of contiguous device tensors of this type and these numbers of elements."""
+    for t, n in zip(tensors, sizes):
+        if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} device tensors of the parameters' sizes")
+    return [t.data_ptr() for t in tensors]
 
 
 def _code_room(K: int) -> int:

@@ -43,7 +43,8 @@ def test_codes_are_the_definition_and_the_room_is_cleared(N, K, bf16):
 
 
 SIZES = [(1, 1, 1), (1, 1000, 1025), (2, 33, 64), (3, 40, 65), (5, 1000, 300), (8, 777, 129), (9, 500, 1001), (16, 65, 40), (17, 300, 2049), (40, 63, 5),
-         (64, 64, 128), (65, 129, 127), (300, 257, 70), (130, 3000, 513), (1, 7, 10241), (4, 4, 131072)]
+         (64, 64, 128), (65, 129, 127), (300, 257, 70), (130, 3000, 513), (1, 7, 10241), (4, 4, 131072),
+         (8, 100, 1024), (8, 100, 1025), (16, 300, 511), (3, 17000, 129), (12, 16385, 200), (16, 20001, 70), (260, 17000, 33), (2500, 5124, 40)]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
