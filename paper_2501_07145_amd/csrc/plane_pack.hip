@@ -10,7 +10,23 @@ namespace {
 constexpr int kEdge = 64;                 // of a tile that is packed
 constexpr int kRowsPerGroup = 4;          // rows of a workgroup that searches, one a wavefront
 
-// A wavefront takes a row, four numbers of it a lane and step.
+// Eight numbers of a row from k on.
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Eight { T v[8]; };
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int64_t k, int64_t K, float (&x)[8])
+{
+    if (k + 8 <= K) {
+        const Eight<T> c = *reinterpret_cast<const Eight<T> *>(row + k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = plane::number(c.v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e < K ? plane::number(row[k + e]) : 0.f;
+    }
+}
+
+// A wavefront takes a row, eight numbers of it a lane and load, two loads at a time.
 template <typename T>
 __global__ __launch_bounds__(64 * kRowsPerGroup) void largest_kernel(PackPair pair, unsigned groups_of_first)
 {
@@ -23,10 +39,12 @@ __global__ __launch_bounds__(64 * kRowsPerGroup) void largest_kernel(PackPair pa
     uint32_t largest = 0;
     if (!(job.labels && job.labels[row] < 0)) {
         const T *src = static_cast<const T *>(job.src) + row * job.ld;
-        for (int64_t k = lane; k < job.K; k += 256) {
+        for (int64_t k = 8 * lane; k < job.K; k += 1024) {
+            float x[2][8];
+            load8(src, k, job.K, x[0]);
+            load8(src, k + 512, job.K, x[1]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (k + 64 * u < job.K) largest = max(largest, __float_as_uint(plane::number(src[k + 64 * u])) & 0x7fffffffu);
+            for (int e = 0; e < 8; ++e) largest = max(largest, max(__float_as_uint(x[0][e]) & 0x7fffffffu, __float_as_uint(x[1][e]) & 0x7fffffffu));
         }
 #pragma unroll
         for (int o = 32; o > 0; o /= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, o));
@@ -44,27 +62,41 @@ __global__ __launch_bounds__(256) void pack_kernel(PackPair pair, unsigned tiles
     const int64_t r0 = (int64_t)(id / across) * kEdge, c0 = (int64_t)(id % across) * kEdge;
     const T *src = static_cast<const T *>(job.src);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = c0 + lane;
-#pragma unroll 4
-    for (int r = wave; r < kEdge; r += 4) {
-        const int64_t row = r0 + r;
-        const bool there = row < job.R && c < job.K && !(job.labels && job.labels[row] < 0);
-        tile[r][lane] = there ? ldexpf(plane::number(src[row * job.ld + c]), shift_of(job.largest[row])) : 0.f;
-    }
-    __syncthreads();
     const int at = threadIdx.x >> 3, group = threadIdx.x & 7;       // a row (column) of the tile and eight numbers of it
+    float x[kEdge / 32][8];
+    int shift[kEdge / 32];
 #pragma unroll
-    for (int u = 0; u < kEdge; u += 32) {
-        float x[8];
-        if (r0 + at + u < job.R) {
+    for (int u = 0; u < kEdge / 32; ++u) {
+        const int64_t row = r0 + at + 32 * u;
+        const bool there = row < job.R && !(job.labels && job.labels[row] < 0);
+        shift[u] = there ? shift_of(job.largest[row]) : 0;
+        if (there) {
+            load8(src + row * job.ld, c0 + 8 * group, job.K, x[u]);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = tile[at + u][8 * group + e];
-            plane::store_terms<TWO>(job.rows + (r0 + at + u) * job.pitch_rows, c0 + 8 * group, plane::terms_of<TWO>(x));
+            for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
         }
-        if (job.columns && c0 + at + u < job.K) {
+    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = tile[8 * group + e][at + u];
-            plane::store_terms<TWO>(job.columns + (c0 + at + u) * job.pitch_columns, r0 + 8 * group, plane::terms_of<TWO>(x));
+    for (int u = 0; u < kEdge / 32; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] = ldexpf(x[u][e], shift[u]);
+        const int64_t row = r0 + at + 32 * u;
+        if (row < job.R) plane::store_terms<TWO>(job.rows + row * job.pitch_rows, c0 + 8 * group, plane::terms_of<TWO>(x[u]));
+        if (job.columns) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[at + 32 * u][8 * group + e] = x[u][e];
+        }
+    }
+    if (job.columns) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kEdge; u += 32) {
+            if (c0 + at + u >= job.K) break;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = tile[8 * group + e][at + u];
+            plane::store_terms<TWO>(job.columns + (c0 + at + u) * job.pitch_columns, r0 + 8 * group, plane::terms_of<TWO>(y));
         }
     }
     if (second && pair.stats && c0 == 0 && wave == 0) {             // the rows of this tile

@@ -305,18 +305,30 @@ inline bool plane_extra(int64_t rows_a, int tile) { return tile == 256 && rows_a
 inline int64_t plane_tiles_a(int64_t rows_a, int tile) { return plane_extra(rows_a, tile) ? rows_a / tile : (rows_a + tile - 1) / tile; }
 inline int64_t plane_tiles(int64_t rows_a, int64_t rows_b, int tile) { return plane_tiles_a(rows_a, tile) * ((rows_b + tile - 1) / tile); }
 
-// The edge of a launch's tiles, from their number at an edge. 256: eight wavefronts, one workgroup a CU; the smaller ones where
-// the larger would leave CUs without work.
+// The edge of a launch's tiles: the one of which the steps take the least time, from the number of tiles that each edge makes (of the longest
+// product's steps). A CU holds one tile of 256 or 128, or two of 64; a step of a tile takes 1.2, 0.48 and 0.22 us where few CUs have any and
+// up to 2.1, 0.88 and 0.57 where all do, as the L2s deliver about 9.5 TB/s. (us a step over all tiles, edges 64, 128, 256, 8-bit
+// products of 81 steps but the last: 128 x 16384 rows 0.36, 0.62, 1.29; 128 x 24576 0.96, 0.67, 1.42; 128 x 65536 2.55, 1.91, 1.98; 256 x 32768 2.22,
+// 1.52, 1.74, where 256 is chosen; 256 x 65536 4.51, 3.10, 2.45; 333 x 10000, 41 steps 0.80, 0.65, 1.73.)
 template <typename Tiles>
 int plane_tile_of(const Tiles &tiles)
 {
-    if (tiles(256) >= 192) return 256;
-    if (tiles(128) >= 192) return 128;
-    return 64;
+    struct { int edge; double slots, alone, beside; } const ways[] = {{256, 256, 1.2, 0.9}, {128, 256, 0.48, 0.4}, {64, 512, 0.22, 0.35}};
+    int best = 0;
+    double least = 0.0;
+    for (const auto &way : ways) {
+        const double n = tiles(way.edge), full = (double)(int64_t)(n / way.slots), rest = n - full * way.slots;
+        const double time = full * (way.alone + way.beside) + (rest > 0 ? way.alone + way.beside * rest / way.slots : 0.0);
+        if (best == 0 || time < least) {
+            best = way.edge;
+            least = time;
+        }
+    }
+    return best;
 }
 inline int plane_tile(int64_t rows_a, int64_t rows_b)
 {
-    return plane_tile_of([&](int edge) { return plane_tiles(rows_a, rows_b, edge); });
+    return plane_tile_of([&](int edge) { return (double)plane_tiles(rows_a, rows_b, edge); });
 }
 
 namespace plane {

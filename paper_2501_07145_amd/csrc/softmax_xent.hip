@@ -510,9 +510,11 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
                                              Gradient{to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr,
                                                       stats, count, add, sums ? K : shape.ld_dw}};
         }
+        const int64_t longest = count_of_products > 1 ? std::max(products[0].steps, products[1].steps) : products[0].steps;
         const int edge = plane_tile_of([&](int e) {
-            int64_t tiles = 0;
-            for (int k = 0; k < count_of_products; ++k) tiles += plane_tiles(products[k].A.rows, products[k].B.rows, e);
+            double tiles = 0;
+            for (int k = 0; k < count_of_products; ++k)
+                tiles += (double)plane_tiles(products[k].A.rows, products[k].B.rows, e) * (double)products[k].steps / (double)longest;
             return tiles;
         });
         RFSF_TRY(launch_plane_products<MODE>(products, count_of_products, edge, stream));
