@@ -261,14 +261,22 @@ __global__ __launch_bounds__(256) void count_kernel(XentDirect job)
 
 // Scores to loss and G, a workgroup per row, and with many classes (job.partial: the maxima and sums of 16 classes each are known) per
 // kPart classes of it. Scores cut in columns are added up on the way.
+// THREADS a row, and rows of few classes several to a workgroup of 256.
 constexpr int kSoftmaxThreads = 512, kAhead = 4, kPart = 4 * kAhead * kSoftmaxThreads;
-__global__ __launch_bounds__(kSoftmaxThreads) void softmax_kernel(XentDirect job)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void softmax_kernel(XentDirect job)
 {
-    __shared__ float2 part[kSoftmaxThreads / 64];
-    __shared__ float label_score;
-    const int64_t n = blockIdx.x, label = job.labels[n];
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1, STEP = 4 * kAhead * THREADS;
+    static_assert(THREADS == 64 || ROWS == 1, "a wavefront or a workgroup for a row");
+    __shared__ float2 part[THREADS / 64];
+    __shared__ float label_scores[ROWS];
+    const int thread = threadIdx.x % THREADS;
+    float &label_score = label_scores[threadIdx.x / THREADS];
+    const int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    if (n >= job.N) return;                              // (whole wavefronts that meet no barrier)
+    const int64_t label = job.labels[n];
     const float *row = job.scores + n * job.ld_scores;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = thread >> 6;
     const int64_t begin = job.partial ? (int64_t)blockIdx.y * kPart : 0, end = job.partial ? std::min(begin + kPart, job.C) : job.C;
     // four classes of G, in the row's place, or one after the other in rows of the classes
     auto store = [&](int64_t c, const float (&g)[4]) {
@@ -282,9 +290,9 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_kernel(XentDirect job
     };
     if (label < 0) {
         const float none[4] = {0.f, 0.f, 0.f, 0.f};
-        if (threadIdx.x == 0 && begin == 0) job.loss[n] = 0.f;
+        if (thread == 0 && begin == 0) job.loss[n] = 0.f;
         if (job.gradients)
-            for (int64_t c = begin + 4 * (int64_t)threadIdx.x; c < end; c += 4 * kSoftmaxThreads) store(c, none);
+            for (int64_t c = begin + 4 * (int64_t)thread; c < end; c += 4 * THREADS) store(c, none);
         return;
     }
     auto load = [&](int64_t c) {
@@ -301,21 +309,21 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_kernel(XentDirect job
     };
     float2 v = make_float2(-INFINITY, 0.f);
     if (job.partial) {
-        for (int64_t t = threadIdx.x; t < (job.C + 15) / 16; t += kSoftmaxThreads) v = add(v, job.partial[t * job.N + n]);
-        if (threadIdx.x == 0) label_score = label < job.C ? row[label] : 0.f;
+        for (int64_t t = thread; t < (job.C + 15) / 16; t += THREADS) v = add(v, job.partial[t * job.N + n]);
+        if (thread == 0) label_score = label < job.C ? row[label] : 0.f;
     } else {
-        for (int64_t c0 = 4 * (int64_t)threadIdx.x; c0 < job.C; c0 += kPart) {
+        for (int64_t c0 = 4 * (int64_t)thread; c0 < job.C; c0 += STEP) {
             float4 f[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+                const int64_t c = c0 + 4 * u * THREADS;
                 f[u] = c < job.C ? load(c) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
                 if (job.column_cuts > 1 && c < job.C) *const_cast<float4 *>(reinterpret_cast<const float4 *>(row + c)) = f[u];
             }
             float m = v.x;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+                const int64_t c = c0 + 4 * u * THREADS;
                 float x[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -334,26 +342,30 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_kernel(XentDirect job
     }
 #pragma unroll
     for (int o = 32; o > 0; o /= 2) v = add(v, make_float2(__shfl_xor(v.x, o), __shfl_xor(v.y, o)));
-    if (lane == 0) part[wave] = v;
-    __syncthreads();
-    v = part[0];
+    if constexpr (THREADS > 64) {
+        if (lane == 0) part[wave] = v;
+        __syncthreads();
+        v = part[0];
 #pragma unroll
-    for (int w = 1; w < kSoftmaxThreads / 64; ++w) v = add(v, part[w]);
+        for (int w = 1; w < THREADS / 64; ++w) v = add(v, part[w]);
+    } else {
+        __builtin_amdgcn_wave_barrier();                 // (label_score: written and read by one wavefront)
+    }
     const float from = v.x == -INFINITY ? 0.f : v.x;
     const bool known = label < job.C;
-    if (threadIdx.x == 0 && begin == 0) job.loss[n] = known ? logf(v.y) + (from - label_score) : NAN;
+    if (thread == 0 && begin == 0) job.loss[n] = known ? logf(v.y) + (from - label_score) : NAN;
     if (!job.gradients) return;
     const float inverse = 1.0f / v.y, scale = job.weight ? job.weight[n] : 1.0f;
-    for (int64_t c0 = begin + 4 * (int64_t)threadIdx.x; c0 < end; c0 += kPart) {
+    for (int64_t c0 = begin + 4 * (int64_t)thread; c0 < end; c0 += STEP) {
         float4 f[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+            const int64_t c = c0 + 4 * u * THREADS;
             f[u] = c < end ? *reinterpret_cast<const float4 *>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);       // (a thread's own, added up above)
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int64_t c = c0 + 4 * u * kSoftmaxThreads;
+            const int64_t c = c0 + 4 * u * THREADS;
             if (c >= end) break;
             float g[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
 #pragma unroll
@@ -388,24 +400,21 @@ __device__ __forceinline__ void store(T *dst, float v)
 
 // Gradients of few (up to FEW) rows and many classes, or of few classes and many rows: with G[m][f], the many by the few, one pass over the
 // many gives  of_many[m, :] = sum_f G[m][f] small[f, :]  and  of_few[f, :] += G[m][f] big[m, :].  A lane has four columns of K, in which it
-// keeps the few rows of `small` and the sums; G's rows are the same for all lanes and come through scalar registers. The
-// wavefronts of a workgroup take rows in turn and add their sums up in LDS; the many are cut among workgroups.
+// keeps the few rows of `small` and the sums; G's rows are the same for all lanes and come from LDS, kFewTile at a time, of which each
+// wavefront takes every fourth. The wavefronts' sums are added up in LDS; the many are cut among workgroups.
 // What bounds it is reading `big` and writing of_many.
-constexpr int kFewWaves = 4, kFewColumns = 256;
+constexpr int kFewWaves = 4, kFewColumns = 256, kFewTile = 64;
 template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
-// memory that no kernel writes while this one runs: uniform addresses become scalar loads
-template <typename T>
-using Constant = const __attribute__((address_space(4))) T;
 template <typename T, int FEW, bool OF_MANY, bool OF_FEW>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
 {
-    __shared__ float4 parts[OF_FEW ? kFewWaves : 1][FEW][64];
+    __shared__ float4 parts[OF_FEW ? kFewWaves / 2 : 1][FEW][64];
+    __shared__ __attribute__((aligned(16))) float g_tile[kFewTile][FEW];
+    __shared__ bool counts[kFewTile];
     const bool rows_are_few = job.by_class;
     const DirectGradient &of_few = rows_are_few ? job.dphi : job.dw, &of_many = rows_are_few ? job.dw : job.dphi;
     const int64_t few = rows_are_few ? job.N : job.C, many = rows_are_few ? job.C : job.N;
-    Constant<float> *G = (Constant<float> *)(uintptr_t)job.G;
-    Constant<int64_t> *labels = (Constant<int64_t> *)(uintptr_t)job.labels;
     const T *small = static_cast<const T *>(rows_are_few ? job.Phi : job.W), *big = static_cast<const T *>(rows_are_few ? job.W : job.Phi);
     const int64_t ld_small = rows_are_few ? job.ld_phi : job.ld_w, ld_big = rows_are_few ? job.ld_w : job.ld_phi;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -427,7 +436,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
     if constexpr (OF_MANY) {
 #pragma unroll
         for (int f = 0; f < FEW; ++f) {
-            if (f < few && !(rows_are_few && labels[f] < 0)) {          // rows left out may hold anything
+            if (f < few && !(rows_are_few && job.labels[f] < 0)) {          // rows left out may hold anything
                 load4(small + f * ld_small, s[f]);
             } else {
 #pragma unroll
@@ -443,73 +452,110 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
     }
     const float scale = OF_MANY || of_few.cuts == 1 ? mean_scale(job) : 1.0f;
     constexpr int AHEAD = 4;
-    for (int64_t m0 = begin + wave; m0 < end; m0 += AHEAD * kFewWaves) {
-        float x[AHEAD][4];
-        if constexpr (OF_FEW) {
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int64_t m = m0 + u * kFewWaves;
-                if (m < end && !(!rows_are_few && labels[m] < 0)) {
-                    load4(big + m * ld_big, x[u]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[u][e] = 0.f;
-                }
+    for (int64_t tile = begin; tile < end; tile += kFewTile) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kFewTile * FEW / 4; i += 64 * kFewWaves) {
+            const int r = i / (FEW / 4), f = 4 * (i % (FEW / 4));
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (tile + r < end && f < few) {                   // (rows are a multiple of four numbers; what lies beyond the few is nobody's)
+                v = *reinterpret_cast<const float4 *>(job.G + (tile + r) * job.ld_g + f);
+                if (f + 1 >= few) v.y = 0.f;
+                if (f + 2 >= few) v.z = 0.f;
+                if (f + 3 >= few) v.w = 0.f;
             }
+            *reinterpret_cast<float4 *>(&g_tile[r][f]) = v;
         }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int64_t m = m0 + u * kFewWaves;
-            if (m >= end) break;
-            float g[FEW];
-#pragma unroll
-            for (int f = 0; f < FEW; ++f) {            // (behind the last row's numbers lie others of the workspace)
-                const float v = G[m * job.ld_g + f];
-                g[f] = f < few ? v : 0.f;
-            }
+        if (OF_FEW && threadIdx.x < kFewTile) {
+            const int64_t m = tile + threadIdx.x;
+            counts[threadIdx.x] = m < end && (rows_are_few || job.labels[m] >= 0);          // rows left out may hold anything
+        }
+        __syncthreads();
+        for (int r0 = wave; r0 < kFewTile && tile + r0 < end; r0 += AHEAD * kFewWaves) {
+            float x[AHEAD][4];
             if constexpr (OF_FEW) {
 #pragma unroll
-                for (int f = 0; f < FEW; ++f)
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int r = r0 + u * kFewWaves;
+                    if (counts[r]) {
+                        load4(big + (tile + r) * ld_big, x[u]);
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sums[f][e] = fmaf(g[f], x[u][e], sums[f][e]);
+                        for (int e = 0; e < 4; ++e) x[u][e] = 0.f;
+                    }
+                }
             }
-            if constexpr (OF_MANY) {
-                float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int f = 0; f < FEW; ++f)
+            for (int u = 0; u < AHEAD; ++u) {
+                const int r = r0 + u * kFewWaves;
+                const int64_t m = tile + r;
+                if (m >= end) break;
+                float g[FEW];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = fmaf(g[f], s[f][e], y[e]);
-                T *dst = static_cast<T *>(of_many.out) + m * of_many.ld + k;
-                if (whole) {
-                    Four<T> v;
+                for (int f = 0; f < FEW; f += 4) {
+                    const float4 v = *reinterpret_cast<const float4 *>(&g_tile[r][f]);
+                    g[f] = v.x;
+                    g[f + 1] = v.y;
+                    g[f + 2] = v.z;
+                    g[f + 3] = v.w;
+                }
+                if constexpr (OF_FEW) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) store(&v.v[e], y[e] * scale);
-                    *reinterpret_cast<Four<T> *>(dst) = v;
-                } else {
+                    for (int f = 0; f < FEW; ++f)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (k + e < job.K) store(dst + e, y[e] * scale);
+                        for (int e = 0; e < 4; ++e) sums[f][e] = fmaf(g[f], x[u][e], sums[f][e]);
+                }
+                if constexpr (OF_MANY) {
+                    float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int f = 0; f < FEW; ++f)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = fmaf(g[f], s[f][e], y[e]);
+                    T *dst = static_cast<T *>(of_many.out) + m * of_many.ld + k;
+                    if (whole) {
+                        Four<T> v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store(&v.v[e], y[e] * scale);
+                        *reinterpret_cast<Four<T> *>(dst) = v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (k + e < job.K) store(dst + e, y[e] * scale);
+                    }
                 }
             }
         }
     }
     if constexpr (OF_FEW) {
+        // the wavefronts' sums: 2 and 3 to 0 and 1, then 1 to 0
+        static_assert(kFewWaves == 4, "");
 #pragma unroll
-        for (int f = 0; f < FEW; ++f) parts[wave][f][lane] = make_float4(sums[f][0], sums[f][1], sums[f][2], sums[f][3]);
-        __syncthreads();
-        for (int f = wave; f < few; f += kFewWaves) {
-            float4 v = parts[0][f][lane];
+        for (int half = 2; half > 0; half /= 2) {
+            if (wave >= half && wave < 2 * half) {
 #pragma unroll
-            for (int w = 1; w < kFewWaves; ++w) {
-                const float4 o = parts[w][f][lane];
-                v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+                for (int f = 0; f < FEW; ++f) parts[wave - half][f][lane] = make_float4(sums[f][0], sums[f][1], sums[f][2], sums[f][3]);
             }
-            const float sum[4] = {v.x, v.y, v.z, v.w};
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int f = 0; f < FEW; ++f) {
+                    const float4 o = parts[wave][f][lane];
+                    sums[f][0] += o.x;
+                    sums[f][1] += o.y;
+                    sums[f][2] += o.z;
+                    sums[f][3] += o.w;
+                }
+            }
+            __syncthreads();
+        }
+        if (wave != 0) return;
+#pragma unroll
+        for (int f = 0; f < FEW; ++f) {
+            if (f >= few) break;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (k + e >= job.K) break;
-                if (of_few.cuts > 1) of_few.parts[((int64_t)cut * few + f) * job.K + k + e] = sum[e];
-                else store(static_cast<T *>(of_few.out) + f * of_few.ld + k + e, sum[e] * scale);
+                if (of_few.cuts > 1) of_few.parts[((int64_t)cut * few + f) * job.K + k + e] = sums[f][e];
+                else store(static_cast<T *>(of_few.out) + f * of_few.ld + k + e, sums[f][e] * scale);
             }
         }
     }
@@ -625,7 +671,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(XentDirect job)
 
 constexpr int64_t kWorkgroups = 768;         // three for every CU
 constexpr int64_t kLeastSummed = 128;        // of a cut
-constexpr int64_t kFew = 16, kOwn = 64;
+constexpr int64_t kFew = 16, kOwn = 64, kWaveClasses = 256;
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 // How a gradient's sum is cut: into as many parts as fill the GPU.
@@ -646,7 +692,7 @@ void cuts_of(const rfsf_xent_shape &s, DirectGradient *dphi, DirectGradient *dw)
 {
     if (is_few(s)) {
         const int64_t many = std::max(s.N, s.C), across = (s.K + kFewColumns - 1) / kFewColumns;
-        const int64_t cuts = std::max<int64_t>(std::min(std::min(kWorkgroups / across, kMostParts), many / kLeastMany), 1);
+        const int64_t cuts = std::max<int64_t>(std::min(std::min((std::min(s.N, s.C) > 8 ? 512 : kWorkgroups) / across, kMostParts), many / kLeastMany), 1);
         DirectGradient g = {};
         g.per_cut = (many + cuts - 1) / cuts;
         g.cuts = (uint32_t)((many + g.per_cut - 1) / g.per_cut);
@@ -693,7 +739,8 @@ hipError_t run(const XentDirect &job, bool few, hipStream_t stream)
         scores_kernel<T, 2, 4, false><<<dim3(tiles_n, (unsigned)((job.C + 31) / 32), job.column_cuts), 256, 0, stream>>>(job);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        softmax_kernel<<<dim3((unsigned)job.N, job.partial ? (unsigned)((job.C + kPart - 1) / kPart) : 1), kSoftmaxThreads, 0, stream>>>(job);
+        if (job.C <= kWaveClasses) softmax_kernel<64><<<dim3((unsigned)((job.N + 3) / 4)), 256, 0, stream>>>(job);
+        else softmax_kernel<kSoftmaxThreads><<<dim3((unsigned)job.N, job.partial ? (unsigned)((job.C + kPart - 1) / kPart) : 1), kSoftmaxThreads, 0, stream>>>(job);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !job.gradients) return e;
