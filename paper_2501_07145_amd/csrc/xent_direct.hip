@@ -288,9 +288,10 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void softmax_kernel(
             *reinterpret_cast<float4 *>(job.G + n * job.ld_g + c) = make_float4(g[0], g[1], g[2], g[3]);
         }
     };
+    const bool mine = label >= begin && label < end, first = begin == 0;       // the loss is written where the label's score is
     if (label < 0) {
         const float none[4] = {0.f, 0.f, 0.f, 0.f};
-        if (thread == 0 && begin == 0) job.loss[n] = 0.f;
+        if (thread == 0 && first) job.loss[n] = 0.f;
         if (job.gradients)
             for (int64_t c = begin + 4 * (int64_t)thread; c < end; c += 4 * THREADS) store(c, none);
         return;
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void softmax_kernel(
     float2 v = make_float2(-INFINITY, 0.f);
     if (job.partial) {
         for (int64_t t = thread; t < (job.C + 15) / 16; t += THREADS) v = add(v, job.partial[t * job.N + n]);
-        if (thread == 0) label_score = label < job.C ? row[label] : 0.f;
+        if (thread == 0 && mine && label < job.C) label_score = row[label];           // (before G takes its place)
     } else {
         for (int64_t c0 = 4 * (int64_t)thread; c0 < job.C; c0 += STEP) {
             float4 f[kAhead];
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void softmax_kernel(
     }
     const float from = v.x == -INFINITY ? 0.f : v.x;
     const bool known = label < job.C;
-    if (thread == 0 && begin == 0) job.loss[n] = known ? logf(v.y) + (from - label_score) : NAN;
+    if (thread == 0 && (mine || (!known && first))) job.loss[n] = known ? logf(v.y) + (from - label_score) : NAN;
     if (!job.gradients) return;
     const float inverse = 1.0f / v.y, scale = job.weight ? job.weight[n] : 1.0f;
     for (int64_t c0 = begin + 4 * (int64_t)thread; c0 < end; c0 += STEP) {
