@@ -286,7 +286,7 @@ int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W
  * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. Sums are held in 32 bits. A row of Phi
  * or W that holds an infinity or a NaN makes what is computed from it NaN (bfloat16: or what infinities give). Equal calls with workspaces
  * of equal sizes give equal bits.
- * Limits: K, C <= 4000000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW.
+ * Limits: K, C <= 3500000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW.
  */
 enum { RFSF_XENT_DPHI = 1, RFSF_XENT_DW = 2 };
 typedef struct {
@@ -345,7 +345,7 @@ int rfsf_int8_quantize(const void *X, int32_t bf16, int64_t N, int64_t ldx, int6
  *   out[i, j] = s_i scales[j] sum_k q[i, k] codes[j, k]
  * where q, s are the codes and scales of X's rows, which are quantised on the way. The sums are exact.
  *   X [Nx, ldx] float32 or bfloat16; codes [Ny, ld_codes] as rfsf_int8_quantize lays them out (all ld_codes bytes of every row exist and may be
- *   read); out [Nx, ld_out] float32. Limits: K <= 131072, Ny <= 10^8. Nx = 0 or Ny = 0 is a no-op.
+ *   read); out [Nx, ld_out] float32. Limits: K <= 131072, ld_codes <= 2^23, Ny <= 10^8. Nx = 0 or Ny = 0 is a no-op.
  */
 int rfsf_int8_gram_workspace_bytes(int64_t Nx, int64_t Ny, int64_t K, size_t *recommended_bytes, size_t *minimum_bytes);
 int rfsf_int8_gram(const void *X, int32_t bf16, int64_t Nx, int64_t ldx, const int8_t *codes, const float *scales, int64_t Ny,

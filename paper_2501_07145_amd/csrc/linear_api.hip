@@ -5,7 +5,7 @@
 
 namespace {
 
-constexpr int64_t kMostColumns = 4000000;       // 255 packed rows of a tile stay below 2^32 bytes; grids
+constexpr int64_t kMostColumns = 3500000;       // 287 packed rows of a tile stay below 2^32 bytes; grids
 constexpr int64_t kMostRows = 0x7fffffffLL;
 constexpr int64_t kMostCodes = 131072;          // 127 * 128 times that stays below 2^31
 constexpr int64_t kMostStored = 100000000;
@@ -131,7 +131,7 @@ extern "C" int rfsf_int8_gram(const void *X, int32_t bf16, int64_t Nx, int64_t l
     if (ldx < K || ld_codes < code_room(K) || ld_out < Ny) return RFSF_E_BAD_STRIDE;
     if (Nx == 0 || Ny == 0) return RFSF_OK;
     if (!X || !codes || !scales || !out || !workspace) return RFSF_E_NULLPTR;
-    if (misplaced(codes, ld_codes) || ld_codes > (1 << 24)) return RFSF_E_BAD_STRIDE;     // 255 rows of a tile stay below 2^32 bytes
+    if (misplaced(codes, ld_codes) || ld_codes > (1 << 23)) return RFSF_E_BAD_STRIDE;     // 287 rows of a tile stay below 2^32 bytes
     if (workspace_bytes < minimum) return RFSF_E_WORKSPACE_TOO_SMALL;
     return rfsf::launch_int8_gram(X, bf16 != 0, Nx, ldx, codes, scales, Ny, ld_codes, K, out, ld_out, workspace, workspace_bytes,
                                   static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK : RFSF_E_HIP;

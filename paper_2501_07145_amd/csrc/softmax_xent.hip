@@ -39,9 +39,16 @@ __global__ __launch_bounds__(256) void clear_rows_kernel(T *rows, int64_t count,
         for (int64_t c = threadIdx.x; c < columns; c += 256) rows[r * ld + c] = 0;
 }
 
-// Of the scores of some classes: their maximum, the sum of exponentials from there, and the largest of score + exponent(the
-// class's weights) in powers of two, which bounds G[n, c] 2^exponent(W[c, :]).
+// Of the scores of some classes: their maximum, the sum of exponentials from there, and the largest exponential times 2^exponent(the
+// class's weights), as a power of two, which bounds G[n, c] 2^exponent(W[c, :]). All from the maximum: nothing of it is lost where
+// the scores are large.
 struct Partial { float top, sum, reach; };
+__device__ __forceinline__ Partial joined(const Partial &a, const Partial &b)
+{
+    const float m = fmaxf(a.top, b.top), from = m == -INFINITY ? 0.f : m;
+    const float ta = (a.top - from) * kLog2e, tb = (b.top - from) * kLog2e;
+    return {m, a.sum * __builtin_amdgcn_exp2f(ta) + b.sum * __builtin_amdgcn_exp2f(tb), fmaxf(a.reach + ta, b.reach + tb)};
+}
 
 // Scores: classes along the tile's rows, sequences along its columns, so that a lane holds many classes of one sequence and
 // nearly all of the maximum and the sum is taken inside it.
@@ -80,8 +87,7 @@ struct Scores {
         t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int i = (int)(first - c0) + 8 * q + 4 * half;
-                const int4 p = *reinterpret_cast<const int4 *>(powers + i);
+                const int4 p = *reinterpret_cast<const int4 *>(powers + (int)(first - c0) + 8 * q + 4 * half);
                 acc[4 * q] = ldexpf(acc[4 * q], p.x - shift_n[b]);
                 acc[4 * q + 1] = ldexpf(acc[4 * q + 1], p.y - shift_n[b]);
                 acc[4 * q + 2] = ldexpf(acc[4 * q + 2], p.z - shift_n[b]);
@@ -105,12 +111,6 @@ struct Scores {
                         if (y == e) target[n] = acc[4 * q + e];
                 }
                 top[b] = fmaxf(top[b], fmaxf(fmaxf(acc[4 * q], acc[4 * q + 1]), fmaxf(acc[4 * q + 2], acc[4 * q + 3])));
-                if (with_reach) {
-                    const int4 p = *reinterpret_cast<const int4 *>(powers + i);
-                    const float r0 = fmaxf(fmaf(acc[4 * q], kLog2e, (float)p.x), fmaf(acc[4 * q + 1], kLog2e, (float)p.y));
-                    const float r1 = fmaxf(fmaf(acc[4 * q + 2], kLog2e, (float)p.z), fmaf(acc[4 * q + 3], kLog2e, (float)p.w));
-                    reach[b] = fmaxf(reach[b], fmaxf(r0, r1) + (float)kTopBit);
-                }
                 if (scores && n < rows && c0 + i < C)             // (ld is a multiple of four: numbers beyond C are nobody's)
                     *reinterpret_cast<float4 *>(scores + n * ld + c0 + i) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
             }
@@ -118,15 +118,27 @@ struct Scores {
 #pragma unroll
         for (int b = 0; b < BN; ++b) {
             top[b] = fmaxf(top[b], __shfl_xor(top[b], 32));
-            reach[b] = fmaxf(reach[b], __shfl_xor(reach[b], 32));
-            from[b] = top[b] == -INFINITY ? 0.f : top[b] * kLog2e;
+            from[b] = top[b] == -INFINITY ? 0.f : top[b];
         }
-        t.each_block([&](auto &acc, int64_t, int b) __attribute__((always_inline)) {
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum[b] += __builtin_amdgcn_exp2f(fmaf(acc[e], kLog2e, -from[b]));
+            for (int e = 0; e < 16; ++e) acc[e] = (acc[e] - from[b]) * kLog2e;
+            if (with_reach) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int4 p = *reinterpret_cast<const int4 *>(powers + (int)(first - c0) + 8 * q + 4 * half);
+                    const float r0 = fmaxf(acc[4 * q] + (float)p.x, acc[4 * q + 1] + (float)p.y), r1 = fmaxf(acc[4 * q + 2] + (float)p.z, acc[4 * q + 3] + (float)p.w);
+                    reach[b] = fmaxf(reach[b], fmaxf(r0, r1) + (float)kTopBit);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[b] += __builtin_amdgcn_exp2f(acc[e]);
         });
 #pragma unroll
-        for (int b = 0; b < BN; ++b) sum[b] += __shfl_xor(sum[b], 32);
+        for (int b = 0; b < BN; ++b) {
+            sum[b] += __shfl_xor(sum[b], 32);
+            reach[b] = fmaxf(reach[b], __shfl_xor(reach[b], 32));
+        }
         // the wavefronts that hold other classes of the same sequences
         Partial *shared = reinterpret_cast<Partial *>(t.lds);
         constexpr int WIDE = T::COLUMNS, ROWS = T::WAVES_I;
@@ -141,11 +153,7 @@ struct Scores {
             if (first + j >= rows) break;
             Partial v = shared[j];
 #pragma unroll
-            for (int w = 1; w < ROWS; ++w) {
-                const Partial o = shared[w * WIDE + j];
-                const float m = fmaxf(v.top, o.top), from = m == -INFINITY ? 0.f : m;
-                v = {m, v.sum * exp_of(v.top - from) + o.sum * exp_of(o.top - from), fmaxf(v.reach, o.reach)};
-            }
+            for (int w = 1; w < ROWS; ++w) v = joined(v, shared[w * WIDE + j]);
             partial[t.tile_i * rows_ld + first + j] = v;
         }
     }
@@ -172,22 +180,18 @@ __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
     const int r = threadIdx.x % kJoinRows, group = threadIdx.x / kJoinRows;
     const int64_t n = (int64_t)blockIdx.x * kJoinRows + r;
     Partial v = {-INFINITY, 0.f, -INFINITY};
-    auto add = [](const Partial &a, const Partial &b) {
-        const float m = fmaxf(a.top, b.top), from = m == -INFINITY ? 0.f : m;
-        return Partial{m, a.sum * exp_of(a.top - from) + b.sum * exp_of(b.top - from), fmaxf(a.reach, b.reach)};
-    };
     if (n < job.rows)
-        for (int64_t t = group; t < job.tiles; t += 16) v = add(v, job.partial[t * job.rows_ld + n]);
+        for (int64_t t = group; t < job.tiles; t += 16) v = joined(v, job.partial[t * job.rows_ld + n]);
     part[group][r] = v;
     __syncthreads();
     if (group != 0 || n >= job.rows) return;
-    for (int g = 1; g < 16; ++g) v = add(v, part[g][r]);
+    for (int g = 1; g < 16; ++g) v = joined(v, part[g][r]);
     const float from = v.top == -INFINITY ? 0.f : v.top, s = v.sum;
     const int64_t label = job.labels[n];
     const bool known = label >= 0 && label < job.C;
     job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (from - job.target[n]) : NAN;
     if (!job.terms) return;
-    float bound = v.reach - fmaf(from, kLog2e, log2f(s));
+    float bound = v.reach - log2f(s);
     if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
     job.terms[n] = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : 1.0f / (float)*job.count,
                     (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
@@ -329,7 +333,7 @@ struct Gradient {
 constexpr int64_t kUnit = 64;                           // rows of a block are counted in these
 constexpr size_t kScoreBytes = (size_t)128 << 20;       // of scores in flight: half of the last-level cache
 constexpr size_t kBlockBytes = (size_t)8 << 30;         // recommended, of what grows with the rows of a block
-constexpr int64_t kMostBlockRows = 4000000 / kUnit * kUnit;
+constexpr int64_t kMostBlockRows = 3500000 / kUnit * kUnit;
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 int64_t units(int64_t rows) { return (rows + kUnit - 1) / kUnit * kUnit; }

@@ -43,7 +43,7 @@ def _check(phi, w, y, s, got):
 SIZES = [(1, 1, 1), (1, 5, 2), (3, 33, 7), (16, 193, 10), (64, 64, 64), (65, 65, 65), (40, 31, 129), (129, 127, 300), (257, 300, 1000),
          (300, 70, 4097), (1000, 129, 31), (2, 2049, 513), (700, 50, 32), (130, 1001, 10), (1, 1000, 33), (513, 64, 16),
          # every way of making the scores and the gradients: few rows, few classes, a long sum cut, many classes, packed operands
-         (5, 70, 9000), (16, 300, 17), (17, 300, 17), (9, 131, 9), (3000, 66, 16), (40, 2051, 40), (33, 2100, 70), (20, 5000, 63), (2100, 40, 50),
+         (5, 70, 9000), (16, 300, 17), (17, 300, 17), (9, 131, 9), (3000, 66, 16), (40, 2051, 40), (33, 2100, 70), (20, 5000, 63), (2100, 40, 50), (40, 33, 9000), (19, 20, 30000),
          (620, 300, 600), (530, 291, 777)]
 # rows, columns, classes: by the ways above, the last one packed
 WAYS = [(90, 40, 20), (90, 40, 300), (12, 40, 300), (300, 40, 7), (620, 300, 600)]
@@ -130,6 +130,24 @@ def test_scores_far_from_zero(N, K, C, off, bf16):
     phi[:, 0] = 0.5
     w[:, 0] = off
     _check(phi, w, y, s, rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("off", [-1e30, 1e30])
+@pytest.mark.parametrize("N,K,C", WAYS)
+def test_scores_whose_differences_are_lost(N, K, C, off, bf16):
+    """Scores near 1e30: equal to 32 bits, so that every class has its share, and nothing overflows."""
+    phi, w, y, s = _inputs(N, K, C, bf16, left=0.0)
+    phi[:, 0] = 0.5
+    w[:, 0] = off
+    phi[:, 1:] *= 2.0 ** -30
+    loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=True)
+    g = (torch.full((N, C), 1.0 / C, device="cuda", dtype=torch.float64) - torch.nn.functional.one_hot(y, C)) * s.double()[:, None]
+    assert torch.all((loss.double() - torch.log(torch.tensor(float(C)))).abs() < 1e-5)
+    assert torch.isfinite(dPhi).all() and torch.isfinite(dW).all()
+    # column 0 alone, the largest of its rows: the others lie so far below it that packing leaves them a few bits
+    want, size, dW = g.T @ phi[:, :1].double(), g.abs().T @ phi[:, :1].double().abs(), dW[:, :1]
+    assert torch.all((dW.double() - want).abs() <= ((2.0 ** -11 if bf16 else 2.0 ** -20) + 4 * N * 2.0 ** -24) * size + 2.0 ** -8 * want.abs() * bf16 + 1e-30)
 
 
 @pytest.mark.parametrize("N,K,C", WAYS)
