@@ -19,6 +19,7 @@ struct XentDirect {
     float *loss;
     int64_t N, K, C, ld_phi, ld_w;
     int32_t gradients;
+    bool one_pass;              // all in one launch, the sum over the parts of dW left out
     bool fused;                 // scores and softmax in one launch. Otherwise:
     float *scores;              // [column_cuts][N][ld_scores]
     int64_t ld_scores, columns_per_cut;
@@ -29,6 +30,7 @@ struct XentDirect {
     bool by_class;              // there are at most 16 rows, and fewer than classes
     uint32_t *counts;           // rows that count, of every 16, or in count_tiles numbers altogether
     int32_t count_tiles;
+    bool count_here;            // one_pass_kernel: counts all rows before it starts
     DirectGradient dphi, dw;
     unsigned blocks_phi;        // workgroups of dPhi, those of dW follow
 };

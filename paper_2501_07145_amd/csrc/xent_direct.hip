@@ -9,6 +9,7 @@
 #include "xent_direct.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace rfsf {
 namespace {
@@ -562,6 +563,251 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
     }
 }
 
+// Up to 16 classes and 2048 columns: scores, softmax and both gradients in one pass over Phi. A lane has four columns of K: of the classes' weights
+// and of their sums dW, which stay in registers, and of the R rows that its wavefront is at, which are read once, while the rows before are worked on.
+// CW wavefronts share a row's columns; 8 / CW groups of them take rows of their own and add their sums up in LDS at the end.
+// A wavefront's R FEW sums over its columns are spread over its lanes as they are added up: at each step a lane keeps one half of
+// them and gives the other half to the lane that keeps that one, 2 R FEW steps instead of 6 R FEW. What bounds it is reading Phi once.
+constexpr int kOnePassWaves = 8, kOnePassColumns = 256 * kOnePassWaves, kOnePassFew = 16;
+constexpr int64_t kCountHere = 8192;             // rows that a workgroup counts by itself, 64 KB of labels out of a cache, rather than in a launch before it
+constexpr int one_pass_at_a_time(int few, bool of_phi) { return few <= 4 ? 16 : few <= 8 || !of_phi ? 8 : 4; }        // rows of a wavefront; registers
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140, kRotate8 = 0x128;
+// The sum of a over the pair of lanes that STEP stands for in the lower one, that of b in the other.
+template <int STEP>
+__device__ __forceinline__ float shared_sum(float a, float b, int lane)
+{
+    if constexpr (STEP >= 16) {
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        if constexpr (STEP == 32) {
+            const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+            return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+        } else {
+            const auto s = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+            return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+        }
+    } else {
+        const bool upper = (lane & STEP) != 0;
+        const float keep = upper ? b : a, give = upper ? a : b;
+        return keep + from_lane<STEP == 8 ? kRotate8 : STEP == 4 ? kMirror8 : STEP == 2 ? kXor2 : kXor1>(give);
+    }
+}
+// The sums over all lanes of COUNT numbers, spread over the lanes: the first half of them to the lanes whose bit STEP is not set, and so on.
+template <int COUNT, int STEP>
+__device__ __forceinline__ void spread_sums(float *v, int lane)
+{
+    if constexpr (COUNT > 1 && STEP > 0) {
+#pragma unroll
+        for (int i = 0; i < COUNT / 2; ++i) v[i] = shared_sum<STEP>(v[i], v[i + COUNT / 2], lane);
+        spread_sums<COUNT / 2, STEP / 2>(v, lane);
+    }
+}
+template <int FEW, bool MAX>
+__device__ __forceinline__ float among_few(float v)
+{
+    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+    v = join(v, from_lane<kXor1>(v));
+    v = join(v, from_lane<kXor2>(v));
+    if constexpr (FEW >= 8) v = join(v, from_lane<kMirror8>(v));
+    if constexpr (FEW >= 16) v = join(v, from_lane<kMirror16>(v));
+    return v;
+}
+template <typename T, int FEW, int CW, bool OF_PHI>
+__global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDirect job)
+{
+    constexpr int GROUPS = kOnePassWaves / CW, R = one_pass_at_a_time(FEW, OF_PHI), VALUES = R * FEW, PER = VALUES / 64;
+    constexpr int SHARED = GROUPS > 1 ? kOnePassWaves / 2 * FEW * 256 : 0, LEAST = (kOnePassWaves + GROUPS) * VALUES + 8;
+    __shared__ __attribute__((aligned(16))) float shared[SHARED > LEAST ? SHARED : LEAST];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave / CW, part = wave % CW;
+    float *parts = shared + group * CW * VALUES, *g_rows = shared + kOnePassWaves * VALUES + group * VALUES;
+    uint32_t *counted = reinterpret_cast<uint32_t *>(shared + (kOnePassWaves + GROUPS) * VALUES);
+    const int64_t begin = (int64_t)blockIdx.x * job.dw.per_cut, end = std::min(begin + job.dw.per_cut, job.N);
+    const int K = (int)job.K, C = (int)job.C;
+    // The last numbers of a row are read together with some before them, and shifted to their place.
+    const unsigned k = 256 * part + 4 * lane, from_k = std::min((int)k, K - 4), shift = k - from_k;
+    const bool all_whole = 256 * part + 256 <= K;
+    auto load4 = [&](const T *row) { return *reinterpret_cast<const Four<T> *>(row + from_k); };
+    auto placed = [&](float (&x)[4]) __attribute__((always_inline)) {
+        if (all_whole) return;
+        const bool one = (shift & 1) != 0, two = (shift & 2) != 0, gone = shift >= 4;
+        const float a[4] = {one ? x[1] : x[0], one ? x[2] : x[1], one ? x[3] : x[2], one ? 0.f : x[3]};
+        x[0] = gone ? 0.f : two ? a[2] : a[0];
+        x[1] = gone ? 0.f : two ? a[3] : a[1];
+        x[2] = gone || two ? 0.f : a[2];
+        x[3] = gone || two ? 0.f : a[3];
+    };
+    auto store4 = [&](auto *row, const float (&x)[4], float by) __attribute__((always_inline)) {
+        typedef std::remove_reference_t<decltype(*row)> O;
+        if (shift == 0) {
+            Four<O> v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store(&v.v[e], x[e] * by);
+            *reinterpret_cast<Four<O> *>(row + k) = v;
+        } else if (shift < 4) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if ((int)k + e < K) store(row + k + e, x[e] * by);
+        }
+    };
+    float w[FEW][4], sums[FEW][4];
+#pragma unroll
+    for (int f = 0; f < FEW; ++f) {
+        const Four<T> v = load4(static_cast<const T *>(job.W) + std::min(f, C - 1) * job.ld_w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[f][e] = number(v.v[e]);
+            sums[f][e] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < FEW; ++f) placed(w[f]);                    // (of classes that do not exist, the last one's, which only meets G = 0)
+    Four<T> next[R];
+    int next_label;
+    float next_weight;
+    auto fetch = [&](int64_t first) {
+        const int64_t mine = first + (lane & (R - 1));
+        const int64_t label = mine < end ? job.labels[mine] : -1;
+        next_label = label < 0 ? -1 : label < C ? (int)label : C;
+        next_weight = job.weight && mine < end ? job.weight[mine] : 1.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) next[r] = load4(static_cast<const T *>(job.Phi) + std::min(first + r, job.N - 1) * job.ld_phi);
+    };
+    int64_t first = begin + group * R;
+    fetch(first);
+    float scale = 1.0f;
+    uint32_t all_rows = 0;
+    if (job.count_here) {
+        for (int64_t n = threadIdx.x; n < job.N; n += 64 * kOnePassWaves) all_rows += job.labels[n] >= 0 ? 1 : 0;
+#pragma unroll
+        for (int o = 32; o > 0; o /= 2) all_rows += (uint32_t)__shfl_xor((int)all_rows, o);
+        if (lane == 0) counted[wave] = all_rows;
+        __syncthreads();
+        all_rows = 0;
+#pragma unroll
+        for (int i = 0; i < kOnePassWaves; ++i) all_rows += counted[i];
+        __syncthreads();
+        scale = 1.0f / (float)max(all_rows, 1u);
+        if (blockIdx.x == 0 && threadIdx.x == 0) job.counts[0] = all_rows;
+    } else if (OF_PHI) {
+        scale = mean_scale(job);
+    }
+    uint32_t rows_here = 0;
+    for (int64_t tile = begin; tile < end; tile += GROUPS * R, first += GROUPS * R) {
+        const int label_of = next_label;
+        const float weight_of = next_weight;
+        const uint64_t there = __ballot(lane < R && label_of >= 0);
+        rows_here += (uint32_t)__popcll(there);
+        float x[R][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[r][e] = (there >> r & 1) != 0 ? number(next[r].v[e]) : 0.f;          // rows left out may hold anything
+#pragma unroll
+        for (int r = 0; r < R; ++r) placed(x[r]);
+        if (tile + GROUPS * R < end) fetch(first + GROUPS * R);
+        float of_class[FEW];                     // of the row that the lane's upper bits say
+#pragma unroll
+        for (int f = 0; f < FEW; ++f) {
+            float v[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) v[r] = fmaf(x[r][3], w[f][3], fmaf(x[r][2], w[f][2], fmaf(x[r][1], w[f][1], x[r][0] * w[f][0])));
+            spread_sums<R, 32>(v, lane);
+            of_class[f] = v[0];
+            // one class after the other: all products at a time would not fit the registers
+            if (f + 1 < FEW) asm volatile("" : "+v"(of_class[f]), "+v"(w[f + 1][0]), "+v"(w[f + 1][1]), "+v"(w[f + 1][2]), "+v"(w[f + 1][3]));
+        }
+        spread_sums<FEW, 32 / R>(of_class, lane);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) parts[part * VALUES + PER * lane + p] = of_class[p];
+        __syncthreads();
+#pragma unroll
+        for (int v0 = 0; v0 < VALUES; v0 += 64 * CW) {
+            const int v = v0 + 64 * part + lane, f = v % FEW, r = v / FEW;
+            if (VALUES % (64 * CW) != 0 && v >= VALUES) continue;               // (whole wavefronts)
+            float score = 0.f;
+#pragma unroll
+            for (int i = 0; i < CW; ++i) score += parts[i * VALUES + v];
+            const int label = __shfl(label_of, r);
+            const float weight = __shfl(weight_of, r), top = among_few<FEW, true>(f < C ? score : -INFINITY), from = top == -INFINITY ? 0.f : top;
+            const float share = f < C ? exp_of(score - from) : 0.f, total = among_few<FEW, false>(share);
+            if (first + r < end) {
+                if (f == label) job.loss[first + r] = logf(total) + (from - score);
+                if (f == 0 && label < 0) job.loss[first + r] = 0.f;
+                if (f == 0 && label == C) job.loss[first + r] = NAN;
+            }
+            float g = share * (1.0f / total);
+            if (f == label) g -= 1.0f;
+            g_rows[v] = label < 0 || f >= C ? 0.f : label < C ? g * weight : NAN;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+            if (r % 2 == 0) asm volatile("" : "+v"(sums[0][0]) : : "memory");          // two rows of G after the other, for the registers too
+#pragma unroll
+            for (int f = 0; f < FEW; f += 4) {
+                const float4 g4 = *reinterpret_cast<const float4 *>(g_rows + r * FEW + f);
+                const float g[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sums[f + i][e] = fmaf(g[i], x[r][e], sums[f + i][e]);
+                        if constexpr (OF_PHI) y[e] = fmaf(g[i], w[f + i][e], y[e]);
+                    }
+            }
+            if constexpr (OF_PHI) {
+                if ((there >> r & 1) == 0) y[0] = y[1] = y[2] = y[3] = 0.f;                     // (whatever W holds)
+                if (first + r < end) store4(static_cast<T *>(job.dphi.out) + (first + r) * job.dphi.ld, y, scale);
+            }
+        }
+    }
+    if (!job.dw.out) return;
+    if (!job.weight && !job.count_here && !OF_PHI) {
+        // the rows that count, of this workgroup: all there are if it is the only one
+        __syncthreads();
+        if (lane == 0) counted[wave] = part == 0 ? rows_here : 0;
+        __syncthreads();
+        all_rows = 0;
+#pragma unroll
+        for (int i = 0; i < kOnePassWaves; ++i) all_rows += counted[i];
+        if (job.dw.cuts == 1) scale = 1.0f / (float)max(all_rows, 1u);
+        else if (threadIdx.x == 0) job.counts[blockIdx.x] = all_rows;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int half = GROUPS / 2; half > 0; half /= 2) {
+        float4 *sent = reinterpret_cast<float4 *>(shared) + ((group & (half - 1)) * CW + part) * FEW * 64 + lane;
+        if (group >= half && group < 2 * half) {
+#pragma unroll
+            for (int f = 0; f < FEW; ++f) sent[64 * f] = make_float4(sums[f][0], sums[f][1], sums[f][2], sums[f][3]);
+        }
+        __syncthreads();
+        if (group < half) {
+#pragma unroll
+            for (int f = 0; f < FEW; ++f) {
+                const float4 o = sent[64 * f];
+                sums[f][0] += o.x;
+                sums[f][1] += o.y;
+                sums[f][2] += o.z;
+                sums[f][3] += o.w;
+            }
+        }
+        __syncthreads();
+    }
+    if (group != 0) return;
+    const bool cut = job.dw.cuts > 1;
+#pragma unroll
+    for (int f = 0; f < FEW; ++f) {
+        if (f < C && cut) store4(job.dw.parts + ((int64_t)blockIdx.x * C + f) * K, sums[f], 1.0f);
+        if (f < C && !cut) store4(static_cast<T *>(job.dw.out) + f * job.dw.ld, sums[f], scale);
+    }
+}
+
 // Both gradients of more of either, in tiles of 32 rows (sequences, summed over classes, or classes, summed over sequences) x 64 columns of K,
 // in blocks of 32 x 32. The wavefronts of a workgroup share out the sum, or (OWN: sums of up to 64 numbers) have tiles of their own next to each
 // other. A lane's column of the result is its number in the wavefront, so that 32 lanes write 128 bytes of a row.
@@ -642,10 +888,10 @@ __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect jo
 }
 
 // Adds the parts of the cut sums up: 64 numbers a workgroup, whose wavefronts take parts in turn.
-template <typename T>
-__global__ __launch_bounds__(256) void add_parts_kernel(XentDirect job)
+template <typename T, int NW>
+__global__ __launch_bounds__(64 * NW) void add_parts_kernel(XentDirect job)
 {
-    __shared__ float shared[4][64];
+    __shared__ float shared[NW][64];
     const int64_t of_phi = job.dphi.cuts > 1 ? job.N * job.K : 0, of_w = job.dw.cuts > 1 ? job.C * job.K : 0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float scale = mean_scale(job);
@@ -656,13 +902,15 @@ __global__ __launch_bounds__(256) void add_parts_kernel(XentDirect job)
         const int64_t m = (int64_t)(group - (is_w ? groups_phi : 0)) * 64 + lane, all = is_w ? of_w : of_phi;
         float sum = 0.f;
         if (m < all) {
-#pragma unroll 4
-            for (unsigned c = wave; c < g.cuts; c += 4) sum += g.parts[(int64_t)c * all + m];
+#pragma unroll 8
+            for (unsigned c = wave; c < g.cuts; c += NW) sum += g.parts[(int64_t)c * all + m];
         }
         shared[wave][lane] = sum;
         __syncthreads();
         if (wave == 0 && m < all) {
-            sum = (shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]);
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) sum += shared[w][lane];
             const int64_t r = m / job.K;
             store(static_cast<T *>(g.out) + r * g.ld + (m - r * job.K), sum * scale);
         }
@@ -686,12 +934,26 @@ DirectGradient cut_of(int64_t tiles, int64_t summed, int64_t unit)
     return g;
 }
 bool is_few(const rfsf_xent_shape &s) { return std::min(s.N, s.C) <= kFew; }
+bool is_one_pass(const rfsf_xent_shape &s) { return s.gradients && s.C <= kOnePassFew && s.K >= 4 && s.K <= kOnePassColumns; }
+int one_pass_wide(int64_t K) { return K <= 256 ? 1 : K <= 512 ? 2 : K <= 1024 ? 4 : 8; }           // wavefronts that share a row
+int64_t one_pass_rows(const rfsf_xent_shape &s)                       // of a workgroup, at a time
+{
+    return kOnePassWaves / one_pass_wide(s.K) * one_pass_at_a_time((int)s.C, (s.gradients & RFSF_XENT_DPHI) != 0);
+}
 // The few of the two: rows (G then lies by classes), or classes.
-bool rows_are_few(const rfsf_xent_shape &s) { return is_few(s) && s.N < s.C; }
+bool rows_are_few(const rfsf_xent_shape &s) { return is_few(s) && s.N < s.C && !is_one_pass(s); }
+constexpr int64_t kOnePassCuts = 256;                          // workgroups: one for every CU
 constexpr int64_t kLeastMany = 16, kMostParts = 128;           // rows of a workgroup of few_kernel; parts to add up
 void cuts_of(const rfsf_xent_shape &s, DirectGradient *dphi, DirectGradient *dw)
 {
-    if (is_few(s)) {
+    if (is_one_pass(s)) {
+        const int64_t at_a_time = one_pass_rows(s), tiles = (s.N + at_a_time - 1) / at_a_time, each = (tiles + kOnePassCuts - 1) / kOnePassCuts;
+        DirectGradient g = {};
+        g.per_cut = each * at_a_time;
+        g.cuts = (uint32_t)((s.N + g.per_cut - 1) / g.per_cut);
+        *dphi = *dw = g;
+        dphi->cuts = 1;
+    } else if (is_few(s)) {
         const int64_t many = std::max(s.N, s.C), across = (s.K + kFewColumns - 1) / kFewColumns;
         const int64_t cuts = std::max<int64_t>(std::min(std::min((std::min(s.N, s.C) > 8 ? 512 : kWorkgroups) / across, kMostParts), many / kLeastMany), 1);
         DirectGradient g = {};
@@ -717,6 +979,31 @@ void launch_few(const XentDirect &job, unsigned blocks, hipStream_t stream)
     else few_kernel<T, FEW, true, false><<<dim3(blocks), 64 * kFewWaves, 0, stream>>>(job);
 }
 
+template <typename T, int FEW>
+void launch_one_pass(const XentDirect &job, unsigned blocks, hipStream_t stream)
+{
+    const int wide = one_pass_wide(job.K), threads = 64 * kOnePassWaves;
+    auto launch = [&](auto of_phi) {
+        constexpr bool PHI = decltype(of_phi)::value;
+        if (wide == 1) one_pass_kernel<T, FEW, 1, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
+        else if (wide == 2) one_pass_kernel<T, FEW, 2, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
+        else if (wide == 4) one_pass_kernel<T, FEW, 4, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
+        else one_pass_kernel<T, FEW, 8, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
+    };
+    if (job.dphi.out) launch(std::true_type{});
+    else launch(std::false_type{});
+}
+template <typename T>
+hipError_t add_parts(const XentDirect &job, hipStream_t stream)
+{
+    const int64_t numbers = (job.dphi.cuts > 1 ? job.N * job.K : 0) + (job.dw.cuts > 1 ? job.C * job.K : 0);
+    if (numbers == 0) return hipSuccess;
+    const unsigned groups = (unsigned)std::min<int64_t>((numbers + 63) / 64 + 1, 4096);
+    if (std::max(job.dphi.cuts, job.dw.cuts) > 32) add_parts_kernel<T, 16><<<dim3(groups), 1024, 0, stream>>>(job);
+    else add_parts_kernel<T, 4><<<dim3(groups), 256, 0, stream>>>(job);
+    return hipGetLastError();
+}
+
 template <typename T, int BM>
 void launch_fused(const XentDirect &job, unsigned tiles, hipStream_t stream)
 {
@@ -730,6 +1017,15 @@ template <typename T>
 hipError_t run(const XentDirect &job, bool few, hipStream_t stream)
 {
     const unsigned tiles_n = (unsigned)((job.N + kRows - 1) / kRows);
+    if (job.one_pass) {
+        if (job.dphi.out && !job.weight && !job.count_here) count_kernel<<<dim3(kCountTiles), 256, 0, stream>>>(job);
+        const unsigned blocks = (unsigned)((job.N + job.dw.per_cut - 1) / job.dw.per_cut);
+        if (job.C <= 4) launch_one_pass<T, 4>(job, blocks, stream);
+        else if (job.C <= 8) launch_one_pass<T, 8>(job, blocks, stream);
+        else launch_one_pass<T, 16>(job, blocks, stream);
+        const hipError_t e = hipGetLastError();
+        return e != hipSuccess ? e : add_parts<T>(job, stream);
+    }
     if (job.fused && job.C <= 16) {
         launch_fused<T, 1>(job, tiles_n, stream);
     } else if (job.fused && job.C <= 32) {
@@ -774,10 +1070,7 @@ hipError_t run(const XentDirect &job, bool few, hipStream_t stream)
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t numbers = (job.dphi.cuts > 1 ? job.N * job.K : 0) + (job.dw.cuts > 1 ? job.C * job.K : 0);
-    if (numbers == 0) return hipSuccess;
-    add_parts_kernel<T><<<dim3((unsigned)std::min<int64_t>((numbers + 63) / 64 + 1, 4096)), 256, 0, stream>>>(job);
-    return hipGetLastError();
+    return add_parts<T>(job, stream);
 }
 
 // How the scores are made: with up to 64 classes in one launch with the softmax, unless few rows of many columns leave CUs without work;
@@ -872,6 +1165,11 @@ hipError_t launch_xent_direct(const rfsf_xent_shape &s, const void *Phi, const v
     job.ld_g = four(job.by_class ? s.N : s.C);
     job.counts = reinterpret_cast<uint32_t *>(ws + p.counts);
     job.count_tiles = s.N > kCountedRows ? kCountTiles : (int32_t)((s.N + kRows - 1) / kRows);
+    job.one_pass = is_one_pass(s);
+    if (job.one_pass) {
+        job.count_here = (s.gradients & RFSF_XENT_DPHI) && !weight && s.N <= kCountHere;
+        job.count_tiles = job.count_here ? 1 : (s.gradients & RFSF_XENT_DPHI) ? kCountTiles : (int32_t)job.dw.cuts;
+    }
     job.dphi.parts = reinterpret_cast<float *>(ws + p.parts_phi);
     job.dw.parts = reinterpret_cast<float *>(ws + p.parts_w);
     job.dphi.ld = s.ld_dphi;

@@ -69,6 +69,18 @@ def test_what_is_not_asked_for(N, K, C, bf16, need_dPhi, need_dW):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("need_dPhi,need_dW", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("N,K,C", [(1, 4, 1), (2, 5, 3), (7, 3, 2), (17, 255, 4), (130, 256, 5), (129, 257, 8), (701, 514, 9), (2100, 1025, 16), (300, 2047, 16),
+                                   (301, 2048, 4), (300, 2049, 16), (9001, 67, 3), (8193, 130, 12), (5000, 1001, 10)])
+def test_few_classes(N, K, C, need_dPhi, need_dW, weighted, bf16):
+    """Widths around those that one, two, four and eight wavefronts share, rows that are counted in each way."""
+    phi, w, y, s = _inputs(N, K, C, bf16)
+    s = s if weighted else None
+    _check(phi, w, y, s, rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=need_dPhi, need_dW=need_dW))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("weighted", [False, True])
 @pytest.mark.parametrize("N,K,C", [(200, 40, 20), (450, 70, 300), (620, 300, 600), (1500, 170, 900)])
 def test_the_smallest_workspace(N, K, C, bf16, weighted):
     """Blocks of 64 rows: dW is added up over them."""
