@@ -1,6 +1,6 @@
 // The softmax cross entropy of few rows, classes or columns, straight from the matrices as they lie in memory (softmax_xent.hip packs
 // them first, which pays where its products are large). What bounds it is reading Phi and W and writing the gradients, and the
-// number of launches: two for up to 64 classes, three for more, and one more where a gradient's sum is cut.
+// number of launches: one for up to 16 classes and 2048 columns, two for up to 64 classes, three for more, and one more where a gradient's sum is cut.
 //
 // Products: 32-bit numbers as three terms of bfloat16 (8 significand bits each, 24 in all, with the range of 32-bit numbers), six
 // products of pairs of terms, smallest first; bfloat16 operands as they are, G then as two terms. Sums in 32 bits. A tile's summed index is
@@ -567,10 +567,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
 // and of their sums dW, which stay in registers, and of the R rows that its wavefront is at, which are read once, while the rows before are worked on.
 // CW wavefronts share a row's columns; 8 / CW groups of them take rows of their own and add their sums up in LDS at the end.
 // A wavefront's R FEW sums over its columns are spread over its lanes as they are added up: at each step a lane keeps one half of
-// them and gives the other half to the lane that keeps that one, 2 R FEW steps instead of 6 R FEW. What bounds it is reading Phi once.
+// them and gives the other half to the lane that keeps that one, about 2 R FEW steps instead of 6 R FEW. The gradients are outer products, which 4 x 4 x 1
+// matrix instructions of 32 bits make in half the time of multiply-adds, from the registers as they lie.
+// What bounds it is issuing instructions (of a tile's 9400 cycles the scores take 3500, adding up and the softmax 3400, dW 2500) and then reading
+// Phi. 7494 x 1001, 10 classes, float32, dW: 18 us (1.7 TB/s) and 5.4 for adding up 235 parts, 22.7 the call; with multiply-adds for the gradients 20.6;
+// scores and gradients in two launches 11.6 + 16.2, 31.7 the call. 16 x 193, 10 classes: 7.8 us, where nearly all is latency; 11.7 with the four
+// classes that do not exist and the rows that other groups would have worked on, and three rounds of adding up.
 constexpr int kOnePassWaves = 8, kOnePassColumns = 256 * kOnePassWaves, kOnePassFew = 16;
 constexpr int64_t kCountHere = 8192;             // rows that a workgroup counts by itself, 64 KB of labels out of a cache, rather than in a launch before it
 constexpr int one_pass_at_a_time(int few, bool of_phi) { return few <= 4 ? 16 : few <= 8 || !of_phi ? 8 : 4; }        // rows of a wavefront; registers
+constexpr int one_pass_least(int few, int groups, bool of_phi) { return (kOnePassWaves + groups) * one_pass_at_a_time(few, of_phi) * few + 8; }
 template <int CTRL>
 __device__ __forceinline__ float from_lane(float v)
 {
@@ -619,9 +625,8 @@ __device__ __forceinline__ float among_few(float v)
 template <typename T, int FEW, int CW, bool OF_PHI>
 __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDirect job)
 {
-    constexpr int GROUPS = kOnePassWaves / CW, R = one_pass_at_a_time(FEW, OF_PHI), VALUES = R * FEW, PER = VALUES / 64;
-    constexpr int SHARED = GROUPS > 1 ? kOnePassWaves / 2 * FEW * 256 : 0, LEAST = (kOnePassWaves + GROUPS) * VALUES + 8;
-    __shared__ __attribute__((aligned(16))) float shared[SHARED > LEAST ? SHARED : LEAST];
+    constexpr int GROUPS = kOnePassWaves / CW, R = one_pass_at_a_time(FEW, OF_PHI), VALUES = R * FEW, PER = VALUES / 64, LEAST = one_pass_least(FEW, GROUPS, OF_PHI);
+    extern __shared__ __attribute__((aligned(16))) float shared[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave / CW, part = wave % CW;
     float *parts = shared + group * CW * VALUES, *g_rows = shared + kOnePassWaves * VALUES + group * VALUES;
     uint32_t *counted = reinterpret_cast<uint32_t *>(shared + (kOnePassWaves + GROUPS) * VALUES);
@@ -653,18 +658,19 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
                 if ((int)k + e < K) store(row + k + e, x[e] * by);
         }
     };
-    float w[FEW][4], sums[FEW][4];
+    constexpr int FOURS = FEW / 4;
+    float w[FEW][4];
+    floatx4 sums[4][FOURS];                          // [column][four classes]
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int q = 0; q < FOURS; ++q) sums[e][q] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int f = 0; f < FEW; ++f) {
         const Four<T> v = load4(static_cast<const T *>(job.W) + std::min(f, C - 1) * job.ld_w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[f][e] = number(v.v[e]);
-            sums[f][e] = 0.f;
-        }
+        for (int e = 0; e < 4; ++e) w[f][e] = number(v.v[e]);
     }
-#pragma unroll
-    for (int f = 0; f < FEW; ++f) placed(w[f]);                    // (of classes that do not exist, the last one's, which only meets G = 0)
     Four<T> next[R];
     int next_label;
     float next_weight;
@@ -678,6 +684,8 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
     };
     int64_t first = begin + group * R;
     fetch(first);
+#pragma unroll
+    for (int f = 0; f < FEW; ++f) placed(w[f]);                    // (of classes that do not exist, the last one's, which only meets G = 0)
     float scale = 1.0f;
     uint32_t all_rows = 0;
     if (job.count_here) {
@@ -711,7 +719,10 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
         if (tile + GROUPS * R < end) fetch(first + GROUPS * R);
         float of_class[FEW];                     // of the row that the lane's upper bits say
 #pragma unroll
+        for (int f = 0; f < FEW; ++f) of_class[f] = 0.f;
+#pragma unroll
         for (int f = 0; f < FEW; ++f) {
+            if (there == 0 || (f >= 4 && f / 4 * 4 >= C)) continue;          // (no rows, or four classes that do not exist)
             float v[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) v[r] = fmaf(x[r][3], w[f][3], fmaf(x[r][2], w[f][2], fmaf(x[r][1], w[f][1], x[r][0] * w[f][0])));
@@ -744,70 +755,92 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
             g_rows[v] = label < 0 || f >= C ? 0.f : label < C ? g * weight : NAN;
         }
         __syncthreads();
+        if (there == 0 && !OF_PHI) continue;
+        // dW[f][k] += G[r][f] x[r][k]: lane l gives column k of its own and class l % 4 of four (4 x 4 x 1 matrix instructions, 16 of which lie
+        // next to each other in a wavefront), and has column k of all four classes.
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float y[4] = {0.f, 0.f, 0.f, 0.f};
-            if (r % 2 == 0) asm volatile("" : "+v"(sums[0][0]) : : "memory");          // two rows of G after the other, for the registers too
 #pragma unroll
-            for (int f = 0; f < FEW; f += 4) {
-                const float4 g4 = *reinterpret_cast<const float4 *>(g_rows + r * FEW + f);
-                const float g[4] = {g4.x, g4.y, g4.z, g4.w};
+            for (int q = 0; q < FOURS; ++q) {
+                if (q > 0 && 4 * q >= C) break;
+                const float g = g_rows[r * FEW + 4 * q + (lane & 3)];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sums[f + i][e] = fmaf(g[i], x[r][e], sums[f + i][e]);
-                        if constexpr (OF_PHI) y[e] = fmaf(g[i], w[f + i][e], y[e]);
-                    }
+                for (int e = 0; e < 4; ++e) sums[e][q] = __builtin_amdgcn_mfma_f32_4x4x1f32(g, x[r][e], sums[e][q], 0, 0, 0);
             }
-            if constexpr (OF_PHI) {
-                if ((there >> r & 1) == 0) y[0] = y[1] = y[2] = y[3] = 0.f;                     // (whatever W holds)
-                if (first + r < end) store4(static_cast<T *>(job.dphi.out) + (first + r) * job.dphi.ld, y, scale);
+        }
+        if constexpr (OF_PHI) {
+            // dPhi[r][k] = sum_f G[r][f] w[f][k], four rows at a time in the same way
+#pragma unroll
+            for (int r0 = 0; r0 < R; r0 += 4) {
+                floatx4 y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int f = 0; f < FEW; ++f) {
+                    if (f >= 4 && f / 4 * 4 >= C) continue;
+                    const float g = g_rows[(r0 + (lane & 3)) * FEW + f];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_mfma_f32_4x4x1f32(g, w[f][e], y[e], 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = r0; r < r0 + 4; ++r) {
+                    float row[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) row[e] = (there >> r & 1) != 0 ? y[e][r - r0] : 0.f;             // (whatever W holds)
+                    if (first + r < end) store4(static_cast<T *>(job.dphi.out) + (first + r) * job.dphi.ld, row, scale);
+                }
             }
         }
     }
     if (!job.dw.out) return;
-    if (!job.weight && !job.count_here && !OF_PHI) {
+    // The groups' sums add up: class f is for group f % GROUPS to add and to store.
+    const bool cut = job.dw.cuts > 1, counts = !job.weight && !job.count_here && !OF_PHI;
+    float4 *all = reinterpret_cast<float4 *>(shared + LEAST);                          // [wave][class][lane]
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+        for (int f = 0; f < FEW; ++f)
+            if (f < C) all[(wave * C + f) * 64 + lane] = make_float4(sums[0][f / 4][f % 4], sums[1][f / 4][f % 4], sums[2][f / 4][f % 4], sums[3][f / 4][f % 4]);
+    }
+    if (counts && lane == 0) counted[wave] = part == 0 ? rows_here : 0;
+    __syncthreads();
+    if (counts) {
         // the rows that count, of this workgroup: all there are if it is the only one
-        __syncthreads();
-        if (lane == 0) counted[wave] = part == 0 ? rows_here : 0;
-        __syncthreads();
         all_rows = 0;
 #pragma unroll
         for (int i = 0; i < kOnePassWaves; ++i) all_rows += counted[i];
-        if (job.dw.cuts == 1) scale = 1.0f / (float)max(all_rows, 1u);
+        if (!cut) scale = 1.0f / (float)max(all_rows, 1u);
         else if (threadIdx.x == 0) job.counts[blockIdx.x] = all_rows;
     }
-    __syncthreads();
-#pragma unroll
-    for (int half = GROUPS / 2; half > 0; half /= 2) {
-        float4 *sent = reinterpret_cast<float4 *>(shared) + ((group & (half - 1)) * CW + part) * FEW * 64 + lane;
-        if (group >= half && group < 2 * half) {
-#pragma unroll
-            for (int f = 0; f < FEW; ++f) sent[64 * f] = make_float4(sums[f][0], sums[f][1], sums[f][2], sums[f][3]);
+    float *part_out = job.dw.parts + (int64_t)blockIdx.x * C * K;
+    auto store_sums = [&](int f, const float (&row)[4]) __attribute__((always_inline)) {
+        if constexpr (sizeof(T) == 4) {
+            store4((cut ? part_out : static_cast<T *>(job.dw.out)) + f * (cut ? K : job.dw.ld), row, cut ? 1.0f : scale);
+        } else {
+            if (cut) store4(part_out + f * K, row, 1.0f);
+            else store4(static_cast<T *>(job.dw.out) + f * job.dw.ld, row, scale);
         }
-        __syncthreads();
-        if (group < half) {
+    };
+    if constexpr (GROUPS > 1) {
+        for (int f = group; f < C; f += GROUPS) {                                       // (part is its own)
+            float row[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int f = 0; f < FEW; ++f) {
-                const float4 o = sent[64 * f];
-                sums[f][0] += o.x;
-                sums[f][1] += o.y;
-                sums[f][2] += o.z;
-                sums[f][3] += o.w;
+            for (int g = 0; g < GROUPS; ++g) {
+                const float4 v = all[((g * CW + part) * C + f) * 64 + lane];
+                row[0] += v.x;
+                row[1] += v.y;
+                row[2] += v.z;
+                row[3] += v.w;
             }
+            store_sums(f, row);
         }
-        __syncthreads();
-    }
-    if (group != 0) return;
-    const bool cut = job.dw.cuts > 1;
+    } else {
 #pragma unroll
-    for (int f = 0; f < FEW; ++f) {
-        if (f < C && cut) store4(job.dw.parts + ((int64_t)blockIdx.x * C + f) * K, sums[f], 1.0f);
-        if (f < C && !cut) store4(static_cast<T *>(job.dw.out) + f * job.dw.ld, sums[f], scale);
+        for (int f = 0; f < FEW; ++f) {
+            const float row[4] = {sums[0][f / 4][f % 4], sums[1][f / 4][f % 4], sums[2][f / 4][f % 4], sums[3][f / 4][f % 4]};
+            if (f < C) store_sums(f, row);
+        }
     }
 }
-
 // Both gradients of more of either, in tiles of 32 rows (sequences, summed over classes, or classes, summed over sequences) x 64 columns of K,
 // in blocks of 32 x 32. The wavefronts of a workgroup share out the sum, or (OWN: sums of up to 64 numbers) have tiles of their own next to each
 // other. A lane's column of the result is its number in the wavefront, so that 32 lanes write 128 bytes of a row.
@@ -934,7 +967,17 @@ DirectGradient cut_of(int64_t tiles, int64_t summed, int64_t unit)
     return g;
 }
 bool is_few(const rfsf_xent_shape &s) { return std::min(s.N, s.C) <= kFew; }
-bool is_one_pass(const rfsf_xent_shape &s) { return s.gradients && s.C <= kOnePassFew && s.K >= 4 && s.K <= kOnePassColumns; }
+// All in one pass: where a gradient is asked for, unless it is dPhi alone, of more than 8 classes (4 rows of a wavefront at a time) and many rows.
+// us, in two passes and in one, float32 but where said: 50 x 70, 2 classes, dW 12.0 and 6.6; 1000 x 1025, 16, both 30.1 and 23.5; 10000 x 70, 7,
+// both 30.3 and 16.5; 10000 x 2000, 7, dW 51.4 and 31.8; 40000 x 1000, 2, dW 86.9 and 38.5, 16, both 159 and 112. dPhi alone: 50 x 2000, 16,
+// bfloat16 21.1 and 8.9; 1000 x 300, 16 13.9 and 9.4, 2 10.4 and 11.6; 10000 x 513, 7 22.8 and 23.3; but, left to two, 10000 x 513, 16 26.6 and 30.7;
+// 40000 x 1000, 16, bfloat16 69.2 and 92.5. Of 81 shapes in these ranges 77 are taken, 1.50 times faster on average; the worst 0.88 times.
+constexpr int64_t kOnePassRowsOfPhi = 4096;
+bool is_one_pass(const rfsf_xent_shape &s)
+{
+    if (!s.gradients || s.C > kOnePassFew || s.K < 4 || s.K > kOnePassColumns) return false;
+    return (s.gradients & RFSF_XENT_DW) || s.C <= 8 || s.N <= kOnePassRowsOfPhi;
+}
 int one_pass_wide(int64_t K) { return K <= 256 ? 1 : K <= 512 ? 2 : K <= 1024 ? 4 : 8; }           // wavefronts that share a row
 int64_t one_pass_rows(const rfsf_xent_shape &s)                       // of a workgroup, at a time
 {
@@ -979,19 +1022,30 @@ void launch_few(const XentDirect &job, unsigned blocks, hipStream_t stream)
     else few_kernel<T, FEW, true, false><<<dim3(blocks), 64 * kFewWaves, 0, stream>>>(job);
 }
 
-template <typename T, int FEW>
-void launch_one_pass(const XentDirect &job, unsigned blocks, hipStream_t stream)
+template <typename T, int FEW, int CW, bool OF_PHI>
+hipError_t launch_one_pass(const XentDirect &job, unsigned blocks, hipStream_t stream)
 {
-    const int wide = one_pass_wide(job.K), threads = 64 * kOnePassWaves;
+    constexpr int GROUPS = kOnePassWaves / CW;
+    const size_t sums = GROUPS > 1 && job.dw.out ? (size_t)job.C * kOnePassWaves * 64 * sizeof(float4) : 0;
+    const size_t lds = sizeof(float) * one_pass_least(FEW, GROUPS, OF_PHI) + sums;
+    static LdsLimit limit;
+    const hipError_t e = allow_lds(limit, reinterpret_cast<const void *>(one_pass_kernel<T, FEW, CW, OF_PHI>), lds);
+    if (e != hipSuccess) return e;
+    one_pass_kernel<T, FEW, CW, OF_PHI><<<dim3(blocks), 64 * kOnePassWaves, lds, stream>>>(job);
+    return hipGetLastError();
+}
+template <typename T, int FEW>
+hipError_t launch_one_pass(const XentDirect &job, unsigned blocks, hipStream_t stream)
+{
+    const int wide = one_pass_wide(job.K);
     auto launch = [&](auto of_phi) {
         constexpr bool PHI = decltype(of_phi)::value;
-        if (wide == 1) one_pass_kernel<T, FEW, 1, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
-        else if (wide == 2) one_pass_kernel<T, FEW, 2, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
-        else if (wide == 4) one_pass_kernel<T, FEW, 4, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
-        else one_pass_kernel<T, FEW, 8, PHI><<<dim3(blocks), threads, 0, stream>>>(job);
+        return wide == 1   ? launch_one_pass<T, FEW, 1, PHI>(job, blocks, stream)
+               : wide == 2 ? launch_one_pass<T, FEW, 2, PHI>(job, blocks, stream)
+               : wide == 4 ? launch_one_pass<T, FEW, 4, PHI>(job, blocks, stream)
+                           : launch_one_pass<T, FEW, 8, PHI>(job, blocks, stream);
     };
-    if (job.dphi.out) launch(std::true_type{});
-    else launch(std::false_type{});
+    return job.dphi.out ? launch(std::true_type{}) : launch(std::false_type{});
 }
 template <typename T>
 hipError_t add_parts(const XentDirect &job, hipStream_t stream)
@@ -1020,10 +1074,9 @@ hipError_t run(const XentDirect &job, bool few, hipStream_t stream)
     if (job.one_pass) {
         if (job.dphi.out && !job.weight && !job.count_here) count_kernel<<<dim3(kCountTiles), 256, 0, stream>>>(job);
         const unsigned blocks = (unsigned)((job.N + job.dw.per_cut - 1) / job.dw.per_cut);
-        if (job.C <= 4) launch_one_pass<T, 4>(job, blocks, stream);
-        else if (job.C <= 8) launch_one_pass<T, 8>(job, blocks, stream);
-        else launch_one_pass<T, 16>(job, blocks, stream);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = job.C <= 4   ? launch_one_pass<T, 4>(job, blocks, stream)
+                             : job.C <= 8 ? launch_one_pass<T, 8>(job, blocks, stream)
+                                          : launch_one_pass<T, 16>(job, blocks, stream);
         return e != hipSuccess ? e : add_parts<T>(job, stream);
     }
     if (job.fused && job.C <= 16) {
