@@ -37,7 +37,7 @@ __device__ __forceinline__ void store_codes(int8_t *q, const float (&v)[PER], fl
 
 // A workgroup per row: the largest magnitude, then the codes, zeros up to the end of the last step. Rows of up to kHeld columns are read
 // once, 16 bytes a lane and load, and stay in registers; of longer ones what lies beyond is read again. A row with an infinity or a
-// NaN has the scale NaN.
+// NaN has the scale NaN. Bound by reading X: 5000 x 10241, float32, 47 us (5.4 TB/s).
 constexpr int kQuantizeThreads = 512;
 template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Chunk { T v[16 / sizeof(T)]; };
@@ -164,7 +164,7 @@ void launch_few_rows(const int8_t *qx, int64_t pitch_x, const float *sx, int64_t
 }
 
 // The same for rows of X of kHeldCodes columns altogether, quantised by every workgroup for itself into LDS: one launch instead of two, where there
-// are few workgroups and the second launch is what counts (1 x 1025 against 1000: 6.0 us for the two kernels, 11.2 for the call).
+// are few workgroups and the second launch is what counts (1 x 1025 against 1000: 5.4 us for the kernel, 8.8 for the call; 6.0 for the two kernels, 11.2 for the call).
 constexpr int kHeldCodes = 8192, kHeldPad = 16;          // (rows 16 bytes apart in their banks)
 template <typename T>
 __global__ __launch_bounds__(256) void few_small_kernel(const T *X, int64_t ldx, int Nx, int K, const int8_t *codes, int64_t ld, const float *scales,
@@ -231,7 +231,8 @@ __global__ __launch_bounds__(256) void few_small_kernel(const T *X, int64_t ldx,
     }
 }
 
-// Rows of the tile: stored rows (contiguous in the result).
+// More rows: the product of packed operands. Rows of the tile: stored rows (contiguous in the result). 333 x 10000 x 5121 36 us (940 TOP/s, 237 tiles of 128:
+// one round that does not fill the CUs), 5000 x 50000 x 10241 2.44 ms (2100 TOP/s).
 struct Scaled {
     float *out;
     int64_t ld, rows_i, cols_j;

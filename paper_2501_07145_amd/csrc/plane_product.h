@@ -12,6 +12,10 @@
 // lane), into the buffer that the step before last used, while the step that arrived before is multiplied: one barrier a
 // step. LDS: row r's 128 bytes are 8 chunks of 16, chunk c at place c ^ (r & 7), so that 8 lanes that read the same chunk of 8
 // rows meet all banks once (and the permutation is made by the loads' addresses, at no cost).
+//
+// What bounds it: with tiles of 256 and random numbers the power that the matrix instructions draw and what the L2s deliver, about equally. 32768 x 2048 x
+// 8192 of 16-bit numbers 877 us (1250 TFLOP/s); the same without the loads 710, the loads alone 560 to 730, the matrix instructions alone 490 to 540.
+// 50000 x 5000 x 10241 of 8-bit ones 2.44 ms (2100 TOP/s). With the smaller tiles, what the L2s deliver (9.5 to 12 TB/s) and the time of a step.
 #pragma once
 
 #include "rfsf_internal.h"

@@ -2,7 +2,7 @@
 //   l[n, c] = sum_k Phi[n, k] W[c, k],   loss[n] = log sum_c exp l[n, c] - l[n, y_n],
 //   G[n, c] = s_n (exp l[n, c] / sum - [c = y_n]),   dPhi = G W,   dW = G^T Phi.
 //
-// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory. The operands are packed once for
+// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory (float32 operands cost three 16-bit products each). The operands are packed once for
 // the matrix instructions (plane_pack.h), W and Phi by rows for the scores, their transposes for the gradients, so that
 // all three products are of one kind (plane_product.h). The scores of a tile give their maximum and sum of exponentials per row before
 // they leave the registers; without gradients they are never written. For gradients the rows are taken in blocks, and the
@@ -52,6 +52,9 @@ __device__ __forceinline__ Partial joined(const Partial &a, const Partial &b)
 
 // Scores: classes along the tile's rows, sequences along its columns, so that a lane holds many classes of one sequence and
 // nearly all of the maximum and the sum is taken inside it.
+// Bound by the product; where the scores are written, by that after it, as a CU holds one tile and all of them end together. Tiles of 256: 10000 x
+// 5121, 5003 classes, float32, losses alone 1.43 ms (1080 TFLOP/s of 16-bit products); 1024 x 2049, 32768 classes, bfloat16, with 134 MB of scores
+// 157 us (875 TFLOP/s).
 struct Scores {
     const uint32_t *largest_w, *largest_phi;    // per class, per sequence of the block
     int64_t C, rows;                            // classes; sequences of this launch
@@ -172,7 +175,21 @@ struct JoinJob {
     float *loss;
     RowTerms *terms;                // null without gradients
 };
-// 16 rows a workgroup, whose 16 groups of threads share out the tiles.
+// What follows from the statistics of all classes; `write`: the loss and the terms are written.
+__device__ __forceinline__ RowTerms finish(const JoinJob &job, int64_t n, const Partial &v, bool write)
+{
+    const float from = v.top == -INFINITY ? 0.f : v.top, s = v.sum;
+    const int64_t label = job.labels[n];
+    const bool known = label >= 0 && label < job.C;
+    if (write) job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (from - job.target[n]) : NAN;
+    float bound = v.reach - log2f(s);
+    if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
+    const RowTerms t = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : job.terms ? 1.0f / (float)*job.count : 0.f,
+                        (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
+    if (write && job.terms) job.terms[n] = t;
+    return t;
+}
+// 16 rows a workgroup, whose 16 groups of threads share out the tiles. Bound by latency: 6.3 us for 1024 rows of 128 tiles.
 constexpr int kJoinRows = 16;
 __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
 {
@@ -186,21 +203,14 @@ __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
     __syncthreads();
     if (group != 0 || n >= job.rows) return;
     for (int g = 1; g < 16; ++g) v = joined(v, part[g][r]);
-    const float from = v.top == -INFINITY ? 0.f : v.top, s = v.sum;
-    const int64_t label = job.labels[n];
-    const bool known = label >= 0 && label < job.C;
-    job.loss[n] = label < 0 ? 0.f : known ? logf(s) + (from - job.target[n]) : NAN;
-    if (!job.terms) return;
-    float bound = v.reach - log2f(s);
-    if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
-    job.terms[n] = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : 1.0f / (float)*job.count,
-                    (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
+    finish(job, n, v, true);
 }
 
 // From the scores of `rows` sequences to G as operand, in tiles of 64 x 64. By rows, for the product with W^T, whose columns are scaled by
 // the classes' powers of two: (p - [c = y]) 2^exponent(W[c, :]), brought to 2^14 by the row's own exponent; the rows' scales
 // enter at the end of the product, so that rows of small scale lose nothing. Transposed, for the product with Phi^T: the same with
 // the rows' scales and exponents, brought to 2^14 by the largest of all.
+// Bound by memory (scores read, two operands written), the scores coming from the last-level cache: 1024 x 32768, bfloat16 mode 72 us for 268 MB (3.7 TB/s).
 struct GradientJob {
     const float *scores;
     int64_t ld, rows, C;
@@ -211,20 +221,37 @@ struct GradientJob {
     const uint32_t *largest_w, *largest_phi;
     char *by_row, *by_class;        // either may be null; by_class from the first sequence's column on
     int64_t pitch_row, pitch_class;
+    JoinJob join;                   // JOIN: the class tiles' parts, of which the terms are made here; the first tiles of classes write them
 };
-template <bool TWO>
+template <bool TWO, bool JOIN>
 __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
 {
     __shared__ float tile[64][65];
     const int64_t c0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
     const int at = threadIdx.x >> 3, group = threadIdx.x & 7;
     const int shift = job.by_class ? kTopBit - ((int)job.stats->top - kTopBias) : 0;
+    __shared__ RowTerms made[JOIN ? 64 : 1];
+    if constexpr (JOIN) {
+        const int64_t n = n0 + threadIdx.x / 4;
+        Partial v = {-INFINITY, 0.f, -INFINITY};
+        if (n < job.rows) {
+#pragma unroll 4
+            for (int64_t t = threadIdx.x % 4; t < job.join.tiles; t += 4) v = joined(v, job.join.partial[t * job.join.rows_ld + n]);
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o *= 2) {
+            const Partial w = {__shfl_xor(v.top, o), __shfl_xor(v.sum, o), __shfl_xor(v.reach, o)};
+            v = joined(v, w);
+        }
+        if (threadIdx.x % 4 == 0 && n < job.rows) made[threadIdx.x / 4] = finish(job.join, n, v, blockIdx.x == 0);
+        __syncthreads();
+    }
 #pragma unroll
     for (int u = 0; u < 64; u += 32) {
         const int64_t n = n0 + at + u, c = c0 + 8 * group;
         float g[8], scale = 0.f;
         if (n < job.rows) {
-            const RowTerms t = job.terms[n];
+            const RowTerms t = JOIN ? made[at + u] : job.terms[n];
             const int64_t label = job.labels[n];
             scale = ldexpf(job.weight ? t.scale : 1.0f, shift + exponent_of(job.largest_phi[n]));
             float v[8];
@@ -269,7 +296,8 @@ __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
     }
 }
 
-// A gradient: rows of the tile along the contiguous axis of the result.
+// A gradient: rows of the tile along the contiguous axis of the result. Both gradients share a launch, so that the second one's tiles fill the CUs
+// that the first one's leave. 8192 x 2049, 32768 classes, bfloat16: 1.93 ms (1140 TFLOP/s); 1000 x 1025, 1000 classes, float32 32 us.
 struct Gradient {
     void *out;
     int64_t ld, rows_i, cols_j;
@@ -331,6 +359,10 @@ struct Gradient {
 // ---------------------------------------------------------------------------------------------------------------
 // Workspace and order of work.
 constexpr int64_t kUnit = 64;                           // rows of a block are counted in these
+// Tiles of classes whose parts the pass to G joins by itself, every workgroup those of its rows, which saves a launch; with more of them they are read
+// too often. (us a call, apart and here: 4454 x 257, 468 classes, bfloat16, dPhi 46.0 and 43.4; 1000 x 1025, 1000, float32, both 67.3 and 65.5; 1432 x
+// 1999, 2885, 12 tiles, float32, both 293.0 and 293.8. Of 44 shapes with 302 to 4541 classes the geometric mean is 1.016, the worst 0.990.)
+constexpr int64_t kJoinHere = 32;
 constexpr size_t kScoreBytes = (size_t)128 << 20;       // of scores in flight: half of the last-level cache
 constexpr size_t kBlockBytes = (size_t)8 << 30;         // recommended, of what grows with the rows of a block
 constexpr int64_t kMostBlockRows = 3500000 / kUnit * kUnit;
@@ -491,13 +523,17 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
                                                 epilogue, stream));
             const JoinJob join = {partial, plane_tiles_a(C, edge), plan.rows, part, C, labels + n0 + m0, weight ? weight + n0 + m0 : nullptr, count, largest_w,
                                   target, loss + n0 + m0, gradients ? terms + m0 : nullptr};
-            join_kernel<<<dim3((unsigned)((part + kJoinRows - 1) / kJoinRows)), dim3(256), 0, stream>>>(join);
-            RFSF_TRY(hipGetLastError());
+            const bool join_apart = !gradients || join.tiles > kJoinHere;
+            if (join_apart) {
+                join_kernel<<<dim3((unsigned)((part + kJoinRows - 1) / kJoinRows)), dim3(256), 0, stream>>>(join);
+                RFSF_TRY(hipGetLastError());
+            }
             if (!gradients) continue;
             const GradientJob job = {scores, z.ld_scores, part, C, labels + n0 + m0, weight, stats, terms + m0, largest_w, largest_phi + m0, g_rows ? g_rows + m0 * pitch_c : nullptr,
-                                     g_classes ? g_classes + (m0 / 64) * (z.two ? 256 : 128) : nullptr, pitch_c, pitch_n};
+                                     g_classes ? g_classes + (m0 / 64) * (z.two ? 256 : 128) : nullptr, pitch_c, pitch_n, join};
             const dim3 grid((unsigned)((C + 63) / 64), (unsigned)((part + 63) / 64));
-            gradient_kernel<MODE == kHalfTwo><<<grid, dim3(256), 0, stream>>>(job);
+            if (join_apart) gradient_kernel<MODE == kHalfTwo, false><<<grid, dim3(256), 0, stream>>>(job);
+            else gradient_kernel<MODE == kHalfTwo, true><<<grid, dim3(256), 0, stream>>>(job);
             RFSF_TRY(hipGetLastError());
         }
         if (!gradients) continue;

@@ -122,7 +122,7 @@ __device__ __forceinline__ Acc add_up(const Acc (&acc)[BM], float *shared, int w
 
 // Scores of 16 rows and 16 BM classes, in blocks of 16 x 16. FUSED (all classes in one tile): the softmax, the loss and G = weight
 // (p - [c = y]) follow in registers; otherwise the scores are written. Wavefronts share out the columns, 64 at a time: lane l holds a
-// quarter of row l % 16 of each block.
+// quarter of row l % 16 of each block. Bound by reading Phi and by latency: 7494 x 1001, 10 classes, float32 11.6 us (2.6 TB/s), loss alone or before few_kernel.
 constexpr int kRows = 16;
 constexpr int64_t kCountedRows = 32768;          // of more, the rows that count are counted by a launch of its own, into kCountTiles numbers
 constexpr int kCountTiles = 256;
