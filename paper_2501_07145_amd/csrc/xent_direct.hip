@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) void count_kernel(XentDirect job)
 
 // Scores to loss and G, a workgroup per row, and with many classes (job.partial: the maxima and sums of 16 classes each are known) per
 // kPart classes of it. Scores cut in columns are added up on the way.
-// THREADS a row, and rows of few classes several to a workgroup of 256.
+// THREADS a row, and rows of few classes several to a workgroup of 256. Bound by latency: 12 x 9000 9.3 us, 100 x 300 4.7.
 constexpr int kSoftmaxThreads = 512, kAhead = 4, kPart = 4 * kAhead * kSoftmaxThreads;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void softmax_kernel(XentDirect job)
@@ -404,7 +404,8 @@ __device__ __forceinline__ void store(T *dst, float v)
 // many gives  of_many[m, :] = sum_f G[m][f] small[f, :]  and  of_few[f, :] += G[m][f] big[m, :].  A lane has four columns of K, in which it
 // keeps the few rows of `small` and the sums; G's rows are the same for all lanes and come from LDS, kFewTile at a time, of which each
 // wavefront takes every fourth. The wavefronts' sums are added up in LDS; the many are cut among workgroups.
-// What bounds it is reading `big` and writing of_many.
+// What bounds it is reading `big` and writing of_many. 12 x 2000, 9000 classes, float32, both gradients 44 us (144 MB, 3.3 TB/s), with 32-bit multiply-adds
+// of 11 us; 7494 x 3001, 10 classes, dW 35 us (90 MB, 2.6 TB/s).
 constexpr int kFewWaves = 4, kFewColumns = 256, kFewTile = 64;
 template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
@@ -843,7 +844,8 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
 }
 // Both gradients of more of either, in tiles of 32 rows (sequences, summed over classes, or classes, summed over sequences) x 64 columns of K,
 // in blocks of 32 x 32. The wavefronts of a workgroup share out the sum, or (OWN: sums of up to 64 numbers) have tiles of their own next to each
-// other. A lane's column of the result is its number in the wavefront, so that 32 lanes write 128 bytes of a row.
+// other. A lane's column of the result is its number in the wavefront, so that 32 lanes write 128 bytes of a row. Bound by latency, and where there are many
+// tiles by splitting 32-bit numbers into terms: 3000 x 500, 40 classes, float32 dPhi 12.7 us, dW 15.8; 100 x 500, 300 classes, both 13.1.
 constexpr int kWide = 64, kSumWaves = 4;
 template <typename T, bool OWN>
 __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect job)
@@ -920,7 +922,8 @@ __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect jo
     }
 }
 
-// Adds the parts of the cut sums up: 64 numbers a workgroup, whose wavefronts take parts in turn.
+// Adds the parts of the cut sums up: 64 numbers a workgroup, whose wavefronts take parts in turn. Bound by latency: 235 parts of 10010 numbers 5.5 us
+// (1.7 TB/s; as long with four wavefronts and 118 parts), few parts 3.7.
 template <typename T, int NW>
 __global__ __launch_bounds__(64 * NW) void add_parts_kernel(XentDirect job)
 {
