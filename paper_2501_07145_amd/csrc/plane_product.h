@@ -66,11 +66,13 @@ __device__ __forceinline__ void direct_load16(const char *base, uint32_t off, ui
 
 // Tiles in the order that the XCDs' L2s see them: eight contiguous pieces of an order that goes through strips of kStrip tiles of A.
 constexpr int kStrip = 8;
-__device__ __forceinline__ bool tile_of_block(unsigned block, int64_t tiles_i, int64_t tiles_j, int64_t *ti, int64_t *tj)
+__device__ __forceinline__ bool tile_of_block(unsigned block, int64_t tiles_i, int64_t tiles_j, int cuts, int64_t *ti, int64_t *tj, int *cut)
 {
-    const int64_t tiles = tiles_i * tiles_j, per = (tiles + 7) / 8;
-    const int64_t rank = (int64_t)(block % 8) * per + block / 8;
-    if (rank >= tiles) return false;
+    const int64_t tiles = tiles_i * tiles_j, all = tiles * cuts, per = (all + 7) / 8;
+    int64_t rank = (int64_t)(block % 8) * per + block / 8;
+    if (rank >= all) return false;
+    *cut = cuts > 1 ? (int)(rank / tiles) : 0;          // (an XCD's tiles are of few cuts, whose columns no other one reads)
+    rank -= *cut * tiles;
     const int64_t strip = rank / (kStrip * tiles_j), at = rank - strip * kStrip * tiles_j;
     const int64_t left = tiles_i - strip * kStrip, width = left < kStrip ? left : kStrip;
     *tj = at / width;
@@ -90,7 +92,7 @@ struct Tile {
     static constexpr bool HAS_EXTRA = EXTRA;
     typename Acc<MODE>::type acc[BM][BN], extra;
     int64_t i0, j0, tile_i, tile_j, extra_i;
-    int wave_i, wave_j;
+    int wave_i, wave_j, cut;
     char *lds;                  // free for the epilogue after a barrier
     // f(block, first row, number of the block of columns), for every block
     template <typename F>
@@ -109,7 +111,7 @@ struct Tile {
 };
 
 template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA, typename Epilogue>
-__device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const Planes &B, int64_t steps, int64_t tile_i, int64_t tile_j, const Epilogue &epilogue)
+__device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const Planes &B, int64_t steps, int64_t tile_i, int64_t tile_j, int cut, const Epilogue &epilogue)
 {
     typedef Tile<MODE, TM, TN, WM, WN, EXTRA> T;
     constexpr int BM = T::BM, BN = T::BN, kRows = TM + TN + (EXTRA ? 32 : 0), kBuffer = kRows * kStepBytes, NL = (TM + TN) / 8 / (WM * WN);
@@ -119,6 +121,7 @@ __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const P
     T t;
     t.tile_i = tile_i;
     t.tile_j = tile_j;
+    t.cut = cut;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int half = lane >> 5, col = lane & 31;
     const int64_t first_i = t.tile_i * TM, first_j = t.tile_j * TN;
@@ -269,12 +272,15 @@ __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const P
 
 }  // namespace plane
 
-// Products of one launch: the second one's tiles follow the first one's and share the GPU with their rest.
+// Products of one launch: the second one's tiles follow the first one's and share the GPU with their rest. The sum of a product may be cut into
+// parts of per_cut steps, each of which gives tiles of its own (Tile::cut) for the epilogue to keep apart.
 template <typename Epilogue>
 struct Product {
     Planes A, B;
     int64_t steps;
     Epilogue epilogue;
+    int64_t per_cut = 0;        // 0: not cut
+    int cuts() const { return per_cut > 0 ? (int)((steps + per_cut - 1) / per_cut) : 1; }
 };
 
 namespace plane {
@@ -283,6 +289,7 @@ template <typename Epilogue>
 struct Products {
     Product<Epilogue> product[2];
     int64_t tiles_i[2], tiles_j[2];
+    int cuts[2];
     unsigned blocks_of_first;
 };
 
@@ -294,12 +301,19 @@ void plane_product(Products<Epilogue> all)
     const int which = blockIdx.x < all.blocks_of_first ? 0 : 1;
     const Product<Epilogue> &p = all.product[which];
     const int64_t tiles_i = all.tiles_i[which];
-    int64_t tile_i, tile_j;
-    if (!tile_of_block(blockIdx.x - (which ? all.blocks_of_first : 0), tiles_i, all.tiles_j[which], &tile_i, &tile_j)) return;
+    int64_t tile_i, tile_j, steps = p.steps;
+    int cut;
+    if (!tile_of_block(blockIdx.x - (which ? all.blocks_of_first : 0), tiles_i, all.tiles_j[which], all.cuts[which], &tile_i, &tile_j, &cut)) return;
+    Planes A = p.A, B = p.B;
+    if (p.per_cut > 0) {
+        A.data += cut * p.per_cut * kStepBytes;
+        B.data += cut * p.per_cut * kStepBytes;
+        steps = steps - cut * p.per_cut < p.per_cut ? steps - cut * p.per_cut : p.per_cut;
+    }
     if (EXTRA && tile_i == tiles_i - 1 && p.A.rows > tiles_i * TM)
-        run_tile<MODE, TM, TN, WM, WN, STAGES, EXTRA>(buffers, p.A, p.B, p.steps, tile_i, tile_j, p.epilogue);
+        run_tile<MODE, TM, TN, WM, WN, STAGES, EXTRA>(buffers, A, B, steps, tile_i, tile_j, cut, p.epilogue);
     else
-        run_tile<MODE, TM, TN, WM, WN, STAGES, false>(buffers, p.A, p.B, p.steps, tile_i, tile_j, p.epilogue);
+        run_tile<MODE, TM, TN, WM, WN, STAGES, false>(buffers, A, B, steps, tile_i, tile_j, cut, p.epilogue);
 }
 
 }  // namespace plane
@@ -314,15 +328,20 @@ inline int64_t plane_tiles(int64_t rows_a, int64_t rows_b, int tile) { return pl
 // up to 2.1, 0.88 and 0.57 where all do, as the L2s deliver about 9.5 TB/s. (us a step over all tiles, edges 64, 128, 256, 8-bit
 // products of 81 steps but the last: 128 x 16384 rows 0.36, 0.62, 1.29; 128 x 24576 0.96, 0.67, 1.42; 128 x 65536 2.55, 1.91, 1.98; 256 x 32768 2.22,
 // 1.52, 1.74, where 256 is chosen; 256 x 65536 4.51, 3.10, 2.45; 333 x 10000, 41 steps 0.80, 0.65, 1.73.)
+struct PlaneWay { int edge; double slots, alone, beside; };
+constexpr PlaneWay kPlaneWays[] = {{256, 256, 1.2, 0.9}, {128, 256, 0.48, 0.4}, {64, 512, 0.22, 0.35}};
+inline double plane_step_time(const PlaneWay &way, double tiles)
+{
+    const double full = (double)(int64_t)(tiles / way.slots), rest = tiles - full * way.slots;
+    return full * (way.alone + way.beside) + (rest > 0 ? way.alone + way.beside * rest / way.slots : 0.0);
+}
 template <typename Tiles>
 int plane_tile_of(const Tiles &tiles)
 {
-    struct { int edge; double slots, alone, beside; } const ways[] = {{256, 256, 1.2, 0.9}, {128, 256, 0.48, 0.4}, {64, 512, 0.22, 0.35}};
     int best = 0;
     double least = 0.0;
-    for (const auto &way : ways) {
-        const double n = tiles(way.edge), full = (double)(int64_t)(n / way.slots), rest = n - full * way.slots;
-        const double time = full * (way.alone + way.beside) + (rest > 0 ? way.alone + way.beside * rest / way.slots : 0.0);
+    for (const PlaneWay &way : kPlaneWays) {
+        const double time = plane_step_time(way, tiles(way.edge));
         if (best == 0 || time < least) {
             best = way.edge;
             least = time;
@@ -351,7 +370,8 @@ hipError_t launch_tiles(const Product<Epilogue> *p, int count, hipStream_t strea
         all.product[k] = p[k < count ? k : 0];
         all.tiles_i[k] = plane_tiles_a(all.product[k].A.rows, TM);
         all.tiles_j[k] = (all.product[k].B.rows + TN - 1) / TN;
-        if (k < count) blocks[k] = blocks_of(all.tiles_i[k] * all.tiles_j[k]);
+        all.cuts[k] = all.product[k].cuts();
+        if (k < count) blocks[k] = blocks_of(all.tiles_i[k] * all.tiles_j[k] * all.cuts[k]);
     }
     all.blocks_of_first = blocks[0];
     kernel<<<dim3(blocks[0] + blocks[1]), dim3(64 * WM * WN), lds, stream>>>(all);
@@ -373,7 +393,7 @@ hipError_t launch_plane_products(const Product<Epilogue> *p, int count, int tile
 template <PlaneMode MODE, typename Epilogue>
 hipError_t launch_plane_product(const Planes &A, const Planes &B, int64_t steps, int tile, const Epilogue &epilogue, hipStream_t stream)
 {
-    const Product<Epilogue> p = {A, B, steps, epilogue};
+    const Product<Epilogue> p = {A, B, steps, epilogue, 0};
     return launch_plane_products<MODE>(&p, 1, tile, stream);
 }
 

@@ -307,6 +307,7 @@ struct Gradient {
     const uint32_t *count;              // ... and, without weights (else null), one scale
     const float *add;                   // [cols_j][add_ld] of the blocks before, or null
     int64_t add_ld;
+    int64_t cut_stride;                 // numbers from one part of a cut sum to the next
 
     template <typename T>
     __device__ __forceinline__ void operator()(T &t) const
@@ -314,9 +315,11 @@ struct Gradient {
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
         const int all = terms ? 0 : (int)stats->top - kTopBias;
         const float mean = count ? 1.0f / (float)max(*count, 1u) : 1.0f;
+        const int64_t first_of_cut = t.cut * cut_stride;
         t.each_block([&](const auto &acc, int64_t first, int b) __attribute__((always_inline)) {
             const int64_t j = t.j0 + 32 * b + col;
             if (j >= cols_j) return;
+            const int64_t row = first_of_cut + j * ld;
             const float scale = terms ? terms[j].scale : mean;
             const int shift = (terms ? terms[j].reach : all) - 2 * kTopBit;
 #pragma unroll
@@ -328,7 +331,7 @@ struct Gradient {
                     v[e] = ldexpf(acc[4 * q + e], shift) * scale;
                     if (add && i + e < rows_i) v[e] += add[j * add_ld + i + e];
                 }
-                if (i < rows_i) store(j * ld + i, rows_i - i, v);
+                if (i < rows_i) store(row + i, rows_i - i, v);
             }
         });
     }
@@ -356,8 +359,74 @@ struct Gradient {
     }
 };
 
+// Adds the parts of cut sums up. Bound by memory.
+struct CutSum {
+    const float *parts;                 // [cuts][numbers / K][K]
+    void *out;
+    const float *add;                   // or null
+    int64_t ld, add_ld, numbers, cuts, bf16;
+};
+// (A sum is chosen as a whole, by whole words: flags of a byte, indexed in the arguments beside longer fields, have been read with scalar loads from addresses
+// that are no multiples of four, whose last bits these ignore.)
+struct AddJob {
+    CutSum first, second;
+    int64_t K;
+    unsigned groups_of_first;
+};
+__global__ __launch_bounds__(256) void add_kernel(AddJob job)
+{
+    const bool is_first = blockIdx.x < job.groups_of_first;
+    const CutSum s = is_first ? job.first : job.second;
+    const int64_t m = (int64_t)(blockIdx.x - (is_first ? 0 : job.groups_of_first)) * 256 + threadIdx.x;
+    if (m >= s.numbers) return;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t c = 0; c < s.cuts; ++c) sum += s.parts[c * s.numbers + m];
+    const int64_t j = m / job.K, i = m - j * job.K;
+    if (s.add) sum += s.add[j * s.add_ld + i];
+    if (s.bf16) static_cast<__bf16 *>(s.out)[j * s.ld + i] = (__bf16)sum;
+    else static_cast<float *>(s.out)[j * s.ld + i] = sum;
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // Workspace and order of work.
+// How the gradients' products of a block of rows are made: the tiles' edge, and the parts of their sums (dPhi, dW), by the steps' time. A long sum of few tiles
+// leaves CUs without work; cut, it costs its parts' way through memory and a launch. (us a call, whole and cut: 7487 x 316, 365 classes, float32, dW
+// 105 and 56; 1209 x 88, 7765, float32, dPhi 129 and 81; 9000 x 4000, 300, bfloat16, both 278 and 237, of which some by the longer tiles' being first; 8638 x
+// 3613, 172, float32, dPhi, not cut, 255 and 266. Of 60 shapes with 65 to 10000 rows and 65 to 33000 classes the geometric mean is 1.11.)
+struct GradientPlan { int edge, cuts[2]; };
+constexpr double kPartRate = 3e6, kAddTime = 5.0;                  // bytes a us, written and read; us
+constexpr int64_t kMostPartBytes = (int64_t)256 << 20;
+constexpr int kStartSteps = 4;                                     // what a tile costs besides its steps, in steps
+GradientPlan plan_gradients(bool d_phi, bool d_w, bool two, int64_t rows, int64_t K, int64_t C, bool may_cut)
+{
+    const bool asked[2] = {d_phi, d_w};
+    const int64_t steps[2] = {d_phi ? plane_steps(C, two) : 0, d_w ? plane_steps(rows, two) : 0}, across[2] = {rows, C};
+    GradientPlan best = {0, {1, 1}};
+    double least = 0.0;
+    for (const PlaneWay &way : kPlaneWays) {
+        const double tiles[2] = {d_phi ? (double)plane_tiles(K, rows, way.edge) : 0.0, d_w ? (double)plane_tiles(K, C, way.edge) : 0.0};
+        int most[2];
+        for (int p = 0; p < 2; ++p) {
+            most[p] = 1;
+            while (may_cut && asked[p] && 2 * most[p] <= 32 && tiles[p] * most[p] < way.slots && steps[p] / (2 * most[p]) >= 8 &&
+                   4 * K * across[p] * 2 * most[p] <= kMostPartBytes)
+                most[p] *= 2;
+        }
+        for (int a = 1; a <= most[0]; a *= 2)
+            for (int b = 1; b <= most[1]; b *= 2) {
+                const double s0 = asked[0] ? (double)steps[0] / a + kStartSteps : 0.0, s1 = asked[1] ? (double)steps[1] / b + kStartSteps : 0.0;
+                const double longest = std::max(s0, s1), count = (tiles[0] * a * s0 + tiles[1] * b * s1) / longest;
+                double time = plane_step_time(way, count) * longest;
+                if (a > 1 || b > 1) time += kAddTime + 8.0 * (double)K * ((a > 1 ? (double)a * (double)rows : 0.0) + (b > 1 ? (double)b * (double)C : 0.0)) / kPartRate;
+                if (best.edge == 0 || time < least) {
+                    best = {way.edge, {a, b}};
+                    least = time;
+                }
+            }
+    }
+    return best;
+}
 constexpr int64_t kUnit = 64;                           // rows of a block are counted in these
 // Tiles of classes whose parts the pass to G joins by itself, every workgroup those of its rows, which saves a launch; with more of them they are read
 // too often. (us a call, apart and here: 4454 x 257, 468 classes, bfloat16, dPhi 46.0 and 43.4; 1000 x 1025, 1000, float32, both 67.3 and 65.5; 1432 x
@@ -391,8 +460,15 @@ struct Sizes {
         if (d_phi) b += up((size_t)rows * plane_pitch(C, two));
         if (d_w) b += up((size_t)C * plane_pitch(rows, two)) + up((size_t)K * plane_pitch(rows, two));
         if (d_w && !two && rows < N) b += up(4 * (size_t)C * (size_t)K);        // sums of the blocks before
+        if (d_phi || d_w) {
+            const GradientPlan plan = gradients(rows);
+            b += parts(plan.cuts[0], rows) + parts(plan.cuts[1], C);
+        }
         return b;
     }
+    // (a workspace for small blocks only has none for parts either)
+    GradientPlan gradients(int64_t rows) const { return plan_gradients(d_phi, d_w, two, rows, K, C, rows >= std::min<int64_t>(N, 1024)); }
+    size_t parts(int cuts, int64_t across) const { return cuts > 1 ? up(4 * (size_t)cuts * (size_t)K * (size_t)across) : 0; }
     size_t scores(int64_t rows) const { return d_phi || d_w ? up(4 * (size_t)rows * (size_t)ld_scores) : 0; }
     int64_t score_rows(int64_t rows) const
     {
@@ -496,6 +572,8 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
     char *g_classes = z.d_w ? ws.take<char>((size_t)C * pitch_n) : nullptr;
     char *phi_columns = z.d_w ? ws.take<char>((size_t)K * pitch_n) : nullptr;
     float *sums = z.d_w && bf16 && plan.rows < N ? ws.take<float>(4 * (size_t)C * (size_t)K) : nullptr;
+    const GradientPlan how = gradients ? z.gradients(plan.rows) : GradientPlan{64, {1, 1}};
+    float *parts_phi = ws.take<float>(z.parts(how.cuts[0], plan.rows)), *parts_w = ws.take<float>(z.parts(how.cuts[1], C));
     float *scores = gradients ? ws.take<float>(4 * (size_t)plan.score_rows * (size_t)z.ld_scores) : nullptr;
 
     // the scale of rows without weights is known from the rows' packing, unless they are packed in several blocks
@@ -538,26 +616,44 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
         }
         if (!gradients) continue;
         Product<Gradient> products[2];
-        int count_of_products = 0;
-        if (z.d_phi)
-            products[count_of_products++] = {Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two),
-                                             Gradient{static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16,
-                                                      terms, nullptr, nullptr, nullptr, 0}};
+        AddJob sum = {};
+        int count_of_products = 0, cut_sums = 0;
+        // a product whose sum is cut writes parts, which are added up to what it would have written
+        auto cut = [&](Product<Gradient> &p, int cuts, float *parts) {
+            p.per_cut = (p.steps + cuts - 1) / cuts;
+            if (p.cuts() == 1) return;
+            Gradient &g = p.epilogue;
+            (cut_sums++ == 0 ? sum.first : sum.second) = {parts, g.out, g.add, g.ld, g.add_ld, K * g.cols_j, p.cuts(), g.bf16};
+            g.out = parts;
+            g.ld = K;
+            g.bf16 = false;
+            g.add = nullptr;
+            g.cut_stride = K * g.cols_j;
+        };
+        if (z.d_phi) {
+            products[count_of_products] = {Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two),
+                                           Gradient{static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16,
+                                                    terms, nullptr, nullptr, nullptr, 0, 0}, 0};
+            cut(products[count_of_products++], how.cuts[0], parts_phi);
+        }
         if (z.d_w) {
             const bool to_sums = sums && n0 + rows < N;
             const float *add = n0 == 0 ? nullptr : sums ? sums : static_cast<const float *>(dW);
-            products[count_of_products++] = {Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two),
-                                             Gradient{to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr,
-                                                      stats, count, add, sums ? K : shape.ld_dw}};
+            products[count_of_products] = {Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two),
+                                           Gradient{to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr,
+                                                    stats, count, add, sums ? K : shape.ld_dw, 0}, 0};
+            cut(products[count_of_products++], how.cuts[1], parts_w);
         }
-        const int64_t longest = count_of_products > 1 ? std::max(products[0].steps, products[1].steps) : products[0].steps;
-        const int edge = plane_tile_of([&](int e) {
-            double tiles = 0;
-            for (int k = 0; k < count_of_products; ++k)
-                tiles += (double)plane_tiles(products[k].A.rows, products[k].B.rows, e) * (double)products[k].steps / (double)longest;
-            return tiles;
-        });
-        RFSF_TRY(launch_plane_products<MODE>(products, count_of_products, edge, stream));
+        // the longer tiles first, so that the others fill up behind them
+        if (count_of_products == 2 && products[1].per_cut > products[0].per_cut) std::swap(products[0], products[1]);
+        RFSF_TRY(launch_plane_products<MODE>(products, count_of_products, how.edge, stream));
+        if (cut_sums > 0) {
+            sum.K = K;
+            sum.groups_of_first = (unsigned)((sum.first.numbers + 255) / 256);
+            const unsigned groups = sum.groups_of_first + (unsigned)((sum.second.numbers + 255) / 256);
+            add_kernel<<<dim3(groups), dim3(256), 0, stream>>>(sum);
+            RFSF_TRY(hipGetLastError());
+        }
     }
     return hipSuccess;
 }

@@ -1168,19 +1168,23 @@ Places places_of(const rfsf_xent_shape &s, const DirectGradient &dphi, const Dir
 
 }  // namespace
 
-// Where this way is the faster one: for up to 16 rows or classes everywhere, otherwise by the products N K C and by h = N C / (N + C),
-// their ratio to what the packed way reads and writes beside them. Of 260 shapes with 17 to 10000 rows, 65 to 10241 columns and 17 to
-// 50000 classes, N K C from 5e6 to 6e9, both types and any gradients, all timed both ways, the way chosen takes 2.3 % longer than the better one
-// on average. (us, packed and here: 24 x 5648, 2103 classes, bfloat16, dW 104 and 60; 93 x 2829, 1310, float32, dW 80 and 56;
-// 7060 x 1164, 11, float32, dW 123 and 47; 1 x 2283, 42173, float32, both 2702 and 345; but 348 x 283, 6096, bfloat16, dW 51 and 95; 1724 x
-// 897, 589, bfloat16, dPhi 52 and 130; 7843 x 1026, 288, float32, dW 152 and 257.)
+// Where this way is the faster one: for up to 16 rows or classes everywhere, otherwise by the products N K C, of which each gradient weighs four times as
+// much as before it (the packed way packs and makes scores in any case), and by h = N C / (N + C), their ratio to what the packed way reads and
+// writes beside them. Of 150 shapes with 17 to 10000 rows, 65 to 10241 columns and 17 to 50000 classes, N K C from 3e7 to 6e9, both types and
+// any gradients, all timed both ways, the way chosen takes 1.8 % longer than the better one on average; fitted to half of them, 3.4 % with the other
+// half. (us, packed and here: 30 x 7544, 158 classes, float32, losses 81 and 13; 2845 x 6843, 47, float32, dPhi 153 and 102; 375 x 4022, 283,
+// bfloat16, losses 40 and 21; but 8161 x 4507, 42, bfloat16, both 193 and 330; 129 x 1805, 4490, bfloat16, dW 68 and 166; 222 x 565, 34570, bfloat16,
+// both 162 and 637.)
 bool xent_direct(const rfsf_xent_shape &s)
 {
     const double n = (double)s.N, c = (double)s.C;
     if (s.N < 1 || s.C > 1000000 || n * c > 1 << 26) return false;
     if (is_few(s)) return true;
-    const double h = n * c / (n + c), products = n * c * (double)s.K;
-    return products <= (h <= 64 ? 4e9 : h <= 128 ? 1e9 : h <= 256 ? 2.5e8 : 1e8);
+    const double h = n * c / (n + c);
+    double products = n * c * (double)s.K;
+    if (s.gradients & RFSF_XENT_DPHI) products *= 4;
+    if (s.gradients & RFSF_XENT_DW) products *= 4;
+    return products <= (h <= 64 ? 4e9 : h <= 128 ? 1.5e9 : h <= 256 ? 3e8 : 6e7);
 }
 
 size_t xent_direct_bytes(const rfsf_xent_shape &s)

@@ -92,6 +92,20 @@ def test_the_smallest_workspace(N, K, C, bf16, weighted):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("need_dPhi,need_dW", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("N,K,C", [(3000, 130, 150), (150, 130, 3000), (2501, 259, 210), (5000, 67, 1300)])
+@pytest.mark.parametrize("share", [1.0, 0.4])
+def test_long_sums_of_few_tiles(N, K, C, share, need_dPhi, need_dW, bf16):
+    """Gradients whose sums are cut into parts; with less workspace, of blocks of rows that add to those before."""
+    phi, w, y, s = _inputs(N, K, C, bf16)
+    most, least = rfsf.rfsf_softmax_xent_workspace_bytes(N, K, C, phi.dtype, need_dPhi, need_dW)
+    size = max(least, int(share * most))
+    guard = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+    _check(phi, w, y, s, rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=need_dPhi, need_dW=need_dW, workspace=guard[:size]))
+    assert torch.all(guard[size:] == 255)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("N,K,C", [(130, 40, 20), (130, 40, 300), (14, 40, 300), (300, 40, 7), (620, 300, 600)])
 def test_rows_left_out_may_hold_anything(N, K, C, bf16):
     phi, w, y, s = _inputs(N, K, C, bf16, left=0.5)
