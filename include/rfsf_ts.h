@@ -278,12 +278,14 @@ int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W
  *          there. Labels >= C give NaN (they are not used as addresses).
  *   weight [N] float32 or NULL; loss [N] float32
  *   dPhi, dW: read only if RFSF_XENT_DPHI, RFSF_XENT_DW are set in `gradients`; columns beyond K are untouched
- * The scores are never held whole: without gradients they stay in registers, with gradients the workspace holds them for a part of
+ * The scores are never held whole where there are many: without gradients they stay in registers, with gradients the workspace holds them for a part of
  * the rows. A smaller workspace means more parts.
- * Accuracy: float32 operands enter the products with 22 significand bits down to 2^-17 of the largest number of their row, and with an
+ * Accuracy: sums are held in 32 bits. Small problems (which ones follows from N, K, C, the type and `gradients` alone) are worked on straight from the matrices:
+ * float32 operands enter the products whole; G enters those of the gradients whole too, or with bfloat16 operands as two terms of bfloat16, 16 bits.
+ * Of the others, float32 operands enter the products with 22 significand bits down to 2^-17 of the largest number of their row, and with an
  * error below 2^-38 of it beyond; bfloat16 operands enter whole down to 2^-30 of it. G enters the gradients' products with 22 bits (11
  * with bfloat16 operands), or with an error of 2^-38 of the largest product that it takes part in: of the largest |G[n, c]| max_k |W[c, k]| of
- * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. Sums are held in 32 bits. A row of Phi
+ * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. A row of Phi
  * or W that holds an infinity or a NaN makes what is computed from it NaN (bfloat16: or what infinities give). Equal calls with workspaces
  * of equal sizes give equal bits.
  * Limits: K, C <= 3500000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW.
