@@ -33,13 +33,14 @@ class _AdamwTensor(ctypes.Structure):
 
 def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
     """Row stride of a 2-D device tensor of float32 or bfloat16 with unit column stride."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in _BF16 or (t.shape[1] > 1 and t.stride(1) != 1):
+    sizes, strides = t.shape, t.stride()
+    if len(sizes) != 2 or not t.is_cuda or t.dtype not in _BF16 or (strides[1] != 1 and sizes[1] > 1):
         raise ValueError(f"{name} must be float32 or bfloat16 [rows, cols] on the device with unit column stride")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and sizes != shape:
         raise ValueError(f"{name} must have shape {list(shape)}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    return strides[0] if sizes[0] > 1 else max(sizes[1], 1)
 
 
 def rfsf_softmax_xent_workspace_bytes(N: int, K: int, C: int, dtype: torch.dtype = torch.float32, need_dPhi: bool = False,
@@ -63,17 +64,16 @@ def rfsf_softmax_xent(Phi: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, 
     allocated."""
     ld_phi, ld_w = _matrix(Phi, "Phi"), _matrix(W, "W", dtype=Phi.dtype)
     N, K = Phi.shape
-    C = W.shape[0]
-    if W.shape[1] != K:
+    C, columns = W.shape
+    if columns != K:
         raise ValueError("Phi and W need the same number of columns")
-    labels = _dev(labels, torch.int64, "labels")
-    if tuple(labels.shape) != (N,):
+    if _dev(labels, torch.int64, "labels").shape != (N,):
         raise ValueError("labels must have shape [N]")
-    if weight is not None and tuple(_dev(weight, torch.float32, "weight").shape) != (N,):
+    if weight is not None and _dev(weight, torch.float32, "weight").shape != (N,):
         raise ValueError("weight must have shape [N]")
     if loss is None:
         loss = _empty_on(stream, N, dtype=torch.float32, device=Phi.device)
-    elif tuple(_dev(loss, torch.float32, "loss").shape) != (N,):
+    elif _dev(loss, torch.float32, "loss").shape != (N,):
         raise ValueError("loss must have shape [N]")
     ld_dphi = ld_dw = 0
     if need_dPhi:
@@ -148,6 +148,8 @@ class RfsfAdamW:
             if tensors:
                 self._words[:, k] = [t.data_ptr() for t in tensors]
         self._words[:, 7] = self._sizes
+        self._address = self._words.ctypes.data
+        self._flat = memoryview(self._words).cast("B").cast("q") if self.params else None
 
     def step(self, grads: Sequence[torch.Tensor], step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -160,9 +162,10 @@ class RfsfAdamW:
         dtype = grads[0].dtype
         if dtype not in _BF16:
             raise ValueError("grads must be float32 or bfloat16")
-        self._words[:, 1] = _addresses(grads, self._sizes, dtype, "grads")
+        for k, address in enumerate(_addresses(grads, self._sizes, dtype, "grads")):
+            self._flat[8 * k + 1] = address
         config = _AdamwConfig(lr, betas[0], betas[1], eps, weight_decay, grad_scale, step, self.state_bits, _BF16[dtype])
-        _check(load_library().rfsf_adamw_step(self._words.ctypes.data, len(grads), ctypes.byref(config), _stream_ptr(stream)))
+        _check(load_library().rfsf_adamw_step(self._address, len(grads), ctypes.byref(config), _stream_ptr(stream)))
 
     def moments(self, out=None, stream: Optional[torch.cuda.Stream] = None):
         """(m, v): lists of float32 tensors, what the states hold. 32 bits: the states themselves; 8 bits: the numbers that the codes
@@ -174,7 +177,7 @@ class RfsfAdamW:
         if any(len(tensors) != len(self.params) for tensors in out):
             raise ValueError("out must hold a tensor for each parameter, twice")
         places = [np.array(_addresses(tensors, self._sizes, torch.float32, "out"), dtype=np.int64) for tensors in out]
-        _check(load_library().rfsf_adamw_moments(self._words.ctypes.data, len(self.params), places[0].ctypes.data, places[1].ctypes.data,
+        _check(load_library().rfsf_adamw_moments(self._address, len(self.params), places[0].ctypes.data, places[1].ctypes.data,
                                                  _stream_ptr(stream)))
         return out
 
@@ -193,13 +196,14 @@ def _code_room(K: int) -> int:
 
 def _codes(codes: torch.Tensor, scales: torch.Tensor) -> int:
     """Row stride of codes [N, K] laid out as rfsf_int8_quantize does, whose rows exist up to their stride."""
-    if codes.dim() != 2 or codes.dtype != torch.int8 or not codes.is_cuda or (codes.shape[1] > 1 and codes.stride(1) != 1):
+    sizes, strides = codes.shape, codes.stride()
+    if len(sizes) != 2 or codes.dtype is not torch.int8 or not codes.is_cuda or (strides[1] != 1 and sizes[1] > 1):
         raise ValueError("codes must be int8 [rows, cols] on the device with unit column stride")
-    N, K = codes.shape
-    ld = codes.stride(0) if N > 1 else _code_room(K)
+    N, K = sizes
+    ld = strides[0] if N > 1 else _code_room(K)
     if N > 0 and codes.storage_offset() + N * ld > codes.untyped_storage().nbytes():
         raise ValueError("rows of codes must have room for their columns rounded up to 128, as rfsf_int8_quantize lays them out")
-    if tuple(_dev(scales, torch.float32, "scales").shape) != (N,):
+    if _dev(scales, torch.float32, "scales").shape != (N,):
         raise ValueError("scales must have shape [rows]")
     return ld
 
@@ -235,8 +239,8 @@ def rfsf_int8_gram(PhiX: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor
     way: the Gram with stored training features, or the scores of a classifier with quantised weights."""
     ldx, ldy = _matrix(PhiX, "PhiX"), _codes(codes, scales)
     Nx, ncols = PhiX.shape
-    Ny = codes.shape[0]
-    if codes.shape[1] != ncols:
+    Ny, columns = codes.shape
+    if columns != ncols:
         raise ValueError("PhiX and codes need the same number of columns")
     if K is None:
         K = _empty_on(stream, (Nx, Ny), dtype=torch.float32, device=PhiX.device)

@@ -177,3 +177,12 @@ def test_gradients_of_the_reference_against_differences():
         d = np.zeros_like(w)
         d[at] = h
         assert abs((total(x, w + d) - total(x, w - d)) / (2 * h) - r["dW"][at]) < 1e-8
+
+
+@pytest.mark.parametrize("state_bits", [8, 32])
+def test_an_optimizer_without_parameters_does_nothing(state_bits):
+    optimizer = rfsf.RfsfAdamW([], state_bits=state_bits)
+    optimizer.step([], step=1, lr=1e-3)
+    assert optimizer.params == [] and optimizer.state["m"] == []
+    with pytest.raises(ValueError):
+        optimizer.step([torch.zeros(3)], step=2, lr=1e-3)
