@@ -337,7 +337,7 @@ int rfsf_adamw_moments(const rfsf_adamw_tensor *tensors, int64_t count, float *c
  * Feature rows as 8-bit integers: codes[n, k] = round(X[n, k] (127 (1 / largest))), ties to even, and scales[n] = largest (1 / 127), with the
  * row's largest magnitude, every operation rounded to float32; rows with nothing above 2^-119 get zeros. X [N, ldx] float32 or bfloat16. codes [N, ld_codes] bytes, rows a multiple of 16
  * bytes apart, from a multiple of 16 on, with room for K rounded up to 128: what lies beyond K up to there is zeroed.
- * A row with an infinity or a NaN gets the scale NaN.
+ * A row with an infinity or a NaN gets the scale NaN. Limits: K <= 131072, N < 2^31.
  */
 int rfsf_int8_quantize(const void *X, int32_t bf16, int64_t N, int64_t ldx, int64_t K, int8_t *codes, int64_t ld_codes, float *scales,
                        void *hip_stream);

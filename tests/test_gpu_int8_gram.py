@@ -42,6 +42,31 @@ def test_codes_are_the_definition_and_the_room_is_cleared(N, K, bf16):
     assert torch.equal(again, codes) and again.stride(0) % 128 == 0
 
 
+def test_more_rows_than_a_launch_has():
+    """2^23 + 9 rows of three columns: every one is quantised, the ones about the launches' ends too."""
+    N = (1 << 23) + 9
+    x = (torch.arange(3 * N, device="cuda", dtype=torch.float32).reshape(N, 3) % 251) - 125
+    codes, scales = rfsf.rfsf_int8_quantize(x)
+    top = x.abs().amax(dim=1)
+    assert torch.equal(scales, top * torch.tensor(1.0 / 127.0, dtype=torch.float32, device="cuda"))
+    for at in (0, (1 << 22) - 4, (1 << 22) + 1, (1 << 23) - 4, N - 9):
+        assert np.array_equal(codes[at:at + 9].cpu().numpy(), _codes(x[at:at + 9])[0])
+    assert torch.equal(codes.abs().amax(dim=1) == 127, top > 0) and torch.all(codes[top == 0] == 0)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,K", [(9, 1), (4096, 1), (4095, 255), (4097, 256), (4103, 511), (5000, 1000), (4099, 1023), (4111, 1024), (4100, 1025)])
+def test_narrow_rows(N, K, bf16):
+    """Few and many of them: a workgroup and a wavefront per row."""
+    x = _rows(N, K, 1, bf16)
+    room = (K + 127) // 128 * 128
+    buf = torch.full((N, room + 16), 77, dtype=torch.int8, device="cuda")
+    codes, scales = rfsf.rfsf_int8_quantize(x, codes=buf[:, :K])
+    want, want_scales = _codes(x)
+    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), want_scales)
+    assert torch.all(buf[:, K:room] == 0) and torch.all(buf[:, room:] == 77)
+
+
 SIZES = [(1, 1, 1), (1, 1000, 1025), (2, 33, 64), (3, 40, 65), (5, 1000, 300), (8, 777, 129), (9, 500, 1001), (16, 65, 40), (17, 300, 2049), (40, 63, 5),
          (64, 64, 128), (65, 129, 127), (300, 257, 70), (130, 3000, 513), (1, 7, 10241), (4, 4, 131072),
          (8, 100, 1024), (8, 100, 1025), (16, 300, 511), (3, 17000, 129), (12, 16385, 200), (16, 20001, 70), (260, 17000, 33), (2500, 5124, 40)]
