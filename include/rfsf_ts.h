@@ -322,7 +322,7 @@ typedef struct {
     void *m, *v;                /* updated */
     float *m_scale, *v_scale;   /* 8-bit states only */
     void *copy;
-    int64_t n;                  /* >= 0 */
+    int64_t n;                  /* >= 0, <= 2^35 (RFSF_E_UNSUPPORTED) */
 } rfsf_adamw_tensor;
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay, grad_scale;  /* finite; 0 <= beta < 1, eps, lr, weight_decay >= 0 */

@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void moments_kernel(Job job)
 
 bool four(const void *p, size_t element) { return reinterpret_cast<uintptr_t>(p) % (4 * element) == 0; }
 
-// Goes through the tensors, at most kTensors and 2^30 workgroups a launch; tensors without numbers take no part.
+// Goes through the tensors, at most kTensors a launch, and not more than 2^32 threads; tensors without numbers take no part.
 template <typename Tensor, typename Launch>
 hipError_t for_each_launch(const Tensor &tensor, int64_t count, size_t grad_size, size_t state_size, size_t copy_size, const Launch &launch)
 {
@@ -247,7 +247,7 @@ hipError_t for_each_launch(const Tensor &tensor, int64_t count, size_t grad_size
     int64_t chunks = 0;
     for (int64_t k = 0; k <= count; ++k) {
         const int64_t more = k < count ? (tensor(k).n + kChunk - 1) / kChunk : 0;
-        if (job.count > 0 && (k == count || job.count == kTensors || chunks + more > (1 << 30))) {
+        if (job.count > 0 && (k == count || job.count == kTensors || chunks + more > (1 << 23))) {
             job.first_chunk[job.count] = (int32_t)chunks;
             launch(job, (unsigned)chunks);
             const hipError_t e = hipGetLastError();

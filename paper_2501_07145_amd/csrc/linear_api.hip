@@ -9,7 +9,7 @@ constexpr int64_t kMostColumns = 3500000;       // 287 packed rows of a tile sta
 constexpr int64_t kMostRows = 0x7fffffffLL;
 constexpr int64_t kMostCodes = 131072;          // 127 * 128 times that stays below 2^31
 constexpr int64_t kMostStored = 100000000;
-constexpr int64_t kMostNumbers = (int64_t)1 << 42;
+constexpr int64_t kMostNumbers = (int64_t)1 << 35;          // 2^23 workgroups of 256 threads: a launch has fewer than 2^32 threads
 
 int check(const rfsf_xent_shape *s)
 {
