@@ -94,5 +94,8 @@ struct PackPair {
 };
 hipError_t launch_largest(const PackPair &pair, bool bf16, hipStream_t stream);
 hipError_t launch_pack(const PackPair &pair, bool bf16, hipStream_t stream);
+// Both in one, for matrices of up to kPackRowsColumns columns that are packed by rows alone, without stats.
+constexpr int64_t kPackRowsColumns = 12288;
+hipError_t launch_pack_rows(const PackPair &pair, bool bf16, hipStream_t stream);
 
 }  // namespace rfsf

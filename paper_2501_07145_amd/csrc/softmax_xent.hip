@@ -590,8 +590,12 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
                                   phi_rows, phi_columns, pitch_k, pitch_n};
         PackPair pair = {{pack_w, pack_phi}, gradients ? stats : nullptr, weight ? weight + n0 : nullptr};
         if (n0 > 0) pair.job[0].R = 0;
-        RFSF_TRY(launch_largest(pair, bf16, stream));
-        RFSF_TRY(launch_pack(pair, bf16, stream));
+        if (!gradients && K <= kPackRowsColumns) {
+            RFSF_TRY(launch_pack_rows(pair, bf16, stream));
+        } else {
+            RFSF_TRY(launch_largest(pair, bf16, stream));
+            RFSF_TRY(launch_pack(pair, bf16, stream));
+        }
         const int64_t step = gradients ? plan.score_rows : rows;
         for (int64_t m0 = 0; m0 < rows; m0 += step) {
             const int64_t part = std::min(step, rows - m0);

@@ -68,6 +68,18 @@ def test_what_is_not_asked_for(N, K, C, bf16, need_dPhi, need_dW):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,K,C", [(700, 1, 900), (700, 64, 901), (701, 1023, 900), (900, 1024, 701), (600, 1025, 702), (330, 4096, 600), (331, 4097, 601), (300, 12288, 500),
+                                   (301, 12289, 500)])
+def test_losses_of_packed_operands(N, K, C, bf16):
+    """Widths around those that are packed in each way; rows that are left out hold anything."""
+    phi, w, y, s = _inputs(N, K, C, bf16)
+    phi[y < 0] = float("nan")
+    loss, dPhi, dW = rfsf.rfsf_softmax_xent(phi, w, y, weight=s)
+    assert dPhi is None and dW is None
+    _check(phi, w, y, s, (loss, None, None))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("weighted", [False, True])
 @pytest.mark.parametrize("need_dPhi,need_dW", [(True, True), (True, False), (False, True)])
 @pytest.mark.parametrize("N,K,C", [(1, 4, 1), (2, 5, 3), (7, 3, 2), (17, 255, 4), (130, 256, 5), (129, 257, 8), (701, 514, 9), (2100, 1025, 16), (300, 2047, 16),
