@@ -173,7 +173,7 @@ void launch_few_rows(const int8_t *qx, int64_t pitch_x, const float *sx, int64_t
 }
 
 // The same for rows of X of kHeldCodes columns altogether, quantised by every workgroup for itself into LDS: one launch instead of two, where there
-// are few workgroups and the second launch is what counts (1 x 1025 against 1000: 5.4 us for the kernel, 8.8 for the call; 6.0 for the two kernels, 11.2 for the call).
+// are few workgroups and the second launch is what counts (1 x 1025 against 1000: 5.5 us for the kernel, 7.6 for the call; 6.0 for the two kernels).
 constexpr int kHeldCodes = 8192, kHeldPad = 16;          // (rows 16 bytes apart in their banks)
 template <typename T>
 __global__ __launch_bounds__(256) void few_small_kernel(const T *X, int64_t ldx, int Nx, int K, const int8_t *codes, int64_t ld, const float *scales,
