@@ -283,8 +283,8 @@ int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W
  * Accuracy: sums are held in 32 bits. Small problems (which ones follows from N, K, C, the type and `gradients` alone) are worked on straight from the matrices:
  * float32 operands enter the products whole; G enters those of the gradients whole too, or with bfloat16 operands as two terms of bfloat16, 16 bits.
  * Of the others, float32 operands enter the products with 22 significand bits down to 2^-17 of the largest number of their row, and with an
- * error below 2^-38 of it beyond; bfloat16 operands enter whole down to 2^-30 of it. G enters the gradients' products with 22 bits (11
- * with bfloat16 operands), or with an error of 2^-38 of the largest product that it takes part in: of the largest |G[n, c]| max_k |W[c, k]| of
+ * error below 2^-38 of it beyond; bfloat16 operands enter whole down to 2^-30 of it. G enters the gradients' products with 22 bits,
+ * or with an error of 2^-38 of the largest product that it takes part in: of the largest |G[n, c]| max_k |W[c, k]| of
  * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. A row of Phi
  * or W that holds an infinity or a NaN makes what is computed from it NaN (bfloat16: or what infinities give). Equal calls with workspaces
  * of equal sizes give equal bits.

@@ -8,6 +8,8 @@
 // The transposed operand holds the same 16-bit numbers. Where it is multiplied, a row's power of two belongs to an index that is
 // summed over, and is taken back in the other factor: (G[n, c] 2^e_c) (W[c, k] 2^-e_c). A class whose weights are far larger than the
 // others' (an offset of -1e30 that shuts it off) then costs the others nothing, as long as its G is zero.
+//
+// That other factor, G, always enters as two terms, whatever the operands' type: differences of almost equal numbers of G are gradients like any others.
 #pragma once
 
 #include "rfsf_internal.h"

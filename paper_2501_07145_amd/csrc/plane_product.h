@@ -5,13 +5,14 @@
 //   kHalfTwo  32 columns of two terms: 64 bytes of the rounded numbers, then 64 bytes of what rounding left over. The product
 //             of a pair of numbers is lo*hi + hi*lo + hi*hi, accumulated in 32 bits in this order (lo*lo is below 2^-22 of it);
 //   kInt8     128 columns of 8-bit integers, accumulated exactly in 32 bits.
-// Columns beyond the operands' are zero in one of the two at least (kInt8) or in both. All three ways move the same bytes from
+// Columns beyond the operands' are zero in one of the two at least (kInt8) or in both. These ways move the same bytes from
 // memory through LDS into registers and differ in the matrix instructions alone: a lane's 16 bytes are 8 or 16 consecutive columns of one row.
+//   kHalfByTwo  A as in kHalf, half a step of it at a time, B as in kHalfTwo: lo*x + hi*x of 32 columns.
 //
 // Tile TM x TN, WM x WN wavefronts, blocks of 32 x 32. A step of the tile goes from memory straight into LDS (16 bytes a
 // lane), into the buffer that the step before last used, while the step that arrived before is multiplied: one barrier a
 // step. LDS: row r's 128 bytes are 8 chunks of 16, chunk c at place c ^ (r & 7), so that 8 lanes that read the same chunk of 8
-// rows meet all banks once (and the permutation is made by the loads' addresses, at no cost).
+// rows meet all banks once (and the permutation is made by the loads' addresses, at no cost). Rows of 64 bytes: chunk c at place c ^ (r / 2 & 3).
 //
 // What bounds it: with tiles of 256 and random numbers the power that the matrix instructions draw and what the L2s deliver, about equally. 32768 x 2048 x
 // 8192 of 16-bit numbers 877 us (1250 TFLOP/s); the same without the loads 710, the loads alone 560 to 730, the matrix instructions alone 490 to 540.
@@ -24,8 +25,9 @@
 
 namespace rfsf {
 
-enum PlaneMode { kHalf = 0, kHalfTwo = 1, kInt8 = 2 };
+enum PlaneMode { kHalf = 0, kHalfTwo = 1, kInt8 = 2, kHalfByTwo = 3 };
 constexpr int kStepBytes = 128;
+constexpr int step_bytes_a(PlaneMode mode) { return mode == kHalfByTwo ? kStepBytes / 2 : kStepBytes; }
 
 struct Planes {
     const char *data;
@@ -114,9 +116,11 @@ template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA
 __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const Planes &B, int64_t steps, int64_t tile_i, int64_t tile_j, int cut, const Epilogue &epilogue)
 {
     typedef Tile<MODE, TM, TN, WM, WN, EXTRA> T;
-    constexpr int BM = T::BM, BN = T::BN, kRows = TM + TN + (EXTRA ? 32 : 0), kBuffer = kRows * kStepBytes, NL = (TM + TN) / 8 / (WM * WN);
-    static_assert((TM + TN) % (8 * WM * WN) == 0 && TM % 8 == 0, "every wavefront loads whole groups of eight rows");
-    static_assert(!EXTRA || (WM == BN && WM * WN >= 4 && STAGES == 2), "a block for every wavefront, eight rows for each of four");
+    constexpr int BM = T::BM, BN = T::BN, kStepA = step_bytes_a(MODE), kLoadRows = 1024 / kStepA;           // rows of A that a load of a wavefront brings
+    constexpr int kLoadsA = TM / kLoadRows, kStartB = TM * kStepA, kStartX = kStartB + TN * kStepBytes, kBuffer = kStartX + (EXTRA ? 32 * kStepA : 0);
+    constexpr int NL = (kLoadsA + TN / 8) / (WM * WN);
+    static_assert((kLoadsA + TN / 8) % (WM * WN) == 0 && TM % kLoadRows == 0, "every wavefront makes as many loads, of whole groups of rows");
+    static_assert(!EXTRA || (WM == BN && WM * WN >= 4 && STAGES == 2), "a block for every wavefront, one load of its rows for each of a few");
     static_assert(STAGES >= 2 && (STAGES - 1) * NL < 64, "loads in flight can be counted");
     T t;
     t.tile_i = tile_i;
@@ -138,19 +142,21 @@ __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const P
     uint32_t off[NL + 1];       // from the tile's first row: at most 287 rows on, checked by the callers to stay below 2^32
 #pragma unroll
     for (int l = 0; l <= NL; ++l) {
-        const int row0 = l < NL ? 8 * (wave * NL + l) : TM + TN + 8 * wave, row = row0 + (lane >> 3);
-        const bool is_b = l < NL && row0 >= TM;
-        const int64_t last = is_b ? B.rows - 1 - first_j : A.rows - 1 - first_i, r = is_b ? row - TM : l < NL ? row : row - TN;
-        off[l] = (uint32_t)((r < last ? r : last) * (is_b ? B.pitch : A.pitch)) + 16u * (uint32_t)((lane & 7) ^ (lane >> 3));
+        const int at = l < NL ? wave * NL + l : wave;
+        const bool is_b = l < NL && at >= kLoadsA;
+        const int row = is_b ? 8 * (at - kLoadsA) + (lane >> 3) : (l < NL ? 0 : TM) + kLoadRows * at + lane / (kStepA / 16);
+        const int chunk = is_b || kStepA == kStepBytes ? (lane & 7) ^ (lane >> 3) : (lane & 3) ^ (lane >> 3 & 3);
+        const int64_t last = is_b ? B.rows - 1 - first_j : A.rows - 1 - first_i;
+        off[l] = (uint32_t)((row < last ? row : last) * (is_b ? B.pitch : A.pitch)) + 16u * (uint32_t)chunk;
     }
     auto load = [&](int64_t step, int buffer) {
 #pragma unroll
         for (int l = 0; l < NL; ++l) {
-            const int row0 = 8 * (wave * NL + l);
-            direct_load16((row0 >= TM ? base_b : base_a) + step * kStepBytes, off[l], lds + (uint32_t)(buffer * kBuffer + row0 * kStepBytes));
+            const int at = wave * NL + l;
+            direct_load16(at >= kLoadsA ? base_b + step * kStepBytes : base_a + step * kStepA, off[l], lds + (uint32_t)(buffer * kBuffer + 1024 * at));
         }
-        if (EXTRA && wave < 4)
-            direct_load16(base_a + step * kStepBytes, off[NL], lds + (uint32_t)(buffer * kBuffer + (TM + TN + 8 * wave) * kStepBytes));
+        if (EXTRA && wave < 32 / kLoadRows)
+            direct_load16(base_a + step * kStepA, off[NL], lds + (uint32_t)(buffer * kBuffer + kStartX + 1024 * wave));
     };
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -165,20 +171,20 @@ __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const P
     // so that a wavefront's matrix instructions follow one another. Before the last phases of a step, when all of it has been read, the
     // wavefront waits for its loads of the next step (those of the steps after it stay in flight) and then for everybody: the
     // next step can be read, and this step's buffer takes the loads of the step STAGES ahead.
-    const int row_a = t.wave_i * (TM / WM) + col, row_b = TM + t.wave_j * (TN / WN) + col;
+    const int row_a = t.wave_i * (TM / WM) + col, row_b = t.wave_j * (TN / WN) + col, turn_a = kStepA == kStepBytes ? col & 7 : col >> 1 & 3;
     const char *buf = buffers;
     int slot = 0;
     auto read_a = [&](intx4 (&f)[BM], const char *from, int c) {
 #pragma unroll
-        for (int a = 0; a < BM; ++a) f[a] = *reinterpret_cast<const intx4 *>(from + (row_a + 32 * a) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+        for (int a = 0; a < BM; ++a) f[a] = *reinterpret_cast<const intx4 *>(from + (row_a + 32 * a) * kStepA + 16 * ((c + half) ^ turn_a));
     };
     auto read_b = [&](intx4 (&f)[BN], const char *from, int c) {
 #pragma unroll
-        for (int b = 0; b < BN; ++b) f[b] = *reinterpret_cast<const intx4 *>(from + (row_b + 32 * b) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+        for (int b = 0; b < BN; ++b) f[b] = *reinterpret_cast<const intx4 *>(from + kStartB + (row_b + 32 * b) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
     };
     auto read_x = [&](const char *from, int c) {
         if constexpr (!EXTRA) return intx4{0, 0, 0, 0};
-        return *reinterpret_cast<const intx4 *>(from + (TM + TN + col) * kStepBytes + 16 * ((c + half) ^ (col & 7)));
+        return *reinterpret_cast<const intx4 *>(from + kStartX + col * kStepA + 16 * ((c + half) ^ turn_a));
     };
     auto multiply = [&](const intx4 (&fa)[BM], const intx4 (&fb)[BN], const intx4 &fx) {
 #pragma unroll
@@ -239,6 +245,34 @@ __device__ __forceinline__ void run_tile(char *buffers, const Planes &A, const P
                 interleave(std::integral_constant<int, BN>{});
 #pragma unroll
                 for (int b = 0; b < BN; ++b) bh[b] = next[b];
+            }
+            buf = other;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+    } else if constexpr (MODE == kHalfByTwo) {
+        // phases: the rest of columns 0 to 15, their rounded numbers, and the same of 16 to 31; A's fragments serve two of them
+        constexpr int CHUNK[5] = {4, 0, 6, 2, 4};
+        intx4 fa[2][BM], fb[2][BN], fx[2];
+        fx[0] = read_x(buf, 0);
+        read_a(fa[0], buf, 0);
+        read_b(fb[0], buf, CHUNK[0]);
+        for (int64_t s = 0; s < steps; ++s) {
+            const char *other = next_buffer();
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const bool last = ks == 3;
+                if (last) {
+                    landed(s);
+                    if (s + STAGES < steps) load(s + STAGES, slot);
+                }
+                read_b(fb[(ks + 1) & 1], last ? other : buf, CHUNK[ks + 1]);
+                if (ks & 1) {
+                    read_a(fa[last ? 0 : 1], last ? other : buf, last ? 0 : 2);
+                    fx[last ? 0 : 1] = read_x(last ? other : buf, last ? 0 : 2);
+                }
+                multiply(fa[ks >> 1], fb[ks & 1], fx[ks >> 1]);
+                if (ks & 1) interleave(std::integral_constant<int, BM + BN>{});
+                else interleave(std::integral_constant<int, BN>{});
             }
             buf = other;
             slot = slot + 1 == STAGES ? 0 : slot + 1;
@@ -306,7 +340,7 @@ void plane_product(Products<Epilogue> all)
     if (!tile_of_block(blockIdx.x - (which ? all.blocks_of_first : 0), tiles_i, all.tiles_j[which], all.cuts[which], &tile_i, &tile_j, &cut)) return;
     Planes A = p.A, B = p.B;
     if (p.per_cut > 0) {
-        A.data += cut * p.per_cut * kStepBytes;
+        A.data += cut * p.per_cut * step_bytes_a(MODE);
         B.data += cut * p.per_cut * kStepBytes;
         steps = steps - cut * p.per_cut < p.per_cut ? steps - cut * p.per_cut : p.per_cut;
     }
@@ -359,7 +393,7 @@ namespace plane {
 template <PlaneMode MODE, int TM, int TN, int WM, int WN, int STAGES, bool EXTRA, typename Epilogue>
 hipError_t launch_tiles(const Product<Epilogue> *p, int count, hipStream_t stream)
 {
-    constexpr size_t lds = STAGES * (size_t)(TM + TN + (EXTRA ? 32 : 0)) * kStepBytes;
+    constexpr size_t lds = STAGES * (size_t)((TM + (EXTRA ? 32 : 0)) * step_bytes_a(MODE) + TN * kStepBytes);
     static LdsLimit limit;
     auto kernel = plane_product<MODE, TM, TN, WM, WN, STAGES, EXTRA, Epilogue>;
     const hipError_t e = allow_lds(limit, reinterpret_cast<const void *>(kernel), lds);

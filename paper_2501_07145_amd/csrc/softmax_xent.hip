@@ -2,7 +2,7 @@
 //   l[n, c] = sum_k Phi[n, k] W[c, k],   loss[n] = log sum_c exp l[n, c] - l[n, y_n],
 //   G[n, c] = s_n (exp l[n, c] / sum - [c = y_n]),   dPhi = G W,   dW = G^T Phi.
 //
-// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory (float32 operands cost three 16-bit products each). The operands are packed once for
+// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory (float32 operands cost three 16-bit products each, bfloat16 ones one for the scores and two for a gradient, G being two terms). The operands are packed once for
 // the matrix instructions (plane_pack.h), W and Phi by rows for the scores, their transposes for the gradients, so that
 // all three products are of one kind (plane_product.h). The scores of a tile give their maximum and sum of exponentials per row before
 // they leave the registers; without gradients they are never written. For gradients the rows are taken in blocks, and the
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
 // the classes' powers of two: (p - [c = y]) 2^exponent(W[c, :]), brought to 2^14 by the row's own exponent; the rows' scales
 // enter at the end of the product, so that rows of small scale lose nothing. Transposed, for the product with Phi^T: the same with
 // the rows' scales and exponents, brought to 2^14 by the largest of all.
-// Bound by memory (scores read, two operands written), the scores coming from the last-level cache: 1024 x 32768, bfloat16 mode 72 us for 268 MB (3.7 TB/s).
+// Bound by memory (scores read, two operands of two terms written), the scores coming from the last-level cache: 1024 x 32768 100 us for 403 MB (4.0 TB/s).
 struct GradientJob {
     const float *scores;
     int64_t ld, rows, C;
@@ -223,7 +223,7 @@ struct GradientJob {
     int64_t pitch_row, pitch_class;
     JoinJob join;                   // JOIN: the class tiles' parts, of which the terms are made here; the first tiles of classes write them
 };
-template <bool TWO, bool JOIN>
+template <bool JOIN>
 __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
 {
     __shared__ float tile[64][65];
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = c + e < job.C ? ldexpf(g[e], exponent_of(job.largest_w[c + e]) + kTopBit - t.reach) : 0.f;
-                plane::store_terms<TWO>(job.by_row + n * job.pitch_row, c, plane::terms_of<TWO>(x));
+                plane::store_terms<true>(job.by_row + n * job.pitch_row, c, plane::terms_of<true>(x));
             }
         } else {
 #pragma unroll
@@ -292,12 +292,14 @@ __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = tile[8 * group + e][at + u];
-        plane::store_terms<TWO>(job.by_class + c * job.pitch_class, n0 + 8 * group, plane::terms_of<TWO>(x));
+        plane::store_terms<true>(job.by_class + c * job.pitch_class, n0 + 8 * group, plane::terms_of<true>(x));
     }
 }
 
 // A gradient: rows of the tile along the contiguous axis of the result. Both gradients share a launch, so that the second one's tiles fill the CUs
-// that the first one's leave. 8192 x 2049, 32768 classes, bfloat16: 1.93 ms (1140 TFLOP/s); 1000 x 1025, 1000 classes, float32 32 us.
+// that the first one's leave. 8192 x 2049, 32768 classes, bfloat16: 3.61 ms
+// (1220 TFLOP/s of 16-bit products; with G as one term of 11 bits 1.95 ms, and dPhi 3.4e-4 from the rounded exact result instead of 0.9e-4); 1000 x 1025, 1000
+// classes, float32 32 us.
 struct Gradient {
     void *out;
     int64_t ld, rows_i, cols_j;
@@ -398,10 +400,10 @@ struct GradientPlan { int edge, cuts[2]; };
 constexpr double kPartRate = 3e6, kAddTime = 5.0;                  // bytes a us, written and read; us
 constexpr int64_t kMostPartBytes = (int64_t)256 << 20;
 constexpr int kStartSteps = 4;                                     // what a tile costs besides its steps, in steps
-GradientPlan plan_gradients(bool d_phi, bool d_w, bool two, int64_t rows, int64_t K, int64_t C, bool may_cut)
+GradientPlan plan_gradients(bool d_phi, bool d_w, int64_t rows, int64_t K, int64_t C, bool may_cut)
 {
     const bool asked[2] = {d_phi, d_w};
-    const int64_t steps[2] = {d_phi ? plane_steps(C, two) : 0, d_w ? plane_steps(rows, two) : 0}, across[2] = {rows, C};
+    const int64_t steps[2] = {d_phi ? plane_steps(C, true) : 0, d_w ? plane_steps(rows, true) : 0}, across[2] = {rows, C};
     GradientPlan best = {0, {1, 1}};
     double least = 0.0;
     for (const PlaneWay &way : kPlaneWays) {
@@ -457,8 +459,8 @@ struct Sizes {
     {
         size_t b = up((size_t)rows * plane_pitch(K, two)) + up(4 * (size_t)rows) + up(4 * (size_t)rows) + up(sizeof(RowTerms) * (size_t)rows) +
                    up(sizeof(Partial) * (size_t)class_tiles * (size_t)rows);
-        if (d_phi) b += up((size_t)rows * plane_pitch(C, two));
-        if (d_w) b += up((size_t)C * plane_pitch(rows, two)) + up((size_t)K * plane_pitch(rows, two));
+        if (d_phi) b += up((size_t)rows * plane_pitch(C, true));
+        if (d_w) b += up((size_t)C * plane_pitch(rows, true)) + up((size_t)K * plane_pitch(rows, two));
         if (d_w && !two && rows < N) b += up(4 * (size_t)C * (size_t)K);        // sums of the blocks before
         if (d_phi || d_w) {
             const GradientPlan plan = gradients(rows);
@@ -467,7 +469,7 @@ struct Sizes {
         return b;
     }
     // (a workspace for small blocks only has none for parts either)
-    GradientPlan gradients(int64_t rows) const { return plan_gradients(d_phi, d_w, two, rows, K, C, rows >= std::min<int64_t>(N, 1024)); }
+    GradientPlan gradients(int64_t rows) const { return plan_gradients(d_phi, d_w, rows, K, C, rows >= std::min<int64_t>(N, 1024)); }
     size_t parts(int cuts, int64_t across) const { return cuts > 1 ? up(4 * (size_t)cuts * (size_t)K * (size_t)across) : 0; }
     size_t scores(int64_t rows) const { return d_phi || d_w ? up(4 * (size_t)rows * (size_t)ld_scores) : 0; }
     int64_t score_rows(int64_t rows) const
@@ -554,6 +556,7 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
     const bool bf16 = !z.two, gradients = z.d_phi || z.d_w;
     const size_t element = bf16 ? 2 : 4;
     const int64_t pitch_k = plane_pitch(z.K, z.two), pitch_c = plane_pitch(z.C, z.two), pitch_n = plane_pitch(plan.rows, z.two);
+    const int64_t pitch_gc = plane_pitch(z.C, true), pitch_gn = plane_pitch(plan.rows, true);            // of G's two terms
     const int64_t N = z.N, K = z.K, C = z.C;
 
     const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
@@ -568,8 +571,8 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
     RowTerms *terms = ws.take<RowTerms>(sizeof(RowTerms) * (size_t)plan.rows);
     Partial *partial = ws.take<Partial>(sizeof(Partial) * (size_t)z.class_tiles * (size_t)plan.rows);
     char *phi_rows = ws.take<char>((size_t)plan.rows * pitch_k);
-    char *g_rows = z.d_phi ? ws.take<char>((size_t)plan.rows * pitch_c) : nullptr;
-    char *g_classes = z.d_w ? ws.take<char>((size_t)C * pitch_n) : nullptr;
+    char *g_rows = z.d_phi ? ws.take<char>((size_t)plan.rows * pitch_gc) : nullptr;
+    char *g_classes = z.d_w ? ws.take<char>((size_t)C * pitch_gn) : nullptr;
     char *phi_columns = z.d_w ? ws.take<char>((size_t)K * pitch_n) : nullptr;
     float *sums = z.d_w && bf16 && plan.rows < N ? ws.take<float>(4 * (size_t)C * (size_t)K) : nullptr;
     const GradientPlan how = gradients ? z.gradients(plan.rows) : GradientPlan{64, {1, 1}};
@@ -611,11 +614,11 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
                 RFSF_TRY(hipGetLastError());
             }
             if (!gradients) continue;
-            const GradientJob job = {scores, z.ld_scores, part, C, labels + n0 + m0, weight, stats, terms + m0, largest_w, largest_phi + m0, g_rows ? g_rows + m0 * pitch_c : nullptr,
-                                     g_classes ? g_classes + (m0 / 64) * (z.two ? 256 : 128) : nullptr, pitch_c, pitch_n, join};
+            const GradientJob job = {scores, z.ld_scores, part, C, labels + n0 + m0, weight, stats, terms + m0, largest_w, largest_phi + m0, g_rows ? g_rows + m0 * pitch_gc : nullptr,
+                                     g_classes ? g_classes + (m0 / 64) * (2 * kStepBytes) : nullptr, pitch_gc, pitch_gn, join};
             const dim3 grid((unsigned)((C + 63) / 64), (unsigned)((part + 63) / 64));
-            if (join_apart) gradient_kernel<MODE == kHalfTwo, false><<<grid, dim3(256), 0, stream>>>(job);
-            else gradient_kernel<MODE == kHalfTwo, true><<<grid, dim3(256), 0, stream>>>(job);
+            if (join_apart) gradient_kernel<false><<<grid, dim3(256), 0, stream>>>(job);
+            else gradient_kernel<true><<<grid, dim3(256), 0, stream>>>(job);
             RFSF_TRY(hipGetLastError());
         }
         if (!gradients) continue;
@@ -635,7 +638,7 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
             g.cut_stride = K * g.cols_j;
         };
         if (z.d_phi) {
-            products[count_of_products] = {Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_c, rows}, plane_steps(C, z.two),
+            products[count_of_products] = {Planes{w_columns, pitch_c, K}, Planes{g_rows, pitch_gc, rows}, plane_steps(C, true),
                                            Gradient{static_cast<char *>(dPhi) + (size_t)n0 * shape.ld_dphi * element, shape.ld_dphi, K, rows, bf16,
                                                     terms, nullptr, nullptr, nullptr, 0, 0}, 0};
             cut(products[count_of_products++], how.cuts[0], parts_phi);
@@ -643,14 +646,14 @@ hipError_t xent_blocks(const rfsf_xent_shape &shape, const void *Phi, const void
         if (z.d_w) {
             const bool to_sums = sums && n0 + rows < N;
             const float *add = n0 == 0 ? nullptr : sums ? sums : static_cast<const float *>(dW);
-            products[count_of_products] = {Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_n, C}, plane_steps(rows, z.two),
+            products[count_of_products] = {Planes{phi_columns, pitch_n, K}, Planes{g_classes, pitch_gn, C}, plane_steps(rows, true),
                                            Gradient{to_sums ? static_cast<void *>(sums) : dW, to_sums ? K : shape.ld_dw, K, C, bf16 && !to_sums, nullptr,
                                                     stats, count, add, sums ? K : shape.ld_dw, 0}, 0};
             cut(products[count_of_products++], how.cuts[1], parts_w);
         }
         // the longer tiles first, so that the others fill up behind them
         if (count_of_products == 2 && products[1].per_cut > products[0].per_cut) std::swap(products[0], products[1]);
-        RFSF_TRY(launch_plane_products<MODE>(products, count_of_products, how.edge, stream));
+        RFSF_TRY(launch_plane_products<MODE == kHalf ? kHalfByTwo : MODE>(products, count_of_products, how.edge, stream));
         if (cut_sums > 0) {
             sum.K = K;
             sum.groups_of_first = (unsigned)((sum.first.numbers + 255) / 256);
