@@ -747,7 +747,7 @@ __global__ __launch_bounds__(64 * kOnePassWaves, 2) void one_pass_kernel(XentDir
             const float weight = __shfl(weight_of, r), top = among_few<FEW, true>(f < C ? score : -INFINITY), from = top == -INFINITY ? 0.f : top;
             const float share = f < C ? exp_of(score - from) : 0.f, total = among_few<FEW, false>(share);
             if (first + r < end) {
-                if (f == label) job.loss[first + r] = logf(total) + (from - score);
+                if (f == label && f < C) job.loss[first + r] = logf(total) + (from - score);          // (one lane writes a loss)
                 if (f == 0 && label < 0) job.loss[first + r] = 0.f;
                 if (f == 0 && label == C) job.loss[first + r] = NAN;
             }
