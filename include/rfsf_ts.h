@@ -275,7 +275,7 @@ int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W
  * with s_n = weight[n], or 1 / (number of rows that count) if weight is NULL.
  *   Phi [N, ld_phi], W [C, ld_w], dPhi [N, ld_dphi], dW [C, ld_dw]   row-major, float32, or all four bfloat16 (bf16 != 0)
  *   labels [N] int64 on the device. A negative label leaves its row out: loss 0, gradients 0, whatever Phi and weight hold
- *          there. Labels >= C give NaN (they are not used as addresses).
+ *          there and W holds anywhere. Labels >= C give NaN (they are not used as addresses).
  *   weight [N] float32 or NULL; loss [N] float32
  *   dPhi, dW: read only if RFSF_XENT_DPHI, RFSF_XENT_DW are set in `gradients`; columns beyond K are untouched
  * The scores are never held whole where there are many: without gradients they stay in registers, with gradients the workspace holds them for a part of

@@ -165,6 +165,7 @@ struct Scores {
 // Joins the class tiles' parts: the loss, and for the gradients the maximum, 1 / sum, the row's scale and the exponent that bounds
 // G[n, c] 2^exponent(W[c, :]).
 struct __attribute__((aligned(16))) RowTerms { float top, inverse, scale; int32_t reach; };
+constexpr int32_t kLeftOut = 4096;                  // as the exponent (others are within 512): the row's dPhi is 0, also where W holds infinities
 struct JoinJob {
     const Partial *partial;
     int64_t tiles, rows_ld, rows, C;
@@ -185,7 +186,7 @@ __device__ __forceinline__ RowTerms finish(const JoinJob &job, int64_t n, const 
     float bound = v.reach - log2f(s);
     if (known) bound = fmaxf(bound, (float)exponent_of(job.largest_w[label]));
     const RowTerms t = {from, 1.0f / s, label < 0 ? 0.f : job.weight ? job.weight[n] : job.terms ? 1.0f / (float)*job.count : 0.f,
-                        (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
+                        label < 0 ? kLeftOut : (int32_t)ceilf(fminf(fmaxf(bound, -512.f), 512.f))};
     if (write && job.terms) job.terms[n] = t;
     return t;
 }
@@ -323,14 +324,15 @@ struct Gradient {
             if (j >= cols_j) return;
             const int64_t row = first_of_cut + j * ld;
             const float scale = terms ? terms[j].scale : mean;
-            const int shift = (terms ? terms[j].reach : all) - 2 * kTopBit;
+            const int exponent = terms ? terms[j].reach : all, shift = exponent - 2 * kTopBit;
+            const bool left_out = terms && exponent == kLeftOut;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t i = first + 8 * q + 4 * half;
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = ldexpf(acc[4 * q + e], shift) * scale;
+                    v[e] = left_out ? 0.f : ldexpf(acc[4 * q + e], shift) * scale;
                     if (add && i + e < rows_i) v[e] += add[j * add_ld + i + e];
                 }
                 if (i < rows_i) store(row + i, rows_i - i, v);

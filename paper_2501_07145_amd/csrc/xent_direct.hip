@@ -424,6 +424,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
     const unsigned across = (unsigned)((job.K + kFewColumns - 1) / kFewColumns), cut = blockIdx.x / across;
     const int64_t k = (int64_t)(blockIdx.x % across) * kFewColumns + 4 * lane;
     const int64_t begin = (int64_t)cut * of_few.per_cut, end = std::min(begin + of_few.per_cut, many);
+    const uint64_t few_left_out = __ballot(rows_are_few && lane < few && job.labels[lane] < 0);
     const bool whole = k + 4 <= job.K;
     auto load4 = [&](const T *row, float (&x)[4]) {
         if (whole) {
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
     if constexpr (OF_MANY) {
 #pragma unroll
         for (int f = 0; f < FEW; ++f) {
-            if (f < few && !(rows_are_few && job.labels[f] < 0)) {          // rows left out may hold anything
+            if (f < few && (few_left_out >> f & 1) == 0) {          // rows left out may hold anything
                 load4(small + f * ld_small, s[f]);
             } else {
 #pragma unroll
@@ -468,9 +469,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
             }
             *reinterpret_cast<float4 *>(&g_tile[r][f]) = v;
         }
-        if (OF_FEW && threadIdx.x < kFewTile) {
+        if (threadIdx.x < kFewTile) {
             const int64_t m = tile + threadIdx.x;
-            counts[threadIdx.x] = m < end && (rows_are_few || job.labels[m] >= 0);          // rows left out may hold anything
+            counts[threadIdx.x] = m < end && (rows_are_few || job.labels[m] >= 0);          // rows left out may hold anything, and have no gradient whatever W holds
         }
         __syncthreads();
         for (int r0 = wave; r0 < kFewTile && tile + r0 < end; r0 += AHEAD * kFewWaves) {
@@ -513,6 +514,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
                     for (int f = 0; f < FEW; ++f)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[e] = fmaf(g[f], s[f][e], y[e]);
+                    if (!counts[r]) y[0] = y[1] = y[2] = y[3] = 0.f;
                     T *dst = static_cast<T *>(of_many.out) + m * of_many.ld + k;
                     if (whole) {
                         Four<T> v;
@@ -554,6 +556,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
 #pragma unroll
         for (int f = 0; f < FEW; ++f) {
             if (f >= few) break;
+            if (few_left_out >> f & 1) sums[f][0] = sums[f][1] = sums[f][2] = sums[f][3] = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (k + e >= job.K) break;
@@ -868,6 +871,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect jo
     // features beyond K and columns beyond the rows are read as the last ones
     const int64_t ia[2] = {std::min(i0 + col, job.K - 1), std::min(i0 + 32 + col, job.K - 1)};
     const int64_t jb = std::min(j0 + col, rows - 1);
+    const int64_t label = is_w ? 0 : job.labels[jb];
     floatx16 acc[2];
 #pragma unroll
     for (int a = 0; a < 2; ++a)
@@ -902,6 +906,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect jo
         acc[1] = multiply(sb, split<TA>(a1), acc[1]);
     }
     const float scale = g.cuts == 1 ? mean_scale(job) : 1.0f;
+    const uint64_t left_out = __ballot(label < 0);          // rows left out have no gradient whatever W holds
     auto store_block = [&](const floatx16 &sum, int64_t first) {
         const int64_t i = first + col;
         if (i >= job.K) return;
@@ -909,8 +914,9 @@ __global__ __launch_bounds__(64 * kSumWaves) void gradients_kernel(XentDirect jo
         for (int e = 0; e < 16; ++e) {
             const int64_t r = j0 + 8 * (e / 4) + 4 * half + e % 4;
             if (r >= rows) continue;
-            if (g.cuts > 1) g.parts[((int64_t)cut * rows + r) * job.K + i] = sum[e];
-            else store(static_cast<T *>(g.out) + r * g.ld + i, sum[e] * scale);
+            const float v = (left_out >> (r - j0) & 1) == 0 ? sum[e] : 0.f;
+            if (g.cuts > 1) g.parts[((int64_t)cut * rows + r) * job.K + i] = v;
+            else store(static_cast<T *>(g.out) + r * g.ld + i, v * scale);
         }
     };
     if constexpr (OWN) {

@@ -31,3 +31,18 @@ def test_labels_beyond_the_classes(N, K, C, need_dPhi, need_dW, weighted, bf16):
         assert torch.isnan(dPhi[beyond]).all() and torch.isfinite(dPhi[~beyond]).all()
     if need_dW:
         assert torch.isnan(dW).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("need_dW", [True, False])
+@pytest.mark.parametrize("N,K,C", [(300, 40, 7), (7, 3, 2), (9000, 300, 16), (200, 2100, 10), (12, 40, 300), (5, 700, 9000), (90, 40, 33), (90, 40, 300), (40, 33, 9000), (620, 300, 600),
+                                   (150, 130, 3000)])
+def test_rows_left_out_have_no_gradient_whatever_the_weights_hold(N, K, C, need_dW, value, bf16):
+    """One number of W is not finite: loss and dPhi of the rows that are left out are 0 all the same."""
+    phi, w, y, s = _inputs(N, K, C, bf16)
+    w[C // 2, K // 2] = value
+    y[torch.arange(N, device="cuda") % 2 == 1] = -1
+    phi[1] = float("nan")
+    loss, dPhi, _ = rfsf.rfsf_softmax_xent(phi, w, y, weight=s, need_dPhi=True, need_dW=need_dW)
+    assert torch.all(loss[y < 0] == 0) and torch.all(dPhi[y < 0] == 0) and torch.isnan(dPhi[y >= 0]).any()
