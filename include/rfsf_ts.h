@@ -309,8 +309,8 @@ int rfsf_softmax_xent(const rfsf_xent_shape *shape, const void *Phi, const void 
  *   state_bits 32: m, v are float32 [n].
  *   state_bits 8: 256 consecutive numbers share a scale, the largest magnitude among them (m_scale, v_scale: float32
  *     [ceil(n / 256)]). m is int8, a code c standing for scale * u|u| with u = c / 127; v is uint8, c standing for scale * u^4 with u = c / 255.
- *     The step uses m and v before they are rounded to the nearest code; a v above zero never becomes code 0. All zero is a fresh
- *     state. A block that meets an infinity or a NaN gets the scale NaN.
+ *     The step uses m and v before they are rounded to the nearest code. A v above zero keeps a code that stands for more than zero in 32 bits; an m
+ *     of a block with nothing above 2^-119 becomes zero. All zero is a fresh state. A block that meets an infinity or a NaN gets the scale NaN.
  *   copy: bfloat16 [n] that receives the new param, rounded, or NULL.
  * The array and its tensors' addresses are read during the call only. Tensors must not overlap. Addresses aligned to four numbers
  * are fastest; any that fit their type are right.

@@ -8,7 +8,8 @@
 //
 // 8-bit states: 256 numbers share a scale, their largest magnitude. m = scale * u |u| with u = code / 127, code -127 .. 127: the grid is
 // finer near zero, where most of a block lies. v = scale * u^4 with u = code / 255, code 0 .. 255, covers 2^32 : 1 with steps of 4 / code;
-// a v above zero never becomes zero, which would leave m without its divisor.
+// a v above zero never becomes zero, which would leave m without its divisor: its code is at least the first one that does not stand for
+// zero in 32 bits, 1 for scales from 2^-116 on and up to 255 for the smallest. An m of a block with nothing above 2^-119 becomes zero.
 #include "rfsf_internal.h"
 
 #include <algorithm>
@@ -23,7 +24,9 @@ namespace {
 constexpr int kShare = 256;                     // numbers of a scale
 constexpr int kChunk = 4096;                    // numbers of a workgroup
 constexpr int kTensors = 40;                    // of a launch: their descriptions are its arguments
-constexpr float kLeast = 1.504632769052528e-36f;        // 2^-119: scales below count as zero
+constexpr float kLeast = 1.504632769052528e-36f;        // 2^-119: scales of m below count as zero; shares of v below are taken of 2^64 times it and its scale
+constexpr float kLift = 18446744073709551616.0f;        // 2^64
+constexpr float kSmall = 1.2037062152420224e-35f;       // 2^-116: scales from there on have code 1 stand for more than zero
 constexpr float kInv127 = 1.0f / 127.0f, kInv255 = 1.0f / 255.0f;
 
 struct Job {
@@ -134,6 +137,17 @@ __device__ __forceinline__ void scale_and_inverse(uint32_t largest, float *scale
     *scale = largest < 0x7f800000u ? top : NAN;
     *inverse = largest < 0x7f800000u && top >= kLeast ? 1.0f / top : 0.f;
 }
+// The same for v, of v * lift, and the least code of a v above zero: (least code / 255)^4 scale is about 2^-149, the smallest number above zero, or more.
+__device__ __forceinline__ void scale_and_inverse_v(uint32_t largest, float *scale, float *inverse, float *lift, float *least)
+{
+    const float top = __uint_as_float(largest);
+    const bool finite = largest < 0x7f800000u;
+    *scale = finite ? top : NAN;
+    *lift = top < kLeast ? kLift : 1.0f;
+    *inverse = finite && top > 0.f ? 1.0f / (top * *lift) : 0.f;
+    *least = 1.0f;
+    if (top > 0.f && top < kSmall) *least = fminf(ceilf(sqrtf(sqrtf(2.5849394142282115e-26f / (top * kLift))) * 255.0f), 255.0f);          // (2^-85: 2^-149 lifted)
+}
 
 // A wavefront takes 256 numbers at a time, four a lane: a block of 8-bit states is a wavefront's own.
 template <typename G, bool EIGHT>
@@ -184,16 +198,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(Job job, Numbers c)
                     vt = max(vt, __float_as_uint(v[e]) & 0x7fffffffu);
                 }
             }
-            float ms, mi, vs, vi;
+            float ms, mi, vs, vi, lift, least;
             scale_and_inverse(wave_max(mt), &ms, &mi);
-            scale_and_inverse(wave_max(vt), &vs, &vi);
+            scale_and_inverse_v(wave_max(vt), &vs, &vi, &lift, &least);
             uint32_t mw = 0, vw = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float mc = mi == 0.f ? 0.f : fminf(rintf(sqrtf(fabsf(m[e]) * mi) * 127.0f), 127.0f);
-                const float share = vi == 0.f ? 0.f : v[e] * vi;
+                const float share = vi == 0.f ? 0.f : (v[e] * lift) * vi;
                 float vc = fminf(rintf(sqrtf(sqrtf(share)) * 255.0f), 255.0f);
-                if (share > 0.f) vc = fmaxf(vc, 1.0f);
+                if (vi != 0.f && v[e] > 0.f) vc = fmaxf(vc, least);
                 mw |= ((uint32_t)(int)(m[e] < 0.f ? -mc : mc) & 0xffu) << (8 * e);
                 vw |= (uint32_t)(int)vc << (8 * e);
             }
