@@ -21,6 +21,13 @@ __device__ __forceinline__ float inverse_of(uint32_t largest, float *scale)
     *scale = finite ? top * (1.0f / 127.0f) : NAN;
     return top < kLeast || !finite ? 0.f : (1.0f / top) * 127.0f;
 }
+// A sum of products of codes times both scales, the smaller scale first: nothing on the way is beyond what 32 bits hold unless the result is. (The product of
+// the scales may be: two scales of 2^95 made a sum of zero NaN, two of 2^-75 lost everything.) Scales that are NaN stay.
+__device__ __forceinline__ float scaled(int sum, float a, float b)
+{
+    const bool less = a < b;
+    return ((float)sum * (less ? a : b)) * (less ? b : a);
+}
 template <int PER>
 __device__ __forceinline__ void store_codes(int8_t *q, const float (&v)[PER], float inverse)
 {
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const int8_t *qx, int
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += shared[((wave * NW + w) * 4 + e) * 64 + lane];
-        if (first + e < Ny) out[col * ld_out + first + e] = (float)sum * (s * scales[first + e]);
+        if (first + e < Ny) out[col * ld_out + first + e] = scaled(sum, s, scales[first + e]);
     }
 }
 template <int BM, int AHEAD, int NW>
@@ -236,7 +243,7 @@ __global__ __launch_bounds__(256) void few_small_kernel(const T *X, int64_t ldx,
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += shared[(w * 4 + e) * 64 + lane];
         const int64_t j = j0 + 4 * quarter + e;
-        if (j < Ny) out[col * ld_out + j] = (float)sum * (sx[col] * scales[j]);
+        if (j < Ny) out[col * ld_out + j] = scaled(sum, sx[col], scales[j]);
     }
 }
 
@@ -262,7 +269,7 @@ struct Scaled {
                 float *dst = out + j * ld + i;
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (float)acc[4 * q + e] * (sj * (i + e < rows_i ? scale_i[i + e] : 0.f));
+                for (int e = 0; e < 4; ++e) v[e] = scaled(acc[4 * q + e], sj, i + e < rows_i ? scale_i[i + e] : 0.f);
                 if (i + 3 < rows_i) {
                     *reinterpret_cast<Float4u *>(dst) = {v[0], v[1], v[2], v[3]};
                 } else {
