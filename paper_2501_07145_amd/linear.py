@@ -3,6 +3,7 @@ step, and the Gram against rows held in 8-bit integers (include/rfsf_ts.h). Argu
 from __future__ import annotations
 
 import ctypes
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -148,8 +149,7 @@ class RfsfAdamW:
             if tensors:
                 self._words[:, k] = [t.data_ptr() for t in tensors]
         self._words[:, 7] = self._sizes
-        self._address = self._words.ctypes.data
-        self._flat = memoryview(self._words).cast("B").cast("q") if self.params else None
+        self._description = self._words.tobytes()
 
     def step(self, grads: Sequence[torch.Tensor], step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -162,10 +162,10 @@ class RfsfAdamW:
         dtype = grads[0].dtype
         if dtype not in _BF16:
             raise ValueError("grads must be float32 or bfloat16")
-        for k, address in enumerate(_addresses(grads, self._sizes, dtype, "grads")):
-            self._flat[8 * k + 1] = address
+        words = array("q", self._description)                    # (a call's own: another thread may be in another step)
+        words[1::8] = array("q", _addresses(grads, self._sizes, dtype, "grads"))
         config = _AdamwConfig(lr, betas[0], betas[1], eps, weight_decay, grad_scale, step, self.state_bits, _BF16[dtype])
-        _check(load_library().rfsf_adamw_step(self._address, len(grads), ctypes.byref(config), _stream_ptr(stream)))
+        _check(load_library().rfsf_adamw_step(words.buffer_info()[0], len(grads), ctypes.byref(config), _stream_ptr(stream)))
 
     def moments(self, out=None, stream: Optional[torch.cuda.Stream] = None):
         """(m, v): lists of float32 tensors, what the states hold. 32 bits: the states themselves; 8 bits: the numbers that the codes
@@ -177,7 +177,7 @@ class RfsfAdamW:
         if any(len(tensors) != len(self.params) for tensors in out):
             raise ValueError("out must hold a tensor for each parameter, twice")
         places = [np.array(_addresses(tensors, self._sizes, torch.float32, "out"), dtype=np.int64) for tensors in out]
-        _check(load_library().rfsf_adamw_moments(self._address, len(self.params), places[0].ctypes.data, places[1].ctypes.data,
+        _check(load_library().rfsf_adamw_moments(self._words.ctypes.data, len(self.params), places[0].ctypes.data, places[1].ctypes.data,
                                                  _stream_ptr(stream)))
         return out
 
