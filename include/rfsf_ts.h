@@ -325,7 +325,7 @@ typedef struct {
     int64_t n;                  /* >= 0, <= 2^35 (RFSF_E_UNSUPPORTED) */
 } rfsf_adamw_tensor;
 typedef struct {
-    double lr, beta1, beta2, eps, weight_decay, grad_scale;  /* finite; 0 <= beta < 1, eps, lr, weight_decay >= 0 */
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;  /* finite in 32 bits, as lr weight_decay and lr / (1 - beta1^step); 0 <= beta < 1, eps, lr, weight_decay >= 0 */
     int64_t step;               /* >= 1 */
     int32_t state_bits;         /* 8 or 32 */
     int32_t grad_bf16;

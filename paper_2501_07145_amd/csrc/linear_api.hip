@@ -74,15 +74,17 @@ extern "C" int rfsf_adamw_step(const rfsf_adamw_tensor *tensors, int64_t count, 
     const int rc = check_tensors(tensors, count);
     if (rc != RFSF_OK) return rc;
     if (c->state_bits != 8 && c->state_bits != 32) return RFSF_E_UNSUPPORTED;
-    const double all = c->lr + c->beta1 + c->beta2 + c->eps + c->weight_decay + c->grad_scale;
-    if (!std::isfinite(all) || c->lr < 0 || c->eps < 0 || c->weight_decay < 0 || c->beta1 < 0 || c->beta1 >= 1 || c->beta2 < 0 || c->beta2 >= 1 ||
+    const double correction1 = 1.0 - std::pow(c->beta1, (double)c->step), correction2 = std::sqrt(1.0 - std::pow(c->beta2, (double)c->step));
+    // what the step uses of the settings is held in 32 bits
+    for (double v : {c->lr, c->beta1, c->beta2, c->eps, c->weight_decay, c->grad_scale, c->lr * c->weight_decay, c->lr / correction1})
+        if (!std::isfinite((float)v)) return RFSF_E_BAD_SETTING;
+    if (c->lr < 0 || c->eps < 0 || c->weight_decay < 0 || c->beta1 < 0 || c->beta1 >= 1 || c->beta2 < 0 || c->beta2 >= 1 ||
         c->step < 1)
         return RFSF_E_BAD_SETTING;
     for (int64_t k = 0; k < count; ++k) {
         const rfsf_adamw_tensor &t = tensors[k];
         if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (c->state_bits == 8 && (!t.m_scale || !t.v_scale)))) return RFSF_E_NULLPTR;
     }
-    const double correction1 = 1.0 - std::pow(c->beta1, (double)c->step), correction2 = std::sqrt(1.0 - std::pow(c->beta2, (double)c->step));
     return rfsf::launch_adamw(tensors, count, *c, correction1, correction2, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
 }
 
