@@ -1162,8 +1162,10 @@ Places places_of(const rfsf_xent_shape &s, const DirectGradient &dphi, const Dir
         return here;
     };
     const ScorePlan plan = score_plan(s);
-    p.scores = p.g = take(4 * (size_t)s.N * (size_t)four(s.C) * plan.cuts);                                       // G in the scores' place, unless it lies by classes
-    if (rows_are_few(s)) p.g = take(4 * (size_t)s.C * (size_t)four(s.N));
+    // scores that leave the registers, and G in their place unless it lies by classes; one pass holds neither
+    const bool scores = !is_one_pass(s) && !plan.fused, g = !is_one_pass(s) && s.gradients, by_class = rows_are_few(s);
+    p.scores = p.g = take(scores || (g && !by_class) ? 4 * (size_t)s.N * (size_t)four(s.C) * plan.cuts : 0);
+    if (g && by_class) p.g = take(4 * (size_t)s.C * (size_t)four(s.N));
     p.partial = take(plan.partial ? sizeof(float2) * (size_t)s.N * (size_t)((s.C + 31) / 32 * 2) : 0);
     p.counts = take(4 * (size_t)(kCountedRows / kRows));
     p.parts_phi = take(dphi.cuts > 1 ? 4 * (size_t)dphi.cuts * (size_t)s.N * (size_t)s.K : 0);
