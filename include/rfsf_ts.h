@@ -277,19 +277,21 @@ int rfsf_trp_features(const rfsf_ts_shape *shape, const float *X, const float *W
  *   labels [N] int64 on the device. A negative label leaves its row out: loss 0, gradients 0, whatever Phi and weight hold
  *          there and W holds anywhere. Labels >= C give NaN (they are not used as addresses).
  *   weight [N] float32 or NULL; loss [N] float32
- *   dPhi, dW: read only if RFSF_XENT_DPHI, RFSF_XENT_DW are set in `gradients`; columns beyond K are untouched
+ *   dPhi, dW: looked at only if RFSF_XENT_DPHI, RFSF_XENT_DW are set in `gradients`; columns beyond K are untouched
  * Small problems (which ones follows from N, K, C, the type and `gradients` alone, and N C <= 2^26) are worked on straight from the matrices, in one part: the
  * recommended workspace, which is then the minimum, holds their scores and G where these leave the registers. Of the others the workspace holds the
  * packed operands, and with gradients the scores of a part of the rows at a time and G of a block of them, in two layouts of 4 bytes a number for both gradients; a smaller workspace
  * means smaller blocks. Without gradients their scores stay in registers.
- * Accuracy: sums are held in 32 bits. Straight from the matrices, float32 operands enter the products whole; G enters those of the gradients whole too, or with bfloat16 operands as two terms of bfloat16, 16 bits.
+ * Accuracy: sums are held in 32 bits; exponentials have a relative error of 2^-24 of their argument's size besides 2^-22. Straight from the matrices, float32 operands
+ * enter the products whole; G enters those of the gradients whole too, or with bfloat16 operands as two terms of bfloat16, 16 bits.
  * Of the others, float32 operands enter the products with 22 significand bits down to 2^-17 of the largest number of their row, and with an
  * error below 2^-38 of it beyond; bfloat16 operands enter whole down to 2^-30 of it. G enters the gradients' products with 22 bits,
  * or with an error of 2^-38 of the largest product that it takes part in: of the largest |G[n, c]| max_k |W[c, k]| of
  * its row for dPhi, of the largest |s_n| max_k |Phi[n, k]| of the rows that are worked on together for dW. A row of Phi
  * or W that holds an infinity or a NaN makes what is computed from it NaN (bfloat16: or what infinities give). Equal calls with workspaces
  * of equal sizes give equal bits.
- * Limits: K, C <= 3500000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW.
+ * Limits: K, C <= 3500000, N < 2^31 (RFSF_E_UNSUPPORTED). N = 0 clears dW. With N C > 2^26 few classes take longer (10 classes three to four times as
+ * long a row).
  */
 enum { RFSF_XENT_DPHI = 1, RFSF_XENT_DW = 2 };
 typedef struct {

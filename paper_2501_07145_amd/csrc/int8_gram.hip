@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256) void few_small_kernel(const T *X, int64_t ldx,
 }
 
 // More rows: the product of packed operands. Rows of the tile: stored rows (contiguous in the result). 333 x 10000 x 5121 36 us (940 TOP/s, 237 tiles of 128:
-// one round that does not fill the CUs), 5000 x 50000 x 10241 2.44 ms (2100 TOP/s).
+// one round that does not fill the CUs), 5000 x 50000 x 10241 2.43 to 2.56 ms (2000 to 2110 TOP/s).
 struct Scaled {
     float *out;
     int64_t ld, rows_i, cols_j;

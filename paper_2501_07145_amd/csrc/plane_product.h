@@ -14,9 +14,11 @@
 // step. LDS: row r's 128 bytes are 8 chunks of 16, chunk c at place c ^ (r & 7), so that 8 lanes that read the same chunk of 8
 // rows meet all banks once (and the permutation is made by the loads' addresses, at no cost). Rows of 64 bytes: chunk c at place c ^ (r / 2 & 3).
 //
-// What bounds it: with tiles of 256 and random numbers the power that the matrix instructions draw and what the L2s deliver, about equally. 32768 x 2048 x
-// 8192 of 16-bit numbers 877 us (1250 TFLOP/s); the same without the loads 710, the loads alone 560 to 730, the matrix instructions alone 490 to 540.
-// 50000 x 5000 x 10241 of 8-bit ones 2.44 ms (2100 TOP/s). With the smaller tiles, what the L2s deliver (9.5 to 12 TB/s) and the time of a step.
+// What bounds it (counters of the cycles in which a CU holds a tile): with tiles of 256 and two terms the matrix instructions, busy 76 to 80 % of them at a
+// clock of 1.7 GHz, which is what the power allows; with one term or 8 bits, whose steps are shorter, they are busy 42 to 59 %, and the
+// wavefronts wait for the next step 35 to 44 % of their time. 32768 x 2048 x 8192 of 16-bit numbers 877 us (1250 TFLOP/s); the same
+// without the loads 710, the loads alone 560 to 730, the matrix instructions alone 490 to 540. 50000 x 5000 x 10241 of 8-bit ones 2.43 to 2.56
+// ms (2000 to 2110 TOP/s). With the smaller tiles, waiting for the steps (matrix instructions 20 to 39 %), and CUs without a tile.
 #pragma once
 
 #include "rfsf_internal.h"

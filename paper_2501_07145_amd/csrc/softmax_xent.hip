@@ -2,7 +2,8 @@
 //   l[n, c] = sum_k Phi[n, k] W[c, k],   loss[n] = log sum_c exp l[n, c] - l[n, y_n],
 //   G[n, c] = s_n (exp l[n, c] / sum - [c = y_n]),   dPhi = G W,   dW = G^T Phi.
 //
-// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory (float32 operands cost three 16-bit products each, bfloat16 ones one for the scores and two for a gradient, G being two terms). The operands are packed once for
+// Three products of 2 N K C flop, everything else is of the order of N C and bound by memory. float32 operands cost three 16-bit products each, bfloat16 ones
+// one for the scores and two for a gradient, G being two terms. The operands are packed once for
 // the matrix instructions (plane_pack.h), W and Phi by rows for the scores, their transposes for the gradients, so that
 // all three products are of one kind (plane_product.h). The scores of a tile give their maximum and sum of exponentials per row before
 // they leave the registers; without gradients they are never written. For gradients the rows are taken in blocks, and the
@@ -19,6 +20,7 @@ namespace rfsf {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
+// (The rounding of x log2 e is a relative error of |x| 2^-24, that of a score of size |x| rounded to 32 bits.)
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // Rows that count, of all blocks.
@@ -53,7 +55,7 @@ __device__ __forceinline__ Partial joined(const Partial &a, const Partial &b)
 // Scores: classes along the tile's rows, sequences along its columns, so that a lane holds many classes of one sequence and
 // nearly all of the maximum and the sum is taken inside it.
 // Bound by the product; where the scores are written, by that after it, as a CU holds one tile and all of them end together. Tiles of 256: 10000 x
-// 5121, 5003 classes, float32, losses alone 1.43 ms (1080 TFLOP/s of 16-bit products); 1024 x 2049, 32768 classes, bfloat16, with 134 MB of scores
+// 5121, 5003 classes, float32, losses alone 1.46 to 1.50 ms (1030 to 1050 TFLOP/s of 16-bit products; 800 tiles are 3.1 rounds of the CUs, paid as four); 1024 x 2049, 32768 classes, bfloat16, with 134 MB of scores
 // 157 us (875 TFLOP/s).
 struct Scores {
     const uint32_t *largest_w, *largest_phi;    // per class, per sequence of the block
@@ -211,7 +213,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinJob job)
 // the classes' powers of two: (p - [c = y]) 2^exponent(W[c, :]), brought to 2^14 by the row's own exponent; the rows' scales
 // enter at the end of the product, so that rows of small scale lose nothing. Transposed, for the product with Phi^T: the same with
 // the rows' scales and exponents, brought to 2^14 by the largest of all.
-// Bound by memory (scores read, two operands of two terms written), the scores coming from the last-level cache: 1024 x 32768 100 us for 403 MB (4.0 TB/s).
+// Bound by memory (scores read, two operands of two terms written), the scores coming from the last-level cache: 1024 x 32768 98 us for 403 MB (4.1 TB/s).
 struct GradientJob {
     const float *scores;
     int64_t ld, rows, C;
@@ -298,8 +300,8 @@ __global__ __launch_bounds__(256) void gradient_kernel(GradientJob job)
 }
 
 // A gradient: rows of the tile along the contiguous axis of the result. Both gradients share a launch, so that the second one's tiles fill the CUs
-// that the first one's leave. 8192 x 2049, 32768 classes, bfloat16: 3.61 ms
-// (1220 TFLOP/s of 16-bit products; with G as one term of 11 bits 1.95 ms, and dPhi 3.4e-4 from the rounded exact result instead of 0.9e-4); 1000 x 1025, 1000
+// that the first one's leave. 8192 x 2049, 32768 classes, bfloat16: 3.55 to 3.61
+// ms (1220 to 1240 TFLOP/s of 16-bit products; with G as one term of 11 bits 1.95 ms, and dPhi 3.4e-4 from the rounded exact result instead of 0.9e-4); 1000 x 1025, 1000
 // classes, float32 32 us.
 struct Gradient {
     void *out;
@@ -396,8 +398,8 @@ __global__ __launch_bounds__(256) void add_kernel(AddJob job)
 // Workspace and order of work.
 // How the gradients' products of a block of rows are made: the tiles' edge, and the parts of their sums (dPhi, dW), by the steps' time. A long sum of few tiles
 // leaves CUs without work; cut, it costs its parts' way through memory and a launch. (us a call, whole and cut: 7487 x 316, 365 classes, float32, dW
-// 105 and 56; 1209 x 88, 7765, float32, dPhi 129 and 81; 9000 x 4000, 300, bfloat16, both 278 and 237, of which some by the longer tiles' being first; 8638 x
-// 3613, 172, float32, dPhi, not cut, 255 and 266. Of 60 shapes with 65 to 10000 rows and 65 to 33000 classes the geometric mean is 1.11.)
+// 105 and 56; 1209 x 88, 7765, float32, dPhi 129 and 81; 9000 x 4000, 300, bfloat16, both 282 and 263; 8638 x
+// 3613, 172, float32, dPhi, is not cut. Of 60 shapes with 65 to 10000 rows and 65 to 33000 classes the geometric mean is 1.11.)
 struct GradientPlan { int edge, cuts[2]; };
 constexpr double kPartRate = 3e6, kAddTime = 5.0;                  // bytes a us, written and read; us
 constexpr int64_t kMostPartBytes = (int64_t)256 << 20;
@@ -433,7 +435,7 @@ GradientPlan plan_gradients(bool d_phi, bool d_w, int64_t rows, int64_t K, int64
 }
 constexpr int64_t kUnit = 64;                           // rows of a block are counted in these
 // Tiles of classes whose parts the pass to G joins by itself, every workgroup those of its rows, which saves a launch; with more of them they are read
-// too often. (us a call, apart and here: 4454 x 257, 468 classes, bfloat16, dPhi 46.0 and 43.4; 1000 x 1025, 1000, float32, both 67.3 and 65.5; 1432 x
+// too often. (us a call, apart and here: 4454 x 257, 468 classes, bfloat16, dPhi 49.2 and 45.4; 1000 x 1025, 1000, float32, both 67.3 and 65.5; 1432 x
 // 1999, 2885, 12 tiles, float32, both 293.0 and 293.8. Of 44 shapes with 302 to 4541 classes the geometric mean is 1.016, the worst 0.990.)
 constexpr int64_t kJoinHere = 32;
 constexpr size_t kScoreBytes = (size_t)128 << 20;       // of scores in flight: half of the last-level cache

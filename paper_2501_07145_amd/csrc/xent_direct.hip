@@ -573,8 +573,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(XentDirect job)
 // A wavefront's R FEW sums over its columns are spread over its lanes as they are added up: at each step a lane keeps one half of
 // them and gives the other half to the lane that keeps that one, about 2 R FEW steps instead of 6 R FEW. The gradients are outer products, which 4 x 4 x 1
 // matrix instructions of 32 bits make in half the time of multiply-adds, from the registers as they lie.
-// What bounds it is issuing instructions (of a tile's 9400 cycles the scores take 3500, adding up and the softmax 3400, dW 2500) and then reading
-// Phi. 7494 x 1001, 10 classes, float32, dW: 18 us (1.7 TB/s) and 5.4 for adding up 235 parts, 22.7 the call; with multiply-adds for the gradients 20.6;
+// What bounds it is the chain of a tile: of its 9400 cycles (the clock read in the kernel) the scores take 3500, adding up and the softmax 3400, dW 2500; two
+// wavefronts a SIMD wait 45 % of their time (counters), and the matrix instructions are busy 9 %. Then reading Phi. 7494 x 1001, 10 classes, float32, dW: 18.7 us (1.6 TB/s) and 5.4 for adding up 235 parts, 22.7 the call; with multiply-adds for the gradients 20.6;
 // scores and gradients in two launches 11.6 + 16.2, 31.7 the call. 16 x 193, 10 classes: 7.8 us, where nearly all is latency; 11.7 with the four
 // classes that do not exist and the rows that other groups would have worked on, and three rounds of adding up.
 constexpr int kOnePassWaves = 8, kOnePassColumns = 256 * kOnePassWaves, kOnePassFew = 16;
@@ -1180,9 +1180,10 @@ Places places_of(const rfsf_xent_shape &s, const DirectGradient &dphi, const Dir
 // much as before it (the packed way packs and makes scores in any case), and by h = N C / (N + C), their ratio to what the packed way reads and
 // writes beside them. Of 150 shapes with 17 to 10000 rows, 65 to 10241 columns and 17 to 50000 classes, N K C from 3e7 to 6e9, both types and
 // any gradients, all timed both ways, the way chosen takes 1.8 % longer than the better one on average; fitted to half of them, 3.4 % with the other
-// half. (us, packed and here: 30 x 7544, 158 classes, float32, losses 81 and 13; 2845 x 6843, 47, float32, dPhi 153 and 102; 375 x 4022, 283,
-// bfloat16, losses 40 and 21; but 8161 x 4507, 42, bfloat16, both 193 and 330; 129 x 1805, 4490, bfloat16, dW 68 and 166; 222 x 565, 34570, bfloat16,
-// both 162 and 637.)
+// half. (That was with G of one term in the packed bfloat16 way; with two, the 65 of bfloat16 with gradients come to 1.5 %.) Beyond N C = 2^26 all are packed, few classes
+// at a loss: 6.5e6 x 65, 10 classes, dW 2.1 ms here, 6.8e6 rows packed 8.1; losses alone 1.5 and 4.3. (us, packed and here: 30 x 7544, 158 classes, float32, losses 81 and 13; 2845 x 6843, 47, float32, dPhi 153 and 102; 375 x 4022, 283,
+// bfloat16, losses 40 and 21; but 8161 x 4507, 42, bfloat16, both 199 and 332; 129 x 1805, 4490, bfloat16, dW 66 and 169; 222 x 565, 34570, bfloat16,
+// both 202 and 642.)
 bool xent_direct(const rfsf_xent_shape &s)
 {
     const double n = (double)s.N, c = (double)s.C;
