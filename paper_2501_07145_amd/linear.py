@@ -174,7 +174,7 @@ class RfsfAdamW:
             return self.state["m"], self.state["v"]
         if out is None:
             out = tuple([_empty_on(stream, p.shape, dtype=torch.float32, device=p.device) for p in self.params] for _ in range(2))
-        if any(len(tensors) != len(self.params) for tensors in out):
+        if len(out) != 2 or any(len(tensors) != len(self.params) for tensors in out):
             raise ValueError("out must hold a tensor for each parameter, twice")
         places = [np.array(_addresses(tensors, self._sizes, torch.float32, "out"), dtype=np.int64) for tensors in out]
         _check(load_library().rfsf_adamw_moments(self._words.ctypes.data, len(self.params), places[0].ctypes.data, places[1].ctypes.data,

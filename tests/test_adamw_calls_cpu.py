@@ -45,3 +45,11 @@ def test_a_step_that_another_one_overtakes_keeps_its_gradients(library, state_bi
     for words in library.steps:
         assert list(words[:, 0]) == [p.data_ptr() for p in params] and list(words[:, 7]) == [3, 300, 1000]
         assert list(words[:, 2]) == [t.data_ptr() for t in state["m"]] and list(words[:, 3]) == [t.data_ptr() for t in state["v"]]
+
+
+@pytest.mark.parametrize("out", [(), ([torch.zeros(3)],), ([torch.zeros(3)], [torch.zeros(3)], [torch.zeros(3)]), ([torch.zeros(3)], []), ([], [torch.zeros(3)])])
+def test_moments_are_written_to_two_lists(library, out):
+    """Anything else than two lists of a tensor for each parameter is refused, before the library is called (which has no such entry here)."""
+    optimizer = linear.RfsfAdamW([torch.zeros(3)], state_bits=8)
+    with pytest.raises(ValueError):
+        optimizer.moments(out=out)
