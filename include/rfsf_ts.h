@@ -53,8 +53,8 @@ enum {
     RFSF_E_UNSUPPORTED = -9,        /* valid but outside what the kernels cover           */
     RFSF_E_STATIC_SCRATCH_TOO_SMALL = -10, /* rfsf_ts_features_static: one sequence needs */
                                     /* more than the built-in scratch                     */
-    RFSF_E_BAD_SETTING = -11        /* a setting of the optimizer is not finite or out of */
-                                    /* its range                                          */
+    RFSF_E_BAD_SETTING = -11        /* a setting (of the optimizer, a norm, dropout, an   */
+                                    /* adapter) is not finite or out of its range         */
 };
 
 typedef struct {
@@ -355,6 +355,56 @@ int rfsf_int8_quantize(const void *X, int32_t bf16, int64_t N, int64_t ldx, int6
 int rfsf_int8_gram_workspace_bytes(int64_t Nx, int64_t Ny, int64_t K, size_t *recommended_bytes, size_t *minimum_bytes);
 int rfsf_int8_gram(const void *X, int32_t bf16, int64_t Nx, int64_t ldx, const int8_t *codes, const float *scales, int64_t Ny,
                    int64_t ld_codes, int64_t K, float *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Dropout of feature rows (or of gradients: the backward pass is the same call on them):
+ *   Y[n, k] = X[n, k] 65536 / (65536 - t) where u(n, k) >= t, and 0 elsewhere,    t = round(65536 p), ties to even
+ * u(n, k) are 16 bits that are computed when needed and never stored: Philox 4x32 with 10 rounds, key `seed`, counter
+ * (k / 8, first_row + n, offset's lower and upper word); word (k % 8) / 2 of the four, its lower half for even k. The same mask settings give the
+ * same mask in every call of any type and size; another step, layer or rank takes another offset (or first_row, for rows of one batch that are worked on
+ * in parts). What is left out is 0 also where X holds infinities or NaN. p = 0 (or what rounds to it) copies, p = 1 clears.
+ *   offset_on_device: NULL, or a number on the device that is added to offset when the kernel runs, so that a captured graph meets
+ *     another mask each time it is replayed
+ *   X [N, ldx], Y [N, ldy] float32 or both bfloat16 (bf16 != 0); Y may be X (with the same row stride), no other overlap
+ * Limits: first_row + N <= 2^32, N < 2^31, K <= 3500000 (RFSF_E_UNSUPPORTED). p outside [0, 1] is RFSF_E_BAD_SETTING.
+ */
+typedef struct {
+    double p;                       /* probability of leaving a number out */
+    uint64_t seed, offset;
+    const uint64_t *offset_on_device;
+    int64_t first_row;              /* >= 0 */
+} rfsf_dropout_mask;
+int rfsf_dropout(const rfsf_dropout_mask *mask, const void *X, int32_t bf16, int64_t N, int64_t ldx, int64_t K, void *Y, int64_t ldy,
+                 void *hip_stream);
+
+/*
+ * Layer norm of feature rows, with dropout behind it, and its backward pass:
+ *   z = (X[n] - mean_n) rstd_n,   rstd_n = 1 / sqrt(var_n + eps),   Y[n] = dropout(z gain + offset)
+ *   h = dropout(dY[n]),  g = h gain,  dX[n] = rstd_n (g - mean(g) - z mean(g z)),  dgain = sum_n h z,  doffset = sum_n h
+ * mean and variance over the K columns of a row (the constant one of features among them), the latter divided by K.
+ *   X [N, ld_x], Y or dY [N, ld_y], dX [N, ld_dx] row-major, float32, or all bfloat16 (bf16 != 0)
+ *   gain, offset [K] float32, or NULL: 1, 0
+ *   eps finite and above zero, also in 32 bits (RFSF_E_BAD_SETTING)
+ *   mask: NULL for no dropout. The backward pass needs the settings of the forward pass, and what offset_on_device holds has to be the same.
+ *   mean, rstd [N] float32: written by the forward pass (either may be NULL there), read by the backward pass
+ *   dX [N, ld_dx], or NULL if not wanted; dgain, doffset [K] float32, or both NULL
+ * Y may be X and dX may be X or dY (with the same row stride); no other overlap. Columns beyond K are untouched. Statistics and sums are held in 32 bits; the
+ * variance is that of numbers less their mean, so that rows far from zero lose nothing. A row with an infinity or a NaN is NaN (where
+ * dropout keeps it). Equal calls give equal bits.
+ * rfsf_layer_norm_backward_workspace_bytes: scratch for dgain and doffset (without them it may be NULL). with_dx: whether dX is asked for.
+ * Limits: N < 2^31, K <= 3500000 (RFSF_E_UNSUPPORTED). Rows of up to 20480 columns are read once. N = 0 clears dgain and doffset.
+ */
+typedef struct {
+    int64_t N, K;
+    int64_t ld_x, ld_y, ld_dx;      /* row strides in numbers, >= K; ld_dx is looked at if dX is not NULL */
+    int32_t bf16;
+} rfsf_layer_norm_shape;
+int rfsf_layer_norm(const rfsf_layer_norm_shape *shape, const void *X, const float *gain, const float *offset, double eps,
+                    const rfsf_dropout_mask *mask, void *Y, float *mean, float *rstd, void *hip_stream);
+int rfsf_layer_norm_backward_workspace_bytes(const rfsf_layer_norm_shape *shape, int32_t with_dx, size_t *recommended_bytes, size_t *minimum_bytes);
+int rfsf_layer_norm_backward(const rfsf_layer_norm_shape *shape, const void *X, const float *mean, const float *rstd, const float *gain, const void *dY,
+                             const rfsf_dropout_mask *mask, void *dX, float *dgain, float *doffset, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
 
 /*
  * Optional per-kernel timing for benchmarks (not part of the method). While enabled, every

@@ -104,6 +104,14 @@ def load_library():
     lib.rfsf_int8_gram_workspace_bytes.argtypes = [i64, i64, i64, pt(sz), pt(sz)]
     lib.rfsf_int8_gram.restype = ctypes.c_int
     lib.rfsf_int8_gram.argtypes = [vp, i32, i64, i64, vp, vp, i64, i64, i64, vp, i64, vp, sz, vp]
+    lib.rfsf_dropout.restype = ctypes.c_int
+    lib.rfsf_dropout.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, vp]
+    lib.rfsf_layer_norm.restype = ctypes.c_int
+    lib.rfsf_layer_norm.argtypes = [vp, vp, vp, vp, ctypes.c_double, vp, vp, vp, vp, vp]
+    lib.rfsf_layer_norm_backward_workspace_bytes.restype = ctypes.c_int
+    lib.rfsf_layer_norm_backward_workspace_bytes.argtypes = [vp, i32, pt(sz), pt(sz)]
+    lib.rfsf_layer_norm_backward.restype = ctypes.c_int
+    lib.rfsf_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

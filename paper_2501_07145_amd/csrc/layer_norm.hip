@@ -1,0 +1,580 @@
+// Layer norm of feature rows, with dropout behind it, and its backward pass.
+//
+//   z = (x - mean) rstd,  rstd = 1 / sqrt(var + eps),  y = dropout(z gain + offset)
+//   h = dropout(dy),  g = h gain,  dx = rstd (g - mean(g) - z mean(g z)),  dgain = sum over rows of h z,  doffset = sum over rows of h
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/rfsf_ts.h"
+#include "dropout.h"
+#include "rows8.h"
+
+namespace rfsf {
+namespace {
+
+constexpr int64_t kMostHeld = 512 * 5 * 8;      // columns of rows that stay in registers
+constexpr int kCus = 256;
+
+struct NormJob {
+    const void *X;
+    void *Y;
+    const float *gain, *offset;
+    float *mean, *rstd;
+    int64_t N, K, ldx, ldy;
+    float eps;
+    DropoutJob dropout;
+};
+struct BackJob {
+    const void *X, *dY;
+    void *dX;
+    const float *mean, *rstd, *gain;
+    float *sums;                // [workgroups along the rows][2][K], dgain's and doffset's; or these themselves of one workgroup
+    float *dgain, *doffset;
+    int64_t N, K, ldx, ldy, ldd;
+    DropoutJob dropout;
+};
+
+// Sums of two numbers over the THREADS lanes of a row. `part`: LDS of rows of more than a wavefront, not used again before the next barrier.
+template <int THREADS>
+__device__ __forceinline__ void add_up(float &a, float &b, float2 *part)
+{
+#pragma unroll
+    for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o /= 2) {
+        a += __shfl_xor(a, o);
+        b += __shfl_xor(b, o);
+    }
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.f;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            a += part[w].x;
+            b += part[w].y;
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ rows8::Eight<T> load_raw(const T *row, int64_t k, int64_t K)
+{
+    rows8::Eight<T> c = {};
+    if (k + 8 <= K) {
+        c = *reinterpret_cast<const rows8::Eight<T> *>(row + k);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < K) c.v[e] = row[k + e];
+    }
+    return c;
+}
+__device__ __forceinline__ void load_or(const float *p, int64_t k, int64_t K, float otherwise, float (&x)[8])
+{
+    if (p) {
+        rows8::load(p, k, K, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = otherwise;
+    }
+}
+
+// The mean of a row from what was subtracted from its numbers first, and the rest's sums.
+struct Moments { float shift, rest, rstd; };
+__device__ __forceinline__ Moments moments(float shift, float sum, float squares, float inverse, float eps)
+{
+    const float rest = sum * inverse;
+    return {shift, rest, 1.0f / sqrtf(fmaxf(squares * inverse - rest * rest, 0.f) + eps)};
+}
+
+// THREADS lanes hold a row, HELD times eight numbers each; a workgroup goes through rows, whose next one is loaded while the present one is worked on, and
+// keeps its columns' gains and offsets. The mean is subtracted before squares are added up, and what rounding left of it
+// is taken off both afterwards, so that rows far from zero lose nothing.
+template <typename T, int THREADS, int HELD, bool DROP>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(NormJob job)
+{
+    constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1;
+    __shared__ float2 part[2][WAVES];
+    const int lane = threadIdx.x % THREADS;
+    const int64_t K = job.K, step = (int64_t)gridDim.x * ROWS;
+    const float inverse = 1.0f / (float)K;
+    float gain[HELD][8], shift[HELD][8];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+        load_or(job.gain, 8 * (lane + u * THREADS), K, 1.f, gain[u]);
+        load_or(job.offset, 8 * (lane + u * THREADS), K, 0.f, shift[u]);
+    }
+    const uint64_t counter = DROP ? dropout::offset_of(job.dropout) : 0;
+    const T *X = static_cast<const T *>(job.X);
+    T *Y = static_cast<T *>(job.Y);
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    rows8::Eight<T> next[HELD];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) next[u] = load_raw(X + std::min(row, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
+    // (all rows of a workgroup take as many turns, so that everybody meets at the barriers)
+    for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
+        float x[HELD][8];
+        float sum = 0.f, squares = 0.f;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[u][e] = rows8::to_float(next[u].v[e]);
+                sum += x[u][e];
+            }
+        if (turn + step < job.N) {
+#pragma unroll
+            for (int u = 0; u < HELD; ++u) next[u] = load_raw(X + std::min(row + step, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
+        }
+        add_up<THREADS>(sum, squares, part[0]);
+        const float mean = sum * inverse;
+        sum = squares = 0.f;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[u][e] = 8 * (lane + u * THREADS) + e < K ? x[u][e] - mean : 0.f;
+                sum += x[u][e];
+                squares = fmaf(x[u][e], x[u][e], squares);
+            }
+        add_up<THREADS>(sum, squares, part[1]);
+        const Moments m = moments(mean, sum, squares, inverse, job.eps);
+        if (row >= job.N) continue;
+        if (lane == 0) {
+            if (job.mean) job.mean[row] = m.shift + m.rest;
+            if (job.rstd) job.rstd[row] = m.rstd;
+        }
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int64_t k = 8 * (lane + u * THREADS);
+            if (k >= K) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] = fmaf((x[u][e] - m.rest) * m.rstd, gain[u][e], shift[u][e]);
+            if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), x[u]);
+            rows8::store(Y + row * job.ldy, k, K, x[u]);
+        }
+    }
+}
+
+// Longer rows: a workgroup reads a row three times, of which the caches give the last two.
+constexpr int kLongThreads = 1024;
+template <typename T>
+__global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bool drop)
+{
+    __shared__ float2 part[2][kLongThreads / 64];
+    const int64_t K = job.K, row = blockIdx.x;
+    const float inverse = 1.0f / (float)K;
+    const T *x_row = static_cast<const T *>(job.X) + row * job.ldx;
+    float sum = 0.f, squares = 0.f, x[8];
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
+        rows8::load(x_row, k, K, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += x[e];
+    }
+    add_up<kLongThreads>(sum, squares, part[0]);
+    const float mean = sum * inverse;
+    sum = squares = 0.f;
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
+        rows8::load(x_row, k, K, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = k + e < K ? x[e] - mean : 0.f;
+            sum += x[e];
+            squares = fmaf(x[e], x[e], squares);
+        }
+    }
+    add_up<kLongThreads>(sum, squares, part[1]);
+    const Moments m = moments(mean, sum, squares, inverse, job.eps);
+    if (threadIdx.x == 0) {
+        if (job.mean) job.mean[row] = m.shift + m.rest;
+        if (job.rstd) job.rstd[row] = m.rstd;
+    }
+    const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
+        float gain[8], shift[8];
+        rows8::load(x_row, k, K, x);
+        load_or(job.gain, k, K, 1.f, gain);
+        load_or(job.offset, k, K, 0.f, shift);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf((x[e] - mean - m.rest) * m.rstd, gain[e], shift[e]);
+        if (drop) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), x);
+        rows8::store(static_cast<T *>(job.Y) + row * job.ldy, k, K, x);
+    }
+}
+
+// The backward pass of rows that are held in registers as above. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose sums
+// are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
+template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(BackJob job)
+{
+    constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1;
+    __shared__ float2 part[2][WAVES];
+    const int lane = threadIdx.x % THREADS;
+    const int64_t K = job.K, step = (int64_t)gridDim.x * ROWS;
+    const float inverse = 1.0f / (float)K;
+    float gain[HELD][8], of_gain[HELD][8], of_offset[HELD][8];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+        load_or(job.gain, 8 * (lane + u * THREADS), K, 1.f, gain[u]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) of_gain[u][e] = of_offset[u][e] = 0.f;
+    }
+    const uint64_t counter = DROP ? dropout::offset_of(job.dropout) : 0;
+    const T *X = static_cast<const T *>(job.X), *dY = static_cast<const T *>(job.dY);
+    T *dX = static_cast<T *>(job.dX);
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    rows8::Eight<T> next_x[HELD], next_h[HELD];
+    float next_mean, next_rstd;
+    auto load = [&](int64_t r) {
+        r = std::min(r, job.N - 1);
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            next_x[u] = load_raw(X + r * job.ldx, 8 * (lane + u * THREADS), K);
+            next_h[u] = load_raw(dY + r * job.ldy, 8 * (lane + u * THREADS), K);
+        }
+        next_mean = job.mean[r];
+        next_rstd = job.rstd[r];
+    };
+    load(row);
+    int which = 0;
+    for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
+        const float mean = next_mean, rstd = next_rstd;
+        const bool there = row < job.N;
+        float z[HELD][8], g[HELD][8];
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int64_t k = 8 * (lane + u * THREADS);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                z[u][e] = (rows8::to_float(next_x[u].v[e]) - mean) * rstd;
+                g[u][e] = rows8::to_float(next_h[u].v[e]);
+            }
+            if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), g[u]);
+        }
+        if (turn + step < job.N) load(row + step);
+        float sum = 0.f, products = 0.f;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool counts = there && 8 * (lane + u * THREADS) + e < K;
+                if (GAINS) {
+                    of_gain[u][e] += counts ? g[u][e] * z[u][e] : 0.f;
+                    of_offset[u][e] += counts ? g[u][e] : 0.f;
+                }
+                g[u][e] = counts ? g[u][e] * gain[u][e] : 0.f;
+                sum += g[u][e];
+                products += counts ? g[u][e] * z[u][e] : 0.f;
+            }
+        add_up<THREADS>(sum, products, part[which]);
+        which ^= 1;
+        if (!there) continue;
+        sum *= inverse;
+        products *= inverse;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int64_t k = 8 * (lane + u * THREADS);
+            if (k >= K) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[u][e] = (g[u][e] - fmaf(z[u][e], products, sum)) * rstd;
+            rows8::store(dX + row * job.ldd, k, K, g[u]);
+        }
+    }
+    if constexpr (GAINS) {
+        float *mine = job.sums + (int64_t)blockIdx.x * 2 * K;
+        if constexpr (ROWS > 1) {                       // over the workgroup's rows
+            __shared__ float all[ROWS][THREADS][9];
+#pragma unroll
+            for (int u = 0; u < HELD; ++u)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) all[threadIdx.x / THREADS][lane][e] = w ? of_offset[u][e] : of_gain[u][e];
+                    __syncthreads();
+                    for (int at = threadIdx.x; at < THREADS * 8; at += 256) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int r = 0; r < ROWS; ++r) s += all[r][at / 8][at % 8];
+                        const int64_t k = 8 * THREADS * u + at;
+                        if (k < K) mine[w * K + k] = s;
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < HELD; ++u) {
+                rows8::store(mine, 8 * (lane + u * THREADS), K, of_gain[u]);
+                rows8::store(mine + K, 8 * (lane + u * THREADS), K, of_offset[u]);
+            }
+        }
+    }
+}
+
+// dX of longer rows: a workgroup reads a row twice.
+template <typename T>
+__global__ __launch_bounds__(kLongThreads) void back_long_kernel(BackJob job, bool drop)
+{
+    __shared__ float2 part[kLongThreads / 64];
+    const int64_t K = job.K, row = blockIdx.x;
+    const float inverse = 1.0f / (float)K, mean = job.mean[row], rstd = job.rstd[row];
+    const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
+    const T *X = static_cast<const T *>(job.X) + row * job.ldx, *dY = static_cast<const T *>(job.dY) + row * job.ldy;
+    float z[8], g[8];
+    auto load = [&](int64_t k) {
+        float gain[8];
+        rows8::load(X, k, K, z);
+        rows8::load(dY, k, K, g);
+        load_or(job.gain, k, K, 1.f, gain);
+        if (drop) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            z[e] = (z[e] - mean) * rstd;
+            g[e] *= gain[e];
+        }
+    };
+    float sum = 0.f, products = 0.f;
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
+        load(k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < K) {
+                sum += g[e];
+                products = fmaf(g[e], z[e], products);
+            }
+    }
+    add_up<kLongThreads>(sum, products, part);
+    sum *= inverse;
+    products *= inverse;
+    for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
+        load(k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = (g[e] - fmaf(z[e], products, sum)) * rstd;
+        rows8::store(static_cast<T *>(job.dX) + row * job.ldd, k, K, g);
+    }
+}
+
+// dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * THREADS columns of every (number of parts)-th group of rows.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(256) void gains_kernel(BackJob job, uint32_t pieces, bool drop)
+{
+    constexpr int ROWS = 256 / THREADS, AHEAD = 4;
+    __shared__ float all[ROWS][THREADS][17];
+    const int lane = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
+    const int64_t K = job.K, part = blockIdx.x / pieces, parts = gridDim.x / pieces, k = 8 * ((int64_t)(blockIdx.x % pieces) * THREADS + lane);
+    const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
+    const T *X = static_cast<const T *>(job.X), *dY = static_cast<const T *>(job.dY);
+    float of_gain[8], of_offset[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) of_gain[e] = of_offset[e] = 0.f;
+    if (k < K) {
+        for (int64_t row = part * ROWS + sub; row < job.N; row += AHEAD * parts * ROWS) {
+            rows8::Eight<T> x[AHEAD], h[AHEAD];
+            float mean[AHEAD], rstd[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int64_t r = std::min(row + a * parts * ROWS, job.N - 1);
+                x[a] = load_raw(X + r * job.ldx, k, K);
+                h[a] = load_raw(dY + r * job.ldy, k, K);
+                mean[a] = job.mean[r];
+                rstd[a] = job.rstd[r];
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int64_t r = row + a * parts * ROWS;
+                if (r >= job.N) break;
+                float g[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = rows8::to_float(h[a].v[e]);
+                if (drop) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)r, (uint32_t)(k / 8), g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    of_gain[e] = fmaf(g[e], (rows8::to_float(x[a].v[e]) - mean[a]) * rstd[a], of_gain[e]);
+                    of_offset[e] += g[e];
+                }
+            }
+        }
+    }
+    float *mine = job.sums + part * 2 * K;
+    if constexpr (ROWS > 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            all[sub][lane][e] = of_gain[e];
+            all[sub][lane][8 + e] = of_offset[e];
+        }
+        __syncthreads();
+        if (sub != 0) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a = 0.f, b = 0.f;
+            for (int r = 0; r < ROWS; ++r) {
+                a += all[r][lane][e];
+                b += all[r][lane][8 + e];
+            }
+            of_gain[e] = a;
+            of_offset[e] = b;
+        }
+    }
+    if (k < K) {
+        rows8::store(mine, k, K, of_gain);
+        rows8::store(mine + K, k, K, of_offset);
+    }
+}
+
+// Adds the workgroups' sums up, in a fixed order: 64 columns a workgroup, whose wavefronts share the parts.
+constexpr int kAddWaves = 16;
+__global__ __launch_bounds__(64 * kAddWaves) void add_parts_kernel(const float *sums, int64_t parts, int64_t K, float *dgain, float *doffset)
+{
+    __shared__ float all[kAddWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t at = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (at < 2 * K)
+        for (int64_t p = wave; p < parts; p += kAddWaves) s += sums[p * 2 * K + at];
+    all[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || at >= 2 * K) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAddWaves; ++w) s += all[w][lane];
+    if (at < K) dgain[at] = s;
+    else doffset[at - K] = s;
+}
+
+// Lanes a row, and how many times eight numbers each holds: as few turns as hold it.
+template <typename F>
+auto with_shape(int64_t K, const F &f)
+{
+    const int64_t eights = (K + 7) / 8;
+    auto go = [&](auto threads, auto held) { return f(threads, held); };
+    typedef std::integral_constant<int, 16> t16;
+    typedef std::integral_constant<int, 64> t64;
+    typedef std::integral_constant<int, 256> t256;
+    typedef std::integral_constant<int, 512> t512;
+    typedef std::integral_constant<int, 1> h1;
+    typedef std::integral_constant<int, 2> h2;
+    typedef std::integral_constant<int, 3> h3;
+    typedef std::integral_constant<int, 4> h4;
+    typedef std::integral_constant<int, 5> h5;
+    if (eights <= 16) return go(t16(), h1());
+    if (eights <= 32) return go(t16(), h2());
+    if (eights <= 64) return go(t64(), h1());
+    if (eights <= 128) return go(t64(), h2());
+    if (eights <= 256) return go(t256(), h1());
+    if (eights <= 512) return go(t256(), h2());
+    if (eights <= 768) return go(t256(), h3());
+    if (eights <= 1024) return go(t512(), h2());
+    if (eights <= 1536) return go(t512(), h3());
+    if (eights <= 2048) return go(t512(), h4());
+    return go(t512(), h5());
+}
+constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
+constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
+// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time.
+int64_t groups_of(int64_t N, int threads) { return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (1024 / group_threads(threads))); }
+
+// Parts of dgain and doffset. Fused with dX: one for each workgroup.
+int gains_threads(int64_t K) { return K <= 128 ? 16 : K <= 512 ? 64 : 256; }
+int64_t gains_pieces(int64_t K) { return (K + 8 * gains_threads(K) - 1) / (8 * gains_threads(K)); }
+int64_t parts_of(int64_t N, int64_t K, bool with_dx)
+{
+    if (N == 0) return 0;
+    if (with_dx && K <= kMostHeld) return with_shape(K, [&](auto threads, auto) { return groups_of(N, threads); });
+    const int64_t rows = 256 / gains_threads(K), groups = (N + rows - 1) / rows;
+    return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
+}
+
+template <typename T>
+hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
+{
+    if (job.K <= kMostHeld) {
+        with_shape(job.K, [&](auto threads, auto held) {
+            const dim3 grid((unsigned)groups_of(job.N, threads));
+            if (drop) norm_kernel<T, threads, held, true><<<grid, group_threads(threads), 0, stream>>>(job);
+            else norm_kernel<T, threads, held, false><<<grid, group_threads(threads), 0, stream>>>(job);
+        });
+        return hipGetLastError();
+    }
+    constexpr int64_t kMost = 1 << 21;          // workgroups of a launch
+    for (int64_t n0 = 0; n0 < job.N; n0 += kMost) {
+        NormJob part = job;
+        part.X = static_cast<const T *>(job.X) + n0 * job.ldx;
+        part.Y = static_cast<T *>(job.Y) + n0 * job.ldy;
+        if (job.mean) part.mean = job.mean + n0;
+        if (job.rstd) part.rstd = job.rstd + n0;
+        part.dropout.first_row += (uint32_t)n0;
+        norm_long_kernel<T><<<dim3((unsigned)std::min(kMost, job.N - n0)), kLongThreads, 0, stream>>>(part, drop);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
+{
+    BackJob job = whole;
+    const bool gains = job.dgain != nullptr, held = job.K <= kMostHeld;
+    const int64_t parts = gains ? parts_of(job.N, job.K, job.dX != nullptr) : 0;
+    if (job.dX && held) {
+        with_shape(job.K, [&](auto threads, auto held_) {
+            const dim3 grid((unsigned)groups_of(job.N, threads));
+            auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
+            if (drop && gains) launch(back_kernel<T, threads, held_, true, true>);
+            else if (drop) launch(back_kernel<T, threads, held_, true, false>);
+            else if (gains) launch(back_kernel<T, threads, held_, false, true>);
+            else launch(back_kernel<T, threads, held_, false, false>);
+        });
+    } else {
+        if (gains) {                // (first: dX may lie where dY is)
+            const int64_t pieces = gains_pieces(job.K);
+            const dim3 grid((unsigned)(parts * pieces));
+            const int threads = gains_threads(job.K);
+            if (threads == 16) gains_kernel<T, 16><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
+            else if (threads == 64) gains_kernel<T, 64><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
+            else gains_kernel<T, 256><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
+        }
+        constexpr int64_t kMost = 1 << 21;          // workgroups of a launch
+        for (int64_t n0 = 0; job.dX && n0 < job.N; n0 += kMost) {
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            BackJob part = job;
+            part.X = static_cast<const T *>(job.X) + n0 * job.ldx;
+            part.dY = static_cast<const T *>(job.dY) + n0 * job.ldy;
+            part.dX = static_cast<T *>(job.dX) + n0 * job.ldd;
+            part.mean = job.mean + n0;
+            part.rstd = job.rstd + n0;
+            part.dropout.first_row += (uint32_t)n0;
+            back_long_kernel<T><<<dim3((unsigned)std::min(kMost, job.N - n0)), kLongThreads, 0, stream>>>(part, drop);
+        }
+    }
+    if (gains) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        add_parts_kernel<<<dim3((unsigned)((2 * job.K + 63) / 64)), 64 * kAddWaves, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t layer_norm_backward_bytes(const rfsf_layer_norm_shape &s, bool with_dx)
+{
+    return (size_t)std::max<int64_t>(1, parts_of(s.N, s.K, with_dx)) * 2 * (size_t)s.K * sizeof(float) + 256;
+}
+
+hipError_t launch_layer_norm(const rfsf_layer_norm_shape &s, const void *X, const float *gain, const float *offset, float eps, const rfsf_dropout_mask *mask, void *Y,
+                             float *mean, float *rstd, hipStream_t stream)
+{
+    const NormJob job = {X, Y, gain, offset, mean, rstd, s.N, s.K, s.ld_x, s.ld_y, eps, dropout_job(mask)};
+    return s.bf16 ? norm<uint16_t>(job, mask != nullptr, stream) : norm<float>(job, mask != nullptr, stream);
+}
+
+hipError_t launch_layer_norm_backward(const rfsf_layer_norm_shape &s, const void *X, const float *mean, const float *rstd, const float *gain, const void *dY,
+                                      const rfsf_dropout_mask *mask, void *dX, float *dgain, float *doffset, void *workspace, hipStream_t stream)
+{
+    const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
+    float *sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + (mis ? 256 - mis : 0));
+    const BackJob job = {X, dY, dX, mean, rstd, gain, sums, dgain, doffset, s.N, s.K, s.ld_x, s.ld_y, s.ld_dx, dropout_job(mask)};
+    return s.bf16 ? back<uint16_t>(job, mask != nullptr, stream) : back<float>(job, mask != nullptr, stream);
+}
+
+}  // namespace rfsf

@@ -35,6 +35,21 @@ int check_tensors(const rfsf_adamw_tensor *tensors, int64_t count)
     return RFSF_OK;
 }
 
+int check(const rfsf_dropout_mask &m, int64_t N)
+{
+    if (!(m.p >= 0.0 && m.p <= 1.0)) return RFSF_E_BAD_SETTING;
+    if (m.first_row < 0) return RFSF_E_BAD_SHAPE;
+    return m.first_row > ((int64_t)1 << 32) - N ? RFSF_E_UNSUPPORTED : RFSF_OK;
+}
+int check(const rfsf_layer_norm_shape *s, const rfsf_dropout_mask *m, bool with_dx)
+{
+    if (!s) return RFSF_E_NULLPTR;
+    if (s->N < 0 || s->K < 1) return RFSF_E_BAD_SHAPE;
+    if (s->ld_x < s->K || s->ld_y < s->K || (with_dx && s->ld_dx < s->K)) return RFSF_E_BAD_STRIDE;
+    if (s->N > kMostRows || s->K > kMostColumns) return RFSF_E_UNSUPPORTED;
+    return m ? check(*m, s->N) : RFSF_OK;
+}
+
 }  // namespace
 
 extern "C" int rfsf_softmax_xent_workspace_bytes(const rfsf_xent_shape *shape, size_t *recommended_bytes, size_t *minimum_bytes)
@@ -137,4 +152,59 @@ extern "C" int rfsf_int8_gram(const void *X, int32_t bf16, int64_t Nx, int64_t l
     if (workspace_bytes < minimum) return RFSF_E_WORKSPACE_TOO_SMALL;
     return rfsf::launch_int8_gram(X, bf16 != 0, Nx, ldx, codes, scales, Ny, ld_codes, K, out, ld_out, workspace, workspace_bytes,
                                   static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_dropout(const rfsf_dropout_mask *mask, const void *X, int32_t bf16, int64_t N, int64_t ldx, int64_t K, void *Y, int64_t ldy,
+                            void *hip_stream)
+{
+    if (!mask) return RFSF_E_NULLPTR;
+    if (N < 0 || K < 1) return RFSF_E_BAD_SHAPE;
+    if (ldx < K || ldy < K) return RFSF_E_BAD_STRIDE;
+    if (N > kMostRows || K > kMostColumns) return RFSF_E_UNSUPPORTED;
+    const int rc = check(*mask, N);
+    if (rc != RFSF_OK) return rc;
+    if (N == 0) return RFSF_OK;
+    if (!X || !Y) return RFSF_E_NULLPTR;
+    return rfsf::launch_dropout(*mask, X, bf16 != 0, N, ldx, K, Y, ldy, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_layer_norm(const rfsf_layer_norm_shape *shape, const void *X, const float *gain, const float *offset, double eps,
+                               const rfsf_dropout_mask *mask, void *Y, float *mean, float *rstd, void *hip_stream)
+{
+    const int rc = check(shape, mask, false);
+    if (rc != RFSF_OK) return rc;
+    if (!std::isfinite((float)eps) || !((float)eps > 0.f)) return RFSF_E_BAD_SETTING;
+    if (shape->N == 0) return RFSF_OK;
+    if (!X || !Y) return RFSF_E_NULLPTR;
+    return rfsf::launch_layer_norm(*shape, X, gain, offset, (float)eps, mask, Y, mean, rstd, static_cast<hipStream_t>(hip_stream)) == hipSuccess
+               ? RFSF_OK : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_layer_norm_backward_workspace_bytes(const rfsf_layer_norm_shape *shape, int32_t with_dx, size_t *recommended_bytes, size_t *minimum_bytes)
+{
+    const int rc = check(shape, nullptr, with_dx != 0);
+    if (rc != RFSF_OK) return rc;
+    const size_t bytes = rfsf::layer_norm_backward_bytes(*shape, with_dx != 0);
+    if (recommended_bytes) *recommended_bytes = bytes;
+    if (minimum_bytes) *minimum_bytes = bytes;
+    return RFSF_OK;
+}
+
+extern "C" int rfsf_layer_norm_backward(const rfsf_layer_norm_shape *shape, const void *X, const float *mean, const float *rstd, const float *gain, const void *dY,
+                                        const rfsf_dropout_mask *mask, void *dX, float *dgain, float *doffset, void *workspace, size_t workspace_bytes,
+                                        void *hip_stream)
+{
+    const int rc = check(shape, mask, dX != nullptr);
+    if (rc != RFSF_OK) return rc;
+    if (!dgain != !doffset) return RFSF_E_NULLPTR;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (shape->N == 0) {
+        for (float *d : {dgain, doffset})
+            if (d && rfsf::launch_clear_rows(d, 1, shape->K, shape->K, false, stream) != hipSuccess) return RFSF_E_HIP;
+        return RFSF_OK;
+    }
+    if (!dX && !dgain) return RFSF_OK;
+    if (!X || !mean || !rstd || !dY || (dgain && !workspace)) return RFSF_E_NULLPTR;
+    if (dgain && workspace_bytes < rfsf::layer_norm_backward_bytes(*shape, dX != nullptr)) return RFSF_E_WORKSPACE_TOO_SMALL;
+    return rfsf::launch_layer_norm_backward(*shape, X, mean, rstd, gain, dY, mask, dX, dgain, doffset, workspace, stream) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
 }

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -159,6 +160,15 @@ hipError_t launch_int8_quantize(const void *X, bool bf16, int64_t N, int64_t ld,
 void int8_gram_bytes(int64_t Nx, int64_t K, size_t *recommended, size_t *minimum);
 hipError_t launch_int8_gram(const void *X, bool bf16, int64_t Nx, int64_t ldx, const int8_t *codes, const float *scales, int64_t Ny, int64_t ldy,
                             int64_t K, float *out, int64_t ldk, void *workspace, size_t bytes, hipStream_t stream);
+
+// Layer norm and dropout of feature rows (csrc/layer_norm.hip, dropout.hip); arguments are checked by csrc/linear_api.hip. A mask may be null: no dropout.
+inline uint32_t dropout_threshold(double p) { return (uint32_t)nearbyint(p * 65536.0); }
+hipError_t launch_dropout(const rfsf_dropout_mask &mask, const void *X, bool bf16, int64_t N, int64_t ldx, int64_t K, void *Y, int64_t ldy, hipStream_t stream);
+hipError_t launch_layer_norm(const rfsf_layer_norm_shape &shape, const void *X, const float *gain, const float *offset, float eps,
+                             const rfsf_dropout_mask *mask, void *Y, float *mean, float *rstd, hipStream_t stream);
+size_t layer_norm_backward_bytes(const rfsf_layer_norm_shape &shape, bool with_dx);
+hipError_t launch_layer_norm_backward(const rfsf_layer_norm_shape &shape, const void *X, const float *mean, const float *rstd, const float *gain, const void *dY,
+                                      const rfsf_dropout_mask *mask, void *dX, float *dgain, float *doffset, void *workspace, hipStream_t stream);
 
 // Benchmark helper (csrc/probe.hip): read, write, non-temporal write, copy GB/s over `scratch`, fp32 matrix and
 // fp32 vector TFLOP/s of issue loops, in this order; waits for the stream.

@@ -305,7 +305,7 @@ extern "C" const char *rfsf_ts_strerror(int code)
         case RFSF_E_UNSUPPORTED: return "configuration not supported by this build";
         case RFSF_E_STATIC_SCRATCH_TOO_SMALL:
             return "one sequence needs more than the 64 MiB built-in scratch: use rfsf_ts_features with a workspace";
-        case RFSF_E_BAD_SETTING: return "an optimizer setting is not finite or out of its range";
+        case RFSF_E_BAD_SETTING: return "a setting is not finite or out of its range";
         default: return "unknown rfsf_ts error code";
     }
 }

@@ -1,0 +1,48 @@
+// Eight numbers of a row of a matrix at a time, float or bfloat16 (as uint16_t), at any alignment of the type: one load or store of 16 bytes,
+// or two of them, and single numbers at the end of a row.
+#pragma once
+
+#include "rfsf_internal.h"
+
+namespace rfsf {
+namespace rows8 {
+
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Eight { T v[8]; };
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ void from_float(float x, float *out) { *out = x; }
+// the nearest bfloat16, ties to even; a NaN stays one
+__device__ __forceinline__ void from_float(float x, uint16_t *out) { *out = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// Columns k .. k + 7 of a row of K; 0 beyond.
+template <typename T>
+__device__ __forceinline__ void load(const T *row, int64_t k, int64_t K, float (&x)[8])
+{
+    if (k + 8 <= K) {
+        const Eight<T> c = *reinterpret_cast<const Eight<T> *>(row + k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = to_float(c.v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e < K ? to_float(row[k + e]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store(T *row, int64_t k, int64_t K, const float (&x)[8])
+{
+    if (k + 8 <= K) {
+        Eight<T> c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) from_float(x[e], &c.v[e]);
+        *reinterpret_cast<Eight<T> *>(row + k) = c;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < K) from_float(x[e], row + k + e);
+    }
+}
+
+}  // namespace rows8
+}  // namespace rfsf

@@ -1,5 +1,5 @@
 """Binding of the operators of linear models on feature rows: softmax cross entropy with its gradients, the AdamW
-step, and the Gram against rows held in 8-bit integers (include/rfsf_ts.h). Argument marshalling only, as in binding.py."""
+step, the Gram against rows held in 8-bit integers, layer norm and dropout (include/rfsf_ts.h). Argument marshalling only, as in binding.py."""
 from __future__ import annotations
 
 import ctypes
@@ -30,6 +30,16 @@ class _AdamwConfig(ctypes.Structure):
 class _AdamwTensor(ctypes.Structure):
     _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class _DropoutMask(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("offset_on_device", ctypes.c_void_p),
+                ("first_row", ctypes.c_int64)]
+
+
+class _LayerNormShape(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_dx", ctypes.c_int64),
+                ("bf16", ctypes.c_int32)]
 
 
 def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
@@ -252,3 +262,130 @@ def rfsf_int8_gram(PhiX: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor
     _check(load_library().rfsf_int8_gram(PhiX.data_ptr(), _BF16[PhiX.dtype], Nx, ldx, codes.data_ptr(), scales.data_ptr(), Ny, ldy,
                                          ncols, K.data_ptr(), ldk, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
     return K
+
+
+class RfsfDropout:
+    """Which mask dropout uses (rfsf_dropout_mask): everything follows from these numbers, so that the backward pass gets the forward pass's mask from an equal one.
+
+    p: probability of leaving a number out, rounded to a multiple of 2^-16. seed, offset: whole numbers of 64 bits; another step or layer takes another
+    offset. counter: an int64 tensor of one element on the device, added to offset when the kernel runs (a captured graph that
+    adds to it meets another mask each time). first_row: the number of the first row, for rows of one batch that are worked on in parts."""
+
+    __slots__ = ("p", "seed", "offset", "counter", "first_row")
+
+    def __init__(self, p: float, seed: int, offset: int = 0, counter: Optional[torch.Tensor] = None, first_row: int = 0):
+        if not 0 <= p <= 1:
+            raise ValueError("p must be in [0, 1]")
+        if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+            raise ValueError("seed and offset must be whole numbers of 64 bits")
+        if not 0 <= first_row < 1 << 32:
+            raise ValueError("first_row must be a whole number of 32 bits")
+        if counter is not None and (not counter.is_cuda or counter.dtype is not torch.int64 or counter.numel() != 1):
+            raise ValueError("counter must be an int64 device tensor of one element")
+        self.p, self.seed, self.offset, self.counter, self.first_row = p, seed, offset, counter, first_row
+
+    def _mask(self) -> _DropoutMask:
+        return _DropoutMask(self.p, self.seed, self.offset, None if self.counter is None else self.counter.data_ptr(), self.first_row)
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors that are not on the current device, whose stream the work goes to."""
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != current:
+            raise ValueError("all tensors must be on the current device")
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    """Address of a contiguous float32 device tensor [n], or None."""
+    if t is None:
+        return None
+    if _dev(t, torch.float32, name).shape != (n,):
+        raise ValueError(f"{name} must have shape [{n}]")
+    return t.data_ptr()
+
+
+def rfsf_dropout(X: torch.Tensor, dropout: RfsfDropout, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """X [N, K] (float32 or bfloat16) with numbers left out as `dropout` says and the others scaled; gradients go through the same call. out may be X."""
+    ldx = _matrix(X, "X")
+    N, K = X.shape
+    if out is None:
+        out = _empty_on(stream, (N, K), dtype=X.dtype, device=X.device)
+    ldy = _matrix(out, "out", X.dtype, (N, K))
+    _here(X, out, dropout.counter)
+    mask = dropout._mask()
+    _check(load_library().rfsf_dropout(ctypes.byref(mask), X.data_ptr(), _BF16[X.dtype], N, ldx, K, out.data_ptr(), ldy, _stream_ptr(stream)))
+    return out
+
+
+def rfsf_layer_norm(X: torch.Tensor, gain: Optional[torch.Tensor] = None, offset: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                    dropout: Optional[RfsfDropout] = None, out: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                    rstd: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """(Y, mean [N], rstd [N]): rows of X [N, K] (float32 or bfloat16) less their mean, divided by their deviation, times gain [K] plus offset [K]
+    (float32, or None: 1 and 0), with dropout behind. Buffers that are not given are allocated; out may be X."""
+    ldx = _matrix(X, "X")
+    N, K = X.shape
+    if out is None:
+        out = _empty_on(stream, (N, K), dtype=X.dtype, device=X.device)
+    ldy = _matrix(out, "out", X.dtype, (N, K))
+    if mean is None:
+        mean = _empty_on(stream, N, dtype=torch.float32, device=X.device)
+    if rstd is None:
+        rstd = _empty_on(stream, N, dtype=torch.float32, device=X.device)
+    _here(X, out, gain, offset, mean, rstd, dropout and dropout.counter)
+    shape = _LayerNormShape(N, K, ldx, ldy, K, _BF16[X.dtype])
+    mask = dropout._mask() if dropout is not None else None
+    _check(load_library().rfsf_layer_norm(ctypes.byref(shape), X.data_ptr(), _vector(gain, K, "gain"), _vector(offset, K, "offset"), eps,
+                                          mask and ctypes.byref(mask), out.data_ptr(), _vector(mean, N, "mean"), _vector(rstd, N, "rstd"),
+                                          _stream_ptr(stream)))
+    return out, mean, rstd
+
+
+def rfsf_layer_norm_backward_workspace_bytes(N: int, K: int, dtype: torch.dtype = torch.float32, need_dX: bool = True):
+    """(recommended_bytes, minimum_bytes) of scratch for rfsf_layer_norm_backward with the gradients of gain and offset."""
+    if dtype not in _BF16:
+        raise ValueError("dtype must be float32 or bfloat16")
+    shape = _LayerNormShape(N, K, K, K, K, _BF16[dtype])
+    rec, mn = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load_library().rfsf_layer_norm_backward_workspace_bytes(ctypes.byref(shape), int(need_dX), ctypes.byref(rec), ctypes.byref(mn)))
+    return int(rec.value), int(mn.value)
+
+
+def rfsf_layer_norm_backward(X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, dY: torch.Tensor, gain: Optional[torch.Tensor] = None,
+                             dropout: Optional[RfsfDropout] = None, need_dX: bool = True, need_gains: bool = True,
+                             dX: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None, doffset: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """(dX or None, dgain [K] or None, doffset [K] or None): gradients of rfsf_layer_norm with these X, gain and dropout, mean and rstd being what it
+    returned, from the gradient dY of its result. Buffers that are not given are allocated; dX may be X or dY."""
+    ldx = _matrix(X, "X")
+    N, K = X.shape
+    ldy, ldd = _matrix(dY, "dY", X.dtype, (N, K)), K
+    if need_dX:
+        if dX is None:
+            dX = _empty_on(stream, (N, K), dtype=X.dtype, device=X.device)
+        ldd = _matrix(dX, "dX", X.dtype, (N, K))
+    else:
+        dX = None
+    lib = load_library()
+    shape = _LayerNormShape(N, K, ldx, ldy, ldd, _BF16[X.dtype])
+    if need_gains:
+        if dgain is None:
+            dgain = _empty_on(stream, K, dtype=torch.float32, device=X.device)
+        if doffset is None:
+            doffset = _empty_on(stream, K, dtype=torch.float32, device=X.device)
+        if workspace is None:
+            rec = ctypes.c_size_t(0)
+            _check(lib.rfsf_layer_norm_backward_workspace_bytes(ctypes.byref(shape), int(need_dX), ctypes.byref(rec), None))
+            workspace = _empty_on(stream, int(rec.value), dtype=torch.uint8, device=X.device)
+        workspace = _dev(workspace, torch.uint8, "workspace")
+    else:
+        dgain = doffset = workspace = None
+    _here(X, mean, rstd, dY, gain, dX, dgain, doffset, workspace, dropout and dropout.counter)
+    mask = dropout._mask() if dropout is not None else None
+    if _vector(mean, N, "mean") is None or _vector(rstd, N, "rstd") is None:
+        raise ValueError("mean and rstd are needed")
+    _check(lib.rfsf_layer_norm_backward(ctypes.byref(shape), X.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _vector(gain, K, "gain"), dY.data_ptr(),
+                                        mask and ctypes.byref(mask), dX.data_ptr() if need_dX else None, _vector(dgain, K, "dgain"),
+                                        _vector(doffset, K, "doffset"), workspace.data_ptr() if need_gains else None,
+                                        workspace.numel() if need_gains else 0, _stream_ptr(stream)))
+    return dX, dgain, doffset
