@@ -407,6 +407,33 @@ int rfsf_layer_norm_backward(const rfsf_layer_norm_shape *shape, const void *X, 
                              void *hip_stream);
 
 /*
+ * Scores of a linear classifier that many users share, each request (row) with a low-rank adapter of its own beside the shared weights:
+ *   out[n, c] = sum_k X[n, k] W[c, k] + scale[a] sum_r B[a][c, r] sum_k A[a][r, k] X[n, k],     a = adapters[n]
+ *   X [N, ld_x], W [C, ld_w], A[a] [rank, ld_a], B[a] [C, ld_b] row-major, all float32, or all bfloat16 (bf16 != 0); out [N, ld_out] float32
+ *   adapters [N] int64 on the device. Negative: the shared part alone, whatever the adapters hold. >= count: the row is NaN (it is not used as an address).
+ * Weights and adapters are laid out once, in memory of the caller's (rfsf_adapters_layout_bytes; aligned to 256 bytes, RFSF_E_BAD_STRIDE otherwise), and are not
+ * looked at afterwards: rfsf_adapters_set_weights, and rfsf_adapters_set for an adapter, whose place then holds a new one for
+ * the calls that follow on the stream. An adapter of a lower rank is padded with zeros by the caller. A layout that is cleared
+ * first has adapters that add nothing; one that was never set and not cleared must not be used.
+ * Accuracy: X and W, and A, enter the products as for rfsf_softmax_xent without gradients (float32 with 22 significand bits down to 2^-17 of the largest number of their
+ * row, bfloat16 whole), the sums over r with the numbers of B as they are. Sums are held in 32 bits. A row of X, W, A or B with an infinity or a NaN
+ * makes what is computed from it NaN (bfloat16: or what infinities give), and nothing else. Equal calls with workspaces of equal sizes give equal bits.
+ * Limits: K, C <= 3500000, N < 2^31, rank <= 256, count <= 131072 (RFSF_E_UNSUPPORTED). scale has to be finite (RFSF_E_BAD_SETTING). N = 0 is a no-op.
+ */
+typedef struct {
+    int64_t K, C;               /* columns, classes */
+    int64_t rank, count;        /* of every adapter; how many there is room for (>= 1) */
+    int32_t bf16;
+} rfsf_adapters_shape;
+int rfsf_adapters_layout_bytes(const rfsf_adapters_shape *shape, size_t *bytes);
+int rfsf_adapters_set_weights(const rfsf_adapters_shape *shape, const void *W, int64_t ld_w, void *layout, void *hip_stream);
+int rfsf_adapters_set(const rfsf_adapters_shape *shape, int64_t index, const void *A, int64_t ld_a, const void *B, int64_t ld_b, double scale, void *layout,
+                      void *hip_stream);
+int rfsf_adapted_scores_workspace_bytes(const rfsf_adapters_shape *shape, int64_t N, size_t *recommended_bytes, size_t *minimum_bytes);
+int rfsf_adapted_scores(const rfsf_adapters_shape *shape, const void *layout, const void *X, int64_t N, int64_t ld_x, const int64_t *adapters,
+                        float *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Optional per-kernel timing for benchmarks (not part of the method). While enabled, every
  * kernel the library launches is bracketed by HIP events on the stream it is launched on.
  * rfsf_ts_profile_read waits for those events, adds up the elapsed device time per kernel

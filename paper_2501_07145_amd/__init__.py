@@ -5,6 +5,6 @@ from .binding import (  # noqa: F401
     feature_row_stride, rfsf_ts_normalize_features, rfsf_dp1d_features, rfsf_trp_features, rfsf_trp_workspace_bytes,
 )
 from .linear import (  # noqa: F401
-    RfsfAdamW, RfsfDropout, rfsf_dropout, rfsf_int8_gram, rfsf_int8_gram_workspace_bytes, rfsf_int8_quantize, rfsf_layer_norm,
+    RfsfAdamW, RfsfAdapters, RfsfDropout, rfsf_dropout, rfsf_int8_gram, rfsf_int8_gram_workspace_bytes, rfsf_int8_quantize, rfsf_layer_norm,
     rfsf_layer_norm_backward, rfsf_layer_norm_backward_workspace_bytes, rfsf_softmax_xent, rfsf_softmax_xent_workspace_bytes,
 )

@@ -112,6 +112,16 @@ def load_library():
     lib.rfsf_layer_norm_backward_workspace_bytes.argtypes = [vp, i32, pt(sz), pt(sz)]
     lib.rfsf_layer_norm_backward.restype = ctypes.c_int
     lib.rfsf_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rfsf_adapters_layout_bytes.restype = ctypes.c_int
+    lib.rfsf_adapters_layout_bytes.argtypes = [vp, pt(sz)]
+    lib.rfsf_adapters_set_weights.restype = ctypes.c_int
+    lib.rfsf_adapters_set_weights.argtypes = [vp, vp, i64, vp, vp]
+    lib.rfsf_adapters_set.restype = ctypes.c_int
+    lib.rfsf_adapters_set.argtypes = [vp, i64, vp, i64, vp, i64, ctypes.c_double, vp, vp]
+    lib.rfsf_adapted_scores_workspace_bytes.restype = ctypes.c_int
+    lib.rfsf_adapted_scores_workspace_bytes.argtypes = [vp, i64, pt(sz), pt(sz)]
+    lib.rfsf_adapted_scores.restype = ctypes.c_int
+    lib.rfsf_adapted_scores.argtypes = [vp, vp, vp, i64, i64, vp, vp, i64, vp, sz, vp]
     _lib = lib
     return lib
 

@@ -1,0 +1,337 @@
+// Scores of a linear classifier with low-rank adapters of many requests at once (rfsf_adapted_scores):
+//   out[n, c] = x_n . w_c + sum_r s[n, r] B[a][c, r],   s[n, r] = scale[a] (A[a][r] . x_n),   a the row's adapter
+//
+// Weights and adapters lie packed as operands of plane_product.h, the rows of X are packed by each call. Rows are put in the order of their adapters, so that
+// rows that are worked on together share few of them; the inner products s go through matrix instructions in tiles of 16 rows, one
+// adapter of the tile after another; the shared product's epilogue adds B's part to its accumulators, again one
+// adapter of a block of 32 rows after another. What belongs to a row of another adapter is left out by a choice between registers, never by a factor of 0, which
+// infinities and NaN would get through.
+#include "plane_product.h"
+
+#include <algorithm>
+
+#include "../../include/rfsf_ts.h"
+#include "plane_pack.h"
+#include "rows8.h"
+
+#define RFSF_TRY(call)                       \
+    do {                                     \
+        const hipError_t e_ = (call);        \
+        if (e_ != hipSuccess) return e_;     \
+    } while (0)
+
+namespace rfsf {
+namespace {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+// The caller's memory: W's rows, those of the adapters' A (ranks rounded up to 16, zeros beyond), each with their largest numbers, then B in its own type
+// (ranks rounded up to 16 bytes, zeros beyond), and the scales.
+struct Layout {
+    int64_t pitch;                      // bytes of a packed row
+    int ranks, ranks_b;                 // rows of an adapter's A, numbers of a row of its B
+    size_t w, largest_w, a, largest_a, b, scale, bytes;
+};
+Layout layout_of(const rfsf_adapters_shape &s)
+{
+    Layout z;
+    z.pitch = plane_pitch(s.K, !s.bf16);
+    z.ranks = (int)((s.rank + 15) / 16 * 16);
+    z.ranks_b = (int)(s.bf16 ? (s.rank + 7) / 8 * 8 : (s.rank + 3) / 4 * 4);
+    z.w = 0;
+    z.largest_w = z.w + up((size_t)s.C * z.pitch);
+    z.a = z.largest_w + up((size_t)s.C * 4);
+    z.largest_a = z.a + up((size_t)s.count * z.ranks * z.pitch);
+    z.b = z.largest_a + up((size_t)s.count * z.ranks * 4);
+    z.scale = z.b + up((size_t)s.count * s.C * z.ranks_b * (s.bf16 ? 2 : 4));
+    z.bytes = z.scale + up((size_t)s.count * 4);
+    return z;
+}
+
+hipError_t pack(const PackJob &job, bool bf16, hipStream_t stream)
+{
+    PackPair pair = {};
+    pair.job[0] = job;
+    if (job.K <= kPackRowsColumns) return launch_pack_rows(pair, bf16, stream);
+    RFSF_TRY(launch_largest(pair, bf16, stream));
+    return launch_pack(pair, bf16, stream);
+}
+
+// An adapter's B with rows of `ranks_b` numbers, its scale, and zeros for the rows of its A beyond the rank.
+template <typename T>
+__global__ __launch_bounds__(256) void set_kernel(const T *B, int64_t ld_b, int64_t C, int rank, int ranks_b, T *to, char *a_rest, int64_t rest_bytes,
+                                                  uint32_t *largest_rest, int rest, float *scale_at, float scale)
+{
+    const int64_t step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    for (int64_t i = first; i < C * ranks_b; i += step) {
+        const int64_t c = i / ranks_b;
+        const int r = (int)(i - c * ranks_b);
+        to[i] = r < rank ? B[c * ld_b + r] : (T)0;
+    }
+    for (int64_t i = first; i < rest_bytes / 16; i += step) reinterpret_cast<uint4 *>(a_rest)[i] = make_uint4(0, 0, 0, 0);
+    for (int64_t i = first; i < rest; i += step) largest_rest[i] = 0;
+    if (first == 0) *scale_at = scale;
+}
+
+// The rows in the order of their adapters: each row's place is the number of rows that come before it, those with a lower adapter, or the same one and a lower
+// number. A lane has a row, 16 wavefronts share the rows it is compared with.
+constexpr int kMostRows = 8192;             // at a time: 13 bits beside the adapter's number, of which there are fewer than 2^18
+constexpr int kNone = -1, kUnknown = -2;    // who: rows without an adapter, and with one that does not exist
+constexpr int kOrderWaves = 16;
+__device__ __forceinline__ int code_of(int64_t adapter, int64_t count) { return adapter < 0 ? 0 : adapter < count ? (int)adapter + 1 : (int)count + 1; }
+__global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *adapters, int rows, int64_t count, int32_t *order, int32_t *who)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t keys[kMostRows];
+    __shared__ int part[kOrderWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane;
+    const int fours = (rows + 3) / 4;
+    for (int m = threadIdx.x; m < 4 * fours; m += 64 * kOrderWaves) keys[m] = m < rows ? (uint32_t)code_of(adapters[m], count) << 13 | (uint32_t)m : ~0u;
+    __syncthreads();
+    const uint32_t mine = row < rows ? keys[row] : 0;
+    int before = 0;
+    for (int f = wave; f < fours; f += kOrderWaves) {
+        const uint4 k = *reinterpret_cast<const uint4 *>(keys + 4 * f);
+        before += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+    }
+    part[wave][lane] = before;
+    __syncthreads();
+    if (wave != 0 || row >= rows) return;
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < kOrderWaves; ++w) before += part[w][lane];
+    const int code = (int)(mine >> 13);
+    order[before] = row;
+    who[before] = code == 0 ? kNone : code == (int)count + 1 ? kUnknown : code - 1;
+}
+
+// Inner products of 16 rows with 16 rows of their adapters' A. Slot s of a tile takes the adapters number s, s + slots, .. of those that its rows have.
+constexpr int kInnerWaves = 8;
+struct InnerJob {
+    const char *x, *a;                  // packed
+    int64_t pitch;
+    const uint32_t *largest_x, *largest_a;
+    const float *scale;
+    const int32_t *who;
+    float *inner;                       // [rows][ranks]
+    int rows, ranks, rank_blocks, slots, steps;
+};
+template <bool TWO>
+__global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
+{
+    __shared__ float part[kInnerWaves][4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+    int id = blockIdx.x;
+    const int slot = id % job.slots;
+    id /= job.slots;
+    const int block = id % job.rank_blocks, n = id / job.rank_blocks * 16 + col;
+    const int mine = n < job.rows ? job.who[n] : kNone;
+    const char *x = job.x + (int64_t)(n < job.rows ? n : job.rows - 1) * job.pitch + 16 * quarter;
+    uint32_t left = (uint32_t)(__ballot(mine >= 0) & 0xffff);
+    for (int number = 0; left != 0; ++number) {
+        const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+        const bool its = mine == adapter;
+        left &= ~(uint32_t)(__ballot(its) & 0xffff);
+        if (number % job.slots != slot) continue;
+        const int64_t row_a = (int64_t)adapter * job.ranks + 16 * block;
+        const char *a = job.a + (row_a + col) * job.pitch + 16 * quarter;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = wave; s < job.steps; s += kInnerWaves) {
+            const int64_t at = (int64_t)s * kStepBytes;
+            const halfx8 a0 = *reinterpret_cast<const halfx8 *>(a + at), a1 = *reinterpret_cast<const halfx8 *>(a + at + 64);
+            const halfx8 x0 = *reinterpret_cast<const halfx8 *>(x + at), x1 = *reinterpret_cast<const halfx8 *>(x + at + 64);
+            if (TWO) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, x0, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x1, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x0, acc, 0, 0, 0);
+            } else {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x0, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, x1, acc, 0, 0, 0);
+            }
+        }
+        __syncthreads();                // (what was read before has been)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][e][lane] = acc[e];
+        __syncthreads();
+        if (wave < 4 && its) {          // element `wave` of every lane
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kInnerWaves; ++w) sum += part[w][wave][lane];
+            const int r = 4 * quarter + wave;
+            job.inner[(int64_t)n * job.ranks + 16 * block + r] = ldexpf(sum, -shift_of(job.largest_x[n]) - shift_of(job.largest_a[row_a + r])) * job.scale[adapter];
+        }
+    }
+}
+
+// Sums over ranks of a block of 32 classes and 32 rows, added to the accumulators of the rows that have this adapter. v_mfma_f32_32x32x2_f32: lane l holds class
+// (row) l % 32 and rank l / 32 of two; four ranks a lane and load.
+struct Adapted {
+    const uint32_t *largest_w, *largest_x;
+    int64_t C;
+    int rows;                   // of this launch, in the order of their adapters
+    const int32_t *order, *who;
+    const float *inner;
+    const void *B;
+    int ranks, ranks_b;
+    bool bf16;
+    float *out;
+    int64_t ld;
+
+    __device__ __forceinline__ float4 four_of_b(int64_t row, int r) const
+    {
+        if (r >= ranks_b) return make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!bf16) return *reinterpret_cast<const float4 *>(static_cast<const float *>(B) + row * ranks_b + r);
+        const ushort4 v = *reinterpret_cast<const ushort4 *>(static_cast<const uint16_t *>(B) + row * ranks_b + r);
+        return make_float4(rows8::to_float(v.x), rows8::to_float(v.y), rows8::to_float(v.z), rows8::to_float(v.w));
+    }
+    template <typename T>
+    __device__ __forceinline__ void operator()(T &t) const
+    {
+        struct __attribute__((packed, aligned(4))) Float4u { float x, y, z, w; };
+        constexpr int CLASSES = T::ROWS + (T::HAS_EXTRA ? 32 : 0);
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        const int64_t c0 = t.tile_i * T::ROWS;
+        int *powers = reinterpret_cast<int *>(t.lds);
+        __syncthreads();
+        for (int i = threadIdx.x; i < CLASSES; i += blockDim.x) powers[i] = -shift_of(c0 + i < C ? largest_w[c0 + i] : 0);
+        __syncthreads();
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            if (first >= C) return;
+            const int64_t n = t.j0 + 32 * b + col;
+            const bool there = n < rows;
+            const int mine = there ? who[n] : kNone, shift = there ? shift_of(largest_x[n]) : 0;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = ldexpf(acc[e], powers[(int)(first - c0) + 8 * (e / 4) + 4 * half + e % 4] - shift);
+            const float *s = inner + (there ? n : rows - 1) * (int64_t)ranks + 4 * half;
+            const int64_t c = std::min(first + col, C - 1);
+            for (uint64_t left = __ballot(mine >= 0); left != 0;) {
+                const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+                const bool its = mine == adapter;
+                left &= ~__ballot(its);
+                floatx16 sum = {};
+                for (int r = 0; r < ranks_b; r += 8) {
+                    const float4 x = four_of_b((int64_t)adapter * C + c, r + 4 * half), y = *reinterpret_cast<const float4 *>(s + r);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, sum, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] += its ? sum[e] : 0.f;
+            }
+            if (!there) return;
+            float *row = out + (int64_t)order[n] * ld;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = first + 8 * q + 4 * half;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = mine == kUnknown ? NAN : acc[4 * q + e];
+                if (i + 3 < C) {
+                    *reinterpret_cast<Float4u *>(row + i) = {v[0], v[1], v[2], v[3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < C) row[i + e] = v[e];
+                }
+            }
+        });
+    }
+};
+
+struct Workspace {
+    size_t x, largest_x, order, who, inner, bytes;
+};
+Workspace workspace_of(const Layout &z, int64_t rows)
+{
+    Workspace w;
+    w.x = 0;
+    w.largest_x = w.x + up((size_t)rows * z.pitch);
+    w.order = w.largest_x + up((size_t)rows * 4);
+    w.who = w.order + up((size_t)rows * 4);
+    w.inner = w.who + up((size_t)rows * 4);
+    w.bytes = w.inner + up((size_t)rows * z.ranks * 4) + 256;
+    return w;
+}
+
+}  // namespace
+
+size_t adapters_layout_bytes(const rfsf_adapters_shape &s) { return layout_of(s).bytes; }
+
+void adapted_scores_bytes(const rfsf_adapters_shape &s, int64_t N, size_t *recommended, size_t *minimum)
+{
+    const Layout z = layout_of(s);
+    *recommended = workspace_of(z, std::min<int64_t>(std::max<int64_t>(N, 1), kMostRows)).bytes;
+    *minimum = workspace_of(z, 1).bytes;
+}
+
+hipError_t launch_adapters_weights(const rfsf_adapters_shape &s, const void *W, int64_t ld_w, void *layout, hipStream_t stream)
+{
+    const Layout z = layout_of(s);
+    char *to = static_cast<char *>(layout);
+    return pack(PackJob{W, s.C, s.K, ld_w, nullptr, reinterpret_cast<uint32_t *>(to + z.largest_w), to + z.w, nullptr, z.pitch, 0}, s.bf16 != 0, stream);
+}
+
+hipError_t launch_adapters_set(const rfsf_adapters_shape &s, int64_t index, const void *A, int64_t ld_a, const void *B, int64_t ld_b, float scale, void *layout,
+                               hipStream_t stream)
+{
+    const Layout z = layout_of(s);
+    char *to = static_cast<char *>(layout), *a = to + z.a + (size_t)index * z.ranks * z.pitch;
+    uint32_t *largest = reinterpret_cast<uint32_t *>(to + z.largest_a) + index * z.ranks;
+    RFSF_TRY(pack(PackJob{A, s.rank, s.K, ld_a, nullptr, largest, a, nullptr, z.pitch, 0}, s.bf16 != 0, stream));
+    const int rest = z.ranks - (int)s.rank;
+    const size_t at_b = (size_t)index * s.C * z.ranks_b;
+    const dim3 grid((unsigned)std::min<int64_t>(1024, (s.C * z.ranks_b + 255) / 256));
+    float *scale_at = reinterpret_cast<float *>(to + z.scale) + index;
+    auto launch = [&](auto *b, const auto *from) {
+        set_kernel<<<grid, 256, 0, stream>>>(from, ld_b, s.C, (int)s.rank, z.ranks_b, b + at_b, a + s.rank * z.pitch, rest * z.pitch, largest + s.rank, rest, scale_at, scale);
+    };
+    if (s.bf16) launch(reinterpret_cast<uint16_t *>(to + z.b), static_cast<const uint16_t *>(B));
+    else launch(reinterpret_cast<float *>(to + z.b), static_cast<const float *>(B));
+    return hipGetLastError();
+}
+
+hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layout, const void *X, int64_t N, int64_t ld_x, const int64_t *adapters, float *out,
+                                 int64_t ld_out, void *workspace, size_t bytes, hipStream_t stream)
+{
+    const Layout z = layout_of(s);
+    const char *lay = static_cast<const char *>(layout);
+    const bool bf16 = s.bf16 != 0;
+    int64_t most = std::min<int64_t>(N, kMostRows);
+    while (most > 1 && workspace_of(z, most).bytes > bytes) most = (most + 1) / 2;
+    const Workspace w = workspace_of(z, most);
+    const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
+    char *ws = static_cast<char *>(workspace) + (mis ? 256 - mis : 0);
+    uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + w.largest_x);
+    int32_t *order = reinterpret_cast<int32_t *>(ws + w.order), *who = reinterpret_cast<int32_t *>(ws + w.who);
+    float *inner = reinterpret_cast<float *>(ws + w.inner);
+    const uint32_t *largest_w = reinterpret_cast<const uint32_t *>(lay + z.largest_w), *largest_a = reinterpret_cast<const uint32_t *>(lay + z.largest_a);
+    const float *scale = reinterpret_cast<const float *>(lay + z.scale);
+    const int64_t steps = plane_steps(s.K, !bf16);
+    for (int64_t n0 = 0; n0 < N; n0 += most) {
+        const int64_t rows = std::min(N - n0, most);
+        order_kernel<<<dim3((unsigned)((rows + 63) / 64)), 64 * kOrderWaves, 0, stream>>>(adapters + n0, (int)rows, s.count, order, who);
+        RFSF_TRY(hipGetLastError());
+        RFSF_TRY(pack(PackJob{static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4), rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
+                      bf16, stream));
+        const int slots = (int)std::min<int64_t>(16, s.count), blocks = z.ranks / 16;
+        const InnerJob job = {ws + w.x, lay + z.a, z.pitch, largest_x, largest_a, scale, who, inner, (int)rows, z.ranks, blocks, slots, (int)steps};
+        const dim3 grid((unsigned)((rows + 15) / 16 * blocks * slots));
+        if (bf16) inner_kernel<false><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
+        else inner_kernel<true><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
+        RFSF_TRY(hipGetLastError());
+        const Adapted epilogue = {largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks, z.ranks_b, bf16, out + n0 * ld_out, ld_out};
+        const Planes w_rows = {lay + z.w, z.pitch, s.C}, x_rows = {ws + w.x, z.pitch, rows};
+        const int edge = plane_tile(s.C, rows);
+        RFSF_TRY(bf16 ? launch_plane_product<kHalf>(w_rows, x_rows, steps, edge, epilogue, stream)
+                      : launch_plane_product<kHalfTwo>(w_rows, x_rows, steps, edge, epilogue, stream));
+    }
+    return hipSuccess;
+}
+
+}  // namespace rfsf

@@ -50,6 +50,16 @@ int check(const rfsf_layer_norm_shape *s, const rfsf_dropout_mask *m, bool with_
     return m ? check(*m, s->N) : RFSF_OK;
 }
 
+constexpr int64_t kMostRank = 256, kMostAdapters = 131072;
+int check(const rfsf_adapters_shape *s)
+{
+    if (!s) return RFSF_E_NULLPTR;
+    if (s->K < 1 || s->C < 1 || s->rank < 1 || s->count < 1) return RFSF_E_BAD_SHAPE;
+    if (s->K > kMostColumns || s->C > kMostColumns || s->rank > kMostRank || s->count > kMostAdapters) return RFSF_E_UNSUPPORTED;
+    return RFSF_OK;
+}
+bool unaligned(const void *layout) { return reinterpret_cast<uintptr_t>(layout) % 256 != 0; }
+
 }  // namespace
 
 extern "C" int rfsf_softmax_xent_workspace_bytes(const rfsf_xent_shape *shape, size_t *recommended_bytes, size_t *minimum_bytes)
@@ -207,4 +217,64 @@ extern "C" int rfsf_layer_norm_backward(const rfsf_layer_norm_shape *shape, cons
     if (!X || !mean || !rstd || !dY || (dgain && !workspace)) return RFSF_E_NULLPTR;
     if (dgain && workspace_bytes < rfsf::layer_norm_backward_bytes(*shape, dX != nullptr)) return RFSF_E_WORKSPACE_TOO_SMALL;
     return rfsf::launch_layer_norm_backward(*shape, X, mean, rstd, gain, dY, mask, dX, dgain, doffset, workspace, stream) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_adapters_layout_bytes(const rfsf_adapters_shape *shape, size_t *bytes)
+{
+    const int rc = check(shape);
+    if (rc != RFSF_OK) return rc;
+    if (bytes) *bytes = rfsf::adapters_layout_bytes(*shape);
+    return RFSF_OK;
+}
+
+extern "C" int rfsf_adapters_set_weights(const rfsf_adapters_shape *shape, const void *W, int64_t ld_w, void *layout, void *hip_stream)
+{
+    const int rc = check(shape);
+    if (rc != RFSF_OK) return rc;
+    if (ld_w < shape->K) return RFSF_E_BAD_STRIDE;
+    if (!W || !layout) return RFSF_E_NULLPTR;
+    if (unaligned(layout)) return RFSF_E_BAD_STRIDE;
+    return rfsf::launch_adapters_weights(*shape, W, ld_w, layout, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_adapters_set(const rfsf_adapters_shape *shape, int64_t index, const void *A, int64_t ld_a, const void *B, int64_t ld_b, double scale, void *layout,
+                                 void *hip_stream)
+{
+    const int rc = check(shape);
+    if (rc != RFSF_OK) return rc;
+    if (index < 0 || index >= shape->count) return RFSF_E_BAD_SHAPE;
+    if (ld_a < shape->K || ld_b < shape->rank) return RFSF_E_BAD_STRIDE;
+    if (!std::isfinite((float)scale)) return RFSF_E_BAD_SETTING;
+    if (!A || !B || !layout) return RFSF_E_NULLPTR;
+    if (unaligned(layout)) return RFSF_E_BAD_STRIDE;
+    return rfsf::launch_adapters_set(*shape, index, A, ld_a, B, ld_b, (float)scale, layout, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RFSF_OK
+                                                                                                                                               : RFSF_E_HIP;
+}
+
+extern "C" int rfsf_adapted_scores_workspace_bytes(const rfsf_adapters_shape *shape, int64_t N, size_t *recommended_bytes, size_t *minimum_bytes)
+{
+    const int rc = check(shape);
+    if (rc != RFSF_OK) return rc;
+    if (N < 0) return RFSF_E_BAD_SHAPE;
+    if (N > kMostRows) return RFSF_E_UNSUPPORTED;
+    size_t recommended, minimum;
+    rfsf::adapted_scores_bytes(*shape, N, &recommended, &minimum);
+    if (recommended_bytes) *recommended_bytes = recommended;
+    if (minimum_bytes) *minimum_bytes = minimum;
+    return RFSF_OK;
+}
+
+extern "C" int rfsf_adapted_scores(const rfsf_adapters_shape *shape, const void *layout, const void *X, int64_t N, int64_t ld_x, const int64_t *adapters,
+                                   float *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    size_t minimum;
+    const int rc = rfsf_adapted_scores_workspace_bytes(shape, N, nullptr, &minimum);
+    if (rc != RFSF_OK) return rc;
+    if (ld_x < shape->K || ld_out < shape->C) return RFSF_E_BAD_STRIDE;
+    if (N == 0) return RFSF_OK;
+    if (!layout || !X || !adapters || !out || !workspace) return RFSF_E_NULLPTR;
+    if (unaligned(layout)) return RFSF_E_BAD_STRIDE;
+    if (workspace_bytes < minimum) return RFSF_E_WORKSPACE_TOO_SMALL;
+    return rfsf::launch_adapted_scores(*shape, layout, X, N, ld_x, adapters, out, ld_out, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? RFSF_OK : RFSF_E_HIP;
 }

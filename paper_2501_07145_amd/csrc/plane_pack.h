@@ -86,6 +86,7 @@ struct PackJob {
     uint32_t *largest;
     char *rows, *columns;
     int64_t pitch_rows, pitch_columns;
+    const int32_t *order = nullptr;     // the matrix' row that a packed row is (columns null); null: the same one
 };
 // Two matrices in a launch (the second one may have no rows). stats (may be null): launch_largest clears it, launch_pack brings it
 // up to the second matrix' rows, of these weights (null: all one).

@@ -27,6 +27,8 @@ __device__ __forceinline__ void load8(const T *row, int64_t k, int64_t K, float 
     }
 }
 
+__device__ __forceinline__ int64_t source_row(const PackJob &job, int64_t row) { return job.order ? job.order[row] : row; }
+
 // A wavefront takes a row, eight numbers of it a lane and load, two loads at a time.
 template <typename T>
 __global__ __launch_bounds__(64 * kRowsPerGroup) void largest_kernel(PackPair pair, unsigned groups_of_first)
@@ -39,7 +41,7 @@ __global__ __launch_bounds__(64 * kRowsPerGroup) void largest_kernel(PackPair pa
     if (row >= job.R) return;
     uint32_t largest = 0;
     if (!(job.labels && job.labels[row] < 0)) {
-        const T *src = static_cast<const T *>(job.src) + row * job.ld;
+        const T *src = static_cast<const T *>(job.src) + source_row(job, row) * job.ld;
         for (int64_t k = 8 * lane; k < job.K; k += 1024) {
             float x[2][8];
             load8(src, k, job.K, x[0]);
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackPair pair, unsigned tiles
         const bool there = row < job.R && !(job.labels && job.labels[row] < 0);
         shift[u] = there ? shift_of(job.largest[row]) : 0;
         if (there) {
-            load8(src + row * job.ld, c0 + 8 * group, job.K, x[u]);
+            load8(src + source_row(job, row) * job.ld, c0 + 8 * group, job.K, x[u]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(kRowThreads) void pack_rows_kernel(PackPair pair, u
     const int64_t row = ROWS == 1 ? group : group * ROWS + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / THREADS));
     if (ROWS > 1 && row >= job.R) return;
     const bool there = !(job.labels && job.labels[row] < 0);
-    const T *src = static_cast<const T *>(job.src) + row * job.ld;
+    const T *src = static_cast<const T *>(job.src) + source_row(job, row) * job.ld;
     float x[HELD][8];
     uint32_t largest = 0;
 #pragma unroll

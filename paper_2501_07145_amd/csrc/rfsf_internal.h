@@ -170,6 +170,15 @@ size_t layer_norm_backward_bytes(const rfsf_layer_norm_shape &shape, bool with_d
 hipError_t launch_layer_norm_backward(const rfsf_layer_norm_shape &shape, const void *X, const float *mean, const float *rstd, const float *gain, const void *dY,
                                       const rfsf_dropout_mask *mask, void *dX, float *dgain, float *doffset, void *workspace, hipStream_t stream);
 
+// Class scores with low-rank adapters (csrc/adapters.hip).
+size_t adapters_layout_bytes(const rfsf_adapters_shape &shape);
+void adapted_scores_bytes(const rfsf_adapters_shape &shape, int64_t N, size_t *recommended, size_t *minimum);
+hipError_t launch_adapters_weights(const rfsf_adapters_shape &shape, const void *W, int64_t ld_w, void *layout, hipStream_t stream);
+hipError_t launch_adapters_set(const rfsf_adapters_shape &shape, int64_t index, const void *A, int64_t ld_a, const void *B, int64_t ld_b, float scale, void *layout,
+                               hipStream_t stream);
+hipError_t launch_adapted_scores(const rfsf_adapters_shape &shape, const void *layout, const void *X, int64_t N, int64_t ld_x, const int64_t *adapters, float *out,
+                                 int64_t ld_out, void *workspace, size_t bytes, hipStream_t stream);
+
 // Benchmark helper (csrc/probe.hip): read, write, non-temporal write, copy GB/s over `scratch`, fp32 matrix and
 // fp32 vector TFLOP/s of issue loops, in this order; waits for the stream.
 hipError_t probe_peaks(void *scratch, size_t bytes, double out[6], hipStream_t stream);

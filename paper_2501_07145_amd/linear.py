@@ -1,5 +1,6 @@
 """Binding of the operators of linear models on feature rows: softmax cross entropy with its gradients, the AdamW
-step, the Gram against rows held in 8-bit integers, layer norm and dropout (include/rfsf_ts.h). Argument marshalling only, as in binding.py."""
+step, the Gram against rows held in 8-bit integers, layer norm, dropout and low-rank
+adapters (include/rfsf_ts.h). Argument marshalling only, as in binding.py."""
 from __future__ import annotations
 
 import ctypes
@@ -40,6 +41,10 @@ class _DropoutMask(ctypes.Structure):
 class _LayerNormShape(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_dx", ctypes.c_int64),
                 ("bf16", ctypes.c_int32)]
+
+
+class _AdaptersShape(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int64), ("C", ctypes.c_int64), ("rank", ctypes.c_int64), ("count", ctypes.c_int64), ("bf16", ctypes.c_int32)]
 
 
 def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
@@ -389,3 +394,69 @@ def rfsf_layer_norm_backward(X: torch.Tensor, mean: torch.Tensor, rstd: torch.Te
                                         _vector(doffset, K, "doffset"), workspace.data_ptr() if need_gains else None,
                                         workspace.numel() if need_gains else 0, _stream_ptr(stream)))
     return dX, dgain, doffset
+
+
+class RfsfAdapters:
+    """Scores of a linear classifier that many users share, with a low-rank adapter for each request.
+
+    W [C, K] (float32 or bfloat16) is laid out once for the kernels, and so are up to `count` adapters of `rank`: `set` puts one into a place, in which
+    it stays until the next `set` there. Neither W nor the adapters' tensors are looked at afterwards: after W was
+    changed, `set_weights` takes the new one. Places that were never set add nothing."""
+
+    def __init__(self, W: torch.Tensor, count: int, rank: int, stream: Optional[torch.cuda.Stream] = None):
+        _matrix(W, "W")
+        self.C, self.K = W.shape
+        self.count, self.rank, self.dtype, self.device = count, rank, W.dtype, W.device
+        self._shape = _AdaptersShape(self.K, self.C, rank, count, _BF16[W.dtype])
+        self._shape_at = ctypes.addressof(self._shape)
+        size = ctypes.c_size_t(0)
+        _check(load_library().rfsf_adapters_layout_bytes(self._shape_at, ctypes.byref(size)))
+        _here(W)
+        if stream is None:
+            self.layout = torch.zeros(int(size.value), dtype=torch.uint8, device=W.device)
+        else:
+            with torch.cuda.stream(stream):
+                self.layout = torch.zeros(int(size.value), dtype=torch.uint8, device=W.device)
+        self._layout_at = self.layout.data_ptr()
+        self.set_weights(W, stream)
+
+    def set_weights(self, W: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Takes W [C, K], of the type and shape of the first one, for the calls that follow on the stream."""
+        ld = _matrix(W, "W", self.dtype, (self.C, self.K))
+        _here(W, self.layout)
+        _check(load_library().rfsf_adapters_set_weights(self._shape_at, W.data_ptr(), ld, self._layout_at, _stream_ptr(stream)))
+
+    def set(self, index: int, A: torch.Tensor, B: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Puts the adapter scale * B A (A [rank, K], B [C, rank], of W's type) into place `index` for the calls that follow on the stream."""
+        if not 0 <= index < self.count:
+            raise ValueError("index must be that of one of the adapters' places")
+        ld_a, ld_b = _matrix(A, "A", self.dtype, (self.rank, self.K)), _matrix(B, "B", self.dtype, (self.C, self.rank))
+        _here(A, B, self.layout)
+        _check(load_library().rfsf_adapters_set(self._shape_at, index, A.data_ptr(), ld_a, B.data_ptr(), ld_b, scale, self._layout_at,
+                                                _stream_ptr(stream)))
+
+    def workspace_bytes(self, N: int):
+        """(recommended_bytes, minimum_bytes) of scratch for scores of N rows."""
+        rec, mn = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        _check(load_library().rfsf_adapted_scores_workspace_bytes(self._shape_at, N, ctypes.byref(rec), ctypes.byref(mn)))
+        return int(rec.value), int(mn.value)
+
+    def scores(self, X: torch.Tensor, adapters: torch.Tensor, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """out [N, C] float32: the scores of X [N, K] (W's type), row n with the adapter in place adapters[n] (int64 [N]; negative: none)."""
+        ld = _matrix(X, "X", self.dtype)
+        N, K = X.shape
+        if K != self.K:
+            raise ValueError("X and W need the same number of columns")
+        if _dev(adapters, torch.int64, "adapters").shape != (N,):
+            raise ValueError("adapters must have shape [N]")
+        if out is None:
+            out = _empty_on(stream, (N, self.C), dtype=torch.float32, device=X.device)
+        ld_out = _matrix(out, "out", torch.float32, (N, self.C))
+        if workspace is None:
+            workspace = _empty_on(stream, self.workspace_bytes(N)[0], dtype=torch.uint8, device=X.device)
+        _dev(workspace, torch.uint8, "workspace")
+        _here(X, adapters, out, workspace, self.layout)
+        _check(load_library().rfsf_adapted_scores(self._shape_at, self._layout_at, X.data_ptr(), N, ld, adapters.data_ptr(), out.data_ptr(), ld_out,
+                                                  workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+        return out

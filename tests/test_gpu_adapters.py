@@ -1,0 +1,203 @@
+"""Scores with low-rank adapters against the formula in 64 bits, within bounds that follow from the arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2501_07145_amd as rfsf
+from tests import adapters_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16}
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _place(x, ld, shift=0):
+    N, K = x.shape
+    buf = torch.full((shift + N * ld + 8,), -7.0, dtype=x.dtype, device="cuda")
+    view = buf[shift:shift + N * ld].view(N, ld)[:, :K]
+    view.copy_(x)
+    return view
+
+
+def _problem(N, K, C, rank, count, dtype, seed=0, spread=0.0):
+    gen = torch.Generator().manual_seed(seed * 1000003 + N * 31 + K * 7 + C)
+
+    def normal(*shape):
+        t = torch.randn(*shape, generator=gen, dtype=torch.float64)
+        return (t * 10 ** (spread * torch.randn(*shape[:-1], 1, generator=gen, dtype=torch.float64))).to(dtype)
+
+    X, W, A, B = normal(N, K), normal(C, K), normal(count, rank, K), normal(count, C, rank)
+    scale = (0.5 + torch.rand(count, generator=gen)).tolist()
+    adapters = torch.randint(-1, count, (N,), generator=gen)
+    return X, W, A, B, scale, adapters
+
+
+def _handle(W, A, B, scale, pad=0):
+    count, rank = A.shape[:2]
+    h = rfsf.RfsfAdapters(_place(W, W.shape[1] + pad), count, rank)
+    for e in range(count):
+        h.set(e, _place(A[e], A.shape[2] + pad, shift=pad), _place(B[e], rank + pad, shift=pad), scale[e])
+    return h
+
+
+def _check(got, X, W, A, B, scale, adapters, bf16):
+    X, W, A, B, scale, adapters = _np(X), _np(W), _np(A), _np(B), np.float32(scale).astype(np.float64), adapters.cpu().numpy()
+    want, tol = ref.scores(X, W, A, B, scale, adapters), ref.bounds(X, W, A, B, scale, adapters, bf16)
+    got = _np(got)
+    known = adapters < len(A)
+    excess = (np.abs(got - want) - tol)[known]
+    assert excess.size == 0 or np.all(excess <= 0), float(excess.max())
+    assert np.isnan(got[~known]).all()
+
+
+CASES = [
+    # N, K, C, rank, count
+    (1, 1, 1, 1, 1), (1, 9, 5, 3, 2), (1, 1025, 1000, 8, 20), (2, 64, 33, 4, 3), (3, 65, 10, 1, 7), (5, 300, 31, 17, 4), (15, 129, 257, 16, 50), (16, 1025, 77, 5, 16), (17, 193, 64, 20, 3),
+    (33, 100, 100, 33, 40), (64, 513, 300, 8, 64), (65, 257, 130, 12, 5), (130, 333, 65, 64, 9), (300, 129, 515, 16, 100), (333, 1025, 280, 7, 1), (1000, 65, 129, 6, 300), (40, 31, 7, 256, 2),
+    (12, 13001, 40, 9, 5), (600, 40, 600, 100, 11), (20, 5121, 10, 16, 20), (48, 2049, 3, 24, 2), (7, 700, 5000, 16, 7), (1, 300, 17000, 4, 2),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,C,rank,count", CASES)
+def test_scores(dtype, N, K, C, rank, count):
+    X, W, A, B, scale, adapters = _problem(N, K, C, rank, count, TYPES[dtype])
+    for pad, ld_out in ((0, C), (3, C + 5)):
+        h = _handle(W, A, B, scale, pad)
+        out = _place(torch.zeros(N, C), ld_out)
+        assert h.scores(_place(X, K + pad, shift=pad), adapters.cuda(), out=out) is out
+        _check(out, X, W, A, B, scale, adapters, dtype == "bfloat16")
+        assert torch.all(out._base[:N * ld_out].view(N, ld_out)[:, C:] == -7.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,C,rank,count", [(14, 700, 90, 16, 5), (200, 300, 140, 24, 9)])
+def test_rows_of_all_sizes(dtype, N, K, C, rank, count):
+    X, W, A, B, scale, adapters = _problem(N, K, C, rank, count, TYPES[dtype], seed=1, spread=3.0)
+    _check(_handle(W, A, B, scale).scores(X.cuda(), adapters.cuda()), X, W, A, B, scale, adapters, dtype == "bfloat16")
+
+
+@pytest.mark.parametrize("N", [1, 9, 16, 40, 100, 400])
+def test_adapters_that_no_one_has_everyone_has_or_that_do_not_exist(N):
+    X, W, A, B, scale, _ = _problem(N, 130, 70, 8, 6, torch.float32, seed=2)
+    h = _handle(W, A, B, scale)
+    far = torch.arange(N)
+    for adapters in (torch.full((N,), -1), torch.full((N,), -(1 << 62)), torch.full((N,), 5), torch.full((N,), 6), far % 6, 5 - far % 7,
+                     torch.where(far % 3 == 0, torch.full((N,), (1 << 62) + 1), far % 8 - 1), torch.where(far % 3 == 0, torch.full((N,), 1 << 32), far % 6)):
+        _check(h.scores(X.cuda(), adapters.cuda()), X, W, A, B, scale, adapters, False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,C", [(12, 300, 70), (60, 300, 70), (150, 300, 200)])
+def test_infinities_and_nan_stay_where_they_belong(dtype, N, K, C):
+    X, W, A, B, scale, adapters = _problem(N, K, C, 10, 5, TYPES[dtype], seed=3)
+    adapters[:6] = torch.tensor([0, 1, 2, 3, 4, -1])
+    clean = _handle(W, A, B, scale).scores(X.cuda(), adapters.cuda())
+    A, B, W, X = A.clone(), B.clone(), W.clone(), X.clone()
+    A[1, 3, 7], B[2, 5, 2], B[3, :, :] = float("nan"), float("nan"), float("inf")
+    W[C - 2, 11], X[5, 2] = float("nan"), float("nan")
+    got = _handle(W, A, B, scale).scores(X.cuda(), adapters.cuda())
+    for n in range(N):
+        a = int(adapters[n])
+        bad = torch.zeros(C, dtype=torch.bool, device="cuda")
+        bad[C - 2] = True
+        bad |= n == 5 or a == 1
+        if a == 2:
+            bad[5] = True
+        if a == 3:
+            assert not got[n].isfinite().any()
+            continue
+        assert torch.equal(got[n].isnan(), bad), n
+        assert torch.equal(got[n][~bad], clean[n][~bad]), n
+
+
+def test_places_that_were_never_set_and_that_are_set_again():
+    X, W, A, B, scale, adapters = _problem(50, 200, 60, 5, 4, torch.float32, seed=4)
+    h = rfsf.RfsfAdapters(W.cuda(), 4, 5)
+    plain = h.scores(X.cuda(), torch.full((50,), -1).cuda())
+    assert torch.equal(h.scores(X.cuda(), adapters.cuda()), plain)
+    for e in (1, 3):
+        h.set(e, A[e].cuda(), B[e].cuda(), scale[e])
+    _check(h.scores(X.cuda(), torch.where(adapters % 2 == 1, adapters, -1).cuda()), X, W, A, B, scale, torch.where(adapters % 2 == 1, adapters, -1), False)
+    h.set(1, A[0].cuda(), B[0].cuda(), scale[0])
+    assert torch.equal(h.scores(X.cuda(), torch.ones(50, dtype=torch.int64).cuda()), _handle(W, A, B, scale).scores(X.cuda(), torch.zeros(50, dtype=torch.int64).cuda()))
+    h.set_weights(2 * W.cuda())
+    _check(h.scores(X.cuda(), torch.full((50,), -1).cuda()), X, 2 * W, A, B, scale, torch.full((50,), -1), False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_small_and_unaligned_workspaces_and_many_rows(dtype):
+    N, K, C, rank, count = 9000, 33, 20, 4, 50
+    X, W, A, B, scale, adapters = _problem(N, K, C, rank, count, TYPES[dtype], seed=5)
+    h = _handle(W, A, B, scale)
+    rec, least = h.workspace_bytes(N)
+    X, adapters = X.cuda(), adapters.cuda()
+    _check(h.scores(X, adapters), X, W, A, B, scale, adapters, dtype == "bfloat16")
+    for size in (least, least * 7, rec // 2):
+        space = torch.empty(size + 9, dtype=torch.uint8, device="cuda")[9:]
+        _check(h.scores(X[:400], adapters[:400], workspace=space), X[:400], W, A, B, scale, adapters[:400], dtype == "bfloat16")
+
+
+def test_equal_calls_give_equal_bits_on_other_streams_and_in_graphs():
+    N, K, C, rank, count = 100, 500, 300, 16, 8
+    X, W, A, B, scale, adapters = _problem(N, K, C, rank, count, torch.bfloat16, seed=6)
+    h, X, adapters = _handle(W, A, B, scale), X.cuda(), adapters.cuda()
+    want = h.scores(X, adapters)
+    other = h.scores(X, (adapters + 2) % count)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = h.scores(X, adapters, stream=stream)
+    stream.synchronize()
+    assert torch.equal(got, want)
+    space, out = torch.empty(h.workspace_bytes(N)[0], dtype=torch.uint8, device="cuda"), torch.empty(N, C, device="cuda")
+    changing = adapters.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        h.scores(X, changing, out=out, workspace=space)
+    for turn in range(4):
+        changing.copy_((adapters + 2) % count if turn % 2 else adapters)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, other if turn % 2 else want)
+        h.scores(X[:7], adapters[:7], workspace=space)                # the same workspace, between the replays
+
+
+def test_no_rows():
+    X, W, A, B, scale, adapters = _problem(1, 9, 5, 2, 2, torch.float32)
+    h = _handle(W, A, B, scale)
+    assert h.scores(X[:0].cuda(), adapters[:0].cuda()).shape == (0, 5)
+
+
+def test_results_beyond_two_to_the_31_numbers():
+    N, K, C, rank, count = 60000, 16, 40000, 4, 7
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    X, W, A, B = (torch.randn(*s, generator=gen, device="cuda").bfloat16() for s in ((N, K), (C, K), (count, rank, K), (count, C, rank)))
+    adapters = torch.randint(-1, count, (N,), generator=gen, device="cuda")
+    h = rfsf.RfsfAdapters(W, count, rank)
+    for e in range(count):
+        h.set(e, A[e], B[e], 0.5)
+    out = h.scores(X, adapters)
+    at = torch.tensor([0, 8191, 8192, 53687, 53688, N - 1], device="cuda")
+    _check(out[at], X[at], W, A, B, [0.5] * count, adapters[at], True)
+
+
+def test_binding_refuses_what_does_not_fit():
+    X, W, A, B, scale, adapters = (t.cuda() if torch.is_tensor(t) else t for t in _problem(4, 9, 5, 2, 2, torch.float32))
+    h = rfsf.RfsfAdapters(W, 2, 2)
+    for args in ((2, A[0], B[0]), (-1, A[0], B[0]), (0, A[0, :1], B[0]), (0, A[0], B[0, :, :1]), (0, A[0].bfloat16(), B[0]), (0, A[0].cpu(), B[0])):
+        with pytest.raises(ValueError):
+            h.set(*args)
+    for args, kw in (((X.bfloat16(), adapters), {}), ((X[:, :8], adapters), {}), ((X, adapters[:3]), {}), ((X, adapters.int()), {}), ((X, adapters), dict(out=X)),
+                     ((X, adapters), dict(out=torch.zeros(4, 5, dtype=torch.bfloat16, device="cuda"))), ((X, adapters), dict(workspace=X))):
+        with pytest.raises(ValueError):
+            h.scores(*args, **kw)
+    with pytest.raises(rfsf.RfsfTsError):
+        h.scores(X, adapters, workspace=torch.empty(1, dtype=torch.uint8, device="cuda"))
+    for W_ in (W[:4], W.bfloat16()):
+        with pytest.raises(ValueError):
+            h.set_weights(W_)
