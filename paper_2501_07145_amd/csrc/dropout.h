@@ -55,16 +55,26 @@ __device__ __forceinline__ void numbers(const DropoutJob &job, uint64_t offset, 
     word[2] = c2;
     word[3] = c3;
 }
+__device__ __forceinline__ bool kept(const DropoutJob &job, const uint32_t (&word)[4], int e)
+{
+    return (e & 1 ? word[e / 2] >> 16 : word[e / 2] & 0xffffu) >= job.threshold;
+}
 // Eight numbers of a row: those that are kept times the factor, 0 (also of infinities and NaN) for the others.
 __device__ __forceinline__ void apply(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, float (&x)[8])
 {
     uint32_t word[4];
     numbers(job, offset, row, group, word);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t u = e & 1 ? word[e / 2] >> 16 : word[e / 2] & 0xffffu;
-        x[e] = u >= job.threshold ? x[e] * job.factor : 0.f;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = kept(job, word, e) ? x[e] * job.factor : 0.f;
+}
+
+// The same without the factor, for sums that it can multiply afterwards.
+__device__ __forceinline__ void choose(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, float (&x)[8])
+{
+    uint32_t word[4];
+    numbers(job, offset, row, group, word);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = kept(job, word, e) ? x[e] : 0.f;
 }
 
 }  // namespace dropout

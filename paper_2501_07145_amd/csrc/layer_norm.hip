@@ -12,7 +12,8 @@
 namespace rfsf {
 namespace {
 
-constexpr int64_t kMostHeld = 512 * 5 * 8;      // columns of rows that stay in registers
+constexpr int64_t kMostHeld = 512 * 5 * 8, kLeastHeld = 8;      // columns of rows that stay in registers
+constexpr bool is_held(int64_t K) { return K >= kLeastHeld && K <= kMostHeld; }
 constexpr int kCus = 256;
 
 struct NormJob {
@@ -34,40 +35,28 @@ struct BackJob {
     DropoutJob dropout;
 };
 
-// Sums of two numbers over the THREADS lanes of a row. `part`: LDS of rows of more than a wavefront, not used again before the next barrier.
-template <int THREADS>
-__device__ __forceinline__ void add_up(float &a, float &b, float2 *part)
+// Sums of numbers over the THREADS lanes of a row. `part`: LDS of rows of more than a wavefront, not used again before the next barrier.
+template <int THREADS, typename S, int COUNT>
+__device__ __forceinline__ void add_up(S (&v)[COUNT], S (*part)[COUNT])
 {
 #pragma unroll
-    for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o /= 2) {
-        a += __shfl_xor(a, o);
-        b += __shfl_xor(b, o);
-    }
-    if constexpr (THREADS > 64) {
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
-        __syncthreads();
-        a = b = 0.f;
+    for (int o = (THREADS < 64 ? THREADS : 64) / 2; o > 0; o /= 2)
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) {
-            a += part[w].x;
-            b += part[w].y;
+        for (int i = 0; i < COUNT; ++i) v[i] += __shfl_xor(v[i], o);
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) part[threadIdx.x >> 6][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            v[i] = part[0][i];
+#pragma unroll
+            for (int w = 1; w < THREADS / 64; ++w) v[i] += part[w][i];
         }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ rows8::Eight<T> load_raw(const T *row, int64_t k, int64_t K)
-{
-    rows8::Eight<T> c = {};
-    if (k + 8 <= K) {
-        c = *reinterpret_cast<const rows8::Eight<T> *>(row + k);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < K) c.v[e] = row[k + e];
-    }
-    return c;
-}
 __device__ __forceinline__ void load_or(const float *p, int64_t k, int64_t K, float otherwise, float (&x)[8])
 {
     if (p) {
@@ -78,25 +67,42 @@ __device__ __forceinline__ void load_or(const float *p, int64_t k, int64_t K, fl
     }
 }
 
-// The mean of a row from what was subtracted from its numbers first, and the rest's sums.
-struct Moments { float shift, rest, rstd; };
-__device__ __forceinline__ Moments moments(float shift, float sum, float squares, float inverse, float eps)
+// Rows are added up in 64 bits, eight numbers of bfloat16 first in 32 (exact as long as they lie within 2^13 of each other), so that the mean is rounded once; what that
+// leaves over is known, and taken off the differences to it, and its square off their mean square. Rows far from zero lose nothing.
+__device__ __forceinline__ double sum_of(const rows8::Eight<uint16_t> &c)
 {
-    const float rest = sum * inverse;
-    return {shift, rest, 1.0f / sqrtf(fmaxf(squares * inverse - rest * rest, 0.f) + eps)};
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = rows8::to_float(c.v[e]);
+    return (double)(((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])));
+}
+__device__ __forceinline__ double sum_of(const rows8::Eight<float> &c)
+{
+    return (((double)c.v[0] + (double)c.v[1]) + ((double)c.v[2] + (double)c.v[3])) + (((double)c.v[4] + (double)c.v[5]) + ((double)c.v[6] + (double)c.v[7]));
+}
+struct Mean { float mean, rest; };
+__device__ __forceinline__ Mean mean_of(double sum, double inverse)
+{
+    const double mean = sum * inverse;
+    const float rounded = (float)mean;
+    return {rounded, (float)(mean - (double)rounded)};
+}
+__device__ __forceinline__ float rstd_of(float squares, float rest, float inverse, float eps)
+{
+    return 1.0f / sqrtf(fmaxf(squares * inverse - rest * rest, 0.f) + eps);
 }
 
 // THREADS lanes hold a row, HELD times eight numbers each; a workgroup goes through rows, whose next one is loaded while the present one is worked on, and
-// keeps its columns' gains and offsets. The mean is subtracted before squares are added up, and what rounding left of it
-// is taken off both afterwards, so that rows far from zero lose nothing.
+// keeps its columns' gains and offsets.
 template <typename T, int THREADS, int HELD, bool DROP>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(NormJob job)
 {
     constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1;
-    __shared__ float2 part[2][WAVES];
-    const int lane = threadIdx.x % THREADS;
-    const int64_t K = job.K, step = (int64_t)gridDim.x * ROWS;
-    const float inverse = 1.0f / (float)K;
+    __shared__ double part_sum[WAVES][1];
+    __shared__ float part_squares[WAVES][1];
+    const int lane = threadIdx.x % THREADS, K = (int)job.K;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const double inverse = 1.0 / (double)K;
     float gain[HELD][8], shift[HELD][8];
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {
@@ -107,86 +113,96 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
     const T *X = static_cast<const T *>(job.X);
     T *Y = static_cast<T *>(job.Y);
     int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
-    rows8::Eight<T> next[HELD];
+    rows8::Eight<T> next[HELD], now[HELD];
 #pragma unroll
-    for (int u = 0; u < HELD; ++u) next[u] = load_raw(X + std::min(row, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
+    for (int u = 0; u < HELD; ++u) next[u] = rows8::load_raw(X + std::min(row, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
     // (all rows of a workgroup take as many turns, so that everybody meets at the barriers)
     for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
-        float x[HELD][8];
-        float sum = 0.f, squares = 0.f;
+        double sum[1] = {0.0};
 #pragma unroll
-        for (int u = 0; u < HELD; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[u][e] = rows8::to_float(next[u].v[e]);
-                sum += x[u][e];
-            }
+        for (int u = 0; u < HELD; ++u) {
+            now[u] = next[u];
+            sum[0] += sum_of(now[u]);
+        }
         if (turn + step < job.N) {
 #pragma unroll
-            for (int u = 0; u < HELD; ++u) next[u] = load_raw(X + std::min(row + step, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
+            for (int u = 0; u < HELD; ++u) next[u] = rows8::load_raw(X + std::min(row + step, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
         }
-        add_up<THREADS>(sum, squares, part[0]);
-        const float mean = sum * inverse;
-        sum = squares = 0.f;
+        add_up<THREADS>(sum, part_sum);
+        const Mean m = mean_of(sum[0], inverse);
+        float squares[1] = {0.f};
 #pragma unroll
-        for (int u = 0; u < HELD; ++u)
+        for (int u = 0; u < HELD; ++u) {
+            const int k = 8 * (lane + u * THREADS);
+            if (k + 8 <= K) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[u][e] = 8 * (lane + u * THREADS) + e < K ? x[u][e] - mean : 0.f;
-                sum += x[u][e];
-                squares = fmaf(x[u][e], x[u][e], squares);
+                for (int e = 0; e < 8; ++e) {
+                    const float d = rows8::to_float(now[u].v[e]) - m.mean;
+                    squares[0] = fmaf(d, d, squares[0]);
+                }
+            } else if (k < K) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float d = k + e < K ? rows8::to_float(now[u].v[e]) - m.mean : 0.f;
+                    squares[0] = fmaf(d, d, squares[0]);
+                }
             }
-        add_up<THREADS>(sum, squares, part[1]);
-        const Moments m = moments(mean, sum, squares, inverse, job.eps);
+        }
+        add_up<THREADS>(squares, part_squares);
+        const float rstd = rstd_of(squares[0], m.rest, (float)inverse, job.eps);
         if (row >= job.N) continue;
         if (lane == 0) {
-            if (job.mean) job.mean[row] = m.shift + m.rest;
-            if (job.rstd) job.rstd[row] = m.rstd;
+            if (job.mean) job.mean[row] = m.mean;
+            if (job.rstd) job.rstd[row] = rstd;
         }
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            const int64_t k = 8 * (lane + u * THREADS);
+            const int k = 8 * (lane + u * THREADS);
             if (k >= K) continue;
+            float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[u][e] = fmaf((x[u][e] - m.rest) * m.rstd, gain[u][e], shift[u][e]);
-            if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), x[u]);
-            rows8::store(Y + row * job.ldy, k, K, x[u]);
+            for (int e = 0; e < 8; ++e) y[e] = fmaf((rows8::to_float(now[u].v[e]) - m.mean - m.rest) * rstd, gain[u][e], shift[u][e]);
+            if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)k / 8, y);
+            rows8::store(Y + row * job.ldy, k, K, y);
         }
     }
 }
 
-// Longer rows: a workgroup reads a row three times, of which the caches give the last two.
+// Rows of any length: a workgroup reads a row three times, of which the caches give the last two.
 constexpr int kLongThreads = 1024;
 template <typename T>
 __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bool drop)
 {
-    __shared__ float2 part[2][kLongThreads / 64];
+    __shared__ double part_sum[kLongThreads / 64][1];
+    __shared__ float part_squares[kLongThreads / 64][1];
     const int64_t K = job.K, row = blockIdx.x;
-    const float inverse = 1.0f / (float)K;
+    const double inverse = 1.0 / (double)K;
     const T *x_row = static_cast<const T *>(job.X) + row * job.ldx;
-    float sum = 0.f, squares = 0.f, x[8];
+    float x[8];
+    double sum[1] = {0.0};
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
         rows8::load(x_row, k, K, x);
+        double s = 0.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += x[e];
+        for (int e = 0; e < 8; ++e) s += (double)x[e];
+        sum[0] += s;
     }
-    add_up<kLongThreads>(sum, squares, part[0]);
-    const float mean = sum * inverse;
-    sum = squares = 0.f;
+    add_up<kLongThreads>(sum, part_sum);
+    const Mean m = mean_of(sum[0], inverse);
+    float squares[1] = {0.f};
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
         rows8::load(x_row, k, K, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            x[e] = k + e < K ? x[e] - mean : 0.f;
-            sum += x[e];
-            squares = fmaf(x[e], x[e], squares);
+            const float d = k + e < K ? x[e] - m.mean : 0.f;
+            squares[0] = fmaf(d, d, squares[0]);
         }
     }
-    add_up<kLongThreads>(sum, squares, part[1]);
-    const Moments m = moments(mean, sum, squares, inverse, job.eps);
+    add_up<kLongThreads>(squares, part_squares);
+    const float rstd = rstd_of(squares[0], m.rest, (float)inverse, job.eps);
     if (threadIdx.x == 0) {
-        if (job.mean) job.mean[row] = m.shift + m.rest;
-        if (job.rstd) job.rstd[row] = m.rstd;
+        if (job.mean) job.mean[row] = m.mean;
+        if (job.rstd) job.rstd[row] = rstd;
     }
     const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
@@ -195,22 +211,24 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bo
         load_or(job.gain, k, K, 1.f, gain);
         load_or(job.offset, k, K, 0.f, shift);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf((x[e] - mean - m.rest) * m.rstd, gain[e], shift[e]);
+        for (int e = 0; e < 8; ++e) x[e] = fmaf((x[e] - m.mean - m.rest) * rstd, gain[e], shift[e]);
         if (drop) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), x);
         rows8::store(static_cast<T *>(job.Y) + row * job.ldy, k, K, x);
     }
 }
 
-// The backward pass of rows that are held in registers as above. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose sums
-// are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
+// The backward pass of rows that are held in registers as above. Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds
+// its columns' h z and h up over the rows of the workgroup, whose sums are then one of the parts that add_parts_kernel adds up: no atomics, so that
+// equal calls give equal bits.
 template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(BackJob job)
 {
     constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1;
-    __shared__ float2 part[2][WAVES];
-    const int lane = threadIdx.x % THREADS;
-    const int64_t K = job.K, step = (int64_t)gridDim.x * ROWS;
-    const float inverse = 1.0f / (float)K;
+    constexpr bool AHEAD = HELD <= 3;            // registers for the next row
+    __shared__ float part[2][WAVES][2];
+    const int lane = threadIdx.x % THREADS, K = (int)job.K;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const float inverse = 1.0f / (float)K, factor = DROP ? job.dropout.factor : 1.f;
     float gain[HELD][8], of_gain[HELD][8], of_offset[HELD][8];
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {
@@ -222,61 +240,72 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(Bac
     const T *X = static_cast<const T *>(job.X), *dY = static_cast<const T *>(job.dY);
     T *dX = static_cast<T *>(job.dX);
     int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
-    rows8::Eight<T> next_x[HELD], next_h[HELD];
-    float next_mean, next_rstd;
+    rows8::Eight<T> x[HELD], next_x[HELD], next_h[HELD];
+    float mean, rstd, next_mean, next_rstd;
     auto load = [&](int64_t r) {
-        r = std::min(r, job.N - 1);
+        const bool there = r < job.N;
+        r = there ? r : job.N - 1;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            next_x[u] = load_raw(X + r * job.ldx, 8 * (lane + u * THREADS), K);
-            next_h[u] = load_raw(dY + r * job.ldy, 8 * (lane + u * THREADS), K);
+            next_x[u] = rows8::load_raw(X + r * job.ldx, 8 * (lane + u * THREADS), K);
+            next_h[u] = rows8::load_raw(dY + r * job.ldy, 8 * (lane + u * THREADS), K);
         }
         next_mean = job.mean[r];
         next_rstd = job.rstd[r];
     };
-    load(row);
+    if (AHEAD) load(row);
     int which = 0;
     for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
-        const float mean = next_mean, rstd = next_rstd;
+        if (!AHEAD) load(row);
         const bool there = row < job.N;
-        float z[HELD][8], g[HELD][8];
+        float h[HELD][8];
+        mean = next_mean;
+        rstd = next_rstd;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            const int64_t k = 8 * (lane + u * THREADS);
+            x[u] = next_x[u];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[u][e] = (rows8::to_float(next_x[u].v[e]) - mean) * rstd;
-                g[u][e] = rows8::to_float(next_h[u].v[e]);
-            }
-            if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)(k / 8), g[u]);
+            for (int e = 0; e < 8; ++e) h[u][e] = there ? rows8::to_float(next_h[u].v[e]) : 0.f;
         }
-        if (turn + step < job.N) load(row + step);
-        float sum = 0.f, products = 0.f;
-#pragma unroll
-        for (int u = 0; u < HELD; ++u)
+        if (AHEAD && turn + step < job.N) load(row + step);
+        float sums[2] = {0.f, 0.f};             // of g, of g z
+        auto add = [&](int u, auto whole) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool counts = there && 8 * (lane + u * THREADS) + e < K;
+                const bool counts = there && (whole || 8 * (lane + u * THREADS) + e < K);
+                const float z = counts ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, g = h[u][e] * gain[u][e];
                 if (GAINS) {
-                    of_gain[u][e] += counts ? g[u][e] * z[u][e] : 0.f;
-                    of_offset[u][e] += counts ? g[u][e] : 0.f;
+                    of_gain[u][e] = fmaf(h[u][e], z, of_gain[u][e]);
+                    of_offset[u][e] += h[u][e];
                 }
-                g[u][e] = counts ? g[u][e] * gain[u][e] : 0.f;
-                sum += g[u][e];
-                products += counts ? g[u][e] * z[u][e] : 0.f;
+                sums[0] += g;
+                sums[1] = fmaf(g, z, sums[1]);
             }
-        add_up<THREADS>(sum, products, part[which]);
+        };
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int k = 8 * (lane + u * THREADS);
+            if (k >= K) continue;
+            if (DROP) dropout::choose(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)k / 8, h[u]);
+            if (k + 8 <= K) add(u, std::true_type());
+            else add(u, std::false_type());
+        }
+        add_up<THREADS>(sums, part[which]);
         which ^= 1;
         if (!there) continue;
-        sum *= inverse;
-        products *= inverse;
+        sums[0] *= inverse;
+        sums[1] *= inverse;
+        const float scale = rstd * factor;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            const int64_t k = 8 * (lane + u * THREADS);
+            const int k = 8 * (lane + u * THREADS);
             if (k >= K) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[u][e] = (g[u][e] - fmaf(z[u][e], products, sum)) * rstd;
-            rows8::store(dX + row * job.ldd, k, K, g[u]);
+            for (int e = 0; e < 8; ++e) {
+                const float z = (rows8::to_float(x[u].v[e]) - mean) * rstd;
+                h[u][e] = (h[u][e] * gain[u][e] - fmaf(z, sums[1], sums[0])) * scale;
+            }
+            rows8::store(dX + row * job.ldd, k, K, h[u]);
         }
     }
     if constexpr (GAINS) {
@@ -295,13 +324,18 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(Bac
                         float s = 0.f;
 #pragma unroll
                         for (int r = 0; r < ROWS; ++r) s += all[r][at / 8][at % 8];
-                        const int64_t k = 8 * THREADS * u + at;
-                        if (k < K) mine[w * K + k] = s;
+                        const int k = 8 * THREADS * u + at;
+                        if (k < K) mine[w * K + k] = s * factor;
                     }
                 }
         } else {
 #pragma unroll
             for (int u = 0; u < HELD; ++u) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    of_gain[u][e] *= factor;
+                    of_offset[u][e] *= factor;
+                }
                 rows8::store(mine, 8 * (lane + u * THREADS), K, of_gain[u]);
                 rows8::store(mine + K, 8 * (lane + u * THREADS), K, of_offset[u]);
             }
@@ -309,11 +343,11 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(Bac
     }
 }
 
-// dX of longer rows: a workgroup reads a row twice.
+// dX of rows of any length: a workgroup reads a row twice.
 template <typename T>
 __global__ __launch_bounds__(kLongThreads) void back_long_kernel(BackJob job, bool drop)
 {
-    __shared__ float2 part[kLongThreads / 64];
+    __shared__ float part[kLongThreads / 64][2];
     const int64_t K = job.K, row = blockIdx.x;
     const float inverse = 1.0f / (float)K, mean = job.mean[row], rstd = job.rstd[row];
     const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
@@ -331,27 +365,40 @@ __global__ __launch_bounds__(kLongThreads) void back_long_kernel(BackJob job, bo
             g[e] *= gain[e];
         }
     };
-    float sum = 0.f, products = 0.f;
+    float sums[2] = {0.f, 0.f};
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
         load(k);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (k + e < K) {
-                sum += g[e];
-                products = fmaf(g[e], z[e], products);
+                sums[0] += g[e];
+                sums[1] = fmaf(g[e], z[e], sums[1]);
             }
     }
-    add_up<kLongThreads>(sum, products, part);
-    sum *= inverse;
-    products *= inverse;
+    add_up<kLongThreads>(sums, part);
+    sums[0] *= inverse;
+    sums[1] *= inverse;
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
         load(k);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = (g[e] - fmaf(z[e], products, sum)) * rstd;
+        for (int e = 0; e < 8; ++e) g[e] = (g[e] - fmaf(z[e], sums[1], sums[0])) * rstd;
         rows8::store(static_cast<T *>(job.dX) + row * job.ldd, k, K, g);
     }
 }
 
+template <typename T>
+__device__ __forceinline__ rows8::Eight<T> load_any(const T *row, int64_t k, int64_t K)
+{
+    rows8::Eight<T> c = {};
+    if (k + 8 <= K) {
+        c = *reinterpret_cast<const rows8::Eight<T> *>(row + k);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < K) c.v[e] = row[k + e];
+    }
+    return c;
+}
 // dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * THREADS columns of every (number of parts)-th group of rows.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(256) void gains_kernel(BackJob job, uint32_t pieces, bool drop)
@@ -372,8 +419,8 @@ __global__ __launch_bounds__(256) void gains_kernel(BackJob job, uint32_t pieces
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
                 const int64_t r = std::min(row + a * parts * ROWS, job.N - 1);
-                x[a] = load_raw(X + r * job.ldx, k, K);
-                h[a] = load_raw(dY + r * job.ldy, k, K);
+                x[a] = load_any(X + r * job.ldx, k, K);
+                h[a] = load_any(dY + r * job.ldy, k, K);
                 mean[a] = job.mean[r];
                 rstd[a] = job.rstd[r];
             }
@@ -477,7 +524,7 @@ int64_t gains_pieces(int64_t K) { return (K + 8 * gains_threads(K) - 1) / (8 * g
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && K <= kMostHeld) return with_shape(K, [&](auto threads, auto) { return groups_of(N, threads); });
+    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto) { return groups_of(N, threads); });
     const int64_t rows = 256 / gains_threads(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
@@ -485,7 +532,7 @@ int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 template <typename T>
 hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
 {
-    if (job.K <= kMostHeld) {
+    if (is_held(job.K)) {
         with_shape(job.K, [&](auto threads, auto held) {
             const dim3 grid((unsigned)groups_of(job.N, threads));
             if (drop) norm_kernel<T, threads, held, true><<<grid, group_threads(threads), 0, stream>>>(job);
@@ -512,7 +559,7 @@ template <typename T>
 hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
 {
     BackJob job = whole;
-    const bool gains = job.dgain != nullptr, held = job.K <= kMostHeld;
+    const bool gains = job.dgain != nullptr, held = is_held(job.K);
     const int64_t parts = gains ? parts_of(job.N, job.K, job.dX != nullptr) : 0;
     if (job.dX && held) {
         with_shape(job.K, [&](auto threads, auto held_) {

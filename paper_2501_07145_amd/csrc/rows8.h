@@ -29,6 +29,44 @@ __device__ __forceinline__ void load(const T *row, int64_t k, int64_t K, float (
         for (int e = 0; e < 8; ++e) x[e] = k + e < K ? to_float(row[k + e]) : 0.f;
     }
 }
+// The same of a row of at least eight columns, as they lie in memory and without a load for each number at its end: there the row's last eight numbers are loaded and
+// moved down.
+__device__ __forceinline__ void move_down(Eight<float> &c, int by)
+{
+#pragma unroll
+    for (int step = 4; step > 0; step /= 2) {
+        const bool now = (by & step) != 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c.v[e] = now ? (e + step < 8 ? c.v[e + step] : 0.f) : c.v[e];
+    }
+}
+__device__ __forceinline__ void move_down(Eight<uint16_t> &c, int by)
+{
+    uint32_t w[4];
+    __builtin_memcpy(w, &c, 16);
+#pragma unroll
+    for (int step = 2; step > 0; step /= 2) {
+        const bool now = (by & (2 * step)) != 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = now ? (i + step < 4 ? w[i + step] : 0u) : w[i];
+    }
+    if (by & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = w[i] >> 16 | (i < 3 ? w[i + 1] << 16 : 0u);
+    }
+    __builtin_memcpy(&c, w, 16);
+}
+template <typename T>
+__device__ __forceinline__ Eight<T> load_raw(const T *row, int k, int K)
+{
+    Eight<T> c = {};
+    if (k < K) {
+        const int start = k + 8 <= K ? k : K - 8;
+        c = *reinterpret_cast<const Eight<T> *>(row + start);
+        if (start < k) move_down(c, k - start);
+    }
+    return c;
+}
 template <typename T>
 __device__ __forceinline__ void store(T *row, int64_t k, int64_t K, const float (&x)[8])
 {
