@@ -13,6 +13,8 @@ namespace rfsf {
 namespace {
 
 constexpr int64_t kMostHeld = 512 * 5 * 8, kLeastHeld = 8;      // columns of rows that stay in registers
+constexpr int kGroupThreads = 1024;             // of a CU, in launches that go through the rows
+constexpr int64_t kManyRows = 2048;
 constexpr bool is_held(int64_t K) { return K >= kLeastHeld && K <= kMostHeld; }
 constexpr int kCus = 256;
 
@@ -164,6 +166,90 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
             for (int e = 0; e < 8; ++e) y[e] = fmaf((rows8::to_float(now[u].v[e]) - m.mean - m.rest) * rstd, gain[u][e], shift[u][e]);
             if (DROP) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)k / 8, y);
             rows8::store(Y + row * job.ldy, k, K, y);
+        }
+    }
+}
+
+// Numbers that are held from pass to pass as they came, so that what one pass made of them (32 bits of each) is not kept for the next one; and what is done
+// with a lane's eight numbers is done before the next eight's turn. (Without both the compiler holds all of it at once, and spills: 30000 x 10241, bfloat16 1170 us.)
+template <typename T>
+__device__ __forceinline__ void in_turn(rows8::Eight<T> &c)
+{
+    uint32_t w[2 * sizeof(T)];
+    __builtin_memcpy(w, &c, sizeof(c));
+#pragma unroll
+    for (size_t i = 0; i < 2 * sizeof(T); i += 4) asm volatile("" : "+v"(w[i]), "+v"(w[i + 1]), "+v"(w[i + 2]), "+v"(w[i + 3]));
+    __builtin_memcpy(&c, w, sizeof(c));
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Many rows: LANES of a wavefront have a row to themselves, and nobody waits for anybody; gains and offsets lie in LDS, once for all wavefronts of a CU. A row is HELD
+// times eight numbers a lane, of which the first FULL are whole for every lane.
+constexpr int wave_threads(size_t held_bytes) { return held_bytes <= 28 ? 1024 : held_bytes <= 42 ? 768 : 512; }
+template <typename T, int LANES, int FULL, int HELD, bool DROP>
+__global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kernel(NormJob job)
+{
+    constexpr int THREADS = wave_threads(HELD * sizeof(T)), STEP = 8 * LANES, ROWS = THREADS / LANES;
+    extern __shared__ __attribute__((aligned(16))) float columns[];          // gains, then offsets, each of HELD * STEP
+    const int lane = threadIdx.x % LANES, K = (int)job.K;
+    for (int k = threadIdx.x; k < STEP * HELD; k += THREADS) {
+        columns[k] = k < K && job.gain ? job.gain[k] : 1.f;
+        columns[STEP * HELD + k] = k < K && job.offset ? job.offset[k] : 0.f;
+    }
+    __syncthreads();
+    const double inverse = 1.0 / (double)K;
+    const uint64_t counter = DROP ? dropout::offset_of(job.dropout) : 0;
+    int64_t row = (int64_t)blockIdx.x * ROWS + (LANES == 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES)) : threadIdx.x / LANES);
+    for (; row < job.N; row += (int64_t)gridDim.x * ROWS) {
+        const T *x = static_cast<const T *>(job.X) + row * job.ldx;
+        T *y_row = static_cast<T *>(job.Y) + row * job.ldy;
+        rows8::Eight<T> held[HELD];
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int k = 8 * lane + STEP * u;
+            if (u < FULL) held[u] = *reinterpret_cast<const rows8::Eight<T> *>(x + k);
+            else held[u] = rows8::load_raw(x, k, K);
+        }
+        double sum[1] = {0.0};
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            in_turn(held[u]);
+            sum[0] += sum_of(held[u]);
+        }
+        add_up<LANES>(sum, static_cast<double (*)[1]>(nullptr));
+        const Mean m = mean_of(sum[0], inverse);
+        float squares[1] = {0.f};
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            in_turn(held[u]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = u < FULL || 8 * lane + STEP * u + e < K ? rows8::to_float(held[u].v[e]) - m.mean : 0.f;
+                squares[0] = fmaf(d, d, squares[0]);
+            }
+        }
+        add_up<LANES>(squares, static_cast<float (*)[1]>(nullptr));
+        const float rstd = rstd_of(squares[0], m.rest, (float)inverse, job.eps);
+        if (lane == 0) {
+            if (job.mean) job.mean[row] = m.mean;
+            if (job.rstd) job.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int k = 8 * lane + STEP * u;
+            if (u >= FULL && k >= K) continue;
+            in_turn(held[u]);
+            float y[8], gain[8], shift[8];
+            __builtin_memcpy(gain, columns + k, 32);
+            __builtin_memcpy(shift, columns + STEP * HELD + k, 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = fmaf((rows8::to_float(held[u].v[e]) - m.mean - m.rest) * rstd, gain[e], shift[e]);
+            if (DROP) {
+                uint32_t group = (uint32_t)k / 8;
+                asm volatile("" : "+v"(group));            // (the first rounds' products, which are the same for all rows, would be kept for every u)
+                dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, group, y);
+            }
+            rows8::store(y_row, k, u < FULL ? k + 8 : K, y);
         }
     }
 }
@@ -516,7 +602,7 @@ auto with_shape(int64_t K, const F &f)
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
 // Workgroups of a launch that goes through the rows: as many as the CUs hold at a time.
-int64_t groups_of(int64_t N, int threads) { return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (1024 / group_threads(threads))); }
+int64_t groups_of(int64_t N, int threads) { return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (kGroupThreads / group_threads(threads))); }
 
 // Parts of dgain and doffset. Fused with dX: one for each workgroup.
 int gains_threads(int64_t K) { return K <= 128 ? 16 : K <= 512 ? 64 : 256; }
@@ -529,9 +615,44 @@ int64_t parts_of(int64_t N, int64_t K, bool with_dx)
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
 
+// f(FULL, HELD): the numbers that a lane holds, of a list, if `lanes` of them hold a row.
+template <int FULL, int HELD, int... MORE, typename F>
+bool with_held(int64_t K, int lanes, const F &f)
+{
+    if (K <= 8 * lanes * HELD) {
+        f(std::integral_constant<int, FULL>(), std::integral_constant<int, HELD>());
+        return true;
+    }
+    if constexpr (sizeof...(MORE) > 0) return with_held<HELD, MORE...>(K, lanes, f);
+    return false;
+}
+template <typename T, int LANES, int FULL, int HELD>
+hipError_t launch_wave(const NormJob &job, bool drop, hipStream_t stream)
+{
+    constexpr int threads = wave_threads(HELD * sizeof(T)), rows = threads / LANES;
+    constexpr size_t lds = 2 * 8 * LANES * HELD * sizeof(float);
+    constexpr int64_t per_cu = std::min<int64_t>(2048 / threads, kLdsPerCu / lds);
+    const dim3 grid((unsigned)std::min<int64_t>((job.N + rows - 1) / rows, kCus * per_cu));
+    auto launch = [&](LdsLimit &limit, auto kernel) {
+        const hipError_t e = allow_lds(limit, reinterpret_cast<const void *>(kernel), lds);
+        if (e != hipSuccess) return e;
+        kernel<<<grid, threads, lds, stream>>>(job);
+        return hipGetLastError();
+    };
+    static LdsLimit limits[2];
+    return drop ? launch(limits[1], norm_wave_kernel<T, LANES, FULL, HELD, true>) : launch(limits[0], norm_wave_kernel<T, LANES, FULL, HELD, false>);
+}
+
 template <typename T>
 hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
 {
+    if (job.N >= kManyRows && job.K >= kLeastHeld) {
+        hipError_t e = hipSuccess;
+        if (with_held<0, 1, 2, 3>(job.K, 8, [&](auto full, auto held) { e = launch_wave<T, 8, full, held>(job, drop, stream); }) ||
+            with_held<1, 2, 3, 4, 5>(job.K, 16, [&](auto full, auto held) { e = launch_wave<T, 16, full, held>(job, drop, stream); }) ||
+            with_held<1, 2, 3, 4, 5, 7, 9, 11, 13, 17, 21>(job.K, 64, [&](auto full, auto held) { e = launch_wave<T, 64, full, held>(job, drop, stream); }))
+            return e;
+    }
     if (is_held(job.K)) {
         with_shape(job.K, [&](auto threads, auto held) {
             const dim3 grid((unsigned)groups_of(job.N, threads));
