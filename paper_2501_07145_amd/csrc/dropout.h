@@ -8,6 +8,7 @@
 #pragma once
 
 #include "rfsf_internal.h"
+#include "rows8.h"
 
 namespace rfsf {
 
@@ -68,13 +69,22 @@ __device__ __forceinline__ void apply(const DropoutJob &job, uint64_t offset, ui
     for (int e = 0; e < 8; ++e) x[e] = kept(job, word, e) ? x[e] * job.factor : 0.f;
 }
 
-// The same without the factor, for sums that it can multiply afterwards.
-__device__ __forceinline__ void choose(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, float (&x)[8])
+// The same of numbers as they lie in memory, without the factor, for sums that it can multiply afterwards.
+__device__ __forceinline__ void choose(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, rows8::Eight<float> &c)
 {
     uint32_t word[4];
     numbers(job, offset, row, group, word);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = kept(job, word, e) ? x[e] : 0.f;
+    for (int e = 0; e < 8; ++e) c.v[e] = kept(job, word, e) ? c.v[e] : 0.f;
+}
+__device__ __forceinline__ void choose(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, rows8::Eight<uint16_t> &c)
+{
+    uint32_t word[4], two[4];
+    numbers(job, offset, row, group, word);
+    __builtin_memcpy(two, &c, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) two[i] = (kept(job, word, 2 * i) ? two[i] & 0xffffu : 0u) | (kept(job, word, 2 * i + 1) ? two[i] & 0xffff0000u : 0u);
+    __builtin_memcpy(&c, two, 16);
 }
 
 }  // namespace dropout

@@ -13,7 +13,6 @@ namespace rfsf {
 namespace {
 
 constexpr int64_t kMostHeld = 512 * 5 * 8, kLeastHeld = 8;      // columns of rows that stay in registers
-constexpr int kGroupThreads = 1024;             // of a CU, in launches that go through the rows
 constexpr int64_t kManyRows = 2048;
 constexpr bool is_held(int64_t K) { return K >= kLeastHeld && K <= kMostHeld; }
 constexpr int kCus = 256;
@@ -170,19 +169,6 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
     }
 }
 
-// Numbers that are held from pass to pass as they came, so that what one pass made of them (32 bits of each) is not kept for the next one; and what is done
-// with a lane's eight numbers is done before the next eight's turn. (Without both the compiler holds all of it at once, and spills: 30000 x 10241, bfloat16 1170 us.)
-template <typename T>
-__device__ __forceinline__ void in_turn(rows8::Eight<T> &c)
-{
-    uint32_t w[2 * sizeof(T)];
-    __builtin_memcpy(w, &c, sizeof(c));
-#pragma unroll
-    for (size_t i = 0; i < 2 * sizeof(T); i += 4) asm volatile("" : "+v"(w[i]), "+v"(w[i + 1]), "+v"(w[i + 2]), "+v"(w[i + 3]));
-    __builtin_memcpy(&c, w, sizeof(c));
-    __builtin_amdgcn_sched_barrier(0);
-}
-
 // Many rows: LANES of a wavefront have a row to themselves, and nobody waits for anybody; gains and offsets lie in LDS, once for all wavefronts of a CU. A row is HELD
 // times eight numbers a lane, of which the first FULL are whole for every lane.
 constexpr int wave_threads(size_t held_bytes) { return held_bytes <= 28 ? 1024 : held_bytes <= 42 ? 768 : 512; }
@@ -213,7 +199,7 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
         double sum[1] = {0.0};
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            in_turn(held[u]);
+            rows8::in_turn(held[u]);
             sum[0] += sum_of(held[u]);
         }
         add_up<LANES>(sum, static_cast<double (*)[1]>(nullptr));
@@ -221,7 +207,7 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
         float squares[1] = {0.f};
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            in_turn(held[u]);
+            rows8::in_turn(held[u]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float d = u < FULL || 8 * lane + STEP * u + e < K ? rows8::to_float(held[u].v[e]) - m.mean : 0.f;
@@ -238,7 +224,7 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
             if (u >= FULL && k >= K) continue;
-            in_turn(held[u]);
+            rows8::in_turn(held[u]);
             float y[8], gain[8], shift[8];
             __builtin_memcpy(gain, columns + k, 32);
             __builtin_memcpy(shift, columns + STEP * HELD + k, 32);
@@ -303,95 +289,112 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bo
     }
 }
 
-// The backward pass of rows that are held in registers as above. Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds
-// its columns' h z and h up over the rows of the workgroup, whose sums are then one of the parts that add_parts_kernel adds up: no atomics, so that
-// equal calls give equal bits.
+// The backward pass of rows that are held in registers, THREADS lanes a row, HELD times eight numbers each, of which all but the last are whole; gains lie in LDS.
+// Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
+// sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
+constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && held <= 3) ? 4 : held == 2 ? 3 : 2; }
 template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
-__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(BackJob job)
+__global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, GAINS)) void back_kernel(BackJob job)
 {
-    constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1;
-    constexpr bool AHEAD = HELD <= 3;            // registers for the next row
+    constexpr int GROUP = THREADS > 256 ? THREADS : 256, ROWS = GROUP / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1, STEP = 8 * THREADS;
+    constexpr bool AHEAD = HELD <= (sizeof(T) == 2 ? 4 : 3);          // registers for the next row
     __shared__ float part[2][WAVES][2];
+    __shared__ __attribute__((aligned(16))) float gains[STEP * HELD];
     const int lane = threadIdx.x % THREADS, K = (int)job.K;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inverse = 1.0f / (float)K, factor = DROP ? job.dropout.factor : 1.f;
-    float gain[HELD][8], of_gain[HELD][8], of_offset[HELD][8];
+    for (int k = threadIdx.x; k < STEP * HELD; k += GROUP) gains[k] = k < K && job.gain ? job.gain[k] : 1.f;
+    __syncthreads();
+    float of_gain[HELD][8], of_offset[HELD][8];
 #pragma unroll
-    for (int u = 0; u < HELD; ++u) {
-        load_or(job.gain, 8 * (lane + u * THREADS), K, 1.f, gain[u]);
+    for (int u = 0; u < HELD; ++u)
 #pragma unroll
         for (int e = 0; e < 8; ++e) of_gain[u][e] = of_offset[u][e] = 0.f;
-    }
     const uint64_t counter = DROP ? dropout::offset_of(job.dropout) : 0;
     const T *X = static_cast<const T *>(job.X), *dY = static_cast<const T *>(job.dY);
     T *dX = static_cast<T *>(job.dX);
-    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
-    rows8::Eight<T> x[HELD], next_x[HELD], next_h[HELD];
+    int64_t row = (int64_t)blockIdx.x * ROWS + (THREADS >= 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / THREADS)) : threadIdx.x / THREADS);
+    rows8::Eight<T> x[HELD], h[HELD], next_x[HELD], next_h[HELD];
     float mean, rstd, next_mean, next_rstd;
     auto load = [&](int64_t r) {
-        const bool there = r < job.N;
-        r = there ? r : job.N - 1;
+        r = r < job.N ? r : job.N - 1;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            next_x[u] = rows8::load_raw(X + r * job.ldx, 8 * (lane + u * THREADS), K);
-            next_h[u] = rows8::load_raw(dY + r * job.ldy, 8 * (lane + u * THREADS), K);
+            const int k = 8 * lane + STEP * u;
+            if (u < HELD - 1) {
+                next_x[u] = *reinterpret_cast<const rows8::Eight<T> *>(X + r * job.ldx + k);
+                next_h[u] = *reinterpret_cast<const rows8::Eight<T> *>(dY + r * job.ldy + k);
+            } else {
+                next_x[u] = rows8::load_raw(X + r * job.ldx, k, K);
+                next_h[u] = rows8::load_raw(dY + r * job.ldy, k, K);
+            }
         }
         next_mean = job.mean[r];
         next_rstd = job.rstd[r];
     };
     if (AHEAD) load(row);
     int which = 0;
+    // (all rows of a workgroup take as many turns, so that everybody meets at the barriers)
     for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
         if (!AHEAD) load(row);
         const bool there = row < job.N;
-        float h[HELD][8];
         mean = next_mean;
         rstd = next_rstd;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             x[u] = next_x[u];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[u][e] = there ? rows8::to_float(next_h[u].v[e]) : 0.f;
+            h[u] = next_h[u];
         }
         if (AHEAD && turn + step < job.N) load(row + step);
         float sums[2] = {0.f, 0.f};             // of g, of g z
-        auto add = [&](int u, auto whole) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool counts = there && (whole || 8 * (lane + u * THREADS) + e < K);
-                const float z = counts ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, g = h[u][e] * gain[u][e];
-                if (GAINS) {
-                    of_gain[u][e] = fmaf(h[u][e], z, of_gain[u][e]);
-                    of_offset[u][e] += h[u][e];
-                }
-                sums[0] += g;
-                sums[1] = fmaf(g, z, sums[1]);
-            }
-        };
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            const int k = 8 * (lane + u * THREADS);
-            if (k >= K) continue;
-            if (DROP) dropout::choose(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)k / 8, h[u]);
-            if (k + 8 <= K) add(u, std::true_type());
-            else add(u, std::false_type());
+            const int k = 8 * lane + STEP * u;
+            if (u == HELD - 1 && k >= K) continue;
+            rows8::in_turn(x[u]);
+            if (DROP) {
+                uint32_t group = (uint32_t)k / 8;
+                asm volatile("" : "+v"(group));            // (the first rounds' products, which are the same for all rows, would be kept for every u)
+                dropout::choose(job.dropout, counter, job.dropout.first_row + (uint32_t)row, group, h[u]);
+            }
+            float gain[8];
+            __builtin_memcpy(gain, gains + k, 32);
+            auto add = [&](auto whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool counts = (ROWS == 1 || there) && (whole || k + e < K);
+                    const float z = counts ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, d = counts ? rows8::to_float(h[u].v[e]) : 0.f, g = d * gain[e];
+                    if (GAINS) {
+                        of_gain[u][e] = fmaf(d, z, of_gain[u][e]);
+                        of_offset[u][e] += d;
+                    }
+                    sums[0] += g;
+                    sums[1] = fmaf(g, z, sums[1]);
+                }
+            };
+            if (u < HELD - 1 || k + 8 <= K) add(std::true_type());
+            else add(std::false_type());
         }
         add_up<THREADS>(sums, part[which]);
         which ^= 1;
-        if (!there) continue;
+        if (ROWS > 1 && !there) continue;
         sums[0] *= inverse;
         sums[1] *= inverse;
         const float scale = rstd * factor;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
-            const int k = 8 * (lane + u * THREADS);
-            if (k >= K) continue;
+            const int k = 8 * lane + STEP * u;
+            if (u == HELD - 1 && k >= K) continue;
+            rows8::in_turn(x[u]);
+            rows8::in_turn(h[u]);
+            float gain[8], d[8];
+            __builtin_memcpy(gain, gains + k, 32);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float z = (rows8::to_float(x[u].v[e]) - mean) * rstd;
-                h[u][e] = (h[u][e] * gain[u][e] - fmaf(z, sums[1], sums[0])) * scale;
+                d[e] = (rows8::to_float(h[u].v[e]) * gain[e] - fmaf(z, sums[1], sums[0])) * scale;
             }
-            rows8::store(dX + row * job.ldd, k, K, h[u]);
+            rows8::store(dX + row * job.ldd, k, u < HELD - 1 ? k + 8 : K, d);
         }
     }
     if constexpr (GAINS) {
@@ -406,11 +409,11 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(Bac
 #pragma unroll
                     for (int e = 0; e < 8; ++e) all[threadIdx.x / THREADS][lane][e] = w ? of_offset[u][e] : of_gain[u][e];
                     __syncthreads();
-                    for (int at = threadIdx.x; at < THREADS * 8; at += 256) {
+                    for (int at = threadIdx.x; at < THREADS * 8; at += GROUP) {
                         float s = 0.f;
 #pragma unroll
                         for (int r = 0; r < ROWS; ++r) s += all[r][at / 8][at % 8];
-                        const int k = 8 * THREADS * u + at;
+                        const int k = STEP * u + at;
                         if (k < K) mine[w * K + k] = s * factor;
                     }
                 }
@@ -422,8 +425,8 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void back_kernel(Bac
                     of_gain[u][e] *= factor;
                     of_offset[u][e] *= factor;
                 }
-                rows8::store(mine, 8 * (lane + u * THREADS), K, of_gain[u]);
-                rows8::store(mine + K, 8 * (lane + u * THREADS), K, of_offset[u]);
+                rows8::store(mine, 8 * lane + STEP * u, K, of_gain[u]);
+                rows8::store(mine + K, 8 * lane + STEP * u, K, of_offset[u]);
             }
         }
     }
@@ -552,57 +555,56 @@ __global__ __launch_bounds__(256) void gains_kernel(BackJob job, uint32_t pieces
     }
 }
 
-// Adds the workgroups' sums up, in a fixed order: 64 columns a workgroup, whose wavefronts share the parts.
-constexpr int kAddWaves = 16;
-__global__ __launch_bounds__(64 * kAddWaves) void add_parts_kernel(const float *sums, int64_t parts, int64_t K, float *dgain, float *doffset)
+// Adds the workgroups' sums up, in a fixed order: 32 columns a workgroup, 32 groups of lanes that share the parts, eight loads ahead.
+constexpr int kAddColumns = 32, kAddThreads = 1024;
+__global__ __launch_bounds__(kAddThreads) void add_parts_kernel(const float *sums, int64_t parts, int64_t K, float *dgain, float *doffset)
 {
-    __shared__ float all[kAddWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t at = (int64_t)blockIdx.x * 64 + lane;
+    constexpr int SLICES = kAddThreads / kAddColumns, AHEAD = 8;
+    __shared__ float all[SLICES][kAddColumns + 1];
+    const int lane = threadIdx.x % kAddColumns, slice = threadIdx.x / kAddColumns;
+    const int64_t at = (int64_t)blockIdx.x * kAddColumns + lane;
     float s = 0.f;
     if (at < 2 * K)
-        for (int64_t p = wave; p < parts; p += kAddWaves) s += sums[p * 2 * K + at];
-    all[wave][lane] = s;
+        for (int64_t p = slice; p < parts; p += AHEAD * SLICES) {
+            float v[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) v[a] = p + a * SLICES < parts ? sums[(p + a * SLICES) * 2 * K + at] : 0.f;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) s += v[a];
+        }
+    all[slice][lane] = s;
     __syncthreads();
-    if (wave != 0 || at >= 2 * K) return;
+    if (slice != 0 || at >= 2 * K) return;
     s = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAddWaves; ++w) s += all[w][lane];
+    for (int w = 0; w < SLICES; ++w) s += all[w][lane];
     if (at < K) dgain[at] = s;
     else doffset[at - K] = s;
 }
 
-// Lanes a row, and how many times eight numbers each holds: as few turns as hold it.
+// f(lanes of a row, how many times eight numbers each holds), of which all but the last are whole.
+template <int THREADS, int HELD> struct Shape {};
+template <int THREADS, int HELD, typename... MORE, typename F>
+auto with_first(int64_t K, const F &f, Shape<THREADS, HELD>, MORE... more)
+{
+    if constexpr (sizeof...(MORE) > 0) {
+        if (K > 8 * THREADS * HELD) return with_first(K, f, more...);
+    }
+    return f(std::integral_constant<int, THREADS>(), std::integral_constant<int, HELD>());
+}
 template <typename F>
 auto with_shape(int64_t K, const F &f)
 {
-    const int64_t eights = (K + 7) / 8;
-    auto go = [&](auto threads, auto held) { return f(threads, held); };
-    typedef std::integral_constant<int, 16> t16;
-    typedef std::integral_constant<int, 64> t64;
-    typedef std::integral_constant<int, 256> t256;
-    typedef std::integral_constant<int, 512> t512;
-    typedef std::integral_constant<int, 1> h1;
-    typedef std::integral_constant<int, 2> h2;
-    typedef std::integral_constant<int, 3> h3;
-    typedef std::integral_constant<int, 4> h4;
-    typedef std::integral_constant<int, 5> h5;
-    if (eights <= 16) return go(t16(), h1());
-    if (eights <= 32) return go(t16(), h2());
-    if (eights <= 64) return go(t64(), h1());
-    if (eights <= 128) return go(t64(), h2());
-    if (eights <= 256) return go(t256(), h1());
-    if (eights <= 512) return go(t256(), h2());
-    if (eights <= 768) return go(t256(), h3());
-    if (eights <= 1024) return go(t512(), h2());
-    if (eights <= 1536) return go(t512(), h3());
-    if (eights <= 2048) return go(t512(), h4());
-    return go(t512(), h5());
+    return with_first(K, f, Shape<8, 1>(), Shape<8, 2>(), Shape<8, 3>(), Shape<16, 2>(), Shape<16, 3>(), Shape<16, 4>(), Shape<16, 5>(), Shape<64, 2>(), Shape<64, 3>(),
+                      Shape<64, 4>(), Shape<64, 5>(), Shape<256, 2>(), Shape<256, 3>(), Shape<256, 4>(), Shape<256, 5>(), Shape<512, 3>(), Shape<512, 4>(), Shape<512, 5>());
 }
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
-// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time.
-int64_t groups_of(int64_t N, int threads) { return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (kGroupThreads / group_threads(threads))); }
+// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time, of `waves` wavefronts a SIMD.
+int64_t groups_of(int64_t N, int threads, int waves)
+{
+    return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (256 * waves / group_threads(threads)));
+}
 
 // Parts of dgain and doffset. Fused with dX: one for each workgroup.
 int gains_threads(int64_t K) { return K <= 128 ? 16 : K <= 512 ? 64 : 256; }
@@ -610,7 +612,7 @@ int64_t gains_pieces(int64_t K) { return (K + 8 * gains_threads(K) - 1) / (8 * g
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto) { return groups_of(N, threads); });
+    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true)); });
     const int64_t rows = 256 / gains_threads(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
@@ -655,7 +657,7 @@ hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
     }
     if (is_held(job.K)) {
         with_shape(job.K, [&](auto threads, auto held) {
-            const dim3 grid((unsigned)groups_of(job.N, threads));
+            const dim3 grid((unsigned)groups_of(job.N, threads, 4));
             if (drop) norm_kernel<T, threads, held, true><<<grid, group_threads(threads), 0, stream>>>(job);
             else norm_kernel<T, threads, held, false><<<grid, group_threads(threads), 0, stream>>>(job);
         });
@@ -684,7 +686,7 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
     const int64_t parts = gains ? parts_of(job.N, job.K, job.dX != nullptr) : 0;
     if (job.dX && held) {
         with_shape(job.K, [&](auto threads, auto held_) {
-            const dim3 grid((unsigned)groups_of(job.N, threads));
+            const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held_, gains)));
             auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
             if (drop && gains) launch(back_kernel<T, threads, held_, true, true>);
             else if (drop) launch(back_kernel<T, threads, held_, true, false>);
@@ -717,7 +719,7 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
     if (gains) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        add_parts_kernel<<<dim3((unsigned)((2 * job.K + 63) / 64)), 64 * kAddWaves, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
+        add_parts_kernel<<<dim3((unsigned)((2 * job.K + kAddColumns - 1) / kAddColumns)), kAddThreads, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
     }
     return hipGetLastError();
 }
