@@ -475,83 +475,72 @@ __global__ __launch_bounds__(kLongThreads) void back_long_kernel(BackJob job, bo
     }
 }
 
+// dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * LANES columns of some rows, LANES lanes of it a row.
 template <typename T>
-__device__ __forceinline__ rows8::Eight<T> load_any(const T *row, int64_t k, int64_t K)
+__device__ __forceinline__ rows8::Eight<T> load_short(const T *row, int k, int K)
 {
     rows8::Eight<T> c = {};
-    if (k + 8 <= K) {
-        c = *reinterpret_cast<const rows8::Eight<T> *>(row + k);
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < K) c.v[e] = row[k + e];
-    }
+    for (int e = 0; e < 8; ++e)
+        if (k + e < K) c.v[e] = row[k + e];
     return c;
 }
-// dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * THREADS columns of every (number of parts)-th group of rows.
-template <typename T, int THREADS>
-__global__ __launch_bounds__(256) void gains_kernel(BackJob job, uint32_t pieces, bool drop)
+template <typename T, int LANES, bool DROP, bool SHORT>
+__global__ __launch_bounds__(256, 4) void gains_kernel(BackJob job, uint32_t pieces)
 {
-    constexpr int ROWS = 256 / THREADS, AHEAD = 4;
-    __shared__ float all[ROWS][THREADS][17];
-    const int lane = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
-    const int64_t K = job.K, part = blockIdx.x / pieces, parts = gridDim.x / pieces, k = 8 * ((int64_t)(blockIdx.x % pieces) * THREADS + lane);
-    const uint64_t counter = drop ? dropout::offset_of(job.dropout) : 0;
+    constexpr int ROWS = 256 / LANES, AHEAD = 4;
+    __shared__ float all[ROWS][LANES][17];
+    const int lane = threadIdx.x % LANES, sub = LANES == 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES)) : threadIdx.x / LANES, K = (int)job.K;
+    const int64_t part = blockIdx.x / pieces, step = (int64_t)(gridDim.x / pieces) * ROWS;
+    const int k = 8 * ((int)(blockIdx.x % pieces) * LANES + lane);
+    const uint64_t counter = DROP ? dropout::offset_of(job.dropout) : 0;
     const T *X = static_cast<const T *>(job.X), *dY = static_cast<const T *>(job.dY);
     float of_gain[8], of_offset[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) of_gain[e] = of_offset[e] = 0.f;
-    if (k < K) {
-        for (int64_t row = part * ROWS + sub; row < job.N; row += AHEAD * parts * ROWS) {
-            rows8::Eight<T> x[AHEAD], h[AHEAD];
-            float mean[AHEAD], rstd[AHEAD];
+    for (int64_t row = part * ROWS + sub; row < job.N; row += AHEAD * step) {
+        rows8::Eight<T> x[AHEAD], h[AHEAD];
+        float mean[AHEAD], rstd[AHEAD];
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int64_t r = std::min(row + a * parts * ROWS, job.N - 1);
-                x[a] = load_any(X + r * job.ldx, k, K);
-                h[a] = load_any(dY + r * job.ldy, k, K);
-                mean[a] = job.mean[r];
-                rstd[a] = job.rstd[r];
+        for (int a = 0; a < AHEAD; ++a) {
+            const int64_t r = std::min(row + a * step, job.N - 1);
+            x[a] = SHORT ? load_short(X + r * job.ldx, k, K) : rows8::load_raw(X + r * job.ldx, k, K);
+            h[a] = SHORT ? load_short(dY + r * job.ldy, k, K) : rows8::load_raw(dY + r * job.ldy, k, K);
+            mean[a] = job.mean[r];
+            rstd[a] = job.rstd[r];
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int64_t r = row + a * step;
+            if (r >= job.N || k >= K) break;
+            rows8::in_turn(x[a]);
+            if (DROP) {
+                uint32_t group = (uint32_t)k / 8;
+                asm volatile("" : "+v"(group));
+                dropout::choose(job.dropout, counter, job.dropout.first_row + (uint32_t)r, group, h[a]);
             }
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int64_t r = row + a * parts * ROWS;
-                if (r >= job.N) break;
-                float g[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = rows8::to_float(h[a].v[e]);
-                if (drop) dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)r, (uint32_t)(k / 8), g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    of_gain[e] = fmaf(g[e], (rows8::to_float(x[a].v[e]) - mean[a]) * rstd[a], of_gain[e]);
-                    of_offset[e] += g[e];
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float d = rows8::to_float(h[a].v[e]);
+                of_gain[e] = fmaf(d, (rows8::to_float(x[a].v[e]) - mean[a]) * rstd[a], of_gain[e]);
+                of_offset[e] += d;
             }
         }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        all[sub][lane][e] = of_gain[e];
+        all[sub][lane][8 + e] = of_offset[e];
+    }
+    __syncthreads();
+    const float factor = DROP ? job.dropout.factor : 1.f;
     float *mine = job.sums + part * 2 * K;
-    if constexpr (ROWS > 1) {
+    for (int at = threadIdx.x; at < 16 * LANES; at += 256) {
+        const int w = at / (8 * LANES), c = at % (8 * LANES), column = 8 * LANES * (int)(blockIdx.x % pieces) + c;
+        float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            all[sub][lane][e] = of_gain[e];
-            all[sub][lane][8 + e] = of_offset[e];
-        }
-        __syncthreads();
-        if (sub != 0) return;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float a = 0.f, b = 0.f;
-            for (int r = 0; r < ROWS; ++r) {
-                a += all[r][lane][e];
-                b += all[r][lane][8 + e];
-            }
-            of_gain[e] = a;
-            of_offset[e] = b;
-        }
-    }
-    if (k < K) {
-        rows8::store(mine, k, K, of_gain);
-        rows8::store(mine + K, k, K, of_offset);
+        for (int r = 0; r < ROWS; ++r) s += all[r][c / 8][8 * w + c % 8];
+        if (column < K) mine[w * K + column] = s * factor;
     }
 }
 
@@ -607,13 +596,13 @@ int64_t groups_of(int64_t N, int threads, int waves)
 }
 
 // Parts of dgain and doffset. Fused with dX: one for each workgroup.
-int gains_threads(int64_t K) { return K <= 128 ? 16 : K <= 512 ? 64 : 256; }
-int64_t gains_pieces(int64_t K) { return (K + 8 * gains_threads(K) - 1) / (8 * gains_threads(K)); }
+int gains_lanes(int64_t K) { return K <= 128 ? 16 : 64; }
+int64_t gains_pieces(int64_t K) { return (K + 8 * gains_lanes(K) - 1) / (8 * gains_lanes(K)); }
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
     if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true)); });
-    const int64_t rows = 256 / gains_threads(K), groups = (N + rows - 1) / rows;
+    const int64_t rows = 256 / gains_lanes(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
 
@@ -697,10 +686,10 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
         if (gains) {                // (first: dX may lie where dY is)
             const int64_t pieces = gains_pieces(job.K);
             const dim3 grid((unsigned)(parts * pieces));
-            const int threads = gains_threads(job.K);
-            if (threads == 16) gains_kernel<T, 16><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
-            else if (threads == 64) gains_kernel<T, 64><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
-            else gains_kernel<T, 256><<<grid, 256, 0, stream>>>(job, (uint32_t)pieces, drop);
+            auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(job, (uint32_t)pieces); };
+            if (job.K < kLeastHeld) drop ? launch(gains_kernel<T, 16, true, true>) : launch(gains_kernel<T, 16, false, true>);
+            else if (gains_lanes(job.K) == 16) drop ? launch(gains_kernel<T, 16, true, false>) : launch(gains_kernel<T, 16, false, false>);
+            else drop ? launch(gains_kernel<T, 64, true, false>) : launch(gains_kernel<T, 64, false, false>);
         }
         constexpr int64_t kMost = 1 << 21;          // workgroups of a launch
         for (int64_t n0 = 0; job.dX && n0 < job.N; n0 += kMost) {
