@@ -30,7 +30,7 @@ struct BackJob {
     const void *X, *dY;
     void *dX;
     const float *mean, *rstd, *gain;
-    float *sums;                // [workgroups along the rows][2][K], dgain's and doffset's; or these themselves of one workgroup
+    float *sums;                // [workgroups along the rows][2][K], dgain's and doffset's; unused where there is one workgroup
     float *dgain, *doffset;
     int64_t N, K, ldx, ldy, ldd;
     DropoutJob dropout;
@@ -289,6 +289,14 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bo
     }
 }
 
+// Where part number `part` of the sums goes.
+struct Sums { float *gain, *offset; };
+__device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_t parts)
+{
+    if (parts == 1) return {job.dgain, job.doffset};
+    return {job.sums + part * 2 * job.K, job.sums + (part * 2 + 1) * job.K};
+}
+
 // The backward pass of rows that are held in registers, THREADS lanes a row, HELD times eight numbers each, of which all but the last are whole; gains lie in LDS.
 // Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
 // sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
@@ -398,7 +406,7 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
         }
     }
     if constexpr (GAINS) {
-        float *mine = job.sums + (int64_t)blockIdx.x * 2 * K;
+        const Sums mine = sums_of(job, blockIdx.x, gridDim.x);
         if constexpr (ROWS > 1) {                       // over the workgroup's rows
             __shared__ float all[ROWS][THREADS][9];
 #pragma unroll
@@ -414,7 +422,7 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
 #pragma unroll
                         for (int r = 0; r < ROWS; ++r) s += all[r][at / 8][at % 8];
                         const int k = STEP * u + at;
-                        if (k < K) mine[w * K + k] = s * factor;
+                        if (k < K) (w ? mine.offset : mine.gain)[k] = s * factor;
                     }
                 }
         } else {
@@ -425,8 +433,8 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
                     of_gain[u][e] *= factor;
                     of_offset[u][e] *= factor;
                 }
-                rows8::store(mine, 8 * lane + STEP * u, K, of_gain[u]);
-                rows8::store(mine + K, 8 * lane + STEP * u, K, of_offset[u]);
+                rows8::store(mine.gain, 8 * lane + STEP * u, K, of_gain[u]);
+                rows8::store(mine.offset, 8 * lane + STEP * u, K, of_offset[u]);
             }
         }
     }
@@ -534,13 +542,13 @@ __global__ __launch_bounds__(256, 4) void gains_kernel(BackJob job, uint32_t pie
     }
     __syncthreads();
     const float factor = DROP ? job.dropout.factor : 1.f;
-    float *mine = job.sums + part * 2 * K;
+    const Sums mine = sums_of(job, part, gridDim.x / pieces);
     for (int at = threadIdx.x; at < 16 * LANES; at += 256) {
         const int w = at / (8 * LANES), c = at % (8 * LANES), column = 8 * LANES * (int)(blockIdx.x % pieces) + c;
         float s = 0.f;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) s += all[r][c / 8][8 * w + c % 8];
-        if (column < K) mine[w * K + column] = s * factor;
+        if (column < K) (w ? mine.offset : mine.gain)[column] = s * factor;
     }
 }
 
@@ -589,9 +597,12 @@ auto with_shape(int64_t K, const F &f)
 }
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
-// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time, of `waves` wavefronts a SIMD.
-int64_t groups_of(int64_t N, int threads, int waves)
+// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time, of `waves` wavefronts a SIMD. alone: one for what it does in a few turns,
+// which take less time than a second launch for adding parts up.
+constexpr int64_t kFewTurns = 4;
+int64_t groups_of(int64_t N, int threads, int waves, bool alone = false)
 {
+    if (alone && N <= kFewTurns * group_rows(threads)) return 1;
     return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (256 * waves / group_threads(threads)));
 }
 
@@ -601,7 +612,7 @@ int64_t gains_pieces(int64_t K) { return (K + 8 * gains_lanes(K) - 1) / (8 * gai
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true)); });
+    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
     const int64_t rows = 256 / gains_lanes(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
@@ -675,7 +686,7 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
     const int64_t parts = gains ? parts_of(job.N, job.K, job.dX != nullptr) : 0;
     if (job.dX && held) {
         with_shape(job.K, [&](auto threads, auto held_) {
-            const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held_, gains)));
+            const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held_, gains), gains));
             auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
             if (drop && gains) launch(back_kernel<T, threads, held_, true, true>);
             else if (drop) launch(back_kernel<T, threads, held_, true, false>);
@@ -705,7 +716,7 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
             back_long_kernel<T><<<dim3((unsigned)std::min(kMost, job.N - n0)), kLongThreads, 0, stream>>>(part, drop);
         }
     }
-    if (gains) {
+    if (gains && parts > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         add_parts_kernel<<<dim3((unsigned)((2 * job.K + kAddColumns - 1) / kAddColumns)), kAddThreads, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
