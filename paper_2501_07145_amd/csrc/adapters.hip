@@ -28,6 +28,22 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// A number as the sum of three of bfloat16, cut off and not rounded, so that none of them is infinite unless it is.
+struct Terms3 { uint16_t v[3]; };
+__device__ __forceinline__ Terms3 terms3(float x)
+{
+    Terms3 t;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const uint32_t top = __float_as_uint(x) & 0xffff0000u;
+        t.v[i] = (uint16_t)(top >> 16);
+        x -= __uint_as_float(top);
+    }
+    return t;
+}
+
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
 // The caller's memory: W's rows, those of the adapters' A (ranks rounded up to 16, zeros beyond), each with their largest numbers, then B in its own type
@@ -90,10 +106,12 @@ __global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *
     __shared__ int part[kOrderWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane;
     const int fours = (rows + 3) / 4;
+#pragma unroll 4
     for (int m = threadIdx.x; m < 4 * fours; m += 64 * kOrderWaves) keys[m] = m < rows ? (uint32_t)code_of(adapters[m], count) << 13 | (uint32_t)m : ~0u;
     __syncthreads();
     const uint32_t mine = row < rows ? keys[row] : 0;
     int before = 0;
+#pragma unroll 8
     for (int f = wave; f < fours; f += kOrderWaves) {
         const uint4 k = *reinterpret_cast<const uint4 *>(keys + 4 * f);
         before += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
@@ -109,15 +127,16 @@ __global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *
     who[before] = code == 0 ? kNone : code == (int)count + 1 ? kUnknown : code - 1;
 }
 
-// Inner products of 16 rows with 16 rows of their adapters' A. Slot s of a tile takes the adapters number s, s + slots, .. of those that its rows have.
-constexpr int kInnerWaves = 8;
+// Inner products of 16 rows with 16 rows of their adapters' A, as three numbers of 16 bits each whose sum they are. Slot s of a tile takes the adapters number
+// s, s + slots, .. of those that its rows have. The wavefronts share the steps, four of them under way at a time.
+constexpr int kInnerWaves = 8, kInnerAhead = 4;
 struct InnerJob {
     const char *x, *a;                  // packed
     int64_t pitch;
     const uint32_t *largest_x, *largest_a;
     const float *scale;
     const int32_t *who;
-    float *inner;                       // [rows][ranks]
+    uint16_t *inner;                    // [rows][3][ranks], bits of bfloat16
     int rows, ranks, rank_blocks, slots, steps;
 };
 template <bool TWO>
@@ -140,18 +159,28 @@ __global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
         const int64_t row_a = (int64_t)adapter * job.ranks + 16 * block;
         const char *a = job.a + (row_a + col) * job.pitch + 16 * quarter;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int s = wave; s < job.steps; s += kInnerWaves) {
-            const int64_t at = (int64_t)s * kStepBytes;
-            const halfx8 a0 = *reinterpret_cast<const halfx8 *>(a + at), a1 = *reinterpret_cast<const halfx8 *>(a + at + 64);
-            const halfx8 x0 = *reinterpret_cast<const halfx8 *>(x + at), x1 = *reinterpret_cast<const halfx8 *>(x + at + 64);
-            if (TWO) {
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, x0, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x1, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x0, acc, 0, 0, 0);
-            } else {
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, x0, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, x1, acc, 0, 0, 0);
+        for (int s = wave; s < job.steps; s += kInnerWaves * kInnerAhead) {
+            halfx8 fa[kInnerAhead][2], fx[kInnerAhead][2];
+#pragma unroll
+            for (int u = 0; u < kInnerAhead; ++u) {
+                const int64_t at = (int64_t)std::min(s + u * kInnerWaves, job.steps - 1) * kStepBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    fa[u][h] = *reinterpret_cast<const halfx8 *>(a + at + 64 * h);
+                    fx[u][h] = *reinterpret_cast<const halfx8 *>(x + at + 64 * h);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kInnerAhead; ++u) {
+                if (s + u * kInnerWaves >= job.steps) break;
+                if (TWO) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][1], fx[u][0], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][1], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][0], acc, 0, 0, 0);
+                } else {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][0], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][1], fx[u][1], acc, 0, 0, 0);
+                }
             }
         }
         __syncthreads();                // (what was read before has been)
@@ -162,76 +191,127 @@ __global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kInnerWaves; ++w) sum += part[w][wave][lane];
-            const int r = 4 * quarter + wave;
-            job.inner[(int64_t)n * job.ranks + 16 * block + r] = ldexpf(sum, -shift_of(job.largest_x[n]) - shift_of(job.largest_a[row_a + r])) * job.scale[adapter];
+            const int r = 16 * block + 4 * quarter + wave;
+            const Terms3 t = terms3(ldexpf(sum, -shift_of(job.largest_x[n]) - shift_of(job.largest_a[(int64_t)adapter * job.ranks + r])) * job.scale[adapter]);
+            uint16_t *to = job.inner + (int64_t)n * 3 * job.ranks + r;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) to[i * job.ranks] = t.v[i];
         }
     }
 }
 
-// Sums over ranks of a block of 32 classes and 32 rows, added to the accumulators of the rows that have this adapter. v_mfma_f32_32x32x2_f32: lane l holds class
-// (row) l % 32 and rank l / 32 of two; four ranks a lane and load.
+// The shared product's epilogue, which adds to the accumulators the sums over ranks of a block of 32 classes and 32 rows, for one adapter of the rows after the
+// other, and keeps the sums of the rows that have it. v_mfma_f32_32x32x16_bf16: lane l holds eight ranks of class (row) l % 32. B enters as it is (bfloat16) or as
+// three terms, of whose products with those of the inner products the three smallest are left out (below 2^-22 of the product).
+template <bool BF16>
 struct Adapted {
     const uint32_t *largest_w, *largest_x;
     int64_t C;
     int rows;                   // of this launch, in the order of their adapters
     const int32_t *order, *who;
-    const float *inner;
+    const uint16_t *inner;
     const void *B;
     int ranks, ranks_b;
-    bool bf16;
     float *out;
     int64_t ld;
 
-    __device__ __forceinline__ float4 four_of_b(int64_t row, int r) const
+    static constexpr int TERMS = BF16 ? 1 : 3;
+    __device__ __forceinline__ void load_b(int64_t row, int r, bf16x8 (&f)[TERMS]) const
     {
-        if (r >= ranks_b) return make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!bf16) return *reinterpret_cast<const float4 *>(static_cast<const float *>(B) + row * ranks_b + r);
-        const ushort4 v = *reinterpret_cast<const ushort4 *>(static_cast<const uint16_t *>(B) + row * ranks_b + r);
-        return make_float4(rows8::to_float(v.x), rows8::to_float(v.y), rows8::to_float(v.z), rows8::to_float(v.w));
+        if constexpr (BF16) {
+            const uint4 v = r < ranks_b ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(B) + row * ranks_b + r) : make_uint4(0, 0, 0, 0);
+            f[0] = __builtin_bit_cast(bf16x8, v);
+        } else {
+            const float *from = static_cast<const float *>(B) + row * ranks_b + r;
+            float v[8];
+            *reinterpret_cast<float4 *>(v) = r < ranks_b ? *reinterpret_cast<const float4 *>(from) : make_float4(0.f, 0.f, 0.f, 0.f);
+            *reinterpret_cast<float4 *>(v + 4) = r + 4 < ranks_b ? *reinterpret_cast<const float4 *>(from + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            uint32_t w[3][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Terms3 lo = terms3(v[2 * i]), hi = terms3(v[2 * i + 1]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) w[k][i] = lo.v[k] | (uint32_t)hi.v[k] << 16;
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) f[k] = __builtin_bit_cast(bf16x8, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+        }
     }
     template <typename T>
     __device__ __forceinline__ void operator()(T &t) const
     {
         struct __attribute__((packed, aligned(4))) Float4u { float x, y, z, w; };
-        constexpr int CLASSES = T::ROWS + (T::HAS_EXTRA ? 32 : 0);
+        constexpr int CLASSES = T::ROWS + (T::HAS_EXTRA ? 32 : 0), BN = T::BN, BM = T::BM;
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
         const int64_t c0 = t.tile_i * T::ROWS;
         int *powers = reinterpret_cast<int *>(t.lds);
         __syncthreads();
         for (int i = threadIdx.x; i < CLASSES; i += blockDim.x) powers[i] = -shift_of(c0 + i < C ? largest_w[c0 + i] : 0);
         __syncthreads();
-        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
-            if (first >= C) return;
+        int mine[BN], shift[BN];
+#pragma unroll
+        for (int b = 0; b < BN; ++b) {
             const int64_t n = t.j0 + 32 * b + col;
-            const bool there = n < rows;
-            const int mine = there ? who[n] : kNone, shift = there ? shift_of(largest_x[n]) : 0;
+            mine[b] = n < rows ? who[n] : kNone;
+            shift[b] = n < rows ? shift_of(largest_x[n]) : 0;
+        }
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[e] = ldexpf(acc[e], powers[(int)(first - c0) + 8 * (e / 4) + 4 * half + e % 4] - shift);
-            const float *s = inner + (there ? n : rows - 1) * (int64_t)ranks + 4 * half;
-            const int64_t c = std::min(first + col, C - 1);
-            for (uint64_t left = __ballot(mine >= 0); left != 0;) {
-                const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-                const bool its = mine == adapter;
-                left &= ~__ballot(its);
-                floatx16 sum = {};
-                for (int r = 0; r < ranks_b; r += 8) {
-                    const float4 x = four_of_b((int64_t)adapter * C + c, r + 4 * half), y = *reinterpret_cast<const float4 *>(s + r);
-                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, sum, 0, 0, 0);
-                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, sum, 0, 0, 0);
-                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, sum, 0, 0, 0);
-                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, sum, 0, 0, 0);
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] += its ? sum[e] : 0.f;
+            for (int q = 0; q < 4; ++q) {
+                const int4 p = *reinterpret_cast<const int4 *>(powers + (int)(first - c0) + 8 * q + 4 * half);
+                acc[4 * q] = ldexpf(acc[4 * q], p.x - shift[b]);
+                acc[4 * q + 1] = ldexpf(acc[4 * q + 1], p.y - shift[b]);
+                acc[4 * q + 2] = ldexpf(acc[4 * q + 2], p.z - shift[b]);
+                acc[4 * q + 3] = ldexpf(acc[4 * q + 3], p.w - shift[b]);
             }
-            if (!there) return;
+        });
+#pragma unroll
+        for (int b = 0; b < BN; ++b) {
+            const uint64_t with = __ballot(mine[b] >= 0);
+            if (with == 0) continue;
+            const int64_t n = std::min<int64_t>(t.j0 + 32 * b + col, rows - 1);
+            const uint16_t *from = inner + n * 3 * ranks + 8 * half;
+            for (int r0 = 0; r0 < ranks; r0 += 16) {
+                bf16x8 s[3];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) s[i] = *reinterpret_cast<const bf16x8 *>(from + i * ranks + r0);
+                for (uint64_t left = with; left != 0;) {
+                    const int adapter = __builtin_amdgcn_readlane(mine[b], __builtin_ctzll(left));
+                    const bool its = mine[b] == adapter;
+                    left &= ~__ballot(its);
+                    auto add = [&](auto &acc, int64_t first) __attribute__((always_inline)) {
+                        if (first >= C) return;
+                        bf16x8 f[TERMS];
+                        load_b((int64_t)adapter * C + std::min(first + col, C - 1), r0 + 8 * half, f);
+                        floatx16 sum = {};
+                        if constexpr (!BF16) {
+                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[2], s[0], sum, 0, 0, 0);
+                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[1], s[1], sum, 0, 0, 0);
+                        }
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], s[2], sum, 0, 0, 0);
+                        if constexpr (!BF16) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[1], s[0], sum, 0, 0, 0);
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], s[1], sum, 0, 0, 0);
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], s[0], sum, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[e] += its ? sum[e] : 0.f;
+                    };
+#pragma unroll
+                    for (int a = 0; a < BM; ++a) add(t.acc[a][b], t.i0 + 32 * a);
+                    if constexpr (T::HAS_EXTRA)
+                        if (b == t.wave_i) add(t.extra, t.extra_i);
+                }
+            }
+        }
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            const int64_t n = t.j0 + 32 * b + col;
+            if (n >= rows) return;
             float *row = out + (int64_t)order[n] * ld;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t i = first + 8 * q + 4 * half;
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = mine == kUnknown ? NAN : acc[4 * q + e];
+                for (int e = 0; e < 4; ++e) v[e] = mine[b] == kUnknown ? NAN : acc[4 * q + e];
                 if (i + 3 < C) {
                     *reinterpret_cast<Float4u *>(row + i) = {v[0], v[1], v[2], v[3]};
                 } else {
@@ -255,7 +335,7 @@ Workspace workspace_of(const Layout &z, int64_t rows)
     w.order = w.largest_x + up((size_t)rows * 4);
     w.who = w.order + up((size_t)rows * 4);
     w.inner = w.who + up((size_t)rows * 4);
-    w.bytes = w.inner + up((size_t)rows * z.ranks * 4) + 256;
+    w.bytes = w.inner + up((size_t)rows * 3 * z.ranks * 2) + 256;
     return w;
 }
 
@@ -309,7 +389,7 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
     char *ws = static_cast<char *>(workspace) + (mis ? 256 - mis : 0);
     uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + w.largest_x);
     int32_t *order = reinterpret_cast<int32_t *>(ws + w.order), *who = reinterpret_cast<int32_t *>(ws + w.who);
-    float *inner = reinterpret_cast<float *>(ws + w.inner);
+    uint16_t *inner = reinterpret_cast<uint16_t *>(ws + w.inner);
     const uint32_t *largest_w = reinterpret_cast<const uint32_t *>(lay + z.largest_w), *largest_a = reinterpret_cast<const uint32_t *>(lay + z.largest_a);
     const float *scale = reinterpret_cast<const float *>(lay + z.scale);
     const int64_t steps = plane_steps(s.K, !bf16);
@@ -319,17 +399,19 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
         RFSF_TRY(hipGetLastError());
         RFSF_TRY(pack(PackJob{static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4), rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
                       bf16, stream));
-        const int slots = (int)std::min<int64_t>(16, s.count), blocks = z.ranks / 16;
+        const int slots = (int)std::min<int64_t>(16, 16 * std::min(s.count, rows) / rows + 1), blocks = z.ranks / 16;
         const InnerJob job = {ws + w.x, lay + z.a, z.pitch, largest_x, largest_a, scale, who, inner, (int)rows, z.ranks, blocks, slots, (int)steps};
         const dim3 grid((unsigned)((rows + 15) / 16 * blocks * slots));
         if (bf16) inner_kernel<false><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
         else inner_kernel<true><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
         RFSF_TRY(hipGetLastError());
-        const Adapted epilogue = {largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks, z.ranks_b, bf16, out + n0 * ld_out, ld_out};
         const Planes w_rows = {lay + z.w, z.pitch, s.C}, x_rows = {ws + w.x, z.pitch, rows};
         const int edge = plane_tile(s.C, rows);
-        RFSF_TRY(bf16 ? launch_plane_product<kHalf>(w_rows, x_rows, steps, edge, epilogue, stream)
-                      : launch_plane_product<kHalfTwo>(w_rows, x_rows, steps, edge, epilogue, stream));
+        float *to = out + n0 * ld_out;
+        RFSF_TRY(bf16 ? launch_plane_product<kHalf>(w_rows, x_rows, steps, edge, Adapted<true>{largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks,
+                                                                                              z.ranks_b, to, ld_out}, stream)
+                      : launch_plane_product<kHalfTwo>(w_rows, x_rows, steps, edge, Adapted<false>{largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks,
+                                                                                                  z.ranks_b, to, ld_out}, stream));
     }
     return hipSuccess;
 }
