@@ -95,16 +95,17 @@ __global__ __launch_bounds__(256) void set_kernel(const T *B, int64_t ld_b, int6
 }
 
 // The rows in the order of their adapters: each row's place is the number of rows that come before it, those with a lower adapter, or the same one and a lower
-// number. A lane has a row, 16 wavefronts share the rows it is compared with.
+// number. Two lanes have a row, 16 wavefronts share the rows it is compared with. Bound by reading the keys from LDS.
 constexpr int kMostRows = 8192;             // at a time: 13 bits beside the adapter's number, of which there are fewer than 2^18
 constexpr int kNone = -1, kUnknown = -2;    // who: rows without an adapter, and with one that does not exist
-constexpr int kOrderWaves = 16;
+constexpr int kOrderWaves = 16, kOrderRows = 32;
 __device__ __forceinline__ int code_of(int64_t adapter, int64_t count) { return adapter < 0 ? 0 : adapter < count ? (int)adapter + 1 : (int)count + 1; }
+__device__ __forceinline__ int who_of(int64_t adapter, int64_t count) { return adapter < 0 ? kNone : adapter < count ? (int)adapter : kUnknown; }
 __global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *adapters, int rows, int64_t count, int32_t *order, int32_t *who)
 {
     __shared__ __attribute__((aligned(16))) uint32_t keys[kMostRows];
-    __shared__ int part[kOrderWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane;
+    __shared__ int part[2 * kOrderWaves][kOrderRows];
+    const int lane = threadIdx.x % kOrderRows, group = threadIdx.x / kOrderRows, row = blockIdx.x * kOrderRows + lane;
     const int fours = (rows + 3) / 4;
 #pragma unroll 4
     for (int m = threadIdx.x; m < 4 * fours; m += 64 * kOrderWaves) keys[m] = m < rows ? (uint32_t)code_of(adapters[m], count) << 13 | (uint32_t)m : ~0u;
@@ -112,19 +113,64 @@ __global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *
     const uint32_t mine = row < rows ? keys[row] : 0;
     int before = 0;
 #pragma unroll 8
-    for (int f = wave; f < fours; f += kOrderWaves) {
+    for (int f = group; f < fours; f += 2 * kOrderWaves) {
         const uint4 k = *reinterpret_cast<const uint4 *>(keys + 4 * f);
         before += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
     }
-    part[wave][lane] = before;
+    part[group][lane] = before;
     __syncthreads();
-    if (wave != 0 || row >= rows) return;
+    if (group != 0 || row >= rows) return;
     before = 0;
 #pragma unroll
-    for (int w = 0; w < kOrderWaves; ++w) before += part[w][lane];
-    const int code = (int)(mine >> 13);
+    for (int w = 0; w < 2 * kOrderWaves; ++w) before += part[w][lane];
     order[before] = row;
-    who[before] = code == 0 ? kNone : code == (int)count + 1 ? kUnknown : code - 1;
+    who[before] = who_of(adapters[row], count);
+}
+
+// Sums of products of 16 rows of `a` (lane l: row l % 16, already advanced to its quarter of 64 bytes) and 16 of each of NB groups of `x`, over steps first,
+// first + stride, ..: AHEAD steps under way at a time.
+template <bool TWO, int BM, int NB, int AHEAD>
+__device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const char *const (&x)[NB], int first, int stride, int steps, floatx4 (&acc)[BM][NB])
+{
+    auto load = [&](int s, halfx8 (&fa)[BM][2], halfx8 (&fx)[NB][2]) {
+        const int64_t at = (int64_t)s * kStepBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int m = 0; m < BM; ++m) fa[m][h] = *reinterpret_cast<const halfx8 *>(a[m] + at + 64 * h);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) fx[n][h] = *reinterpret_cast<const halfx8 *>(x[n] + at + 64 * h);
+        }
+    };
+    auto multiply = [&](const halfx8 (&fa)[BM][2], const halfx8 (&fx)[NB][2]) {
+#pragma unroll
+        for (int m = 0; m < BM; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                if (TWO) {
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][0], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][1], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
+                } else {
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][1], acc[m][n], 0, 0, 0);
+                }
+            }
+    };
+    int s = first;
+    for (; s + (AHEAD - 1) * stride < steps; s += AHEAD * stride) {
+        halfx8 fa[AHEAD][BM][2], fx[AHEAD][NB][2];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load(s + u * stride, fa[u], fx[u]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) multiply(fa[u], fx[u]);
+    }
+    for (; s < steps; s += stride) {
+        halfx8 fa[BM][2], fx[NB][2];
+        load(s, fa, fx);
+        multiply(fa, fx);
+    }
 }
 
 // Inner products of 16 rows with 16 rows of their adapters' A, as three numbers of 16 bits each whose sum they are. Slot s of a tile takes the adapters number
@@ -158,34 +204,11 @@ __global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
         if (number % job.slots != slot) continue;
         const int64_t row_a = (int64_t)adapter * job.ranks + 16 * block;
         const char *a = job.a + (row_a + col) * job.pitch + 16 * quarter;
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int s = wave; s < job.steps; s += kInnerWaves * kInnerAhead) {
-            halfx8 fa[kInnerAhead][2], fx[kInnerAhead][2];
-#pragma unroll
-            for (int u = 0; u < kInnerAhead; ++u) {
-                const int64_t at = (int64_t)std::min(s + u * kInnerWaves, job.steps - 1) * kStepBytes;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    fa[u][h] = *reinterpret_cast<const halfx8 *>(a + at + 64 * h);
-                    fx[u][h] = *reinterpret_cast<const halfx8 *>(x + at + 64 * h);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kInnerAhead; ++u) {
-                if (s + u * kInnerWaves >= job.steps) break;
-                if (TWO) {
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][1], fx[u][0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][1], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][0], acc, 0, 0, 0);
-                } else {
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][0], fx[u][0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[u][1], fx[u][1], acc, 0, 0, 0);
-                }
-            }
-        }
+        floatx4 acc[1][1] = {{{0.f, 0.f, 0.f, 0.f}}};
+        multiply_steps<TWO, 1, 1, kInnerAhead>({a}, {x}, wave, kInnerWaves, job.steps, acc);
         __syncthreads();                // (what was read before has been)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][e][lane] = acc[e];
+        for (int e = 0; e < 4; ++e) part[wave][e][lane] = acc[0][0][e];
         __syncthreads();
         if (wave < 4 && its) {          // element `wave` of every lane
             float sum = 0.f;
@@ -197,6 +220,148 @@ __global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
 #pragma unroll
             for (int i = 0; i < 3; ++i) to[i * job.ranks] = t.v[i];
         }
+    }
+}
+
+// Few rows: shared and inner products straight from the packed rows, in one launch. A workgroup has 16 BM rows of W, or 16 of an adapter's A with the 16 rows of X
+// that a slot of a tile has, and a cut of the columns; its wavefronts share the steps. What it leaves are sums of products as they are, which join_kernel scales and
+// adds up. Bound by reading W and the adapters once.
+constexpr int64_t kFewGroups = 256;
+constexpr int kFewWaves = 8, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks;
+struct FewJob {
+    const char *x, *w, *a;              // packed
+    int64_t pitch, C;
+    const int64_t *adapters;
+    int64_t count;
+    float *shared, *inner;              // [cuts][rows][C], [cuts_inner][rows][ranks]
+    int rows, ranks, rank_blocks, slots, steps, cuts, per_cut, cuts_inner, per_cut_inner;
+    unsigned inner_groups;
+};
+template <bool TWO, int BM, int NB>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
+{
+    __shared__ float part[kFewWaves][BM * NB * 4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+    if (blockIdx.x < job.inner_groups) {
+        int id = blockIdx.x;
+        const int cut = id % job.cuts_inner;
+        id /= job.cuts_inner;
+        const int slot = id % job.slots;
+        id /= job.slots;
+        const int block = id % job.rank_blocks, n = id / job.rank_blocks * 16 + col;
+        const int mine = n < job.rows ? who_of(job.adapters[n], job.count) : kNone;
+        const char *x = job.x + (int64_t)(n < job.rows ? n : job.rows - 1) * job.pitch + 16 * quarter;
+        const int last = std::min(job.steps, (cut + 1) * job.per_cut_inner);
+        uint32_t left = (uint32_t)(__ballot(mine >= 0) & 0xffff);
+        for (int number = 0; left != 0; ++number) {
+            const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+            const bool its = mine == adapter;
+            left &= ~(uint32_t)(__ballot(its) & 0xffff);
+            if (number % job.slots != slot) continue;
+            const char *a = job.a + ((int64_t)adapter * job.ranks + 16 * block + col) * job.pitch + 16 * quarter;
+            floatx4 acc[1][1] = {{{0.f, 0.f, 0.f, 0.f}}};
+            multiply_steps<TWO, 1, 1, kFewAhead>({a}, {x}, cut * job.per_cut_inner + wave, kFewWaves, last, acc);
+            __syncthreads();                // (what was read before has been)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][e][lane] = acc[0][0][e];
+            __syncthreads();
+            if (wave < 4 && its) {          // element `wave` of every lane
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) sum += part[w][wave][lane];
+                job.inner[((int64_t)cut * job.rows + n) * job.ranks + 16 * block + 4 * quarter + wave] = sum;
+            }
+        }
+        return;
+    }
+    const unsigned id = blockIdx.x - job.inner_groups;
+    const int cut = (int)(id % job.cuts), last = std::min(job.steps, (cut + 1) * job.per_cut);
+    const int64_t c0 = (int64_t)(id / job.cuts) * (16 * BM);
+    const char *w[BM], *x[NB];
+#pragma unroll
+    for (int m = 0; m < BM; ++m) w[m] = job.w + std::min<int64_t>(c0 + 16 * m + col, job.C - 1) * job.pitch + 16 * quarter;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) x[n] = job.x + (int64_t)std::min(16 * n + col, job.rows - 1) * job.pitch + 16 * quarter;
+    floatx4 acc[BM][NB];
+#pragma unroll
+    for (int m = 0; m < BM; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    multiply_steps<TWO, BM, NB, kFewAhead>(w, x, cut * job.per_cut + wave, kFewWaves, last, acc);
+#pragma unroll
+    for (int m = 0; m < BM; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][(n * 4 + e) * BM + m][lane] = acc[m][n][e];
+    __syncthreads();
+    // (n, class) places, classes fastest: 16 BM of them are together in memory
+    for (int at = threadIdx.x; at < BM * NB * 4 * 64; at += 64 * kFewWaves) {
+        const int c = at % (16 * BM), row = at / (16 * BM), m = c / 16, r = c % 16;
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v) sum += part[v][((row / 16) * 4 + r % 4) * BM + m][16 * (r / 4) + row % 16];
+        if (row < job.rows && c0 + c < job.C) job.shared[((int64_t)cut * job.rows + row) * job.C + c0 + c] = sum;
+    }
+}
+
+// The sums of the cuts, scaled, and B's part, by multiply-adds: a lane has a class, and goes through some of the rows.
+struct JoinJob {
+    const float *shared, *inner;
+    const uint32_t *largest_x, *largest_w, *largest_a;
+    const float *scale;
+    const int64_t *adapters;
+    int64_t count, C, ld;
+    const void *B;
+    float *out;
+    int rows, rows_each, ranks, ranks_b, cuts, cuts_inner;
+};
+constexpr int kJoinThreads = 256, kMostRank = 256;
+template <bool BF16>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
+{
+    __shared__ __attribute__((aligned(16))) float s[kMostRank];
+    const int64_t c = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+    const int first = blockIdx.y * job.rows_each, last = std::min(job.rows, first + job.rows_each);
+    const int shift_w = c < job.C ? shift_of(job.largest_w[c]) : 0;
+    for (int n = first; n < last; ++n) {
+        const int adapter = who_of(job.adapters[n], job.count), shift_x = shift_of(job.largest_x[n]);
+        float v = 0.f;
+        if (c < job.C) {
+            for (int p = 0; p < job.cuts; ++p) v += job.shared[((int64_t)p * job.rows + n) * job.C + c];
+            v = ldexpf(v, -shift_x - shift_w);
+        }
+        if (adapter >= 0) {
+            __syncthreads();                // (what was read before has been)
+            for (int r = threadIdx.x; r < job.ranks; r += kJoinThreads) {
+                float sum = 0.f;
+                for (int p = 0; p < job.cuts_inner; ++p) sum += job.inner[((int64_t)p * job.rows + n) * job.ranks + r];
+                s[r] = ldexpf(sum, -shift_x - shift_of(job.largest_a[(int64_t)adapter * job.ranks + r])) * job.scale[adapter];
+            }
+            __syncthreads();
+            if (c < job.C) {
+                float sum = 0.f;
+                const int64_t row = ((int64_t)adapter * job.C + c) * job.ranks_b;
+                if constexpr (BF16) {
+                    for (int r = 0; r < job.ranks_b; r += 8) {
+                        float b[8];
+                        rows8::load(static_cast<const uint16_t *>(job.B) + row + r, 0, 8, b);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum = fmaf(s[r + e], b[e], sum);
+                    }
+                } else {
+                    for (int r = 0; r < job.ranks_b; r += 4) {
+                        const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(job.B) + row + r);
+                        sum = fmaf(s[r], b.x, sum);
+                        sum = fmaf(s[r + 1], b.y, sum);
+                        sum = fmaf(s[r + 2], b.z, sum);
+                        sum = fmaf(s[r + 3], b.w, sum);
+                    }
+                }
+                v += sum;
+            }
+        }
+        if (c < job.C) job.out[n * job.ld + c] = adapter == kUnknown ? NAN : v;
     }
 }
 
@@ -339,6 +504,70 @@ Workspace workspace_of(const Layout &z, int64_t rows)
     return w;
 }
 
+// Few rows: how the columns are cut, so that there are workgroups enough.
+struct Few {
+    int blocks, wide, cuts, per_cut, slots, cuts_inner, per_cut_inner;      // groups of 16 rows of X, of W a workgroup
+    int64_t groups, inner_groups;
+    size_t x, largest_x, shared, inner, bytes;
+};
+Few few_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
+{
+    Few f;
+    const int64_t steps = plane_steps(s.K, !s.bf16);
+    auto cut = [&](int64_t groups, int *cuts, int *per_cut) {
+        const int64_t most = std::max<int64_t>(1, steps / (2 * kFewWaves)), wanted = std::max<int64_t>(1, std::min(most, kFewGroups / groups));
+        *per_cut = (int)((steps + wanted - 1) / wanted);
+        *cuts = (int)((steps + *per_cut - 1) / *per_cut);
+    };
+    f.blocks = (int)((rows + 15) / 16);
+    if (f.blocks == 3) f.blocks = 4;
+    f.wide = s.C >= 16 * 2 * kFewGroups ? 2 : 1;
+    f.groups = (s.C + 16 * f.wide - 1) / (16 * f.wide);
+    cut(f.groups, &f.cuts, &f.per_cut);
+    f.slots = (int)std::min<int64_t>(16, std::min(s.count, rows));
+    f.inner_groups = (rows + 15) / 16 * (z.ranks / 16) * f.slots;
+    cut(f.inner_groups, &f.cuts_inner, &f.per_cut_inner);
+    f.groups *= f.cuts;
+    f.inner_groups *= f.cuts_inner;
+    f.x = 0;
+    f.largest_x = f.x + up((size_t)rows * z.pitch);
+    f.shared = f.largest_x + up((size_t)rows * 4);
+    f.inner = f.shared + up((size_t)f.cuts * rows * s.C * 4);
+    f.bytes = f.inner + up((size_t)f.cuts_inner * rows * z.ranks * 4) + 256;
+    return f;
+}
+size_t bytes_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows) { return rows <= kFewRows ? few_of(s, z, rows).bytes : workspace_of(z, rows).bytes; }
+
+// (f: of as many rows or more)
+hipError_t launch_few(const Few &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
+                      float *out, int64_t ld_out, char *ws, hipStream_t stream)
+{
+    const bool bf16 = s.bf16 != 0;
+    uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + f.largest_x);
+    float *shared = reinterpret_cast<float *>(ws + f.shared), *inner = reinterpret_cast<float *>(ws + f.inner);
+    RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0}, bf16, stream));
+    const FewJob job = {ws + f.x, lay + z.w, lay + z.a, z.pitch, s.C, adapters, s.count, shared, inner, (int)rows, z.ranks, z.ranks / 16, f.slots,
+                        (int)plane_steps(s.K, !bf16), f.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
+    auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)(f.groups + f.inner_groups)), 64 * kFewWaves, 0, stream>>>(job); };
+    auto launch_blocks = [&](auto two) {
+        constexpr bool TWO = decltype(two)::value;
+        if (f.wide == 2) f.blocks == 1 ? launch(few_kernel<TWO, 2, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 2, 2>) : launch(few_kernel<TWO, 2, 4>);
+        else f.blocks == 1 ? launch(few_kernel<TWO, 1, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 1, 2>) : launch(few_kernel<TWO, 1, 4>);
+    };
+    if (bf16) launch_blocks(std::false_type());
+    else launch_blocks(std::true_type());
+    RFSF_TRY(hipGetLastError());
+    const int64_t across = (s.C + kJoinThreads - 1) / kJoinThreads;
+    const int each = (int)std::max<int64_t>(1, rows * across / (4 * kFewGroups));
+    const JoinJob join = {shared, inner, largest_x, reinterpret_cast<const uint32_t *>(lay + z.largest_w), reinterpret_cast<const uint32_t *>(lay + z.largest_a),
+                          reinterpret_cast<const float *>(lay + z.scale), adapters, s.count, s.C, ld_out, lay + z.b, out, (int)rows, each, z.ranks, z.ranks_b, f.cuts,
+                          f.cuts_inner};
+    const dim3 grid((unsigned)across, (unsigned)((rows + each - 1) / each));
+    if (bf16) join_kernel<true><<<grid, kJoinThreads, 0, stream>>>(join);
+    else join_kernel<false><<<grid, kJoinThreads, 0, stream>>>(join);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t adapters_layout_bytes(const rfsf_adapters_shape &s) { return layout_of(s).bytes; }
@@ -346,8 +575,9 @@ size_t adapters_layout_bytes(const rfsf_adapters_shape &s) { return layout_of(s)
 void adapted_scores_bytes(const rfsf_adapters_shape &s, int64_t N, size_t *recommended, size_t *minimum)
 {
     const Layout z = layout_of(s);
-    *recommended = workspace_of(z, std::min<int64_t>(std::max<int64_t>(N, 1), kMostRows)).bytes;
-    *minimum = workspace_of(z, 1).bytes;
+    // (a smaller workspace means fewer rows at a time, which may need more than more rows do: parts of few rows are kept apart)
+    *minimum = bytes_of(s, z, 1);
+    *recommended = std::max(*minimum, bytes_of(s, z, std::min<int64_t>(std::max<int64_t>(N, 1), kMostRows)));
 }
 
 hipError_t launch_adapters_weights(const rfsf_adapters_shape &s, const void *W, int64_t ld_w, void *layout, hipStream_t stream)
@@ -383,7 +613,7 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
     const char *lay = static_cast<const char *>(layout);
     const bool bf16 = s.bf16 != 0;
     int64_t most = std::min<int64_t>(N, kMostRows);
-    while (most > 1 && workspace_of(z, most).bytes > bytes) most = (most + 1) / 2;
+    while (most > 1 && bytes_of(s, z, most) > bytes) most = (most + 1) / 2;
     const Workspace w = workspace_of(z, most);
     const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
     char *ws = static_cast<char *>(workspace) + (mis ? 256 - mis : 0);
@@ -395,9 +625,15 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
     const int64_t steps = plane_steps(s.K, !bf16);
     for (int64_t n0 = 0; n0 < N; n0 += most) {
         const int64_t rows = std::min(N - n0, most);
-        order_kernel<<<dim3((unsigned)((rows + 63) / 64)), 64 * kOrderWaves, 0, stream>>>(adapters + n0, (int)rows, s.count, order, who);
+        const char *x_from = static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4);
+        // (the last rows of many are few, and may need more than many do)
+        if (most <= kFewRows || (rows <= kFewRows && bytes_of(s, z, rows) <= bytes)) {
+            RFSF_TRY(launch_few(few_of(s, z, most <= kFewRows ? most : rows), s, z, lay, x_from, rows, ld_x, adapters + n0, out + n0 * ld_out, ld_out, ws, stream));
+            continue;
+        }
+        order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters + n0, (int)rows, s.count, order, who);
         RFSF_TRY(hipGetLastError());
-        RFSF_TRY(pack(PackJob{static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4), rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
+        RFSF_TRY(pack(PackJob{x_from, rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
                       bf16, stream));
         const int slots = (int)std::min<int64_t>(16, 16 * std::min(s.count, rows) / rows + 1), blocks = z.ranks / 16;
         const InnerJob job = {ws + w.x, lay + z.a, z.pitch, largest_x, largest_a, scale, who, inner, (int)rows, z.ranks, blocks, slots, (int)steps};
