@@ -226,14 +226,16 @@ __global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
 // Few rows: shared and inner products straight from the packed rows, in one launch. A workgroup has 16 BM rows of W, or 16 of an adapter's A with the 16 rows of X
 // that a slot of a tile has, and a cut of the columns; its wavefronts share the steps. What it leaves are sums of products as they are, which join_kernel scales and
 // adds up. Bound by reading W and the adapters once.
-constexpr int64_t kFewGroups = 256;
-constexpr int kFewWaves = 8, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks;
+constexpr int64_t kFewGroups = 512;
+constexpr int kFewWaves = 4, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks, kWide = 2;
 struct FewJob {
     const char *x, *w, *a;              // packed
     int64_t pitch, C;
     const int64_t *adapters;
+    const int32_t *who;                 // in their place, if not null
     int64_t count;
-    float *shared, *inner;              // [cuts][rows][C], [cuts_inner][rows][ranks]
+    float *shared, *inner;              // [cuts][rows][ld], [cuts_inner][rows][ranks]
+    int64_t ld;
     int rows, ranks, rank_blocks, slots, steps, cuts, per_cut, cuts_inner, per_cut_inner;
     unsigned inner_groups;
 };
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
         const int slot = id % job.slots;
         id /= job.slots;
         const int block = id % job.rank_blocks, n = id / job.rank_blocks * 16 + col;
-        const int mine = n < job.rows ? who_of(job.adapters[n], job.count) : kNone;
+        const int mine = n >= job.rows ? kNone : job.who ? job.who[n] : who_of(job.adapters[n], job.count);
         const char *x = job.x + (int64_t)(n < job.rows ? n : job.rows - 1) * job.pitch + 16 * quarter;
         const int last = std::min(job.steps, (cut + 1) * job.per_cut_inner);
         uint32_t left = (uint32_t)(__ballot(mine >= 0) & 0xffff);
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
         float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < kFewWaves; ++v) sum += part[v][((row / 16) * 4 + r % 4) * BM + m][16 * (r / 4) + row % 16];
-        if (row < job.rows && c0 + c < job.C) job.shared[((int64_t)cut * job.rows + row) * job.C + c0 + c] = sum;
+        if (row < job.rows && c0 + c < job.C) job.shared[((int64_t)cut * job.rows + row) * job.ld + c0 + c] = sum;
     }
 }
 
@@ -311,7 +313,8 @@ struct JoinJob {
     const uint32_t *largest_x, *largest_w, *largest_a;
     const float *scale;
     const int64_t *adapters;
-    int64_t count, C, ld;
+    const int32_t *order, *who;         // of rows that are in another order; or both null
+    int64_t count, C, ld_shared, ld;
     const void *B;
     float *out;
     int rows, rows_each, ranks, ranks_b, cuts, cuts_inner;
@@ -325,16 +328,18 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
     const int first = blockIdx.y * job.rows_each, last = std::min(job.rows, first + job.rows_each);
     const int shift_w = c < job.C ? shift_of(job.largest_w[c]) : 0;
     for (int n = first; n < last; ++n) {
-        const int adapter = who_of(job.adapters[n], job.count), shift_x = shift_of(job.largest_x[n]);
+        const int adapter = job.who ? job.who[n] : who_of(job.adapters[n], job.count), shift_x = shift_of(job.largest_x[n]);
         float v = 0.f;
         if (c < job.C) {
-            for (int p = 0; p < job.cuts; ++p) v += job.shared[((int64_t)p * job.rows + n) * job.C + c];
+#pragma unroll 4
+            for (int p = 0; p < job.cuts; ++p) v += job.shared[((int64_t)p * job.rows + n) * job.ld_shared + c];
             v = ldexpf(v, -shift_x - shift_w);
         }
         if (adapter >= 0) {
             __syncthreads();                // (what was read before has been)
             for (int r = threadIdx.x; r < job.ranks; r += kJoinThreads) {
                 float sum = 0.f;
+#pragma unroll 8
                 for (int p = 0; p < job.cuts_inner; ++p) sum += job.inner[((int64_t)p * job.rows + n) * job.ranks + r];
                 s[r] = ldexpf(sum, -shift_x - shift_of(job.largest_a[(int64_t)adapter * job.ranks + r])) * job.scale[adapter];
             }
@@ -361,9 +366,32 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
                 v += sum;
             }
         }
-        if (c < job.C) job.out[n * job.ld + c] = adapter == kUnknown ? NAN : v;
+        if (c < job.C) job.out[(int64_t)(job.order ? job.order[n] : n) * job.ld + c] = adapter == kUnknown ? NAN : v;
     }
 }
+
+// The shared product's epilogue where the sum over columns is cut: the accumulators as they are, for join_kernel.
+struct Parts {
+    float *shared;              // [cuts][rows][ld]
+    int64_t ld, C;
+    int rows;
+
+    template <typename T>
+    __device__ __forceinline__ void operator()(T &t) const
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        t.each_block([&](auto &acc, int64_t first, int b) __attribute__((always_inline)) {
+            const int64_t n = t.j0 + 32 * b + col;
+            if (n >= rows) return;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = first + 8 * q + 4 * half;
+                if (i < C)              // (ld is a multiple of four: numbers beyond C are nobody's)
+                    *reinterpret_cast<float4 *>(shared + ((int64_t)t.cut * rows + n) * ld + i) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+            }
+        });
+    }
+};
 
 // The shared product's epilogue, which adds to the accumulators the sums over ranks of a block of 32 classes and 32 rows, for one adapter of the rows after the
 // other, and keeps the sums of the rows that have it. v_mfma_f32_32x32x16_bf16: lane l holds eight ranks of class (row) l % 32. B enters as it is (bfloat16) or as
@@ -380,21 +408,29 @@ struct Adapted {
     float *out;
     int64_t ld;
 
-    static constexpr int TERMS = BF16 ? 1 : 3;
-    __device__ __forceinline__ void load_b(int64_t row, int r, bf16x8 (&f)[TERMS]) const
+    static constexpr int TERMS = BF16 ? 1 : 3, WORDS = BF16 ? 4 : 8;
+    // Eight ranks of a class of an adapter, as they lie in memory.
+    __device__ __forceinline__ void load_b(int64_t row, int r, uint32_t (&v)[WORDS]) const
+    {
+        const char *from = static_cast<const char *>(B) + (row * ranks_b + r) * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) {
+            const uint4 w = r + (BF16 ? 0 : i) < ranks_b ? *reinterpret_cast<const uint4 *>(from + 4 * i) : make_uint4(0, 0, 0, 0);
+            v[i] = w.x;
+            v[i + 1] = w.y;
+            v[i + 2] = w.z;
+            v[i + 3] = w.w;
+        }
+    }
+    static __device__ __forceinline__ void terms_of_b(const uint32_t (&v)[WORDS], bf16x8 (&f)[TERMS])
     {
         if constexpr (BF16) {
-            const uint4 v = r < ranks_b ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(B) + row * ranks_b + r) : make_uint4(0, 0, 0, 0);
-            f[0] = __builtin_bit_cast(bf16x8, v);
+            f[0] = __builtin_bit_cast(bf16x8, make_uint4(v[0], v[1], v[2], v[3]));
         } else {
-            const float *from = static_cast<const float *>(B) + row * ranks_b + r;
-            float v[8];
-            *reinterpret_cast<float4 *>(v) = r < ranks_b ? *reinterpret_cast<const float4 *>(from) : make_float4(0.f, 0.f, 0.f, 0.f);
-            *reinterpret_cast<float4 *>(v + 4) = r + 4 < ranks_b ? *reinterpret_cast<const float4 *>(from + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
             uint32_t w[3][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Terms3 lo = terms3(v[2 * i]), hi = terms3(v[2 * i + 1]);
+                const Terms3 lo = terms3(__uint_as_float(v[2 * i])), hi = terms3(__uint_as_float(v[2 * i + 1]));
 #pragma unroll
                 for (int k = 0; k < 3; ++k) w[k][i] = lo.v[k] | (uint32_t)hi.v[k] << 16;
             }
@@ -440,14 +476,32 @@ struct Adapted {
                 bf16x8 s[3];
 #pragma unroll
                 for (int i = 0; i < 3; ++i) s[i] = *reinterpret_cast<const bf16x8 *>(from + i * ranks + r0);
+                // (in small tiles the next adapter's part of B is under way while the present one's is multiplied: 100 x 257, 50000 classes, 30 adapters 85 -> 63 us;
+                // in large ones, of which more rows are of one adapter, its registers are not there)
+                constexpr bool AHEAD = BM <= 2;
+                uint32_t next[BM][WORDS];
+                auto load = [&](uint64_t of, int a, int64_t first) __attribute__((always_inline)) {
+                    const int64_t adapter = (int64_t)__builtin_amdgcn_readlane(mine[b], __builtin_ctzll(of)) * C;
+                    load_b(adapter + std::min(first + col, C - 1), r0 + 8 * half, next[a]);
+                };
+                if constexpr (AHEAD) {
+#pragma unroll
+                    for (int a = 0; a < BM; ++a) load(with, a, t.i0 + 32 * a);
+                }
                 for (uint64_t left = with; left != 0;) {
-                    const int adapter = __builtin_amdgcn_readlane(mine[b], __builtin_ctzll(left));
-                    const bool its = mine[b] == adapter;
+                    const uint64_t now = left;
+                    const bool its = mine[b] == __builtin_amdgcn_readlane(mine[b], __builtin_ctzll(now));
                     left &= ~__ballot(its);
-                    auto add = [&](auto &acc, int64_t first) __attribute__((always_inline)) {
-                        if (first >= C) return;
-                        bf16x8 f[TERMS];
-                        load_b((int64_t)adapter * C + std::min(first + col, C - 1), r0 + 8 * half, f);
+                    bf16x8 f[BM][TERMS];
+                    if constexpr (AHEAD) {
+#pragma unroll
+                        for (int a = 0; a < BM; ++a) terms_of_b(next[a], f[a]);
+                        if (left != 0) {
+#pragma unroll
+                            for (int a = 0; a < BM; ++a) load(left, a, t.i0 + 32 * a);
+                        }
+                    }
+                    auto add = [&](auto &acc, const bf16x8 (&f)[TERMS]) __attribute__((always_inline)) {
                         floatx16 sum = {};
                         if constexpr (!BF16) {
                             sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[2], s[0], sum, 0, 0, 0);
@@ -461,9 +515,22 @@ struct Adapted {
                         for (int e = 0; e < 16; ++e) acc[e] += its ? sum[e] : 0.f;
                     };
 #pragma unroll
-                    for (int a = 0; a < BM; ++a) add(t.acc[a][b], t.i0 + 32 * a);
-                    if constexpr (T::HAS_EXTRA)
-                        if (b == t.wave_i) add(t.extra, t.extra_i);
+                    for (int a = 0; a < BM; ++a) {
+                        if constexpr (!AHEAD) {
+                            if (t.i0 + 32 * a >= C) continue;
+                            load(now, 0, t.i0 + 32 * a);
+                            terms_of_b(next[0], f[a]);
+                        }
+                        add(t.acc[a][b], f[a]);
+                    }
+                    if constexpr (T::HAS_EXTRA) {
+                        static_assert(!AHEAD, "");
+                        if (b == t.wave_i) {
+                            load(now, 0, t.extra_i);
+                            terms_of_b(next[0], f[0]);
+                            add(t.extra, f[0]);
+                        }
+                    }
                 }
             }
         }
@@ -504,64 +571,126 @@ Workspace workspace_of(const Layout &z, int64_t rows)
     return w;
 }
 
-// Few rows: how the columns are cut, so that there are workgroups enough.
-struct Few {
-    int blocks, wide, cuts, per_cut, slots, cuts_inner, per_cut_inner;      // groups of 16 rows of X, of W a workgroup
-    int64_t groups, inner_groups;
-    size_t x, largest_x, shared, inner, bytes;
+// Sums over columns cut into parts, which join_kernel adds up, so that there are workgroups enough: few rows straight from their packed form, more of them as tiles.
+struct Split {
+    int edge;                                           // of tiles; 0: straight
+    int blocks, wide;                                   // straight: groups of 16 rows of X, of W a workgroup
+    int cuts, per_cut, slots, cuts_inner, per_cut_inner;
+    int64_t groups, inner_groups, ld;
+    size_t x, largest_x, order, who, shared, inner, bytes;
 };
-Few few_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
+int slots_of(int64_t count, int64_t rows) { return (int)std::min<int64_t>(16, rows <= 16 ? std::min(count, rows) : 16 * std::min(count, rows) / rows + 1); }
+int blocks_of(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : kFewBlocks; }
+int wide_of(int64_t C) { return C >= 16 * kWide ? kWide : 1; }
+Split split_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows, int edge, int cuts)
 {
-    Few f;
+    Split f;
     const int64_t steps = plane_steps(s.K, !s.bf16);
-    auto cut = [&](int64_t groups, int *cuts, int *per_cut) {
-        const int64_t most = std::max<int64_t>(1, steps / (2 * kFewWaves)), wanted = std::max<int64_t>(1, std::min(most, kFewGroups / groups));
-        *per_cut = (int)((steps + wanted - 1) / wanted);
-        *cuts = (int)((steps + *per_cut - 1) / *per_cut);
+    auto cut = [&](int64_t wanted, int *cuts_, int *per_cut) {
+        const int64_t most = std::max<int64_t>(1, std::min(steps / (kFewAhead * kFewWaves), wanted));
+        *per_cut = (int)((steps + most - 1) / most);
+        *cuts_ = (int)((steps + *per_cut - 1) / *per_cut);
     };
-    f.blocks = (int)((rows + 15) / 16);
-    if (f.blocks == 3) f.blocks = 4;
-    f.wide = s.C >= 16 * 2 * kFewGroups ? 2 : 1;
-    f.groups = (s.C + 16 * f.wide - 1) / (16 * f.wide);
-    cut(f.groups, &f.cuts, &f.per_cut);
-    f.slots = (int)std::min<int64_t>(16, std::min(s.count, rows));
+    f.edge = edge;
+    f.blocks = f.wide = 0;
+    f.groups = 0;
+    if (edge == 0) {
+        f.blocks = blocks_of(rows);
+        f.wide = wide_of(s.C);
+        f.groups = (s.C + 16 * f.wide - 1) / (16 * f.wide);
+        cut(kFewGroups / f.groups, &f.cuts, &f.per_cut);
+        f.groups *= f.cuts;
+    } else {
+        f.per_cut = (int)((steps + cuts - 1) / cuts);
+        f.cuts = (int)((steps + f.per_cut - 1) / f.per_cut);
+    }
+    f.slots = edge == 0 ? (int)std::min<int64_t>(16, std::min(s.count, rows)) : slots_of(s.count, rows);
     f.inner_groups = (rows + 15) / 16 * (z.ranks / 16) * f.slots;
-    cut(f.inner_groups, &f.cuts_inner, &f.per_cut_inner);
-    f.groups *= f.cuts;
+    cut(kFewGroups / f.inner_groups, &f.cuts_inner, &f.per_cut_inner);
     f.inner_groups *= f.cuts_inner;
+    f.ld = (s.C + 3) / 4 * 4;
     f.x = 0;
     f.largest_x = f.x + up((size_t)rows * z.pitch);
-    f.shared = f.largest_x + up((size_t)rows * 4);
-    f.inner = f.shared + up((size_t)f.cuts * rows * s.C * 4);
+    f.order = f.largest_x + up((size_t)rows * 4);
+    f.who = f.order + up((size_t)rows * 4);
+    f.shared = f.who + up((size_t)rows * 4);
+    f.inner = f.shared + up((size_t)f.cuts * rows * f.ld * 4);
     f.bytes = f.inner + up((size_t)f.cuts_inner * rows * z.ranks * 4) + 256;
     return f;
 }
-size_t bytes_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows) { return rows <= kFewRows ? few_of(s, z, rows).bytes : workspace_of(z, rows).bytes; }
+
+// The way of a number of rows, by estimates of its time in us: straight, bound by what the L2s deliver to the CUs (rows of W and X); tiles with B's part in their
+// epilogue, which costs them some us each; tiles whose sums are cut where they would not fill the CUs; and join_kernel, bound by its reads and writes.
+// (Straight, tiles, cut tiles, us, float32: 20 x 5121, 5003 classes, 50 adapters of rank 16 39, 83, 39; 40 rows 52, 85, 41; 330 rows -, 124, 106; 64 x 1025, 1000
+// classes 17, 29, 20; 64 x 1025, 30000 classes 75, 47, 61; bfloat16: 64 x 257, 50000 classes 52, 37, 55; 180 x 2049, 2000 classes -, 44, 31.)
+struct Way { bool split; int edge, cuts; };
+Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
+{
+    const int64_t steps = plane_steps(s.K, !s.bf16);
+    auto join = [&](int cuts) { return (double)rows * (double)s.C * (4.0 * cuts + 4.0 + (s.bf16 ? 2 : 4) * z.ranks_b) / 4.0e6; };
+    Way best = {false, 0, 0};
+    double least = 0.0;
+    auto consider = [&](bool split, int edge, int cuts, double time) {
+        if (best.cuts == 0 || time < least) {
+            best = {split, edge, cuts};
+            least = time;
+        }
+    };
+    if (rows <= kFewRows) {
+        const Split f = split_of(s, z, rows, 0, 0);
+        const double moved = ((double)f.groups / f.cuts * 16.0 * (f.wide + f.blocks) + (double)f.inner_groups / f.cuts_inner * 32.0) * (double)steps * kStepBytes;
+        consider(true, 0, f.cuts, 11.0 + moved / (f.blocks == 1 ? 9.0e6 : f.blocks == 2 ? 8.0e6 : 7.0e6) + join(f.cuts));
+    }
+    for (const PlaneWay &way : kPlaneWays) {
+        const double tiles = (double)plane_tiles(s.C, rows, way.edge);
+        consider(false, way.edge, 1, 18.0 + plane_step_time(way, tiles) * (double)steps + (way.edge == 256 ? 18.0 : way.edge == 128 ? 9.0 : 4.0) * std::max(1.0, tiles / way.slots));
+        for (int cuts : {2, 3, 4, 5, 6, 8, 10, 12, 16})
+            if (steps / cuts >= 8) consider(true, way.edge, cuts, 18.0 + plane_step_time(way, tiles * cuts) * (double)((steps + cuts - 1) / cuts) + join(cuts));
+    }
+    return best;
+}
+size_t bytes_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
+{
+    const Way w = way_of(s, z, rows);
+    return w.split ? split_of(s, z, rows, w.edge, w.cuts).bytes : workspace_of(z, rows).bytes;
+}
 
 // (f: of as many rows or more)
-hipError_t launch_few(const Few &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
-                      float *out, int64_t ld_out, char *ws, hipStream_t stream)
+hipError_t launch_split(const Split &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
+                        float *out, int64_t ld_out, char *ws, hipStream_t stream)
 {
     const bool bf16 = s.bf16 != 0;
+    const int64_t steps = plane_steps(s.K, !bf16);
     uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + f.largest_x);
     float *shared = reinterpret_cast<float *>(ws + f.shared), *inner = reinterpret_cast<float *>(ws + f.inner);
-    RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0}, bf16, stream));
-    const FewJob job = {ws + f.x, lay + z.w, lay + z.a, z.pitch, s.C, adapters, s.count, shared, inner, (int)rows, z.ranks, z.ranks / 16, f.slots,
-                        (int)plane_steps(s.K, !bf16), f.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
+    int32_t *order = nullptr, *who = nullptr;
+    if (f.edge != 0) {
+        order = reinterpret_cast<int32_t *>(ws + f.order);
+        who = reinterpret_cast<int32_t *>(ws + f.who);
+        order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters, (int)rows, s.count, order, who);
+        RFSF_TRY(hipGetLastError());
+    }
+    RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
+    const FewJob job = {ws + f.x, lay + z.w, lay + z.a, z.pitch, s.C, adapters, who, s.count, shared, inner, f.ld, (int)rows, z.ranks, z.ranks / 16, f.slots, (int)steps,
+                        f.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
     auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)(f.groups + f.inner_groups)), 64 * kFewWaves, 0, stream>>>(job); };
     auto launch_blocks = [&](auto two) {
         constexpr bool TWO = decltype(two)::value;
-        if (f.wide == 2) f.blocks == 1 ? launch(few_kernel<TWO, 2, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 2, 2>) : launch(few_kernel<TWO, 2, 4>);
-        else f.blocks == 1 ? launch(few_kernel<TWO, 1, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 1, 2>) : launch(few_kernel<TWO, 1, 4>);
+        if (f.wide == kWide) f.blocks == 1 ? launch(few_kernel<TWO, kWide, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, kWide, 2>) : launch(few_kernel<TWO, kWide, 4>);
+        else f.blocks <= 1 ? launch(few_kernel<TWO, 1, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 1, 2>) : launch(few_kernel<TWO, 1, 4>);
     };
     if (bf16) launch_blocks(std::false_type());
     else launch_blocks(std::true_type());
     RFSF_TRY(hipGetLastError());
+    if (f.edge != 0) {
+        const Product<Parts> p = {{lay + z.w, z.pitch, s.C}, {ws + f.x, z.pitch, rows}, steps, {shared, f.ld, s.C, (int)rows}, f.per_cut};
+        RFSF_TRY(bf16 ? launch_plane_products<kHalf>(&p, 1, f.edge, stream) : launch_plane_products<kHalfTwo>(&p, 1, f.edge, stream));
+    }
     const int64_t across = (s.C + kJoinThreads - 1) / kJoinThreads;
     const int each = (int)std::max<int64_t>(1, rows * across / (4 * kFewGroups));
     const JoinJob join = {shared, inner, largest_x, reinterpret_cast<const uint32_t *>(lay + z.largest_w), reinterpret_cast<const uint32_t *>(lay + z.largest_a),
-                          reinterpret_cast<const float *>(lay + z.scale), adapters, s.count, s.C, ld_out, lay + z.b, out, (int)rows, each, z.ranks, z.ranks_b, f.cuts,
-                          f.cuts_inner};
+                          reinterpret_cast<const float *>(lay + z.scale), adapters, order, who, s.count, s.C, f.ld, ld_out, lay + z.b, out, (int)rows, each, z.ranks,
+                          z.ranks_b, f.cuts, f.cuts_inner};
     const dim3 grid((unsigned)across, (unsigned)((rows + each - 1) / each));
     if (bf16) join_kernel<true><<<grid, kJoinThreads, 0, stream>>>(join);
     else join_kernel<false><<<grid, kJoinThreads, 0, stream>>>(join);
@@ -626,23 +755,25 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
     for (int64_t n0 = 0; n0 < N; n0 += most) {
         const int64_t rows = std::min(N - n0, most);
         const char *x_from = static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4);
-        // (the last rows of many are few, and may need more than many do)
-        if (most <= kFewRows || (rows <= kFewRows && bytes_of(s, z, rows) <= bytes)) {
-            RFSF_TRY(launch_few(few_of(s, z, most <= kFewRows ? most : rows), s, z, lay, x_from, rows, ld_x, adapters + n0, out + n0 * ld_out, ld_out, ws, stream));
+        // (the last rows of many are fewer, which may need more room than many do: their way is taken if there is that)
+        const bool last = rows < most && bytes_of(s, z, rows) <= bytes;
+        const Way way = way_of(s, z, last ? rows : most);
+        if (way.split) {
+            RFSF_TRY(launch_split(split_of(s, z, last ? rows : most, way.edge, way.cuts), s, z, lay, x_from, rows, ld_x, adapters + n0, out + n0 * ld_out, ld_out, ws, stream));
             continue;
         }
         order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters + n0, (int)rows, s.count, order, who);
         RFSF_TRY(hipGetLastError());
         RFSF_TRY(pack(PackJob{x_from, rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
                       bf16, stream));
-        const int slots = (int)std::min<int64_t>(16, 16 * std::min(s.count, rows) / rows + 1), blocks = z.ranks / 16;
+        const int slots = slots_of(s.count, rows), blocks = z.ranks / 16;
         const InnerJob job = {ws + w.x, lay + z.a, z.pitch, largest_x, largest_a, scale, who, inner, (int)rows, z.ranks, blocks, slots, (int)steps};
         const dim3 grid((unsigned)((rows + 15) / 16 * blocks * slots));
         if (bf16) inner_kernel<false><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
         else inner_kernel<true><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
         RFSF_TRY(hipGetLastError());
         const Planes w_rows = {lay + z.w, z.pitch, s.C}, x_rows = {ws + w.x, z.pitch, rows};
-        const int edge = plane_tile(s.C, rows);
+        const int edge = way.edge;
         float *to = out + n0 * ld_out;
         RFSF_TRY(bf16 ? launch_plane_product<kHalf>(w_rows, x_rows, steps, edge, Adapted<true>{largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks,
                                                                                               z.ranks_b, to, ld_out}, stream)
