@@ -173,59 +173,9 @@ __device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const
     }
 }
 
-// Inner products of 16 rows with 16 rows of their adapters' A, as three numbers of 16 bits each whose sum they are. Slot s of a tile takes the adapters number
-// s, s + slots, .. of those that its rows have. The wavefronts share the steps, four of them under way at a time.
-constexpr int kInnerWaves = 8, kInnerAhead = 4;
-struct InnerJob {
-    const char *x, *a;                  // packed
-    int64_t pitch;
-    const uint32_t *largest_x, *largest_a;
-    const float *scale;
-    const int32_t *who;
-    uint16_t *inner;                    // [rows][3][ranks], bits of bfloat16
-    int rows, ranks, rank_blocks, slots, steps;
-};
-template <bool TWO>
-__global__ __launch_bounds__(64 * kInnerWaves) void inner_kernel(InnerJob job)
-{
-    __shared__ float part[kInnerWaves][4][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
-    int id = blockIdx.x;
-    const int slot = id % job.slots;
-    id /= job.slots;
-    const int block = id % job.rank_blocks, n = id / job.rank_blocks * 16 + col;
-    const int mine = n < job.rows ? job.who[n] : kNone;
-    const char *x = job.x + (int64_t)(n < job.rows ? n : job.rows - 1) * job.pitch + 16 * quarter;
-    uint32_t left = (uint32_t)(__ballot(mine >= 0) & 0xffff);
-    for (int number = 0; left != 0; ++number) {
-        const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-        const bool its = mine == adapter;
-        left &= ~(uint32_t)(__ballot(its) & 0xffff);
-        if (number % job.slots != slot) continue;
-        const int64_t row_a = (int64_t)adapter * job.ranks + 16 * block;
-        const char *a = job.a + (row_a + col) * job.pitch + 16 * quarter;
-        floatx4 acc[1][1] = {{{0.f, 0.f, 0.f, 0.f}}};
-        multiply_steps<TWO, 1, 1, kInnerAhead>({a}, {x}, wave, kInnerWaves, job.steps, acc);
-        __syncthreads();                // (what was read before has been)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][e][lane] = acc[0][0][e];
-        __syncthreads();
-        if (wave < 4 && its) {          // element `wave` of every lane
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < kInnerWaves; ++w) sum += part[w][wave][lane];
-            const int r = 16 * block + 4 * quarter + wave;
-            const Terms3 t = terms3(ldexpf(sum, -shift_of(job.largest_x[n]) - shift_of(job.largest_a[(int64_t)adapter * job.ranks + r])) * job.scale[adapter]);
-            uint16_t *to = job.inner + (int64_t)n * 3 * job.ranks + r;
-#pragma unroll
-            for (int i = 0; i < 3; ++i) to[i * job.ranks] = t.v[i];
-        }
-    }
-}
-
-// Few rows: shared and inner products straight from the packed rows, in one launch. A workgroup has 16 BM rows of W, or 16 of an adapter's A with the 16 rows of X
-// that a slot of a tile has, and a cut of the columns; its wavefronts share the steps. What it leaves are sums of products as they are, which join_kernel scales and
-// adds up. Bound by reading W and the adapters once.
+// Inner products, and for few rows the shared ones, straight from the packed rows. A workgroup has 16 rows of an adapter's A and 16 of X, of which it keeps what belongs to
+// rows of this adapter, or 16 BM rows of W, and a cut of the columns; its wavefronts share the steps. Slot s of a tile of 16 rows takes the adapters number s, s + slots, ..
+// of those that its rows have. What is left are sums of products as they are, which are scaled and added up where they are used. Bound by reading W and the adapters once.
 constexpr int64_t kFewGroups = 512;
 constexpr int kFewWaves = 4, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks, kWide = 2;
 struct FewJob {
@@ -370,6 +320,29 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
     }
 }
 
+// Inner products from the sums of their cuts, scaled, as three terms for Adapted.
+struct FinishJob {
+    const float *inner;
+    const uint32_t *largest_x, *largest_a;
+    const float *scale;
+    const int32_t *who;
+    uint16_t *terms;
+    int rows, ranks, cuts;
+};
+__global__ __launch_bounds__(256) void finish_kernel(FinishJob job)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int n = (int)(at / job.ranks), r = (int)(at % job.ranks);
+    if (n >= job.rows || job.who[n] < 0) return;
+    const int adapter = job.who[n];
+    float sum = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < job.cuts; ++p) sum += job.inner[((int64_t)p * job.rows + n) * job.ranks + r];
+    const Terms3 t = terms3(ldexpf(sum, -shift_of(job.largest_x[n]) - shift_of(job.largest_a[(int64_t)adapter * job.ranks + r])) * job.scale[adapter]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) job.terms[((int64_t)n * 3 + i) * job.ranks + r] = t.v[i];
+}
+
 // The shared product's epilogue where the sum over columns is cut: the accumulators as they are, for join_kernel.
 struct Parts {
     float *shared;              // [cuts][rows][ld]
@@ -402,7 +375,7 @@ struct Adapted {
     int64_t C;
     int rows;                   // of this launch, in the order of their adapters
     const int32_t *order, *who;
-    const uint16_t *inner;
+    const uint16_t *terms;      // [rows][3][ranks], of finish_kernel
     const void *B;
     int ranks, ranks_b;
     float *out;
@@ -422,20 +395,26 @@ struct Adapted {
             v[i + 3] = w.w;
         }
     }
+    static __device__ __forceinline__ void three_terms(const float (&v)[8], bf16x8 (&f)[3])
+    {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Terms3 lo = terms3(v[2 * i]), hi = terms3(v[2 * i + 1]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) w[k][i] = lo.v[k] | (uint32_t)hi.v[k] << 16;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) f[k] = __builtin_bit_cast(bf16x8, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+    }
     static __device__ __forceinline__ void terms_of_b(const uint32_t (&v)[WORDS], bf16x8 (&f)[TERMS])
     {
         if constexpr (BF16) {
             f[0] = __builtin_bit_cast(bf16x8, make_uint4(v[0], v[1], v[2], v[3]));
         } else {
-            uint32_t w[3][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Terms3 lo = terms3(__uint_as_float(v[2 * i])), hi = terms3(__uint_as_float(v[2 * i + 1]));
-#pragma unroll
-                for (int k = 0; k < 3; ++k) w[k][i] = lo.v[k] | (uint32_t)hi.v[k] << 16;
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) f[k] = __builtin_bit_cast(bf16x8, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+            float x[8];
+            __builtin_memcpy(x, v, 32);
+            three_terms(x, f);
         }
     }
     template <typename T>
@@ -471,7 +450,7 @@ struct Adapted {
             const uint64_t with = __ballot(mine[b] >= 0);
             if (with == 0) continue;
             const int64_t n = std::min<int64_t>(t.j0 + 32 * b + col, rows - 1);
-            const uint16_t *from = inner + n * 3 * ranks + 8 * half;
+            const uint16_t *from = terms + n * 3 * ranks + 8 * half;
             for (int r0 = 0; r0 < ranks; r0 += 16) {
                 bf16x8 s[3];
 #pragma unroll
@@ -556,66 +535,55 @@ struct Adapted {
     }
 };
 
-struct Workspace {
-    size_t x, largest_x, order, who, inner, bytes;
-};
-Workspace workspace_of(const Layout &z, int64_t rows)
-{
-    Workspace w;
-    w.x = 0;
-    w.largest_x = w.x + up((size_t)rows * z.pitch);
-    w.order = w.largest_x + up((size_t)rows * 4);
-    w.who = w.order + up((size_t)rows * 4);
-    w.inner = w.who + up((size_t)rows * 4);
-    w.bytes = w.inner + up((size_t)rows * 3 * z.ranks * 2) + 256;
-    return w;
-}
-
-// Sums over columns cut into parts, which join_kernel adds up, so that there are workgroups enough: few rows straight from their packed form, more of them as tiles.
-struct Split {
-    int edge;                                           // of tiles; 0: straight
+// How a number of rows is worked on. Sums over columns may be cut into parts, which join_kernel adds up, so that there are workgroups enough: those of few rows
+// straight from their packed form, those of more rows as tiles.
+struct Way { bool split; int edge, cuts; };             // edge of tiles, or 0: straight
+struct Plan {
+    Way way;
     int blocks, wide;                                   // straight: groups of 16 rows of X, of W a workgroup
-    int cuts, per_cut, slots, cuts_inner, per_cut_inner;
+    int per_cut, slots, cuts_inner, per_cut_inner;
     int64_t groups, inner_groups, ld;
-    size_t x, largest_x, order, who, shared, inner, bytes;
+    size_t x, largest_x, order, who, inner, shared, terms, bytes;       // (the last two: of a sum that is cut, and of one that is not)
 };
-int slots_of(int64_t count, int64_t rows) { return (int)std::min<int64_t>(16, rows <= 16 ? std::min(count, rows) : 16 * std::min(count, rows) / rows + 1); }
 int blocks_of(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : kFewBlocks; }
 int wide_of(int64_t C) { return C >= 16 * kWide ? kWide : 1; }
-Split split_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows, int edge, int cuts)
+Plan plan_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows, const Way &way)
 {
-    Split f;
+    Plan f;
     const int64_t steps = plane_steps(s.K, !s.bf16);
     auto cut = [&](int64_t wanted, int *cuts_, int *per_cut) {
         const int64_t most = std::max<int64_t>(1, std::min(steps / (kFewAhead * kFewWaves), wanted));
         *per_cut = (int)((steps + most - 1) / most);
         *cuts_ = (int)((steps + *per_cut - 1) / *per_cut);
     };
-    f.edge = edge;
+    f.way = way;
     f.blocks = f.wide = 0;
     f.groups = 0;
-    if (edge == 0) {
+    if (way.edge == 0) {
         f.blocks = blocks_of(rows);
         f.wide = wide_of(s.C);
         f.groups = (s.C + 16 * f.wide - 1) / (16 * f.wide);
-        cut(kFewGroups / f.groups, &f.cuts, &f.per_cut);
-        f.groups *= f.cuts;
+        cut(kFewGroups / f.groups, &f.way.cuts, &f.per_cut);
+        f.groups *= f.way.cuts;
     } else {
-        f.per_cut = (int)((steps + cuts - 1) / cuts);
-        f.cuts = (int)((steps + f.per_cut - 1) / f.per_cut);
+        f.per_cut = (int)((steps + way.cuts - 1) / way.cuts);
+        f.way.cuts = (int)((steps + f.per_cut - 1) / f.per_cut);
     }
-    f.slots = edge == 0 ? (int)std::min<int64_t>(16, std::min(s.count, rows)) : slots_of(s.count, rows);
-    f.inner_groups = (rows + 15) / 16 * (z.ranks / 16) * f.slots;
-    cut(kFewGroups / f.inner_groups, &f.cuts_inner, &f.per_cut_inner);
-    f.inner_groups *= f.cuts_inner;
+    // slots for the adapters that a tile of 16 rows has on average, or for all of them where that makes few workgroups; those without an adapter end at once
+    const int64_t tiles = (rows + 15) / 16 * (z.ranks / 16), most = std::min<int64_t>(16, std::min(s.count, rows));
+    const int64_t average = way.edge == 0 ? most : std::min(most, 16 * std::min(s.count, rows) / rows + 1);
+    f.slots = (int)average;
+    cut(kFewGroups / (tiles * average), &f.cuts_inner, &f.per_cut_inner);
+    f.inner_groups = tiles * f.slots * f.cuts_inner;
     f.ld = (s.C + 3) / 4 * 4;
     f.x = 0;
     f.largest_x = f.x + up((size_t)rows * z.pitch);
     f.order = f.largest_x + up((size_t)rows * 4);
     f.who = f.order + up((size_t)rows * 4);
-    f.shared = f.who + up((size_t)rows * 4);
-    f.inner = f.shared + up((size_t)f.cuts * rows * f.ld * 4);
-    f.bytes = f.inner + up((size_t)f.cuts_inner * rows * z.ranks * 4) + 256;
+    f.inner = f.who + up((size_t)rows * 4);
+    f.shared = f.inner + up((size_t)f.cuts_inner * rows * z.ranks * 4);
+    f.terms = f.shared;
+    f.bytes = f.shared + up(way.split ? (size_t)f.way.cuts * rows * f.ld * 4 : (size_t)rows * 3 * z.ranks * 2) + 256;
     return f;
 }
 
@@ -623,7 +591,6 @@ Split split_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows, int 
 // epilogue, which costs them some us each; tiles whose sums are cut where they would not fill the CUs; and join_kernel, bound by its reads and writes.
 // (Straight, tiles, cut tiles, us, float32: 20 x 5121, 5003 classes, 50 adapters of rank 16 39, 83, 39; 40 rows 52, 85, 41; 330 rows -, 124, 106; 64 x 1025, 1000
 // classes 17, 29, 20; 64 x 1025, 30000 classes 75, 47, 61; bfloat16: 64 x 257, 50000 classes 52, 37, 55; 180 x 2049, 2000 classes -, 44, 31.)
-struct Way { bool split; int edge, cuts; };
 Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
 {
     const int64_t steps = plane_steps(s.K, !s.bf16);
@@ -637,9 +604,10 @@ Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
         }
     };
     if (rows <= kFewRows) {
-        const Split f = split_of(s, z, rows, 0, 0);
-        const double moved = ((double)f.groups / f.cuts * 16.0 * (f.wide + f.blocks) + (double)f.inner_groups / f.cuts_inner * 32.0) * (double)steps * kStepBytes;
-        consider(true, 0, f.cuts, 11.0 + moved / (f.blocks == 1 ? 9.0e6 : f.blocks == 2 ? 8.0e6 : 7.0e6) + join(f.cuts));
+        const Plan f = plan_of(s, z, rows, {true, 0, 0});
+        const int cuts = f.way.cuts;
+        const double moved = ((double)f.groups / cuts * 16.0 * (f.wide + f.blocks) + (double)f.inner_groups / f.cuts_inner * 32.0) * (double)steps * kStepBytes;
+        consider(true, 0, cuts, 11.0 + moved / (f.blocks == 1 ? 9.0e6 : f.blocks == 2 ? 8.0e6 : 7.0e6) + join(cuts));
     }
     for (const PlaneWay &way : kPlaneWays) {
         const double tiles = (double)plane_tiles(s.C, rows, way.edge);
@@ -649,22 +617,20 @@ Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
     }
     return best;
 }
-size_t bytes_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
-{
-    const Way w = way_of(s, z, rows);
-    return w.split ? split_of(s, z, rows, w.edge, w.cuts).bytes : workspace_of(z, rows).bytes;
-}
+Plan plan_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows) { return plan_of(s, z, rows, way_of(s, z, rows)); }
 
 // (f: of as many rows or more)
-hipError_t launch_split(const Split &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
-                        float *out, int64_t ld_out, char *ws, hipStream_t stream)
+hipError_t launch_rows(const Plan &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
+                       float *out, int64_t ld_out, char *ws, hipStream_t stream)
 {
-    const bool bf16 = s.bf16 != 0;
+    const bool bf16 = s.bf16 != 0, straight = f.way.edge == 0;
     const int64_t steps = plane_steps(s.K, !bf16);
     uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + f.largest_x);
     float *shared = reinterpret_cast<float *>(ws + f.shared), *inner = reinterpret_cast<float *>(ws + f.inner);
+    const uint32_t *largest_w = reinterpret_cast<const uint32_t *>(lay + z.largest_w), *largest_a = reinterpret_cast<const uint32_t *>(lay + z.largest_a);
+    const float *scale = reinterpret_cast<const float *>(lay + z.scale);
     int32_t *order = nullptr, *who = nullptr;
-    if (f.edge != 0) {
+    if (!straight) {
         order = reinterpret_cast<int32_t *>(ws + f.order);
         who = reinterpret_cast<int32_t *>(ws + f.who);
         order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters, (int)rows, s.count, order, who);
@@ -672,7 +638,7 @@ hipError_t launch_split(const Split &f, const rfsf_adapters_shape &s, const Layo
     }
     RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
     const FewJob job = {ws + f.x, lay + z.w, lay + z.a, z.pitch, s.C, adapters, who, s.count, shared, inner, f.ld, (int)rows, z.ranks, z.ranks / 16, f.slots, (int)steps,
-                        f.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
+                        f.way.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
     auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)(f.groups + f.inner_groups)), 64 * kFewWaves, 0, stream>>>(job); };
     auto launch_blocks = [&](auto two) {
         constexpr bool TWO = decltype(two)::value;
@@ -682,15 +648,27 @@ hipError_t launch_split(const Split &f, const rfsf_adapters_shape &s, const Layo
     if (bf16) launch_blocks(std::false_type());
     else launch_blocks(std::true_type());
     RFSF_TRY(hipGetLastError());
-    if (f.edge != 0) {
-        const Product<Parts> p = {{lay + z.w, z.pitch, s.C}, {ws + f.x, z.pitch, rows}, steps, {shared, f.ld, s.C, (int)rows}, f.per_cut};
-        RFSF_TRY(bf16 ? launch_plane_products<kHalf>(&p, 1, f.edge, stream) : launch_plane_products<kHalfTwo>(&p, 1, f.edge, stream));
+    const Planes w_rows = {lay + z.w, z.pitch, s.C}, x_rows = {ws + f.x, z.pitch, rows};
+    if (!f.way.split) {
+        uint16_t *terms = reinterpret_cast<uint16_t *>(ws + f.terms);
+        finish_kernel<<<dim3((unsigned)((rows * z.ranks + 255) / 256)), 256, 0, stream>>>(FinishJob{inner, largest_x, largest_a, scale, who, terms, (int)rows, z.ranks,
+                                                                                                   f.cuts_inner});
+        RFSF_TRY(hipGetLastError());
+        auto product = [&](auto is_bf16) {
+            constexpr bool BF16 = decltype(is_bf16)::value;
+            const Adapted<BF16> epilogue = {largest_w, largest_x, s.C, (int)rows, order, who, terms, lay + z.b, z.ranks, z.ranks_b, out, ld_out};
+            return launch_plane_product<BF16 ? kHalf : kHalfTwo>(w_rows, x_rows, steps, f.way.edge, epilogue, stream);
+        };
+        return bf16 ? product(std::true_type()) : product(std::false_type());
+    }
+    if (!straight) {
+        const Product<Parts> p = {w_rows, x_rows, steps, {shared, f.ld, s.C, (int)rows}, f.per_cut};
+        RFSF_TRY(bf16 ? launch_plane_products<kHalf>(&p, 1, f.way.edge, stream) : launch_plane_products<kHalfTwo>(&p, 1, f.way.edge, stream));
     }
     const int64_t across = (s.C + kJoinThreads - 1) / kJoinThreads;
     const int each = (int)std::max<int64_t>(1, rows * across / (4 * kFewGroups));
-    const JoinJob join = {shared, inner, largest_x, reinterpret_cast<const uint32_t *>(lay + z.largest_w), reinterpret_cast<const uint32_t *>(lay + z.largest_a),
-                          reinterpret_cast<const float *>(lay + z.scale), adapters, order, who, s.count, s.C, f.ld, ld_out, lay + z.b, out, (int)rows, each, z.ranks,
-                          z.ranks_b, f.cuts, f.cuts_inner};
+    const JoinJob join = {shared, inner, largest_x, largest_w, largest_a, scale, adapters, order, who, s.count, s.C, f.ld, ld_out, lay + z.b, out, (int)rows, each, z.ranks,
+                          z.ranks_b, f.way.cuts, f.cuts_inner};
     const dim3 grid((unsigned)across, (unsigned)((rows + each - 1) / each));
     if (bf16) join_kernel<true><<<grid, kJoinThreads, 0, stream>>>(join);
     else join_kernel<false><<<grid, kJoinThreads, 0, stream>>>(join);
@@ -705,8 +683,8 @@ void adapted_scores_bytes(const rfsf_adapters_shape &s, int64_t N, size_t *recom
 {
     const Layout z = layout_of(s);
     // (a smaller workspace means fewer rows at a time, which may need more than more rows do: parts of few rows are kept apart)
-    *minimum = bytes_of(s, z, 1);
-    *recommended = std::max(*minimum, bytes_of(s, z, std::min<int64_t>(std::max<int64_t>(N, 1), kMostRows)));
+    *minimum = plan_of(s, z, 1).bytes;
+    *recommended = std::max(*minimum, plan_of(s, z, std::min<int64_t>(std::max<int64_t>(N, 1), kMostRows)).bytes);
 }
 
 hipError_t launch_adapters_weights(const rfsf_adapters_shape &s, const void *W, int64_t ld_w, void *layout, hipStream_t stream)
@@ -739,46 +717,22 @@ hipError_t launch_adapted_scores(const rfsf_adapters_shape &s, const void *layou
                                  int64_t ld_out, void *workspace, size_t bytes, hipStream_t stream)
 {
     const Layout z = layout_of(s);
-    const char *lay = static_cast<const char *>(layout);
-    const bool bf16 = s.bf16 != 0;
     int64_t most = std::min<int64_t>(N, kMostRows);
-    while (most > 1 && bytes_of(s, z, most) > bytes) most = (most + 1) / 2;
-    const Workspace w = workspace_of(z, most);
+    Plan plan = plan_of(s, z, most);
+    while (most > 1 && plan.bytes > bytes) {
+        most = (most + 1) / 2;
+        plan = plan_of(s, z, most);
+    }
     const size_t mis = (size_t)(reinterpret_cast<uintptr_t>(workspace) % 256);
     char *ws = static_cast<char *>(workspace) + (mis ? 256 - mis : 0);
-    uint32_t *largest_x = reinterpret_cast<uint32_t *>(ws + w.largest_x);
-    int32_t *order = reinterpret_cast<int32_t *>(ws + w.order), *who = reinterpret_cast<int32_t *>(ws + w.who);
-    uint16_t *inner = reinterpret_cast<uint16_t *>(ws + w.inner);
-    const uint32_t *largest_w = reinterpret_cast<const uint32_t *>(lay + z.largest_w), *largest_a = reinterpret_cast<const uint32_t *>(lay + z.largest_a);
-    const float *scale = reinterpret_cast<const float *>(lay + z.scale);
-    const int64_t steps = plane_steps(s.K, !bf16);
     for (int64_t n0 = 0; n0 < N; n0 += most) {
         const int64_t rows = std::min(N - n0, most);
-        const char *x_from = static_cast<const char *>(X) + (size_t)n0 * ld_x * (bf16 ? 2 : 4);
-        // (the last rows of many are fewer, which may need more room than many do: their way is taken if there is that)
-        const bool last = rows < most && bytes_of(s, z, rows) <= bytes;
-        const Way way = way_of(s, z, last ? rows : most);
-        if (way.split) {
-            RFSF_TRY(launch_split(split_of(s, z, last ? rows : most, way.edge, way.cuts), s, z, lay, x_from, rows, ld_x, adapters + n0, out + n0 * ld_out, ld_out, ws, stream));
-            continue;
+        if (rows < most) {          // the last ones, which may need more room than more rows do: their way is taken if there is that
+            const Plan last = plan_of(s, z, rows);
+            if (last.bytes <= bytes) plan = last;
         }
-        order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters + n0, (int)rows, s.count, order, who);
-        RFSF_TRY(hipGetLastError());
-        RFSF_TRY(pack(PackJob{x_from, rows, s.K, ld_x, nullptr, largest_x, ws + w.x, nullptr, z.pitch, 0, order},
-                      bf16, stream));
-        const int slots = slots_of(s.count, rows), blocks = z.ranks / 16;
-        const InnerJob job = {ws + w.x, lay + z.a, z.pitch, largest_x, largest_a, scale, who, inner, (int)rows, z.ranks, blocks, slots, (int)steps};
-        const dim3 grid((unsigned)((rows + 15) / 16 * blocks * slots));
-        if (bf16) inner_kernel<false><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
-        else inner_kernel<true><<<grid, 64 * kInnerWaves, 0, stream>>>(job);
-        RFSF_TRY(hipGetLastError());
-        const Planes w_rows = {lay + z.w, z.pitch, s.C}, x_rows = {ws + w.x, z.pitch, rows};
-        const int edge = way.edge;
-        float *to = out + n0 * ld_out;
-        RFSF_TRY(bf16 ? launch_plane_product<kHalf>(w_rows, x_rows, steps, edge, Adapted<true>{largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks,
-                                                                                              z.ranks_b, to, ld_out}, stream)
-                      : launch_plane_product<kHalfTwo>(w_rows, x_rows, steps, edge, Adapted<false>{largest_w, largest_x, s.C, (int)rows, order, who, inner, lay + z.b, z.ranks,
-                                                                                                  z.ranks_b, to, ld_out}, stream));
+        RFSF_TRY(launch_rows(plan, s, z, static_cast<const char *>(layout), static_cast<const char *>(X) + (size_t)n0 * ld_x * (s.bf16 ? 2 : 4), rows, ld_x, adapters + n0,
+                             out + n0 * ld_out, ld_out, ws, stream));
     }
     return hipSuccess;
 }
