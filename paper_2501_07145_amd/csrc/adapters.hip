@@ -178,8 +178,14 @@ __device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const
 // of those that its rows have. What is left are sums of products as they are, which are scaled and added up where they are used. Bound by reading W and the adapters once.
 constexpr int64_t kFewGroups = 512;
 constexpr int kFewWaves = 4, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks, kWide = 2;
+// LOCAL: rows of X that have few numbers altogether are packed by every workgroup for itself, a wavefront each, into LDS: a launch less (1 x 1025, 1000 classes 13.0 ->
+// 10.6 us; seven rows, two a wavefront, 11.2 -> 12.3).
+constexpr int kLocal = 8192, kLocalRows = kFewWaves, kLocalPad = 16;        // numbers, rows; bytes between rows, for their banks
 struct FewJob {
     const char *x, *w, *a;              // packed
+    const void *X;                      // LOCAL: as they are, ld_x numbers apart
+    int64_t ld_x, K;
+    uint32_t *largest_x;                // LOCAL: written for join_kernel
     int64_t pitch, C;
     const int64_t *adapters;
     const int32_t *who;                 // in their place, if not null
@@ -189,11 +195,39 @@ struct FewJob {
     int rows, ranks, rank_blocks, slots, steps, cuts, per_cut, cuts_inner, per_cut_inner;
     unsigned inner_groups;
 };
-template <bool TWO, int BM, int NB>
+template <bool TWO, int BM, int NB, bool LOCAL>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
 {
+    static_assert(!LOCAL || NB == 1, "");
+    typedef std::conditional_t<TWO, float, uint16_t> Number;
     __shared__ float part[kFewWaves][BM * NB * 4][64];
+    __shared__ __attribute__((aligned(16))) char local[LOCAL ? kLocal * (TWO ? 4 : 2) + kLocalRows * (kStepBytes + kLocalPad) : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+    const int64_t pitch_x = LOCAL ? job.steps * kStepBytes + kLocalPad : job.pitch;
+    const char *rows_x = LOCAL ? local : job.x;
+    if constexpr (LOCAL) {
+        for (int n = wave; n < job.rows; n += kFewWaves) {
+            const Number *from = static_cast<const Number *>(job.X) + n * job.ld_x;
+            float v[8];
+            uint32_t largest = 0;
+            for (int64_t k = 8 * lane; k < job.K; k += 512) {
+                rows8::load(from, k, job.K, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o /= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, o));
+            if (blockIdx.x == 0 && lane == 0) job.largest_x[n] = largest;
+            const int shift = shift_of(largest);
+            for (int64_t k = 8 * lane; k < job.steps * (TWO ? 32 : 64); k += 512) {
+                rows8::load(from, k, job.K, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], shift);
+                plane::store_terms<TWO>(local + n * pitch_x, k, plane::terms_of<TWO>(v));
+            }
+        }
+        __syncthreads();
+    }
     if (blockIdx.x < job.inner_groups) {
         int id = blockIdx.x;
         const int cut = id % job.cuts_inner;
@@ -202,7 +236,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
         id /= job.slots;
         const int block = id % job.rank_blocks, n = id / job.rank_blocks * 16 + col;
         const int mine = n >= job.rows ? kNone : job.who ? job.who[n] : who_of(job.adapters[n], job.count);
-        const char *x = job.x + (int64_t)(n < job.rows ? n : job.rows - 1) * job.pitch + 16 * quarter;
+        const char *x = rows_x + (n < job.rows ? n : job.rows - 1) * pitch_x + 16 * quarter;
         const int last = std::min(job.steps, (cut + 1) * job.per_cut_inner);
         uint32_t left = (uint32_t)(__ballot(mine >= 0) & 0xffff);
         for (int number = 0; left != 0; ++number) {
@@ -233,7 +267,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
 #pragma unroll
     for (int m = 0; m < BM; ++m) w[m] = job.w + std::min<int64_t>(c0 + 16 * m + col, job.C - 1) * job.pitch + 16 * quarter;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) x[n] = job.x + (int64_t)std::min(16 * n + col, job.rows - 1) * job.pitch + 16 * quarter;
+    for (int n = 0; n < NB; ++n) x[n] = rows_x + std::min(16 * n + col, job.rows - 1) * pitch_x + 16 * quarter;
     floatx4 acc[BM][NB];
 #pragma unroll
     for (int m = 0; m < BM; ++m)
@@ -636,14 +670,20 @@ hipError_t launch_rows(const Plan &f, const rfsf_adapters_shape &s, const Layout
         order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters, (int)rows, s.count, order, who);
         RFSF_TRY(hipGetLastError());
     }
-    RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
-    const FewJob job = {ws + f.x, lay + z.w, lay + z.a, z.pitch, s.C, adapters, who, s.count, shared, inner, f.ld, (int)rows, z.ranks, z.ranks / 16, f.slots, (int)steps,
+    const bool local = straight && rows <= kLocalRows && f.blocks == 1 && rows * s.K <= kLocal;
+    if (!local) RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
+    const FewJob job = {ws + f.x, lay + z.w, lay + z.a, X, ld_x, s.K, largest_x, z.pitch, s.C, adapters, who, s.count, shared, inner, f.ld, (int)rows, z.ranks, z.ranks / 16, f.slots, (int)steps,
                         f.way.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
     auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)(f.groups + f.inner_groups)), 64 * kFewWaves, 0, stream>>>(job); };
     auto launch_blocks = [&](auto two) {
         constexpr bool TWO = decltype(two)::value;
-        if (f.wide == kWide) f.blocks == 1 ? launch(few_kernel<TWO, kWide, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, kWide, 2>) : launch(few_kernel<TWO, kWide, 4>);
-        else f.blocks <= 1 ? launch(few_kernel<TWO, 1, 1>) : f.blocks == 2 ? launch(few_kernel<TWO, 1, 2>) : launch(few_kernel<TWO, 1, 4>);
+        auto launch_wide = [&](auto wide) {
+            constexpr int BM = decltype(wide)::value;
+            if (f.blocks <= 1) local ? launch(few_kernel<TWO, BM, 1, true>) : launch(few_kernel<TWO, BM, 1, false>);
+            else f.blocks == 2 ? launch(few_kernel<TWO, BM, 2, false>) : launch(few_kernel<TWO, BM, 4, false>);
+        };
+        if (f.wide == kWide) launch_wide(std::integral_constant<int, kWide>());
+        else launch_wide(std::integral_constant<int, 1>());
     };
     if (bf16) launch_blocks(std::false_type());
     else launch_blocks(std::true_type());

@@ -295,9 +295,9 @@ class RfsfDropout:
 
 def _here(*tensors: Optional[torch.Tensor]) -> None:
     """Refuses tensors that are not on the current device, whose stream the work goes to."""
-    current = torch.cuda.current_device()
+    current = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device.index != current:
+        if t is not None and t.get_device() != current:
             raise ValueError("all tensors must be on the current device")
 
 
@@ -305,8 +305,8 @@ def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
     """Address of a contiguous float32 device tensor [n], or None."""
     if t is None:
         return None
-    if _dev(t, torch.float32, name).shape != (n,):
-        raise ValueError(f"{name} must have shape [{n}]")
+    if not t.is_cuda or t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous float32 [{n}] on the device")
     return t.data_ptr()
 
 

@@ -59,6 +59,7 @@ CASES = [
     (1, 1, 1, 1, 1), (1, 9, 5, 3, 2), (1, 1025, 1000, 8, 20), (2, 64, 33, 4, 3), (3, 65, 10, 1, 7), (5, 300, 31, 17, 4), (15, 129, 257, 16, 50), (16, 1025, 77, 5, 16), (17, 193, 64, 20, 3),
     (33, 100, 100, 33, 40), (64, 513, 300, 8, 64), (65, 257, 130, 12, 5), (130, 333, 65, 64, 9), (300, 129, 515, 16, 100), (333, 1025, 280, 7, 1), (1000, 65, 129, 6, 300), (40, 31, 7, 256, 2),
     (12, 13001, 40, 9, 5), (600, 40, 600, 100, 11), (20, 5121, 10, 16, 20), (48, 2049, 3, 24, 2), (7, 700, 5000, 16, 7), (1, 300, 17000, 4, 2),
+    (2000, 129, 8193, 7, 30), (2000, 140, 8200, 40, 3), (2100, 129, 8000, 5, 1500), (129, 5121, 1029, 20, 12), (260, 2500, 700, 33, 90), (4, 2049, 70, 12, 9), (5, 1025, 15, 12, 9),
 ]
 
 
