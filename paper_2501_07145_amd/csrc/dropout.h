@@ -60,6 +60,16 @@ __device__ __forceinline__ bool kept(const DropoutJob &job, const uint32_t (&wor
 {
     return (e & 1 ? word[e / 2] >> 16 : word[e / 2] & 0xffffu) >= job.threshold;
 }
+__device__ __forceinline__ bool keeps(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t column)
+{
+    uint32_t word[4];
+    numbers(job, offset, row, column / 8, word);
+    bool keep = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (column % 8 == e) keep = kept(job, word, e);
+    return keep;
+}
 // Eight numbers of a row: those that are kept times the factor, 0 (also of infinities and NaN) for the others.
 __device__ __forceinline__ void apply(const DropoutJob &job, uint64_t offset, uint32_t row, uint32_t group, float (&x)[8])
 {

@@ -169,18 +169,22 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
     }
 }
 
-// Many rows: LANES of a wavefront have a row to themselves, and nobody waits for anybody; gains and offsets lie in LDS, once for all wavefronts of a CU. A row is HELD
-// times eight numbers a lane, of which the first FULL are whole for every lane.
+// The kernels for many rows take a row as eights of columns, up to HELD a lane, and what is left over, up to seven columns (features have 1 + M*D), as one number more for
+// each of the first lanes: an eight of its own would take as long as a whole one (200003 x 65, bfloat16, backward 29 -> 24 us).
+
+// Many rows: LANES of a wavefront have a row to themselves, and nobody waits for anybody; gains and offsets lie in LDS, once for all wavefronts of a CU. Of a lane's
+// eights the first FULL are there for every lane.
 constexpr int wave_threads(size_t held_bytes) { return held_bytes <= 28 ? 1024 : held_bytes <= 42 ? 768 : 512; }
 template <typename T, int LANES, int FULL, int HELD, bool DROP>
 __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kernel(NormJob job)
 {
     constexpr int THREADS = wave_threads(HELD * sizeof(T)), STEP = 8 * LANES, ROWS = THREADS / LANES;
-    extern __shared__ __attribute__((aligned(16))) float columns[];          // gains, then offsets, each of HELD * STEP
-    const int lane = threadIdx.x % LANES, K = (int)job.K;
-    for (int k = threadIdx.x; k < STEP * HELD; k += THREADS) {
+    extern __shared__ __attribute__((aligned(16))) float columns[];          // gains, then offsets, each of HELD * STEP and eight
+    constexpr int ROOM = STEP * HELD + 8;
+    const int lane = threadIdx.x % LANES, K = (int)job.K, whole = K / 8 * 8, last = whole + lane;
+    for (int k = threadIdx.x; k < ROOM; k += THREADS) {
         columns[k] = k < K && job.gain ? job.gain[k] : 1.f;
-        columns[STEP * HELD + k] = k < K && job.offset ? job.offset[k] : 0.f;
+        columns[ROOM + k] = k < K && job.offset ? job.offset[k] : 0.f;
     }
     __syncthreads();
     const double inverse = 1.0 / (double)K;
@@ -193,10 +197,11 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
-            if (u < FULL) held[u] = *reinterpret_cast<const rows8::Eight<T> *>(x + k);
-            else held[u] = rows8::load_raw(x, k, K);
+            if (u < FULL || k < whole) held[u] = *reinterpret_cast<const rows8::Eight<T> *>(x + k);
+            else held[u] = {};
         }
-        double sum[1] = {0.0};
+        const float x_last = last < K ? rows8::to_float(x[last]) : 0.f;
+        double sum[1] = {(double)x_last};
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             rows8::in_turn(held[u]);
@@ -204,13 +209,15 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
         }
         add_up<LANES>(sum, static_cast<double (*)[1]>(nullptr));
         const Mean m = mean_of(sum[0], inverse);
-        float squares[1] = {0.f};
+        const float d_last = last < K ? x_last - m.mean : 0.f;
+        float squares[1] = {d_last * d_last};
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
+            if (u >= FULL && 8 * lane + STEP * u >= whole) continue;
             rows8::in_turn(held[u]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = u < FULL || 8 * lane + STEP * u + e < K ? rows8::to_float(held[u].v[e]) - m.mean : 0.f;
+                const float d = rows8::to_float(held[u].v[e]) - m.mean;
                 squares[0] = fmaf(d, d, squares[0]);
             }
         }
@@ -223,11 +230,11 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
-            if (u >= FULL && k >= K) continue;
+            if (u >= FULL && k >= whole) continue;
             rows8::in_turn(held[u]);
             float y[8], gain[8], shift[8];
             __builtin_memcpy(gain, columns + k, 32);
-            __builtin_memcpy(shift, columns + STEP * HELD + k, 32);
+            __builtin_memcpy(shift, columns + ROOM + k, 32);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf((rows8::to_float(held[u].v[e]) - m.mean - m.rest) * rstd, gain[e], shift[e]);
             if (DROP) {
@@ -235,7 +242,12 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
                 asm volatile("" : "+v"(group));            // (the first rounds' products, which are the same for all rows, would be kept for every u)
                 dropout::apply(job.dropout, counter, job.dropout.first_row + (uint32_t)row, group, y);
             }
-            rows8::store(y_row, k, u < FULL ? k + 8 : K, y);
+            rows8::store(y_row, k, k + 8, y);
+        }
+        if (last < K) {
+            float y = fmaf((d_last - m.rest) * rstd, columns[last], columns[ROOM + last]);
+            if (DROP) y = dropout::keeps(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)last) ? y * job.dropout.factor : 0.f;
+            rows8::from_float(y, y_row + last);
         }
     }
 }
@@ -297,7 +309,7 @@ __device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_
     return {job.sums + part * 2 * job.K, job.sums + (part * 2 + 1) * job.K};
 }
 
-// The backward pass of rows that are held in registers, THREADS lanes a row, HELD times eight numbers each, of which all but the last are whole; gains lie in LDS.
+// The backward pass of rows that are held in registers, THREADS lanes a row, HELD eights each, of which all but the last are there for every lane; gains lie in LDS.
 // Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
 // sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
 constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && held <= 3) ? 4 : held == 2 ? 3 : 2; }
@@ -307,13 +319,13 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
     constexpr int GROUP = THREADS > 256 ? THREADS : 256, ROWS = GROUP / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1, STEP = 8 * THREADS;
     constexpr bool AHEAD = HELD <= (sizeof(T) == 2 ? 4 : 3);          // registers for the next row
     __shared__ float part[2][WAVES][2];
-    __shared__ __attribute__((aligned(16))) float gains[STEP * HELD];
-    const int lane = threadIdx.x % THREADS, K = (int)job.K;
+    __shared__ __attribute__((aligned(16))) float gains[STEP * HELD + 8];
+    const int lane = threadIdx.x % THREADS, K = (int)job.K, whole = K / 8 * 8, last = whole + lane;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inverse = 1.0f / (float)K, factor = DROP ? job.dropout.factor : 1.f;
-    for (int k = threadIdx.x; k < STEP * HELD; k += GROUP) gains[k] = k < K && job.gain ? job.gain[k] : 1.f;
+    for (int k = threadIdx.x; k < STEP * HELD + 8; k += GROUP) gains[k] = k < K && job.gain ? job.gain[k] : 1.f;
     __syncthreads();
-    float of_gain[HELD][8], of_offset[HELD][8];
+    float of_gain[HELD][8], of_offset[HELD][8], of_gain_last = 0.f, of_offset_last = 0.f;
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
 #pragma unroll
@@ -323,20 +335,19 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
     T *dX = static_cast<T *>(job.dX);
     int64_t row = (int64_t)blockIdx.x * ROWS + (THREADS >= 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / THREADS)) : threadIdx.x / THREADS);
     rows8::Eight<T> x[HELD], h[HELD], next_x[HELD], next_h[HELD];
-    float mean, rstd, next_mean, next_rstd;
+    float mean, rstd, next_mean, next_rstd, x_last, h_last, next_x_last, next_h_last;
     auto load = [&](int64_t r) {
         r = r < job.N ? r : job.N - 1;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
-            if (u < HELD - 1) {
+            if (u < HELD - 1 || k < whole) {
                 next_x[u] = *reinterpret_cast<const rows8::Eight<T> *>(X + r * job.ldx + k);
                 next_h[u] = *reinterpret_cast<const rows8::Eight<T> *>(dY + r * job.ldy + k);
-            } else {
-                next_x[u] = rows8::load_raw(X + r * job.ldx, k, K);
-                next_h[u] = rows8::load_raw(dY + r * job.ldy, k, K);
             }
         }
+        next_x_last = last < K ? rows8::to_float(X[r * job.ldx + last]) : 0.f;
+        next_h_last = last < K ? rows8::to_float(dY[r * job.ldy + last]) : 0.f;
         next_mean = job.mean[r];
         next_rstd = job.rstd[r];
     };
@@ -345,9 +356,11 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
     // (all rows of a workgroup take as many turns, so that everybody meets at the barriers)
     for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
         if (!AHEAD) load(row);
-        const bool there = row < job.N;
+        const bool there = ROWS == 1 || row < job.N;
         mean = next_mean;
         rstd = next_rstd;
+        x_last = next_x_last;
+        h_last = next_h_last;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             x[u] = next_x[u];
@@ -358,7 +371,7 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
-            if (u == HELD - 1 && k >= K) continue;
+            if (u == HELD - 1 && k >= whole) continue;
             rows8::in_turn(x[u]);
             if (DROP) {
                 uint32_t group = (uint32_t)k / 8;
@@ -367,32 +380,39 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
             }
             float gain[8];
             __builtin_memcpy(gain, gains + k, 32);
-            auto add = [&](auto whole) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool counts = (ROWS == 1 || there) && (whole || k + e < K);
-                    const float z = counts ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, d = counts ? rows8::to_float(h[u].v[e]) : 0.f, g = d * gain[e];
-                    if (GAINS) {
-                        of_gain[u][e] = fmaf(d, z, of_gain[u][e]);
-                        of_offset[u][e] += d;
-                    }
-                    sums[0] += g;
-                    sums[1] = fmaf(g, z, sums[1]);
+            for (int e = 0; e < 8; ++e) {
+                const float z = there ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, d = there ? rows8::to_float(h[u].v[e]) : 0.f, g = d * gain[e];
+                if (GAINS) {
+                    of_gain[u][e] = fmaf(d, z, of_gain[u][e]);
+                    of_offset[u][e] += d;
                 }
-            };
-            if (u < HELD - 1 || k + 8 <= K) add(std::true_type());
-            else add(std::false_type());
+                sums[0] += g;
+                sums[1] = fmaf(g, z, sums[1]);
+            }
+        }
+        float z_last = 0.f;
+        if (last < K) {
+            if (DROP) h_last = dropout::keeps(job.dropout, counter, job.dropout.first_row + (uint32_t)row, (uint32_t)last) ? h_last : 0.f;
+            h_last = there ? h_last : 0.f;
+            z_last = there ? (x_last - mean) * rstd : 0.f;
+            const float g = h_last * gains[last];
+            of_gain_last = fmaf(h_last, z_last, of_gain_last);
+            of_offset_last += h_last;
+            sums[0] += g;
+            sums[1] = fmaf(g, z_last, sums[1]);
         }
         add_up<THREADS>(sums, part[which]);
         which ^= 1;
-        if (ROWS > 1 && !there) continue;
+        if (!there) continue;
         sums[0] *= inverse;
         sums[1] *= inverse;
         const float scale = rstd * factor;
+        T *to = dX + row * job.ldd;
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
-            if (u == HELD - 1 && k >= K) continue;
+            if (u == HELD - 1 && k >= whole) continue;
             rows8::in_turn(x[u]);
             rows8::in_turn(h[u]);
             float gain[8], d[8];
@@ -402,8 +422,9 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
                 const float z = (rows8::to_float(x[u].v[e]) - mean) * rstd;
                 d[e] = (rows8::to_float(h[u].v[e]) * gain[e] - fmaf(z, sums[1], sums[0])) * scale;
             }
-            rows8::store(dX + row * job.ldd, k, u < HELD - 1 ? k + 8 : K, d);
+            rows8::store(to, k, k + 8, d);
         }
+        if (last < K) rows8::from_float((h_last * gains[last] - fmaf(z_last, sums[1], sums[0])) * scale, to + last);
     }
     if constexpr (GAINS) {
         const Sums mine = sums_of(job, blockIdx.x, gridDim.x);
@@ -422,19 +443,39 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
 #pragma unroll
                         for (int r = 0; r < ROWS; ++r) s += all[r][at / 8][at % 8];
                         const int k = STEP * u + at;
-                        if (k < K) (w ? mine.offset : mine.gain)[k] = s * factor;
+                        if (k < whole) (w ? mine.offset : mine.gain)[k] = s * factor;
                     }
                 }
+            __syncthreads();
+            all[threadIdx.x / THREADS][lane][0] = of_gain_last;
+            all[threadIdx.x / THREADS][lane][1] = of_offset_last;
+            __syncthreads();
+            if (threadIdx.x < THREADS && last < K) {
+                float a = 0.f, b = 0.f;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    a += all[r][lane][0];
+                    b += all[r][lane][1];
+                }
+                mine.gain[last] = a * factor;
+                mine.offset[last] = b * factor;
+            }
         } else {
 #pragma unroll
             for (int u = 0; u < HELD; ++u) {
+                const int k = 8 * lane + STEP * u;
+                if (u == HELD - 1 && k >= whole) continue;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     of_gain[u][e] *= factor;
                     of_offset[u][e] *= factor;
                 }
-                rows8::store(mine.gain, 8 * lane + STEP * u, K, of_gain[u]);
-                rows8::store(mine.offset, 8 * lane + STEP * u, K, of_offset[u]);
+                rows8::store(mine.gain, k, k + 8, of_gain[u]);
+                rows8::store(mine.offset, k, k + 8, of_offset[u]);
+            }
+            if (last < K) {
+                mine.gain[last] = of_gain_last * factor;
+                mine.offset[last] = of_offset_last * factor;
             }
         }
     }
@@ -579,21 +620,23 @@ __global__ __launch_bounds__(kAddThreads) void add_parts_kernel(const float *sum
     else doffset[at - K] = s;
 }
 
-// f(lanes of a row, how many times eight numbers each holds), of which all but the last are whole.
+// f(lanes of a row, eights that each holds), of which all but the last are there for every lane.
 template <int THREADS, int HELD> struct Shape {};
 template <int THREADS, int HELD, typename... MORE, typename F>
-auto with_first(int64_t K, const F &f, Shape<THREADS, HELD>, MORE... more)
+auto with_first(int64_t eights, const F &f, Shape<THREADS, HELD>, MORE... more)
 {
     if constexpr (sizeof...(MORE) > 0) {
-        if (K > 8 * THREADS * HELD) return with_first(K, f, more...);
+        if (eights > THREADS * HELD) return with_first(eights, f, more...);
     }
     return f(std::integral_constant<int, THREADS>(), std::integral_constant<int, HELD>());
 }
-template <typename F>
-auto with_shape(int64_t K, const F &f)
+// (256 lanes with five eights of 32-bit numbers each have no registers for the next row: 10000 x 10241, backward 280 us, 512 with three 258; bfloat16 156 and 166)
+template <typename T, typename F>
+auto with_shape(int64_t eights, const F &f)
 {
-    return with_first(K, f, Shape<8, 1>(), Shape<8, 2>(), Shape<8, 3>(), Shape<16, 2>(), Shape<16, 3>(), Shape<16, 4>(), Shape<16, 5>(), Shape<64, 2>(), Shape<64, 3>(),
-                      Shape<64, 4>(), Shape<64, 5>(), Shape<256, 2>(), Shape<256, 3>(), Shape<256, 4>(), Shape<256, 5>(), Shape<512, 3>(), Shape<512, 4>(), Shape<512, 5>());
+    typedef std::conditional_t<sizeof(T) == 2, Shape<256, 5>, Shape<512, 3>> Wide;
+    return with_first(eights, f, Shape<8, 1>(), Shape<8, 2>(), Shape<8, 3>(), Shape<16, 2>(), Shape<16, 3>(), Shape<16, 4>(), Shape<16, 5>(), Shape<64, 2>(), Shape<64, 3>(),
+                      Shape<64, 4>(), Shape<64, 5>(), Shape<256, 2>(), Shape<256, 3>(), Shape<256, 4>(), Wide(), Shape<512, 3>(), Shape<512, 4>(), Shape<512, 5>());
 }
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
@@ -609,19 +652,20 @@ int64_t groups_of(int64_t N, int threads, int waves, bool alone = false)
 // Parts of dgain and doffset. Fused with dX: one for each workgroup.
 int gains_lanes(int64_t K) { return K <= 128 ? 16 : 64; }
 int64_t gains_pieces(int64_t K) { return (K + 8 * gains_lanes(K) - 1) / (8 * gains_lanes(K)); }
+template <typename T>
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && is_held(K)) return with_shape(K, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
+    if (with_dx && is_held(K)) return with_shape<T>(K / 8, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
     const int64_t rows = 256 / gains_lanes(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
 
-// f(FULL, HELD): the numbers that a lane holds, of a list, if `lanes` of them hold a row.
+// f(FULL, HELD): the eights that a lane holds, of a list, if `lanes` of them hold a row's.
 template <int FULL, int HELD, int... MORE, typename F>
 bool with_held(int64_t K, int lanes, const F &f)
 {
-    if (K <= 8 * lanes * HELD) {
+    if (K / 8 <= lanes * HELD) {
         f(std::integral_constant<int, FULL>(), std::integral_constant<int, HELD>());
         return true;
     }
@@ -632,7 +676,7 @@ template <typename T, int LANES, int FULL, int HELD>
 hipError_t launch_wave(const NormJob &job, bool drop, hipStream_t stream)
 {
     constexpr int threads = wave_threads(HELD * sizeof(T)), rows = threads / LANES;
-    constexpr size_t lds = 2 * 8 * LANES * HELD * sizeof(float);
+    constexpr size_t lds = 2 * (8 * LANES * HELD + 8) * sizeof(float);
     constexpr int64_t per_cu = std::min<int64_t>(2048 / threads, kLdsPerCu / lds);
     const dim3 grid((unsigned)std::min<int64_t>((job.N + rows - 1) / rows, kCus * per_cu));
     auto launch = [&](LdsLimit &limit, auto kernel) {
@@ -650,13 +694,19 @@ hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
 {
     if (job.N >= kManyRows && job.K >= kLeastHeld) {
         hipError_t e = hipSuccess;
-        if (with_held<0, 1, 2, 3>(job.K, 8, [&](auto full, auto held) { e = launch_wave<T, 8, full, held>(job, drop, stream); }) ||
-            with_held<1, 2, 3, 4, 5>(job.K, 16, [&](auto full, auto held) { e = launch_wave<T, 16, full, held>(job, drop, stream); }) ||
-            with_held<1, 2, 3, 4, 5, 7, 9, 11, 13, 17, 21>(job.K, 64, [&](auto full, auto held) { e = launch_wave<T, 64, full, held>(job, drop, stream); }))
+        auto wave = [&](auto lanes) { return [&, lanes](auto full, auto held) { e = launch_wave<T, lanes, full, held>(job, drop, stream); }; };
+        typedef std::integral_constant<int, 8> l8;
+        typedef std::integral_constant<int, 16> l16;
+        typedef std::integral_constant<int, 64> l64;
+        if (with_held<0, 1, 2, 3>(job.K, 8, wave(l8())) || with_held<1, 2, 3, 4, 5>(job.K, 16, wave(l16())) ||
+            with_held<1, 2, 3, 4, 5, 7, 8, 10, 12, 16, 20>(job.K, 64, wave(l64())))
             return e;
+        if constexpr (sizeof(T) == 2) {         // (32-bit numbers of longer rows have no room in a wavefront's registers)
+            if (with_held<20, 24, 32>(job.K, 64, wave(l64()))) return e;
+        }
     }
     if (is_held(job.K)) {
-        with_shape(job.K, [&](auto threads, auto held) {
+        with_shape<T>((job.K + 7) / 8, [&](auto threads, auto held) {
             const dim3 grid((unsigned)groups_of(job.N, threads, 4));
             if (drop) norm_kernel<T, threads, held, true><<<grid, group_threads(threads), 0, stream>>>(job);
             else norm_kernel<T, threads, held, false><<<grid, group_threads(threads), 0, stream>>>(job);
@@ -683,9 +733,9 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
 {
     BackJob job = whole;
     const bool gains = job.dgain != nullptr, held = is_held(job.K);
-    const int64_t parts = gains ? parts_of(job.N, job.K, job.dX != nullptr) : 0;
+    const int64_t parts = gains ? parts_of<T>(job.N, job.K, job.dX != nullptr) : 0;
     if (job.dX && held) {
-        with_shape(job.K, [&](auto threads, auto held_) {
+        with_shape<T>(job.K / 8, [&](auto threads, auto held_) {
             const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held_, gains), gains));
             auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
             if (drop && gains) launch(back_kernel<T, threads, held_, true, true>);
@@ -728,7 +778,8 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
 
 size_t layer_norm_backward_bytes(const rfsf_layer_norm_shape &s, bool with_dx)
 {
-    return (size_t)std::max<int64_t>(1, parts_of(s.N, s.K, with_dx)) * 2 * (size_t)s.K * sizeof(float) + 256;
+    const int64_t parts = s.bf16 ? parts_of<uint16_t>(s.N, s.K, with_dx) : parts_of<float>(s.N, s.K, with_dx);
+    return (size_t)std::max<int64_t>(1, parts) * 2 * (size_t)s.K * sizeof(float) + 256;
 }
 
 hipError_t launch_layer_norm(const rfsf_layer_norm_shape &s, const void *X, const float *gain, const float *offset, float eps, const rfsf_dropout_mask *mask, void *Y,
