@@ -30,7 +30,7 @@ struct BackJob {
     const void *X, *dY;
     void *dX;
     const float *mean, *rstd, *gain;
-    float *sums;                // [workgroups along the rows][2][K], dgain's and doffset's; unused where there is one workgroup
+    float *sums;                // [workgroups along the rows][2][K rounded up to eight], dgain's and doffset's; unused where there is one workgroup
     float *dgain, *doffset;
     int64_t N, K, ldx, ldy, ldd;
     DropoutJob dropout;
@@ -301,12 +301,14 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bo
     }
 }
 
+__host__ __device__ __forceinline__ int64_t room_of(int64_t K) { return (K + 7) / 8 * 8; }
 // Where part number `part` of the sums goes.
 struct Sums { float *gain, *offset; };
 __device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_t parts)
 {
     if (parts == 1) return {job.dgain, job.doffset};
-    return {job.sums + part * 2 * job.K, job.sums + (part * 2 + 1) * job.K};
+    const int64_t room = room_of(job.K);
+    return {job.sums + part * 2 * room, job.sums + (part * 2 + 1) * room};
 }
 
 // The backward pass of rows that are held in registers, THREADS lanes a row, HELD eights each, of which all but the last are there for every lane; gains lie in LDS.
@@ -600,24 +602,24 @@ __global__ __launch_bounds__(kAddThreads) void add_parts_kernel(const float *sum
     constexpr int SLICES = kAddThreads / kAddColumns, AHEAD = 8;
     __shared__ float all[SLICES][kAddColumns + 1];
     const int lane = threadIdx.x % kAddColumns, slice = threadIdx.x / kAddColumns;
-    const int64_t at = (int64_t)blockIdx.x * kAddColumns + lane;
+    const int64_t at = (int64_t)blockIdx.x * kAddColumns + lane, room = room_of(K);
     float s = 0.f;
-    if (at < 2 * K)
+    if (at < 2 * room)
         for (int64_t p = slice; p < parts; p += AHEAD * SLICES) {
             float v[AHEAD];
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) v[a] = p + a * SLICES < parts ? sums[(p + a * SLICES) * 2 * K + at] : 0.f;
+            for (int a = 0; a < AHEAD; ++a) v[a] = p + a * SLICES < parts ? sums[(p + a * SLICES) * 2 * room + at] : 0.f;
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) s += v[a];
         }
     all[slice][lane] = s;
     __syncthreads();
-    if (slice != 0 || at >= 2 * K) return;
+    const int64_t column = at < room ? at : at - room;
+    if (slice != 0 || column >= K) return;
     s = 0.f;
 #pragma unroll
     for (int w = 0; w < SLICES; ++w) s += all[w][lane];
-    if (at < K) dgain[at] = s;
-    else doffset[at - K] = s;
+    (at < room ? dgain : doffset)[column] = s;
 }
 
 // f(lanes of a row, eights that each holds), of which all but the last are there for every lane.
@@ -640,13 +642,25 @@ auto with_shape(int64_t eights, const F &f)
 }
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
-// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time, of `waves` wavefronts a SIMD. alone: one for what it does in a few turns,
-// which take less time than a second launch for adding parts up.
+// Workgroups of a launch that goes through the rows: as many as the CUs hold at a time, of `waves` wavefronts a SIMD. With gains and offsets' gradients, of which each
+// leaves a part: one for what it does in a few turns, which take less time than a second launch for adding parts up; and two turns rather than more than one workgroup
+// a CU, where a part is as long as a row or two (333 x 5121, float32 23.5 -> 17.2 us).
 constexpr int64_t kFewTurns = 4;
-int64_t groups_of(int64_t N, int threads, int waves, bool alone = false)
+int64_t groups_of(int64_t N, int threads, int waves, bool gains)
 {
-    if (alone && N <= kFewTurns * group_rows(threads)) return 1;
-    return std::min<int64_t>((N + group_rows(threads) - 1) / group_rows(threads), kCus * (256 * waves / group_threads(threads)));
+    const int64_t groups = (N + group_rows(threads) - 1) / group_rows(threads);
+    if (gains && groups <= kFewTurns) return 1;
+    return std::min<int64_t>(gains && threads >= 256 && groups > kCus ? (groups + 1) / 2 : groups, kCus * (256 * waves / group_threads(threads)));
+}
+// Gradients of gains and offsets by a launch of their own, beside that of dX: where reading both matrices again takes fewer bytes than the parts
+// (500 x 10241, bfloat16 33.0 -> 29.9 us; 333 x 5121 15.8 -> 14.2).
+template <typename T>
+bool apart(int64_t N, int64_t K)
+{
+    return with_shape<T>(K / 8, [&](auto threads, auto held) {
+        if (threads < 256 || N <= kCus) return false;
+        return 16 * groups_of(N, threads, back_waves(held, true), true) > 2 * N * (int64_t)sizeof(T) + N / 2 * (int64_t)sizeof(T);
+    });
 }
 
 // Parts of dgain and doffset. Fused with dX: one for each workgroup.
@@ -656,7 +670,7 @@ template <typename T>
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && is_held(K)) return with_shape<T>(K / 8, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
+    if (with_dx && is_held(K) && !apart<T>(N, K)) return with_shape<T>(K / 8, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
     const int64_t rows = 256 / gains_lanes(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
@@ -707,7 +721,7 @@ hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
     }
     if (is_held(job.K)) {
         with_shape<T>((job.K + 7) / 8, [&](auto threads, auto held) {
-            const dim3 grid((unsigned)groups_of(job.N, threads, 4));
+            const dim3 grid((unsigned)groups_of(job.N, threads, 4, false));
             if (drop) norm_kernel<T, threads, held, true><<<grid, group_threads(threads), 0, stream>>>(job);
             else norm_kernel<T, threads, held, false><<<grid, group_threads(threads), 0, stream>>>(job);
         });
@@ -729,49 +743,58 @@ hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
 }
 
 template <typename T>
-hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
+hipError_t back_held(const BackJob &job, bool drop, bool gains, hipStream_t stream)
 {
-    BackJob job = whole;
-    const bool gains = job.dgain != nullptr, held = is_held(job.K);
-    const int64_t parts = gains ? parts_of<T>(job.N, job.K, job.dX != nullptr) : 0;
-    if (job.dX && held) {
-        with_shape<T>(job.K / 8, [&](auto threads, auto held_) {
-            const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held_, gains), gains));
-            auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
-            if (drop && gains) launch(back_kernel<T, threads, held_, true, true>);
-            else if (drop) launch(back_kernel<T, threads, held_, true, false>);
-            else if (gains) launch(back_kernel<T, threads, held_, false, true>);
-            else launch(back_kernel<T, threads, held_, false, false>);
-        });
-    } else {
-        if (gains) {                // (first: dX may lie where dY is)
-            const int64_t pieces = gains_pieces(job.K);
-            const dim3 grid((unsigned)(parts * pieces));
-            auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(job, (uint32_t)pieces); };
-            if (job.K < kLeastHeld) drop ? launch(gains_kernel<T, 16, true, true>) : launch(gains_kernel<T, 16, false, true>);
-            else if (gains_lanes(job.K) == 16) drop ? launch(gains_kernel<T, 16, true, false>) : launch(gains_kernel<T, 16, false, false>);
-            else drop ? launch(gains_kernel<T, 64, true, false>) : launch(gains_kernel<T, 64, false, false>);
-        }
-        constexpr int64_t kMost = 1 << 21;          // workgroups of a launch
-        for (int64_t n0 = 0; job.dX && n0 < job.N; n0 += kMost) {
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            BackJob part = job;
-            part.X = static_cast<const T *>(job.X) + n0 * job.ldx;
-            part.dY = static_cast<const T *>(job.dY) + n0 * job.ldy;
-            part.dX = static_cast<T *>(job.dX) + n0 * job.ldd;
-            part.mean = job.mean + n0;
-            part.rstd = job.rstd + n0;
-            part.dropout.first_row += (uint32_t)n0;
-            back_long_kernel<T><<<dim3((unsigned)std::min(kMost, job.N - n0)), kLongThreads, 0, stream>>>(part, drop);
-        }
-    }
-    if (gains && parts > 1) {
+    with_shape<T>(job.K / 8, [&](auto threads, auto held) {
+        const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held, gains), gains));
+        auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
+        if (drop && gains) launch(back_kernel<T, threads, held, true, true>);
+        else if (drop) launch(back_kernel<T, threads, held, true, false>);
+        else if (gains) launch(back_kernel<T, threads, held, false, true>);
+        else launch(back_kernel<T, threads, held, false, false>);
+    });
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t back_long(const BackJob &job, bool drop, hipStream_t stream)
+{
+    constexpr int64_t kMost = 1 << 21;          // workgroups of a launch
+    for (int64_t n0 = 0; n0 < job.N; n0 += kMost) {
+        BackJob part = job;
+        part.X = static_cast<const T *>(job.X) + n0 * job.ldx;
+        part.dY = static_cast<const T *>(job.dY) + n0 * job.ldy;
+        part.dX = static_cast<T *>(job.dX) + n0 * job.ldd;
+        part.mean = job.mean + n0;
+        part.rstd = job.rstd + n0;
+        part.dropout.first_row += (uint32_t)n0;
+        back_long_kernel<T><<<dim3((unsigned)std::min(kMost, job.N - n0)), kLongThreads, 0, stream>>>(part, drop);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        add_parts_kernel<<<dim3((unsigned)((2 * job.K + kAddColumns - 1) / kAddColumns)), kAddThreads, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
     }
-    return hipGetLastError();
+    return hipSuccess;
+}
+template <typename T>
+hipError_t back(const BackJob &job, bool drop, hipStream_t stream)
+{
+    const bool gains = job.dgain != nullptr, held = is_held(job.K);
+    const bool fused = gains && job.dX && held && !apart<T>(job.N, job.K);
+    const int64_t parts = gains ? parts_of<T>(job.N, job.K, job.dX != nullptr) : 0;
+    hipError_t e = hipSuccess;
+    if (gains && !fused) {          // (first: dX may lie where dY is)
+        const int64_t pieces = gains_pieces(job.K);
+        const dim3 grid((unsigned)(parts * pieces));
+        auto launch = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(job, (uint32_t)pieces); };
+        if (job.K < kLeastHeld) drop ? launch(gains_kernel<T, 16, true, true>) : launch(gains_kernel<T, 16, false, true>);
+        else if (gains_lanes(job.K) == 16) drop ? launch(gains_kernel<T, 16, true, false>) : launch(gains_kernel<T, 16, false, false>);
+        else drop ? launch(gains_kernel<T, 64, true, false>) : launch(gains_kernel<T, 64, false, false>);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && job.dX) e = held ? back_held<T>(job, drop, fused, stream) : back_long<T>(job, drop, stream);
+    if (e == hipSuccess && gains && parts > 1) {
+        add_parts_kernel<<<dim3((unsigned)((2 * room_of(job.K) + kAddColumns - 1) / kAddColumns)), kAddThreads, 0, stream>>>(job.sums, parts, job.K, job.dgain, job.doffset);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace
@@ -779,7 +802,7 @@ hipError_t back(const BackJob &whole, bool drop, hipStream_t stream)
 size_t layer_norm_backward_bytes(const rfsf_layer_norm_shape &s, bool with_dx)
 {
     const int64_t parts = s.bf16 ? parts_of<uint16_t>(s.N, s.K, with_dx) : parts_of<float>(s.N, s.K, with_dx);
-    return (size_t)std::max<int64_t>(1, parts) * 2 * (size_t)s.K * sizeof(float) + 256;
+    return (size_t)std::max<int64_t>(1, parts) * 2 * (size_t)room_of(s.K) * sizeof(float) + 256;
 }
 
 hipError_t launch_layer_norm(const rfsf_layer_norm_shape &s, const void *X, const float *gain, const float *offset, float eps, const rfsf_dropout_mask *mask, void *Y,
