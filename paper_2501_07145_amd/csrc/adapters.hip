@@ -492,6 +492,7 @@ struct Adapted {
                 // (in small tiles the next adapter's part of B is under way while the present one's is multiplied: 100 x 257, 50000 classes, 30 adapters 85 -> 63 us;
                 // in large ones, of which more rows are of one adapter, its registers are not there)
                 constexpr bool AHEAD = BM <= 2;
+                constexpr int GROUP = T::HAS_EXTRA || !BF16 ? 1 : 4;            // blocks of large tiles whose parts of B are loaded together, where registers allow
                 uint32_t next[BM][WORDS];
                 auto load = [&](uint64_t of, int a, int64_t first) __attribute__((always_inline)) {
                     const int64_t adapter = (int64_t)__builtin_amdgcn_readlane(mine[b], __builtin_ctzll(of)) * C;
@@ -530,9 +531,12 @@ struct Adapted {
 #pragma unroll
                     for (int a = 0; a < BM; ++a) {
                         if constexpr (!AHEAD) {
-                            if (t.i0 + 32 * a >= C) continue;
-                            load(now, 0, t.i0 + 32 * a);
-                            terms_of_b(next[0], f[a]);
+                            if (GROUP == 1 && t.i0 + 32 * a >= C) continue;
+                            if (a % GROUP == 0) {
+#pragma unroll
+                                for (int i = a; i < a + GROUP; ++i) load(now, i, t.i0 + 32 * i);
+                            }
+                            terms_of_b(next[a], f[a]);
                         }
                         add(t.acc[a][b], f[a]);
                     }
