@@ -127,6 +127,78 @@ __global__ __launch_bounds__(64 * kOrderWaves) void order_kernel(const int64_t *
     who[before] = who_of(adapters[row], count);
 }
 
+// Both in one launch, for some hundred rows that fit into registers: a workgroup packs a row, and compares it with all others on the way.
+constexpr int kPlaceThreads = 512;
+constexpr int64_t kPlaceRows = 1024, kPlaceColumns = 3 * 8 * kPlaceThreads;
+struct PlaceJob {
+    const void *X;
+    int64_t ld_x, K, count;
+    const int64_t *adapters;
+    int rows;
+    char *x;                            // packed, in the order of the adapters
+    int64_t pitch;
+    uint32_t *largest_x;
+    int32_t *order, *who;
+};
+template <bool TWO, int HELD>
+__global__ __launch_bounds__(kPlaceThreads) void place_kernel(PlaceJob job)
+{
+    typedef std::conditional_t<TWO, float, uint16_t> Number;
+    constexpr int WAVES = kPlaceThreads / 64;
+    __shared__ uint32_t part_largest[WAVES];
+    __shared__ int part_before[WAVES];
+    const int row = blockIdx.x;
+    const Number *from = static_cast<const Number *>(job.X) + row * job.ld_x;
+    float x[HELD][8];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) rows8::load(from, 8 * (int64_t)(threadIdx.x + u * kPlaceThreads), job.K, x[u]);
+    const int64_t adapter = job.adapters[row];
+    const int mine = code_of(adapter, job.count);
+    int before = 0;
+    for (int m = threadIdx.x; m < job.rows; m += kPlaceThreads) {
+        const int other = code_of(job.adapters[m], job.count);
+        before += other < mine || (other == mine && m < row);
+    }
+    uint32_t largest = 0;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(x[u][e]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) {
+        largest = max(largest, (uint32_t)__shfl_xor((int)largest, o));
+        before += __shfl_xor(before, o);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        part_largest[threadIdx.x >> 6] = largest;
+        part_before[threadIdx.x >> 6] = before;
+    }
+    __syncthreads();
+    largest = 0;
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        largest = max(largest, part_largest[w]);
+        before += part_before[w];
+    }
+    if (threadIdx.x == 0) {
+        job.largest_x[before] = largest;
+        job.order[before] = row;
+        job.who[before] = who_of(adapter, job.count);
+    }
+    const int shift = shift_of(largest);
+    char *to = job.x + before * job.pitch;
+    const int64_t end = (job.K + 63) / 64 * 64;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+        const int64_t k = 8 * (int64_t)(threadIdx.x + u * kPlaceThreads);
+        if (k >= end) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] = ldexpf(x[u][e], shift);
+        plane::store_terms<TWO>(to, k, plane::terms_of<TWO>(x[u]));
+    }
+}
+
 // Sums of products of 16 rows of `a` (lane l: row l % 16, already advanced to its quarter of 64 bytes) and 16 of each of NB groups of `x`, over steps first,
 // first + stride, ..: AHEAD steps under way at a time.
 template <bool TWO, int BM, int NB, int AHEAD>
@@ -668,14 +740,24 @@ hipError_t launch_rows(const Plan &f, const rfsf_adapters_shape &s, const Layout
     const uint32_t *largest_w = reinterpret_cast<const uint32_t *>(lay + z.largest_w), *largest_a = reinterpret_cast<const uint32_t *>(lay + z.largest_a);
     const float *scale = reinterpret_cast<const float *>(lay + z.scale);
     int32_t *order = nullptr, *who = nullptr;
+    bool packed = straight && rows <= kLocalRows && f.blocks == 1 && rows * s.K <= kLocal;
+    const bool local = packed;
     if (!straight) {
         order = reinterpret_cast<int32_t *>(ws + f.order);
         who = reinterpret_cast<int32_t *>(ws + f.who);
+    }
+    if (!straight && rows <= kPlaceRows && s.K <= kPlaceColumns) {
+        const PlaceJob job = {X, ld_x, s.K, s.count, adapters, (int)rows, ws + f.x, z.pitch, largest_x, order, who};
+        auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)rows), kPlaceThreads, 0, stream>>>(job); };
+        if (s.K <= 8 * kPlaceThreads) bf16 ? launch(place_kernel<false, 1>) : launch(place_kernel<true, 1>);
+        else bf16 ? launch(place_kernel<false, 3>) : launch(place_kernel<true, 3>);
+        RFSF_TRY(hipGetLastError());
+        packed = true;
+    } else if (!straight) {
         order_kernel<<<dim3((unsigned)((rows + kOrderRows - 1) / kOrderRows)), 64 * kOrderWaves, 0, stream>>>(adapters, (int)rows, s.count, order, who);
         RFSF_TRY(hipGetLastError());
     }
-    const bool local = straight && rows <= kLocalRows && f.blocks == 1 && rows * s.K <= kLocal;
-    if (!local) RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
+    if (!packed) RFSF_TRY(pack(PackJob{X, rows, s.K, ld_x, nullptr, largest_x, ws + f.x, nullptr, z.pitch, 0, order}, bf16, stream));
     const FewJob job = {ws + f.x, lay + z.w, lay + z.a, X, ld_x, s.K, largest_x, z.pitch, s.C, adapters, who, s.count, shared, inner, f.ld, (int)rows, z.ranks, z.ranks / 16, f.slots, (int)steps,
                         f.way.cuts, f.per_cut, f.cuts_inner, f.per_cut_inner, (unsigned)f.inner_groups};
     auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)(f.groups + f.inner_groups)), 64 * kFewWaves, 0, stream>>>(job); };
