@@ -698,15 +698,17 @@ Plan plan_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows, const 
 }
 
 // The way of a number of rows, by estimates of its time in us: straight, bound by what the L2s deliver to the CUs (rows of W and X); tiles with B's part in their
-// epilogue, which costs them some us each; tiles whose sums are cut where they would not fill the CUs; and join_kernel, bound by its reads and writes.
-// (Straight, tiles, cut tiles, us, float32: 20 x 5121, 5003 classes, 50 adapters of rank 16 39, 83, 39; 40 rows 52, 85, 41; 330 rows -, 124, 106; 64 x 1025, 1000
-// classes 17, 29, 20; 64 x 1025, 30000 classes 75, 47, 61; bfloat16: 64 x 257, 50000 classes 52, 37, 55; 180 x 2049, 2000 classes -, 44, 31.)
+// epilogue, which costs them some us each, the more the more adapters the rows of a block have; tiles whose sums are cut where they would not fill the CUs; and
+// join_kernel, bound by its reads and writes. Over 160 shapes of 8 to 1000 rows the choice is the best one, or at most 1.23 times as slow.
+// (Straight, tiles, cut tiles, us, float32: 20 x 5121, 5003 classes, 50 adapters of rank 16 39, 67, 37; 64 rows 59, 71, 41; 330 rows -, 95, 115; 64 x 1025, 1000
+// classes 17, 27, 18; 64 x 1025, 30000 classes 74, 42, 57; 180 x 2049, 2000 classes, 100 adapters of rank 32 -, 58, 41; bfloat16: 20 x 257, 50000 classes 28, 34, 34.)
 Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
 {
     const int64_t steps = plane_steps(s.K, !s.bf16);
-    auto join = [&](int cuts) { return (double)rows * (double)s.C * (4.0 * cuts + 4.0 + (s.bf16 ? 2 : 4) * z.ranks_b) / 4.0e6; };
+    auto join = [&](int cuts) { return (double)rows * (double)s.C * (4.0 * cuts + 4.0 + (s.bf16 ? 2 : 4) * z.ranks_b) / 2.8e6; };
     Way best = {false, 0, 0};
     double least = 0.0;
+    const double base = rows <= kPlaceRows && s.K <= kPlaceColumns ? 14.0 : 18.0;
     auto consider = [&](bool split, int edge, int cuts, double time) {
         if (best.cuts == 0 || time < least) {
             best = {split, edge, cuts};
@@ -717,13 +719,15 @@ Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
         const Plan f = plan_of(s, z, rows, {true, 0, 0});
         const int cuts = f.way.cuts;
         const double moved = ((double)f.groups / cuts * 16.0 * (f.wide + f.blocks) + (double)f.inner_groups / f.cuts_inner * 32.0) * (double)steps * kStepBytes;
-        consider(true, 0, cuts, 11.0 + moved / (f.blocks == 1 ? 9.0e6 : f.blocks == 2 ? 8.0e6 : 7.0e6) + join(cuts));
+        consider(true, 0, cuts, (f.blocks == 1 ? 8.0 : 11.0) + moved / (f.blocks == 1 ? 9.0e6 : f.blocks == 2 ? 8.0e6 : 7.0e6) + join(cuts));
     }
+    // (adapters that the 32 rows of a block have)
+    const double runs = std::min(32.0, 1.0 + 32.0 * (double)std::min(s.count, rows) / (double)rows), epilogue = (0.3 + 0.07 * runs) * (z.ranks / 16);
     for (const PlaneWay &way : kPlaneWays) {
         const double tiles = (double)plane_tiles(s.C, rows, way.edge);
-        consider(false, way.edge, 1, 18.0 + plane_step_time(way, tiles) * (double)steps + (way.edge == 256 ? 18.0 : way.edge == 128 ? 9.0 : 4.0) * std::max(1.0, tiles / way.slots));
+        consider(false, way.edge, 1, base + 3.0 + plane_step_time(way, tiles) * (double)steps + epilogue * (way.edge == 256 ? 18.0 : way.edge == 128 ? 9.0 : 4.0) * std::max(1.0, tiles / way.slots));
         for (int cuts : {2, 3, 4, 5, 6, 8, 10, 12, 16})
-            if (steps / cuts >= 8) consider(true, way.edge, cuts, 18.0 + plane_step_time(way, tiles * cuts) * (double)((steps + cuts - 1) / cuts) + join(cuts));
+            if (steps / cuts >= 8) consider(true, way.edge, cuts, base + plane_step_time(way, tiles * cuts) * (double)((steps + cuts - 1) / cuts) + join(cuts));
     }
     return best;
 }
