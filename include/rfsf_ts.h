@@ -416,7 +416,7 @@ int rfsf_layer_norm_backward(const rfsf_layer_norm_shape *shape, const void *X, 
  * the calls that follow on the stream. An adapter of a lower rank is padded with zeros by the caller. A layout that is cleared
  * first has adapters that add nothing; one that was never set and not cleared must not be used.
  * Accuracy: X and W, and A, enter the products as for rfsf_softmax_xent without gradients (float32 with 22 significand bits down to 2^-17 of the largest number of their
- * row, bfloat16 whole), the sums over r with the numbers of B as they are. Sums are held in 32 bits. A row of X, W, A or B with an infinity or a NaN
+ * row, bfloat16 whole); B enters whole, its products with an error below 2^-21. Sums are held in 32 bits. A row of X, W, A or B with an infinity or a NaN
  * makes what is computed from it NaN (bfloat16: or what infinities give), and nothing else. Equal calls with workspaces of equal sizes give equal bits.
  * Limits: K, C <= 3500000, N < 2^31, rank <= 256, count <= 131072 (RFSF_E_UNSUPPORTED). scale has to be finite (RFSF_E_BAD_SETTING). N = 0 is a no-op.
  */

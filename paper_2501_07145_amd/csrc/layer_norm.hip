@@ -93,8 +93,9 @@ __device__ __forceinline__ float rstd_of(float squares, float rest, float invers
     return 1.0f / sqrtf(fmaxf(squares * inverse - rest * rest, 0.f) + eps);
 }
 
-// THREADS lanes hold a row, HELD times eight numbers each; a workgroup goes through rows, whose next one is loaded while the present one is worked on, and
-// keeps its columns' gains and offsets.
+// Few rows, which should each be spread over many lanes: THREADS lanes hold a row, HELD times eight numbers each; a workgroup goes through rows, whose next one is
+// loaded while the present one is worked on, and keeps its columns' gains and offsets. Bound by latency: 1 x 1025 4.4 us, 333 x 5121, float32, with the launch 8; of
+// longer rows than norm_wave_kernel has registers for by memory (5000 x 16385, float32 148 us, 4.4 TB/s).
 template <typename T, int THREADS, int HELD, bool DROP>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(NormJob job)
 {
@@ -173,7 +174,9 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
 // each of the first lanes: an eight of its own would take as long as a whole one (200003 x 65, bfloat16, backward 29 -> 24 us).
 
 // Many rows: LANES of a wavefront have a row to themselves, and nobody waits for anybody; gains and offsets lie in LDS, once for all wavefronts of a CU. Of a lane's
-// eights the first FULL are there for every lane.
+// eights the first FULL are there for every lane. Bound by memory, with dropout on bfloat16 by the vector units as much (busy 71 % of the cycles, most of that the
+// generator): 30000 x 10241, bfloat16 265 us (4.6 TB/s), with dropout 288; float32 513 (4.8 TB/s), 516; 200003 x 65, bfloat16 13.4. A workgroup to a row
+// (norm_kernel) took 565 us of the second, gains and offsets from the L2 for every row or in registers of few wavefronts, everyone waiting for the row's slowest.
 constexpr int wave_threads(size_t held_bytes) { return held_bytes <= 28 ? 1024 : held_bytes <= 42 ? 768 : 512; }
 template <typename T, int LANES, int FULL, int HELD, bool DROP>
 __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kernel(NormJob job)
@@ -313,7 +316,8 @@ __device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_
 
 // The backward pass of rows that are held in registers, THREADS lanes a row, HELD eights each, of which all but the last are there for every lane; gains lie in LDS.
 // Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
-// sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits.
+// sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits. Bound by memory: 10000 x 10241, float32, with
+// dropout 247 us and 7.5 for the parts (4.8 TB/s); narrow rows by the vector units (200003 x 65, bfloat16 20 us and 4, busy 75 % of the cycles).
 constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && held <= 3) ? 4 : held == 2 ? 3 : 2; }
 template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
 __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, GAINS)) void back_kernel(BackJob job)
@@ -526,7 +530,8 @@ __global__ __launch_bounds__(kLongThreads) void back_long_kernel(BackJob job, bo
     }
 }
 
-// dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * LANES columns of some rows, LANES lanes of it a row.
+// dgain and doffset alone, which need no sums over rows' columns: a workgroup takes 8 * LANES columns of some rows, LANES lanes of it a row, four rows' loads ahead. Bound
+// by memory: 10000 x 10241, float32 153 us (5.4 TB/s), 7494 x 1001 with dropout 14.6 and 3.7 for the parts (a wavefront has 512 columns; with 2048 a workgroup 36).
 template <typename T>
 __device__ __forceinline__ rows8::Eight<T> load_short(const T *row, int k, int K)
 {
