@@ -408,23 +408,21 @@ class RfsfAdapters:
         self.C, self.K = W.shape
         self.count, self.rank, self.dtype, self.device = count, rank, W.dtype, W.device
         self._shape = _AdaptersShape(self.K, self.C, rank, count, _BF16[W.dtype])
-        self._shape_at = ctypes.addressof(self._shape)
         size = ctypes.c_size_t(0)
-        _check(load_library().rfsf_adapters_layout_bytes(self._shape_at, ctypes.byref(size)))
+        _check(load_library().rfsf_adapters_layout_bytes(ctypes.byref(self._shape), ctypes.byref(size)))
         _here(W)
         if stream is None:
             self.layout = torch.zeros(int(size.value), dtype=torch.uint8, device=W.device)
         else:
             with torch.cuda.stream(stream):
                 self.layout = torch.zeros(int(size.value), dtype=torch.uint8, device=W.device)
-        self._layout_at = self.layout.data_ptr()
         self.set_weights(W, stream)
 
     def set_weights(self, W: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Takes W [C, K], of the type and shape of the first one, for the calls that follow on the stream."""
         ld = _matrix(W, "W", self.dtype, (self.C, self.K))
         _here(W, self.layout)
-        _check(load_library().rfsf_adapters_set_weights(self._shape_at, W.data_ptr(), ld, self._layout_at, _stream_ptr(stream)))
+        _check(load_library().rfsf_adapters_set_weights(ctypes.byref(self._shape), W.data_ptr(), ld, self.layout.data_ptr(), _stream_ptr(stream)))
 
     def set(self, index: int, A: torch.Tensor, B: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Puts the adapter scale * B A (A [rank, K], B [C, rank], of W's type) into place `index` for the calls that follow on the stream."""
@@ -432,13 +430,13 @@ class RfsfAdapters:
             raise ValueError("index must be that of one of the adapters' places")
         ld_a, ld_b = _matrix(A, "A", self.dtype, (self.rank, self.K)), _matrix(B, "B", self.dtype, (self.C, self.rank))
         _here(A, B, self.layout)
-        _check(load_library().rfsf_adapters_set(self._shape_at, index, A.data_ptr(), ld_a, B.data_ptr(), ld_b, scale, self._layout_at,
+        _check(load_library().rfsf_adapters_set(ctypes.byref(self._shape), index, A.data_ptr(), ld_a, B.data_ptr(), ld_b, scale, self.layout.data_ptr(),
                                                 _stream_ptr(stream)))
 
     def workspace_bytes(self, N: int):
         """(recommended_bytes, minimum_bytes) of scratch for scores of N rows."""
         rec, mn = ctypes.c_size_t(0), ctypes.c_size_t(0)
-        _check(load_library().rfsf_adapted_scores_workspace_bytes(self._shape_at, N, ctypes.byref(rec), ctypes.byref(mn)))
+        _check(load_library().rfsf_adapted_scores_workspace_bytes(ctypes.byref(self._shape), N, ctypes.byref(rec), ctypes.byref(mn)))
         return int(rec.value), int(mn.value)
 
     def scores(self, X: torch.Tensor, adapters: torch.Tensor, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
@@ -457,6 +455,6 @@ class RfsfAdapters:
             workspace = _empty_on(stream, self.workspace_bytes(N)[0], dtype=torch.uint8, device=X.device)
         _dev(workspace, torch.uint8, "workspace")
         _here(X, adapters, out, workspace, self.layout)
-        _check(load_library().rfsf_adapted_scores(self._shape_at, self._layout_at, X.data_ptr(), N, ld, adapters.data_ptr(), out.data_ptr(), ld_out,
+        _check(load_library().rfsf_adapted_scores(ctypes.byref(self._shape), self.layout.data_ptr(), X.data_ptr(), N, ld, adapters.data_ptr(), out.data_ptr(), ld_out,
                                                   workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
         return out

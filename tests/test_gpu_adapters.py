@@ -1,4 +1,6 @@
 """Scores with low-rank adapters against the formula in 64 bits, within bounds that follow from the arithmetic."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -59,7 +61,8 @@ CASES = [
     (1, 1, 1, 1, 1), (1, 9, 5, 3, 2), (1, 1025, 1000, 8, 20), (2, 64, 33, 4, 3), (3, 65, 10, 1, 7), (5, 300, 31, 17, 4), (15, 129, 257, 16, 50), (16, 1025, 77, 5, 16), (17, 193, 64, 20, 3),
     (33, 100, 100, 33, 40), (64, 513, 300, 8, 64), (65, 257, 130, 12, 5), (130, 333, 65, 64, 9), (300, 129, 515, 16, 100), (333, 1025, 280, 7, 1), (1000, 65, 129, 6, 300), (40, 31, 7, 256, 2),
     (12, 13001, 40, 9, 5), (600, 40, 600, 100, 11), (20, 5121, 10, 16, 20), (48, 2049, 3, 24, 2), (7, 700, 5000, 16, 7), (1, 300, 17000, 4, 2),
-    (2000, 129, 8193, 7, 30), (2000, 140, 8200, 40, 3), (2100, 129, 8000, 5, 1500), (129, 5121, 1029, 20, 12), (260, 2500, 700, 33, 90), (4, 2049, 70, 12, 9), (5, 1025, 15, 12, 9),
+    (2000, 129, 8193, 7, 30), (2000, 140, 8200, 40, 3), (2100, 129, 8000, 5, 1500), (129, 5121, 1029, 20, 12), (260, 2500, 700, 33, 90), (4, 2049, 70, 12, 9), (5, 1025, 15, 12, 9), (70, 12500, 33, 5, 9),
+    (1100, 12500, 21, 5, 9),
 ]
 
 
@@ -166,6 +169,33 @@ def test_equal_calls_give_equal_bits_on_other_streams_and_in_graphs():
         torch.cuda.synchronize()
         assert torch.equal(out, other if turn % 2 else want)
         h.scores(X[:7], adapters[:7], workspace=space)                # the same workspace, between the replays
+
+
+def test_copies_have_layouts_of_their_own():
+    X, W, A, B, scale, adapters = _problem(30, 200, 60, 5, 4, torch.float32, seed=9)
+    h = _handle(W, A, B, scale)
+    other = copy.deepcopy(h)
+    want = h.scores(X.cuda(), adapters.cuda())
+    h.set_weights(torch.zeros_like(W).cuda())
+    del h
+    torch.cuda.empty_cache()
+    assert torch.equal(other.scores(X.cuda(), adapters.cuda()), want)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    problems = [_problem(N, 300, 500, 8, 6, torch.float32, seed=N) for N in (50, 300)]
+    handles, data = [_handle(*p[1:5]) for p in problems], [(p[0].cuda(), p[5].cuda()) for p in problems]
+    want = [h.scores(x, a) for h, (x, a) in zip(handles, data)]
+    outs = [[torch.empty_like(w) for _ in range(10)] for w in want]
+    spaces = [torch.empty(h.workspace_bytes(len(a))[0], dtype=torch.uint8, device="cuda") for h, (_, a) in zip(handles, data)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for t in range(10):
+        for i in range(2):
+            handles[i].scores(*data[i], out=outs[i][t], workspace=spaces[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in outs[i])
 
 
 def test_no_rows():

@@ -193,6 +193,47 @@ def test_many_rows_beyond_two_to_the_31_numbers():
     assert bool(((doffset[columns] - h.sum(0)).abs() <= bound * h.abs().sum(0)).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_graph_whose_first_call_is_captured(dtype):
+    # columns whose gains and offsets need more LDS than a kernel may have without being allowed to
+    x, gain, offset, dy = (t.cuda() for t in _inputs(2050, 9217, TYPES[dtype], seed=6))
+    Y, mean, rstd = torch.empty_like(x), torch.empty(2050, device="cuda"), torch.empty(2050, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rfsf.rfsf_layer_norm(x, gain, offset, dropout=rfsf.RfsfDropout(0.1, 4), out=Y, mean=mean, rstd=rstd)
+    for _ in range(3):
+        Y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = rfsf.rfsf_layer_norm(x, gain, offset, dropout=rfsf.RfsfDropout(0.1, 4))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((Y, mean, rstd), eager))
+
+
+def test_everything_left_out():
+    x, gain, offset, dy = (t.cuda() for t in _inputs(40, 300, torch.float32, seed=7))
+    drop = rfsf.RfsfDropout(1.0, 4)
+    Y, mean, rstd = rfsf.rfsf_layer_norm(x, gain, offset, dropout=drop)
+    assert not Y.any() and bool(rstd.isfinite().all())
+    assert all(not g.any() for g in rfsf.rfsf_layer_norm_backward(x, mean, rstd, dy, gain=gain, dropout=drop))
+
+
+def test_two_streams_at_once():
+    inputs = [[t.cuda() for t in _inputs(N, 1025, torch.float32, seed=8)] for N in (500, 3000)]
+    want = []
+    for x, gain, offset, dy in inputs:
+        Y, mean, rstd = rfsf.rfsf_layer_norm(x, gain, offset)
+        want.append((mean, rstd, rfsf.rfsf_layer_norm_backward(x, mean, rstd, dy, gain=gain)))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[rfsf.rfsf_layer_norm_backward(x, mean, rstd, dy, gain=gain, stream=s) for _ in range(5)]
+           for (x, gain, offset, dy), (mean, rstd, _), s in zip(inputs, want, streams)]
+    torch.cuda.synchronize()
+    for (_, _, w), results in zip(want, got):
+        assert all(torch.equal(a, b) for r in results for a, b in zip(r, w))
+
+
 def test_binding_refuses_shapes_that_do_not_fit():
     x = torch.zeros(4, 9, device="cuda")
     v = torch.zeros(9, device="cuda")
