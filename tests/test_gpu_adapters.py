@@ -75,7 +75,7 @@ def test_scores(dtype, N, K, C, rank, count):
         out = _place(torch.zeros(N, C), ld_out)
         assert h.scores(_place(X, K + pad, shift=pad), adapters.cuda(), out=out) is out
         _check(out, X, W, A, B, scale, adapters, dtype == "bfloat16")
-        assert torch.all(out._base[:N * ld_out].view(N, ld_out)[:, C:] == -7.0)
+        assert torch.all(out._base[:N * ld_out].view(N, ld_out)[:, C:] == -7.0) and torch.all(out._base[N * ld_out:] == -7.0)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -144,6 +144,40 @@ def test_small_and_unaligned_workspaces_and_many_rows(dtype):
     for size in (least, least * 7, rec // 2):
         space = torch.empty(size + 9, dtype=torch.uint8, device="cuda")[9:]
         _check(h.scores(X[:400], adapters[:400], workspace=space), X[:400], W, A, B, scale, adapters[:400], dtype == "bfloat16")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,C,rank,count", [(1, 1025, 100, 8, 3), (9, 300, 70, 20, 5), (40, 2049, 500, 8, 30), (64, 100, 3000, 5, 9), (100, 1500, 333, 40, 10), (400, 65, 600, 7, 400),
+                                              (1500, 129, 2100, 16, 20)])
+def test_nothing_is_written_beyond_the_workspace(dtype, N, K, C, rank, count):
+    X, W, A, B, scale, adapters = _problem(N, K, C, rank, count, TYPES[dtype], seed=10)
+    h, X, adapters = _handle(W, A, B, scale), X.cuda(), adapters.cuda()
+    want = h.scores(X, adapters)
+    rec, least = h.workspace_bytes(N)
+    for size, rows in ((rec, N), (least, 3), ((rec + least) // 2, N)):
+        for shift in (0, 9):
+            space = torch.full((size + shift + 4096,), 77, dtype=torch.uint8, device="cuda")
+            got = h.scores(X[:rows], adapters[:rows], workspace=space[shift:shift + size])
+            assert torch.all(space[shift + size:] == 77) and torch.all(space[:shift] == 77)
+            assert torch.allclose(got, want[:rows], rtol=1e-3, atol=1e-3 * float(want.abs().max()))
+
+
+def test_nothing_is_written_beyond_the_layout():
+    for dtype in (torch.float32, torch.bfloat16):
+        X, W, A, B, scale, adapters = _problem(5, 77, 31, 9, 4, dtype, seed=11)
+        h = rfsf.RfsfAdapters(W.cuda(), 4, 9)
+        size = h.layout.numel()
+        memory = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+        memory[:size] = 0
+        h.layout = memory[:size]
+        h.set_weights(W.cuda())
+        for e in (3, 0, 2, 1):
+            before = h.layout.clone()
+            h.set(e, A[e].cuda(), B[e].cuda(), scale[e])
+            h.set(e, A[e].cuda(), B[e].cuda(), scale[e])
+            assert int((before != h.layout).sum()) <= 16 * (384 + 4) + 31 * 12 * 4 + 4          # one adapter's rows of A, B, and scale
+        assert torch.all(memory[size:] == 77)
+        _check(h.scores(X.cuda(), adapters.cuda()), X, W, A, B, scale, adapters, dtype == torch.bfloat16)
 
 
 def test_equal_calls_give_equal_bits_on_other_streams_and_in_graphs():

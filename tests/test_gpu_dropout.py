@@ -41,7 +41,7 @@ def test_places_and_values(dtype, N, K, p):
         got = rfsf.rfsf_dropout(x, rfsf.RfsfDropout(p, seed=123456789012345678, offset=1 << 40, first_row=3), out=out)
         assert got is out
         _check(got, x, ref.mask(N, K, p, 123456789012345678, 1 << 40, 3), bf16)
-        assert torch.all(out._base[:N * (ld + 2)].view(N, ld + 2)[:, K:] == -7.0)            # columns beyond stay as they were
+        assert torch.all(out._base[:N * (ld + 2)].view(N, ld + 2)[:, K:] == -7.0) and torch.all(out._base[N * (ld + 2):] == -7.0)    # what is beyond stays as it was
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -22,8 +22,10 @@ def _place(x, dtype, ld, shift=0):
 
 
 def _beyond(view, ld):
+    """What lies between and around the rows."""
     N, K = view.shape
-    return view._base[view.storage_offset():view.storage_offset() + N * ld].view(N, ld)[:, K:]
+    rows = view._base[view.storage_offset():view.storage_offset() + N * ld].view(N, ld)
+    return torch.cat([rows[:, K:].flatten(), view._base[:view.storage_offset()], view._base[view.storage_offset() + N * ld:]])
 
 
 def _inputs(N, K, dtype, seed=0, far=0.0):
@@ -232,6 +234,20 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for (_, _, w), results in zip(want, got):
         assert all(torch.equal(a, b) for r in results for a, b in zip(r, w))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("need_dX", [True, False])
+@pytest.mark.parametrize("N,K", [(1, 5), (16, 193), (70, 9), (300, 129), (1000, 257), (333, 5121), (90, 10241), (2000, 2049), (40, 20485), (5000, 65)])
+def test_nothing_is_written_beyond_the_workspace(dtype, need_dX, N, K):
+    x, gain, _, dy = (t.cuda() for t in _inputs(N, K, TYPES[dtype], seed=9))
+    _, mean, rstd = rfsf.rfsf_layer_norm(x, gain)
+    size = rfsf.rfsf_layer_norm_backward_workspace_bytes(N, K, TYPES[dtype], need_dX)[1]
+    for shift in (0, 9):
+        space = torch.full((size + shift + 4096,), 77, dtype=torch.uint8, device="cuda")
+        got = rfsf.rfsf_layer_norm_backward(x, mean, rstd, dy, gain=gain, need_dX=need_dX, workspace=space[shift:shift + size])
+        assert torch.all(space[shift + size:] == 77) and torch.all(space[:shift] == 77)
+        assert all(g is None or bool(g.isfinite().all()) for g in got)
 
 
 def test_binding_refuses_shapes_that_do_not_fit():
