@@ -12,9 +12,9 @@
 namespace rfsf {
 namespace {
 
-constexpr int64_t kMostHeld = 512 * 5 * 8, kLeastHeld = 8;      // columns of rows that stay in registers
+constexpr int64_t kMostHeld = 512 * 5 * 8, kLeastHeld = 8;      // columns of rows that stay in registers; that loads of whole eights need
 constexpr int64_t kManyRows = 2048;
-constexpr bool is_held(int64_t K) { return K >= kLeastHeld && K <= kMostHeld; }
+constexpr bool is_held(int64_t K) { return K <= kMostHeld; }
 constexpr int kCus = 256;
 
 struct NormJob {
@@ -711,7 +711,7 @@ hipError_t launch_wave(const NormJob &job, bool drop, hipStream_t stream)
 template <typename T>
 hipError_t norm(const NormJob &job, bool drop, hipStream_t stream)
 {
-    if (job.N >= kManyRows && job.K >= kLeastHeld) {
+    if (job.N >= kManyRows || job.K < kLeastHeld) {
         hipError_t e = hipSuccess;
         auto wave = [&](auto lanes) { return [&, lanes](auto full, auto held) { e = launch_wave<T, lanes, full, held>(job, drop, stream); }; };
         typedef std::integral_constant<int, 8> l8;

@@ -32,7 +32,7 @@ def _check(out, x, factor, bf16):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,K,p", [(1, 1, 0.5), (1, 7, 0.3), (3, 8, 0.1), (5, 9, 0.9), (17, 65, 0.25), (300, 65, 0.2), (9, 257, 0.5), (4, 512, 0.01), (6, 1025, 0.6),
-                                   (2, 4097, 0.1), (3, 10241, 0.35), (1, 70001, 0.5), (2000, 33, 0.7)])
+                                   (2, 4097, 0.1), (3, 10241, 0.35), (1, 70001, 0.5), (2000, 33, 0.7), (70000, 1, 0.4), (3001, 9, 0.3), (517, 129, 0.3)])
 def test_places_and_values(dtype, N, K, p):
     bf16 = dtype == "bfloat16"
     for ld, shift in ((K, 0), ((K + 7) // 8 * 8, 0), (K + 3, 1)):

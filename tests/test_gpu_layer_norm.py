@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 TYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16}
 SHAPES = [(1, 1), (1, 2), (3, 7), (5, 64), (2, 65), (4, 128), (4, 129), (3, 256), (3, 257), (5, 512), (9, 513), (6, 1024), (7, 1025), (3, 2049), (5, 4097), (3, 6145),
-          (2, 8193), (3, 12289), (2, 16385), (2, 20480), (2, 20481), (1, 50001), (1500, 65), (300, 193), (40, 1001), (2100, 129), (1300, 300), (1030, 2051), (300, 5121), (700, 9003), (2049, 4099)]
+          (2, 8193), (3, 12289), (2, 16385), (2, 20480), (2, 20481), (1, 50001), (1500, 65), (300, 193), (40, 1001), (2100, 129), (1300, 300), (1030, 2051), (300, 5121), (700, 9003), (2049, 4099), (5000, 3), (9000, 1), (4000, 7)]
 
 
 def _place(x, dtype, ld, shift=0):
