@@ -90,7 +90,8 @@ __device__ __forceinline__ Mean mean_of(double sum, double inverse)
 }
 __device__ __forceinline__ float rstd_of(float squares, float rest, float inverse, float eps)
 {
-    return 1.0f / sqrtf(fmaxf(squares * inverse - rest * rest, 0.f) + eps);
+    const float variance = squares * inverse - rest * rest;
+    return 1.0f / sqrtf((variance < 0.f ? 0.f : variance) + eps);           // (a NaN stays)
 }
 
 // Few rows, which should each be spread over many lanes: THREADS lanes hold a row, HELD times eight numbers each; a workgroup goes through rows, whose next one is

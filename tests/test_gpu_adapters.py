@@ -85,6 +85,16 @@ def test_rows_of_all_sizes(dtype, N, K, C, rank, count):
     _check(_handle(W, A, B, scale).scores(X.cuda(), adapters.cuda()), X, W, A, B, scale, adapters, dtype == "bfloat16")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,C", [(3, 70), (60, 90), (400, 3000)])
+@pytest.mark.parametrize("power", [-112, 112])
+def test_adapters_far_from_one(dtype, N, C, power):
+    """B of some size and a scale that takes it back: nothing on the way is lost at the ends of the range of 32 bits."""
+    X, W, A, B, scale, adapters = _problem(N, 300, C, 12, 9, TYPES[dtype], seed=6)
+    B, scale = B * 2.0 ** power, [s * 2.0 ** -power for s in scale]
+    _check(_handle(W, A, B, scale).scores(X.cuda(), adapters.cuda()), X, W, A, B, scale, adapters, dtype == "bfloat16")
+
+
 @pytest.mark.parametrize("N", [1, 9, 16, 40, 100, 400])
 def test_adapters_that_no_one_has_everyone_has_or_that_do_not_exist(N):
     X, W, A, B, scale, _ = _problem(N, 130, 70, 8, 6, torch.float32, seed=2)

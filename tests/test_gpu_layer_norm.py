@@ -121,6 +121,23 @@ def test_infinities_and_nan_stay_in_their_rows(dtype, K):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [7, 2100])
+@pytest.mark.parametrize("K", [3, 65, 1025, 20485])
+def test_statistics_of_rows_with_infinities_and_nan(dtype, N, K):
+    """The mean is what the sum gives, the deviation is NaN and not that of a row without variance; the other rows have theirs."""
+    if N * K > 1 << 22:
+        N = 2050
+    x = torch.ones(N, K, dtype=TYPES[dtype], device="cuda")
+    x[:, 0] = 5.0
+    x[1, 1], x[2, K - 1], x[4, 0] = float("inf"), float("nan"), -float("inf")
+    _, mean, rstd = rfsf.rfsf_layer_norm(x)
+    bad = torch.zeros(N, dtype=torch.bool, device="cuda")
+    bad[[1, 2, 4]] = True
+    assert torch.equal(rstd.isnan(), bad) and torch.equal(mean.isfinite(), ~bad)
+    assert mean[1] == float("inf") and mean[4] == -float("inf") and mean[2].isnan()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,K", [(30, 65), (9, 1025), (7, 10241), (5, 20489)])
 def test_in_place(dtype, N, K):
     x, gain, offset, dy = (t.cuda() for t in _inputs(N, K, TYPES[dtype], seed=4))
