@@ -13,6 +13,7 @@ import torch
 from .binding import _check, _dev, _empty_on, _stream_ptr, load_library
 
 _BF16 = {torch.float32: 0, torch.bfloat16: 1}
+_F32 = torch.float32
 _DPHI, _DW = 1, 2
 
 
@@ -293,20 +294,21 @@ class RfsfDropout:
         return _DropoutMask(self.p, self.seed, self.offset, None if self.counter is None else self.counter.data_ptr(), self.first_row)
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """Refuses tensors that are not on the current device, whose stream the work goes to."""
+def _here(*tensors: Optional[torch.Tensor]) -> int:
+    """Refuses tensors that are not on the current device, whose stream the work goes to; its number."""
     current = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != current:
             raise ValueError("all tensors must be on the current device")
+    return current
 
 
-def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
-    """Address of a contiguous float32 device tensor [n], or None."""
+def _vector(t: Optional[torch.Tensor], n: int, name: str, device: int) -> Optional[int]:
+    """Address of a contiguous float32 tensor [n] on the device of this number, or None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous float32 [{n}] on the device")
+    if t.dtype is not _F32 or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous float32 [{n}] on the current device")
     return t.data_ptr()
 
 
@@ -337,11 +339,11 @@ def rfsf_layer_norm(X: torch.Tensor, gain: Optional[torch.Tensor] = None, offset
         mean = _empty_on(stream, N, dtype=torch.float32, device=X.device)
     if rstd is None:
         rstd = _empty_on(stream, N, dtype=torch.float32, device=X.device)
-    _here(X, out, gain, offset, mean, rstd, dropout and dropout.counter)
+    device = _here(X, out, dropout and dropout.counter)
     shape = _LayerNormShape(N, K, ldx, ldy, K, _BF16[X.dtype])
     mask = dropout._mask() if dropout is not None else None
-    _check(load_library().rfsf_layer_norm(ctypes.byref(shape), X.data_ptr(), _vector(gain, K, "gain"), _vector(offset, K, "offset"), eps,
-                                          mask and ctypes.byref(mask), out.data_ptr(), _vector(mean, N, "mean"), _vector(rstd, N, "rstd"),
+    _check(load_library().rfsf_layer_norm(ctypes.byref(shape), X.data_ptr(), _vector(gain, K, "gain", device), _vector(offset, K, "offset", device), eps,
+                                          mask and ctypes.byref(mask), out.data_ptr(), _vector(mean, N, "mean", device), _vector(rstd, N, "rstd", device),
                                           _stream_ptr(stream)))
     return out, mean, rstd
 
@@ -385,14 +387,14 @@ def rfsf_layer_norm_backward(X: torch.Tensor, mean: torch.Tensor, rstd: torch.Te
         workspace = _dev(workspace, torch.uint8, "workspace")
     else:
         dgain = doffset = workspace = None
-    _here(X, mean, rstd, dY, gain, dX, dgain, doffset, workspace, dropout and dropout.counter)
-    mask = dropout._mask() if dropout is not None else None
-    if _vector(mean, N, "mean") is None or _vector(rstd, N, "rstd") is None:
+    if mean is None or rstd is None:
         raise ValueError("mean and rstd are needed")
-    _check(lib.rfsf_layer_norm_backward(ctypes.byref(shape), X.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _vector(gain, K, "gain"), dY.data_ptr(),
-                                        mask and ctypes.byref(mask), dX.data_ptr() if need_dX else None, _vector(dgain, K, "dgain"),
-                                        _vector(doffset, K, "doffset"), workspace.data_ptr() if need_gains else None,
-                                        workspace.numel() if need_gains else 0, _stream_ptr(stream)))
+    device = _here(X, dY, dX, workspace, dropout and dropout.counter)
+    mask = dropout._mask() if dropout is not None else None
+    _check(lib.rfsf_layer_norm_backward(ctypes.byref(shape), X.data_ptr(), _vector(mean, N, "mean", device), _vector(rstd, N, "rstd", device),
+                                        _vector(gain, K, "gain", device), dY.data_ptr(), mask and ctypes.byref(mask), dX.data_ptr() if need_dX else None,
+                                        _vector(dgain, K, "dgain", device), _vector(doffset, K, "doffset", device),
+                                        workspace.data_ptr() if need_gains else None, workspace.numel() if need_gains else 0, _stream_ptr(stream)))
     return dX, dgain, doffset
 
 
