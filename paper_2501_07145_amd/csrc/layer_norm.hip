@@ -319,12 +319,14 @@ __device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_
 // Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
 // sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits. Bound by memory: 10000 x 10241, float32, with
 // dropout 247 us and 7.5 for the parts (4.8 TB/s); narrow rows by the vector units (200003 x 65, bfloat16 20 us and 4, busy 75 % of the cycles).
-constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && held <= 3) ? 4 : held == 2 ? 3 : 2; }
+template <typename T>
+constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && (held == 2 || (held == 3 && sizeof(T) == 2))) ? 4 : held == 2 ? 3 : 2; }
 template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
-__global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, GAINS)) void back_kernel(BackJob job)
+__global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves<T>(HELD, GAINS)) void back_kernel(BackJob job)
 {
     constexpr int GROUP = THREADS > 256 ? THREADS : 256, ROWS = GROUP / THREADS, WAVES = THREADS > 64 ? THREADS / 64 : 1, STEP = 8 * THREADS;
     constexpr bool AHEAD = HELD <= (sizeof(T) == 2 ? 4 : 3);          // registers for the next row
+    constexpr bool KEEP = HELD <= 2 || (HELD == 3 && sizeof(T) == 2 && (DROP || THREADS <= 64));         // and for z and g from the sums to dX
     __shared__ float part[2][WAVES][2];
     __shared__ __attribute__((aligned(16))) float gains[STEP * HELD + 8];
     const int lane = threadIdx.x % THREADS, K = (int)job.K, whole = K / 8 * 8, last = whole + lane;
@@ -363,7 +365,6 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
     // (all rows of a workgroup take as many turns, so that everybody meets at the barriers)
     for (int64_t turn = (int64_t)blockIdx.x * ROWS; turn < job.N; turn += step, row += step) {
         if (!AHEAD) load(row);
-        const bool there = ROWS == 1 || row < job.N;
         mean = next_mean;
         rstd = next_rstd;
         x_last = next_x_last;
@@ -374,12 +375,14 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
             h[u] = next_h[u];
         }
         if (AHEAD && turn + step < job.N) load(row + step);
+        const bool there = ROWS == 1 || row < job.N;
         float sums[2] = {0.f, 0.f};             // of g, of g z
+        float kept_z[KEEP ? HELD : 1][8], kept_g[KEEP ? HELD : 1][8];
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
             if (u == HELD - 1 && k >= whole) continue;
-            rows8::in_turn(x[u]);
+            if (!KEEP) rows8::in_turn(x[u]);
             if (DROP) {
                 uint32_t group = (uint32_t)k / 8;
                 asm volatile("" : "+v"(group));            // (the first rounds' products, which are the same for all rows, would be kept for every u)
@@ -390,6 +393,10 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float z = there ? (rows8::to_float(x[u].v[e]) - mean) * rstd : 0.f, d = there ? rows8::to_float(h[u].v[e]) : 0.f, g = d * gain[e];
+                if (KEEP) {
+                    kept_z[u][e] = z;
+                    kept_g[u][e] = g;
+                }
                 if (GAINS) {
                     of_gain[u][e] = fmaf(d, z, of_gain[u][e]);
                     of_offset[u][e] += d;
@@ -420,14 +427,20 @@ __global__ __launch_bounds__((THREADS > 256 ? THREADS : 256), back_waves(HELD, G
         for (int u = 0; u < HELD; ++u) {
             const int k = 8 * lane + STEP * u;
             if (u == HELD - 1 && k >= whole) continue;
-            rows8::in_turn(x[u]);
-            rows8::in_turn(h[u]);
-            float gain[8], d[8];
-            __builtin_memcpy(gain, gains + k, 32);
+            float d[8];
+            if constexpr (KEEP) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float z = (rows8::to_float(x[u].v[e]) - mean) * rstd;
-                d[e] = (rows8::to_float(h[u].v[e]) * gain[e] - fmaf(z, sums[1], sums[0])) * scale;
+                for (int e = 0; e < 8; ++e) d[e] = (kept_g[u][e] - fmaf(kept_z[u][e], sums[1], sums[0])) * scale;
+            } else {
+                rows8::in_turn(x[u]);
+                rows8::in_turn(h[u]);
+                float gain[8];
+                __builtin_memcpy(gain, gains + k, 32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = (rows8::to_float(x[u].v[e]) - mean) * rstd;
+                    d[e] = (rows8::to_float(h[u].v[e]) * gain[e] - fmaf(z, sums[1], sums[0])) * scale;
+                }
             }
             rows8::store(to, k, k + 8, d);
         }
@@ -665,7 +678,7 @@ bool apart(int64_t N, int64_t K)
 {
     return with_shape<T>(K / 8, [&](auto threads, auto held) {
         if (threads < 256 || N <= kCus) return false;
-        return 16 * groups_of(N, threads, back_waves(held, true), true) > 2 * N * (int64_t)sizeof(T) + N / 2 * (int64_t)sizeof(T);
+        return 16 * groups_of(N, threads, back_waves<T>(held, true), true) > 2 * N * (int64_t)sizeof(T) + N / 2 * (int64_t)sizeof(T);
     });
 }
 
@@ -676,7 +689,7 @@ template <typename T>
 int64_t parts_of(int64_t N, int64_t K, bool with_dx)
 {
     if (N == 0) return 0;
-    if (with_dx && is_held(K) && !apart<T>(N, K)) return with_shape<T>(K / 8, [&](auto threads, auto held) { return groups_of(N, threads, back_waves(held, true), true); });
+    if (with_dx && is_held(K) && !apart<T>(N, K)) return with_shape<T>(K / 8, [&](auto threads, auto held) { return groups_of(N, threads, back_waves<T>(held, true), true); });
     const int64_t rows = 256 / gains_lanes(K), groups = (N + rows - 1) / rows;
     return std::max<int64_t>(1, std::min<int64_t>(groups / 4, kCus * 4 / gains_pieces(K)));
 }
@@ -752,7 +765,7 @@ template <typename T>
 hipError_t back_held(const BackJob &job, bool drop, bool gains, hipStream_t stream)
 {
     with_shape<T>(job.K / 8, [&](auto threads, auto held) {
-        const dim3 grid((unsigned)groups_of(job.N, threads, back_waves(held, gains), gains));
+        const dim3 grid((unsigned)groups_of(job.N, threads, back_waves<T>(held, gains), gains));
         auto launch = [&](auto kernel) { kernel<<<grid, group_threads(threads), 0, stream>>>(job); };
         if (drop && gains) launch(back_kernel<T, threads, held, true, true>);
         else if (drop) launch(back_kernel<T, threads, held, true, false>);
