@@ -317,8 +317,10 @@ __device__ __forceinline__ Sums sums_of(const BackJob &job, int64_t part, int64_
 
 // The backward pass of rows that are held in registers, THREADS lanes a row, HELD eights each, of which all but the last are there for every lane; gains lie in LDS.
 // Dropout's factor is taken out of all sums: it multiplies what comes of them. GAINS: a lane adds its columns' h z and h up over the rows of the workgroup, whose
-// sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits. Bound by memory: 10000 x 10241, float32, with
-// dropout 247 us and 7.5 for the parts (4.8 TB/s); narrow rows by the vector units (200003 x 65, bfloat16 20 us and 4, busy 75 % of the cycles).
+// sums are then one of the parts that add_parts_kernel adds up: no atomics, so that equal calls give equal bits. KEEP: z and g stay in registers until dX is written, where
+// there are some (200003 x 65, bfloat16, with dropout, all launches 28.7 -> 27.0 us; 30000 x 5121 without dropout 180 -> 197). Bound by memory: 10000 x 10241, float32,
+// with dropout 247 us and 7.5 for the parts (4.8 TB/s), dX alone 242 (with registers for four wavefronts a SIMD, which spill, 313); narrow rows by the vector units
+// (200003 x 65, bfloat16 19 us and 4).
 template <typename T>
 constexpr int back_waves(int held, bool gains) { return held == 1 || (!gains && (held == 2 || (held == 3 && sizeof(T) == 2))) ? 4 : held == 2 ? 3 : 2; }
 template <typename T, int THREADS, int HELD, bool DROP, bool GAINS>
@@ -651,13 +653,15 @@ auto with_first(int64_t eights, const F &f, Shape<THREADS, HELD>, MORE... more)
     }
     return f(std::integral_constant<int, THREADS>(), std::integral_constant<int, HELD>());
 }
-// (256 lanes with five eights of 32-bit numbers each have no registers for the next row: 10000 x 10241, backward 280 us, 512 with three 258; bfloat16 156 and 166)
+// (256 lanes with five eights of 32-bit numbers each have no registers for the next row: 10000 x 10241, backward 280 us, 512 with three 258; bfloat16 156 and 166. Less
+// than a workgroup, where a row's next one is loaded later anyway, spill with five: 30000 x 2305 with dropout 236 us, more lanes with fewer 172; bfloat16 109 and 120.)
 template <typename T, typename F>
 auto with_shape(int64_t eights, const F &f)
 {
     typedef std::conditional_t<sizeof(T) == 2, Shape<256, 5>, Shape<512, 3>> Wide;
-    return with_first(eights, f, Shape<8, 1>(), Shape<8, 2>(), Shape<8, 3>(), Shape<16, 2>(), Shape<16, 3>(), Shape<16, 4>(), Shape<16, 5>(), Shape<64, 2>(), Shape<64, 3>(),
-                      Shape<64, 4>(), Shape<64, 5>(), Shape<256, 2>(), Shape<256, 3>(), Shape<256, 4>(), Wide(), Shape<512, 3>(), Shape<512, 4>(), Shape<512, 5>());
+    constexpr int most = sizeof(T) == 2 ? 5 : 4;
+    return with_first(eights, f, Shape<8, 1>(), Shape<8, 2>(), Shape<8, 3>(), Shape<16, 2>(), Shape<16, 3>(), Shape<16, 4>(), Shape<16, most>(), Shape<64, 2>(), Shape<64, 3>(),
+                      Shape<64, 4>(), Shape<64, most>(), Shape<256, 2>(), Shape<256, 3>(), Shape<256, 4>(), Wide(), Shape<512, 3>(), Shape<512, 4>(), Shape<512, 5>());
 }
 constexpr int group_threads(int threads) { return threads > 256 ? threads : 256; }
 constexpr int group_rows(int threads) { return threads >= 256 ? 1 : 256 / threads; }
