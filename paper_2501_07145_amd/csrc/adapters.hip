@@ -200,6 +200,25 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(PlaceJob job)
     }
 }
 
+// A step of products of 16 rows of each of `fa` and 16 of each of `fx`.
+template <bool TWO, int BM, int NB>
+__device__ __forceinline__ void multiply_step(const halfx8 (&fa)[BM][2], const halfx8 (&fx)[NB][2], floatx4 (&acc)[BM][NB])
+{
+#pragma unroll
+    for (int m = 0; m < BM; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            if (TWO) {
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][0], acc[m][n], 0, 0, 0);
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][1], acc[m][n], 0, 0, 0);
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
+            } else {
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][1], acc[m][n], 0, 0, 0);
+            }
+        }
+}
+
 // Sums of products of 16 rows of `a` (lane l: row l % 16, already advanced to its quarter of 64 bytes) and 16 of each of NB groups of `x`, over steps first,
 // first + stride, ..: AHEAD steps under way at a time.
 template <bool TWO, int BM, int NB, int AHEAD>
@@ -215,21 +234,6 @@ __device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const
             for (int n = 0; n < NB; ++n) fx[n][h] = *reinterpret_cast<const halfx8 *>(x[n] + at + 64 * h);
         }
     };
-    auto multiply = [&](const halfx8 (&fa)[BM][2], const halfx8 (&fx)[NB][2]) {
-#pragma unroll
-        for (int m = 0; m < BM; ++m)
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                if (TWO) {
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][0], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][1], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
-                } else {
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][0], fx[n][0], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[m][1], fx[n][1], acc[m][n], 0, 0, 0);
-                }
-            }
-    };
     int s = first;
     for (; s + (AHEAD - 1) * stride < steps; s += AHEAD * stride) {
         halfx8 fa[AHEAD][BM][2], fx[AHEAD][NB][2];
@@ -237,12 +241,12 @@ __device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const
         for (int u = 0; u < AHEAD; ++u) load(s + u * stride, fa[u], fx[u]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) multiply(fa[u], fx[u]);
+        for (int u = 0; u < AHEAD; ++u) multiply_step<TWO>(fa[u], fx[u], acc);
     }
     for (; s < steps; s += stride) {
         halfx8 fa[BM][2], fx[NB][2];
         load(s, fa, fx);
-        multiply(fa, fx);
+        multiply_step<TWO>(fa, fx, acc);
     }
 }
 
@@ -253,9 +257,63 @@ __device__ __forceinline__ void multiply_steps(const char *const (&a)[BM], const
 // classes, all launches, 410 us (5.1 TB/s).
 constexpr int64_t kFewGroups = 512;
 constexpr int kFewWaves = 4, kFewAhead = 2, kFewBlocks = 4, kFewRows = 16 * kFewBlocks, kWide = 2;
-// LOCAL: rows of X that have few numbers altogether are packed by every workgroup for itself, a wavefront each, into LDS: a launch less (1 x 1025, 1000 classes 13.0 ->
-// 10.6 us; seven rows, two a wavefront, 11.2 -> 12.3).
+// LOCAL: up to four rows of X that have few numbers altogether are packed by every workgroup for itself into LDS: a launch less (1 x 1025, 1000 classes 13.0 -> 9.6 us;
+// seven rows 11.2 -> 12.3), all numbers at once (1 x 8192, 1000 classes, float32 14.4 us; a wavefront a row, in turns, 25.4).
+constexpr int kMostRank = 256;              // that is accepted
 constexpr int kLocal = 8192, kLocalRows = kFewWaves, kLocalPad = 16;        // numbers, rows; bytes between rows, for their banks
+constexpr size_t local_bytes(bool two) { return kLocal * (two ? 4 : 2) + kLocalRows * (kStepBytes + kLocalPad); }
+// Packs the rows into `local`, all wavefronts together, some to a row: every number is loaded once, all loads are under way at the same time. largest: in LDS, the
+// wavefronts' largest numbers of a row (largest_in), there when this returns. meanwhile(): called when the loads are under way, which come back in their order.
+template <int WAVES>
+__device__ __forceinline__ uint32_t largest_in(const uint32_t (&largest)[WAVES])
+{
+    uint32_t v = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v = max(v, largest[w]);
+    return v;
+}
+template <bool TWO, int WAVES, typename F>
+__device__ __forceinline__ void pack_local(const void *X, int64_t ld_x, int64_t K, int rows, int steps, int64_t pitch, char *local, uint32_t (&largest)[kLocalRows][WAVES],
+                                           const F &meanwhile)
+{
+    typedef std::conditional_t<TWO, float, uint16_t> Number;
+    constexpr int EIGHTS = TWO ? 4 : 8, HELD = (kLocal / 8 / 3 + EIGHTS + 16 * WAVES - 1) / (16 * WAVES);        // eights of a step; of a lane at most: three rows, a wavefront in four each
+    static_assert(kLocalRows == 4 && HELD * 64 * WAVES >= kLocal / 8 + EIGHTS, "");
+    const int each = steps * EIGHTS, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), sharing = rows == 1 ? WAVES : rows == 2 ? WAVES / 2 : WAVES / 4;
+    const int row = wave / sharing, first = wave % sharing * 64 + (int)(threadIdx.x & 63);
+    float v[HELD][8];
+    if (row < rows) {
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+            if (first + u * sharing * 64 < each) rows8::load(static_cast<const Number *>(X) + row * ld_x, 8 * (first + u * sharing * 64), K, v[u]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    meanwhile();
+    __builtin_amdgcn_sched_barrier(0);
+    if (row < rows) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+            if (first + u * sharing * 64 < each)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(v[u][e]) & 0x7fffffffu);
+#pragma unroll
+        for (int o = 32; o > 0; o /= 2) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+        for (int w = wave % sharing; w < WAVES; w += sharing) largest[row][w] = most;
+    }
+    __syncthreads();
+    if (row < rows) {
+        const int shift = shift_of(largest_in(largest[row]));
+#pragma unroll
+        for (int u = 0; u < HELD; ++u)
+            if (first + u * sharing * 64 < each) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = ldexpf(v[u][e], shift);
+                plane::store_terms<TWO>(local + row * pitch, 8 * (first + u * sharing * 64), plane::terms_of<TWO>(v[u]));
+            }
+    }
+    __syncthreads();
+}
 struct FewJob {
     const char *x, *w, *a;              // packed
     const void *X;                      // LOCAL: as they are, ld_x numbers apart
@@ -274,34 +332,15 @@ template <bool TWO, int BM, int NB, bool LOCAL>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewJob job)
 {
     static_assert(!LOCAL || NB == 1, "");
-    typedef std::conditional_t<TWO, float, uint16_t> Number;
     __shared__ float part[kFewWaves][BM * NB * 4][64];
-    __shared__ __attribute__((aligned(16))) char local[LOCAL ? kLocal * (TWO ? 4 : 2) + kLocalRows * (kStepBytes + kLocalPad) : 16];
+    __shared__ __attribute__((aligned(16))) char local[LOCAL ? local_bytes(TWO) : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
     const int64_t pitch_x = LOCAL ? job.steps * kStepBytes + kLocalPad : job.pitch;
     const char *rows_x = LOCAL ? local : job.x;
     if constexpr (LOCAL) {
-        for (int n = wave; n < job.rows; n += kFewWaves) {
-            const Number *from = static_cast<const Number *>(job.X) + n * job.ld_x;
-            float v[8];
-            uint32_t largest = 0;
-            for (int64_t k = 8 * lane; k < job.K; k += 512) {
-                rows8::load(from, k, job.K, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
-            }
-#pragma unroll
-            for (int o = 32; o > 0; o /= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, o));
-            if (blockIdx.x == 0 && lane == 0) job.largest_x[n] = largest;
-            const int shift = shift_of(largest);
-            for (int64_t k = 8 * lane; k < job.steps * (TWO ? 32 : 64); k += 512) {
-                rows8::load(from, k, job.K, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], shift);
-                plane::store_terms<TWO>(local + n * pitch_x, k, plane::terms_of<TWO>(v));
-            }
-        }
-        __syncthreads();
+        __shared__ uint32_t largest[kLocalRows][kFewWaves];
+        pack_local<TWO>(job.X, job.ld_x, job.K, job.rows, job.steps, pitch_x, local, largest, [] {});
+        if (blockIdx.x == 0 && (int)threadIdx.x < job.rows) job.largest_x[threadIdx.x] = largest_in(largest[threadIdx.x]);
     }
     if (blockIdx.x < job.inner_groups) {
         int id = blockIdx.x;
@@ -379,7 +418,7 @@ struct JoinJob {
     float *out;
     int rows, rows_each, ranks, ranks_b, cuts, cuts_inner;
 };
-constexpr int kJoinThreads = 256, kMostRank = 256;      // (the rank that is accepted at most)
+constexpr int kJoinThreads = 256;
 template <bool BF16>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
 {
@@ -428,6 +467,91 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinJob job)
         }
         if (c < job.C) job.out[(int64_t)(job.order ? job.order[n] : n) * job.ld + c] = adapter == kUnknown ? NAN : v;
     }
+}
+
+// One request, up to 16 ranks, and so few classes and columns that latency is all that counts: everything in one launch. A workgroup has 16 classes, packs the row and forms
+// its adapter's inner products for itself, its wavefronts sharing the steps. All that it reads is under way before the row is packed. 1 x 1025, 1000 classes, rank 8: float32
+// 7.8 us a call (few_kernel and join_kernel 9.6; replayed in a graph 7.9 and 8.5), bfloat16 8.0 (9.6; 8.0 and 8.2).
+constexpr int kOneWaves = 16, kOneSteps = 3, kCus = 256;         // steps of a wavefront at most
+struct OneJob {
+    const char *w, *a;                  // packed
+    const void *X, *B;
+    int64_t K, pitch, C, count;
+    const int64_t *adapters;
+    const uint32_t *largest_w, *largest_a;
+    const float *scale;
+    float *out;
+    int ranks_b, steps;
+};
+template <bool TWO>
+__global__ __launch_bounds__(64 * kOneWaves) void one_kernel(OneJob job)
+{
+    constexpr int SIXTEEN = TWO ? 4 : 2;
+    __shared__ float part[kOneWaves][32];                   // shared products of 16 classes, inner ones of 16 ranks
+    __shared__ __attribute__((aligned(16))) char local[local_bytes(TWO)];
+    __shared__ uint32_t largest[kLocalRows][kOneWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+    const int64_t c0 = (int64_t)blockIdx.x * 16, c = std::min(c0 + col, job.C - 1);
+    halfx8 f[kOneSteps][2][2];
+    auto load = [&](int m, const char *row) {
+#pragma unroll
+        for (int u = 0; u < kOneSteps; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                f[u][m][h] = *reinterpret_cast<const halfx8 *>(row + (int64_t)std::min(wave + u * kOneWaves, job.steps - 1) * kStepBytes + 16 * quarter + 64 * h);
+    };
+    // the first wavefront writes the results: class l % 16 and rank l % 16 in all four quarters
+    int adapter = kNone, shift = 0;
+    uint4 b[SIXTEEN];
+    float scale = 0.f;
+    pack_local<TWO>(job.X, 0, job.K, 1, job.steps, 0, local, largest, [&] {
+        load(0, job.w + c * job.pitch);
+        adapter = who_of(job.adapters[0], job.count);
+        load(1, adapter >= 0 ? job.a + ((int64_t)adapter * 16 + col) * job.pitch : job.w + c * job.pitch);
+        if (wave != 0) return;
+        shift = -shift_of(lane & 16 ? (adapter >= 0 ? job.largest_a[(int64_t)adapter * 16 + col] : 0u) : job.largest_w[c]);
+        if (adapter < 0) return;
+        scale = job.scale[adapter];
+        const char *b_row = static_cast<const char *>(job.B) + ((int64_t)adapter * job.C + c) * job.ranks_b * (TWO ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < SIXTEEN; ++i) b[i] = i * 16 < job.ranks_b * (TWO ? 4 : 2) ? *reinterpret_cast<const uint4 *>(b_row + 16 * i) : make_uint4(0, 0, 0, 0);
+    });
+    floatx4 acc[2][1] = {{{0.f, 0.f, 0.f, 0.f}}, {{0.f, 0.f, 0.f, 0.f}}};
+#pragma unroll
+    for (int u = 0; u < kOneSteps; ++u) {
+        const int step = wave + u * kOneWaves;
+        if (step >= job.steps) break;
+        halfx8 x[1][2];                                     // (the row, for all columns of the product)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[0][h] = *reinterpret_cast<const halfx8 *>(local + step * kStepBytes + 64 * h + 16 * quarter);
+        multiply_step<TWO>(f[u], x, acc);
+    }
+    if (col == 0) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][16 * m + 4 * quarter + e] = acc[m][0][e];
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    float sum = 0.f;                                        // of half the wavefronts: lanes 0 to 15 and 32 to 47 a class, the others a rank
+#pragma unroll
+    for (int v = 0; v < kOneWaves / 2; ++v) sum += part[lane / 32 * (kOneWaves / 2) + v][lane % 32];
+    sum = ldexpf(sum + __shfl_xor(sum, 32), shift - shift_of(largest_in(largest[0])));
+    if (adapter >= 0) {
+        const float inner = sum * scale;
+        float added = 0.f;
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += 8) {
+            float v[8];
+            if constexpr (TWO) __builtin_memcpy(v, b + r0 / 4, 32);
+            else rows8::load(reinterpret_cast<const uint16_t *>(b + r0 / 8), 0, 8, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) added = fmaf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(inner), 16 + r0 + e)), v[e], added);
+        }
+        sum += added;
+    }
+    if (lane < 16 && c0 + col < job.C) job.out[c0 + col] = adapter == kUnknown ? NAN : sum;
 }
 
 // Inner products from the sums of their cuts, scaled, as three terms for Adapted.
@@ -738,6 +862,13 @@ Way way_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
 }
 Plan plan_of(const rfsf_adapters_shape &s, const Layout &z, int64_t rows) { return plan_of(s, z, rows, way_of(s, z, rows)); }
 
+// Whether one_kernel works on a row that fits into LDS: as long as every workgroup has a CU to itself (1 x 1025, 5003 classes, float32 15 us instead of 11) and every wavefront
+// has all of its steps' loads under way at once.
+bool one_launch(const rfsf_adapters_shape &s, const Layout &z, int64_t rows)
+{
+    return rows == 1 && z.ranks == 16 && s.C <= 16 * kCus && plane_steps(s.K, !s.bf16) <= kOneWaves * kOneSteps;
+}
+
 // (f: of as many rows or more)
 hipError_t launch_rows(const Plan &f, const rfsf_adapters_shape &s, const Layout &z, const char *lay, const void *X, int64_t rows, int64_t ld_x, const int64_t *adapters,
                        float *out, int64_t ld_out, char *ws, hipStream_t stream)
@@ -751,6 +882,13 @@ hipError_t launch_rows(const Plan &f, const rfsf_adapters_shape &s, const Layout
     int32_t *order = nullptr, *who = nullptr;
     bool packed = straight && rows <= kLocalRows && f.blocks == 1 && rows * s.K <= kLocal;
     const bool local = packed;
+    if (local && one_launch(s, z, rows)) {
+        const OneJob job = {lay + z.w, lay + z.a, X, lay + z.b, s.K, z.pitch, s.C, s.count, adapters, largest_w, largest_a, scale, out, z.ranks_b, (int)steps};
+        const dim3 grid((unsigned)((s.C + 15) / 16));
+        if (bf16) one_kernel<false><<<grid, 64 * kOneWaves, 0, stream>>>(job);
+        else one_kernel<true><<<grid, 64 * kOneWaves, 0, stream>>>(job);
+        return hipGetLastError();
+    }
     if (!straight) {
         order = reinterpret_cast<int32_t *>(ws + f.order);
         who = reinterpret_cast<int32_t *>(ws + f.who);

@@ -63,6 +63,8 @@ CASES = [
     (12, 13001, 40, 9, 5), (600, 40, 600, 100, 11), (20, 5121, 10, 16, 20), (48, 2049, 3, 24, 2), (7, 700, 5000, 16, 7), (1, 300, 17000, 4, 2),
     (2000, 129, 8193, 7, 30), (2000, 140, 8200, 40, 3), (2100, 129, 8000, 5, 1500), (129, 5121, 1029, 20, 12), (260, 2500, 700, 33, 90), (4, 2049, 70, 12, 9), (5, 1025, 15, 12, 9), (70, 12500, 33, 5, 9),
     (1100, 12500, 21, 5, 9),
+    (1, 1536, 4096, 16, 3), (1, 1537, 4095, 15, 3), (1, 1000, 4097, 16, 3), (1, 70, 16, 17, 2), (1, 33, 4090, 1, 2), (1, 8192, 50, 16, 2), (2, 4096, 65, 8, 3), (2, 4090, 30, 8, 3),
+    (3, 2730, 40, 8, 4), (4, 2048, 4100, 16, 4), (4, 3, 2, 2, 4), (3, 1, 20, 2, 3),
 ]
 
 
@@ -127,6 +129,29 @@ def test_infinities_and_nan_stay_where_they_belong(dtype, N, K, C):
             continue
         assert torch.equal(got[n].isnan(), bad), n
         assert torch.equal(got[n][~bad], clean[n][~bad]), n
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K,rank", [(40, 3), (1025, 16), (1500, 9), (1025, 20)])
+def test_one_request(dtype, K, rank):
+    """Without an adapter, with one that does not exist, with infinities and NaN in what belongs to it and in what does not."""
+    X, W, A, B, scale, _ = _problem(1, K, 90, rank, 4, TYPES[dtype], seed=5)
+    A[1, rank - 1, K - 1], B[2, 7, rank // 2], W[88, 0] = float("nan"), float("nan"), float("inf")
+    h = _handle(W, A, B, scale)
+    good = torch.ones(90, dtype=torch.bool)
+    good[88] = False
+    for adapter in (-1, 0, 3, 2, 1, 4, 1 << 40):
+        adapters = torch.tensor([adapter])
+        got = h.scores(X.cuda(), adapters.cuda()).cpu()
+        keep = good.clone()
+        if adapter == 2:
+            keep[7] = False
+        if adapter == 1 or adapter >= 4:
+            keep[:] = False
+        assert torch.equal(got[0].isfinite(), keep), adapter
+        if keep.any():
+            clean = torch.nan_to_num(B, nan=0.0), torch.nan_to_num(A, nan=0.0), torch.where(W.isfinite(), W, torch.zeros_like(W))
+            _check(got[:, keep], X, clean[2][keep], clean[1], clean[0][:, keep], scale, adapters, dtype == "bfloat16")
 
 
 def test_places_that_were_never_set_and_that_are_set_again():
