@@ -61,6 +61,23 @@ def test_forward(dtype, N, K):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K", [5130, 7171, 8192, 10239, 10300, 12289, 13001, 14336, 14343, 15361, 16384, 16391, 16400])
+def test_forward_of_many_long_rows(dtype, K):
+    """Some of the rows against the formula, for every number of columns that lanes hold."""
+    x, gain, offset, _ = _inputs(5, K, TYPES[dtype])
+    rows = [0, 1, 777, 2047, 2052]
+    X = torch.zeros(2053, K, dtype=TYPES[dtype], device="cuda")
+    X[rows] = x.cuda()
+    Y, mean, rstd = rfsf.rfsf_layer_norm(X, gain.cuda(), offset.cuda(), eps=1e-3, dropout=rfsf.RfsfDropout(0.3, seed=K, offset=7, first_row=3))
+    factor = np.concatenate([ref.mask(1, K, 0.3, K, 7, 3 + n) for n in rows])
+    want = ref.norm(_np(x), _np(gain), _np(offset), 1e-3, factor)
+    bounds = ref.norm_bounds(_np(x), _np(gain), _np(offset), 1e-3, factor, dtype == "bfloat16")
+    for name, g, w, t in zip(("mean", "rstd", "Y"), (mean, rstd, Y), want, bounds):
+        excess = np.abs(_np(g[rows]) - w) - t
+        assert np.all(excess <= 0), (name, float(excess.max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,K", SHAPES)
 def test_backward(dtype, N, K):
     bf16 = dtype == "bfloat16"
