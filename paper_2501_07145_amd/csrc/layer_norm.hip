@@ -70,16 +70,25 @@ __device__ __forceinline__ void load_or(const float *p, int64_t k, int64_t K, fl
 
 // Rows are added up in 64 bits, eight numbers of bfloat16 first in 32 (exact as long as they lie within 2^13 of each other), so that the mean is rounded once; what that
 // leaves over is known, and taken off the differences to it, and its square off their mean square. Rows far from zero lose nothing. (Eighths of the numbers, which have
-// no error, the smallest one's being 2^-136, and whose sum is finite.)
+// no error, the smallest one's being 2^-136, and whose sum is finite. FEW: of rows that wait for each other, as products and sums apart, 1 x 1025 with dropout 7.1 us, the
+// other way 7.5; of many rows, whose number of instructions counts, as multiply-adds, 100000 x 400 39.0, the other way 39.6.)
+template <bool FEW>
 __device__ __forceinline__ double sum_of(const rows8::Eight<uint16_t> &c)
 {
     constexpr float EIGHTH = 0.125f;
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = rows8::to_float(c.v[e]);
-    auto two = [&](int e) { return fmaf(x[e], EIGHTH, x[e + 1] * EIGHTH); };
-    return 8.0 * (double)((two(0) + two(2)) + (two(4) + two(6)));
+    for (int e = 0; e < 8; ++e) x[e] = rows8::to_float(c.v[e]) * (FEW ? EIGHTH : 1.f);
+    if (FEW) return 8.0 * (double)(((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])));
+    float even = x[0] * EIGHTH, odd = x[1] * EIGHTH;
+#pragma unroll
+    for (int e = 2; e < 8; e += 2) {
+        even = fmaf(x[e], EIGHTH, even);
+        odd = fmaf(x[e + 1], EIGHTH, odd);
+    }
+    return 8.0 * (double)(even + odd);
 }
+template <bool FEW>
 __device__ __forceinline__ double sum_of(const rows8::Eight<float> &c)
 {
     return (((double)c.v[0] + (double)c.v[1]) + ((double)c.v[2] + (double)c.v[3])) + (((double)c.v[4] + (double)c.v[5]) + ((double)c.v[6] + (double)c.v[7]));
@@ -128,7 +137,7 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             now[u] = next[u];
-            sum[0] += sum_of(now[u]);
+            sum[0] += sum_of<true>(now[u]);
         }
         if (turn + step < job.N) {
 #pragma unroll
@@ -212,7 +221,7 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
             rows8::in_turn(held[u]);
-            sum[0] += sum_of(held[u]);
+            sum[0] += sum_of<false>(held[u]);
         }
         add_up<LANES>(sum, static_cast<double (*)[1]>(nullptr));
         const Mean m = mean_of(sum[0], inverse);
