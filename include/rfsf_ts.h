@@ -390,7 +390,8 @@ int rfsf_dropout(const rfsf_dropout_mask *mask, const void *X, int32_t bf16, int
  *   dX [N, ld_dx], or NULL if not wanted; dgain, doffset [K] float32, or both NULL
  * Y may be X and dX may be X or dY (with the same row stride); no other overlap. Columns beyond K are untouched. Statistics and sums are held in 32 bits; the
  * variance is that of numbers less their mean, so that rows far from zero lose nothing. A row with an infinity or a NaN is NaN (where
- * dropout keeps it), and so is its rstd; where the variance is beyond 32 bits (numbers above 2^63 or so), rstd is 0. Equal calls give equal bits.
+ * dropout keeps it), and so is its rstd. Where the sum of the squares of a finite row's differences to its mean is beyond 32 bits (differences of 2^64 / sqrt(K) or
+ * so), rstd is 0, the row is its offset, and its dX is 0. Equal calls give equal bits.
  * rfsf_layer_norm_backward_workspace_bytes: scratch for dgain and doffset (without them it may be NULL). with_dx: whether dX is asked for.
  * Limits: N < 2^31, K <= 3500000 (RFSF_E_UNSUPPORTED). Rows of up to 20480 columns are read once. N = 0 clears dgain and doffset.
  */

@@ -47,3 +47,53 @@ def test_sums_of_large_numbers(dtype, N, K):
         gain, offset, at, Y, mean, rstd = _forward(rows, N)
         assert torch.equal(mean.cpu(), torch.tensor([2.0 ** 128 / K, -2.0 ** 128 / K])[at])
         assert not rstd.any() and torch.equal(Y.cpu(), offset.to(Y.dtype).expand(N, -1))
+
+
+SIZES = [(9, 3), (9, 65), (9, 300), (9, 1025), (9, 9001), (2100, 3), (2100, 65), (2100, 129), (2100, 1025), (2061, 5121), (2061, 16001), (5, 20485)]
+
+
+def _beyond(K, dtype):
+    """Rows whose squares' sum is beyond 32 bits (all of one sign; of both, so that differences are too; numbers whose mean is rounded by more than 2^64), and two that are not."""
+    gen = torch.Generator().manual_seed(K + 1)
+    most = float(torch.finfo(dtype).max)
+    rows = torch.randn(5, K, generator=gen, dtype=torch.float64) * torch.tensor([[0.0], [0.0], [2.0 ** 90], [2.0 ** 50], [1.0]], dtype=torch.float64)
+    rows[0] = (1 + torch.rand(K, generator=gen, dtype=torch.float64)) * 2.0 ** 125
+    rows[0, 0], rows[0, 1] = 2.0 ** 125, 1.5 * 2.0 ** 125
+    rows[1] = torch.where(torch.arange(K) % 3 == 0, most, -most)
+    rows[2, 0], rows[2, 1] = 2.0 ** 90, -2.0 ** 91
+    return rows.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K", SIZES)
+def test_squares_beyond_32_bits(dtype, N, K):
+    rows = _beyond(K, TYPES[dtype])
+    gain, offset, at, Y, mean, rstd = _forward(rows, N)
+    want = ref.norm(_np(rows), _np(gain), _np(offset), EPS, np.ones((5, K)))
+    bounds = ref.norm_bounds(_np(rows), _np(gain), _np(offset), EPS, np.ones((5, K)), dtype == "bfloat16")
+    assert np.all(np.abs(_np(mean) - want[0][at]) <= bounds[0][at])
+    beyond = at < 3
+    assert torch.equal(rstd.cpu() == 0, beyond)
+    assert torch.equal(Y[beyond.cuda()].cpu(), offset.to(Y.dtype).expand(int(beyond.sum()), -1))
+    for n in range(3, min(N, 10)):
+        for g, w, t in ((rstd, want[1], bounds[1]), (Y, want[2], bounds[2])):
+            if not beyond[n]:
+                assert np.all(np.abs(_np(g[n]) - w[at[n]]) <= t[at[n]]), n
+    for n in range(5, N, 5 * max(1, N // 50)):
+        assert torch.equal(Y[n:n + 5][:min(5, N - n)], Y[:min(5, N - n)])          # (equal rows, equal results)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("need_dX", [True, False])
+@pytest.mark.parametrize("N,K", [(9, 3), (9, 65), (40, 1025), (300, 129), (333, 5121), (2100, 65), (30, 9001), (5, 20485)])
+def test_gradients_of_rows_whose_squares_are_beyond_32_bits(dtype, need_dX, N, K):
+    rows = _beyond(K, TYPES[dtype])
+    gain, offset, at, Y, mean, rstd = _forward(rows, N)
+    gen = torch.Generator().manual_seed(K + 2)
+    X, dY = rows[at], torch.randn(N, K, generator=gen).to(TYPES[dtype])
+    got = rfsf.rfsf_layer_norm_backward(X.cuda(), mean, rstd, dY.cuda(), gain=gain.cuda(), need_dX=need_dX)
+    args = (_np(X), _np(mean), _np(rstd), _np(gain), _np(dY), np.ones((N, K)))
+    for g, w, t in zip(got, ref.back(*args), ref.back_bounds(*args, dtype == "bfloat16")):
+        assert g is None or np.all(np.abs(_np(g) - w) <= t)
+    if need_dX:
+        assert not got[0][(at < 3).cuda()].any()
