@@ -94,10 +94,12 @@ __device__ __forceinline__ double sum_of(const rows8::Eight<float> &c)
     return (((double)c.v[0] + (double)c.v[1]) + ((double)c.v[2] + (double)c.v[3])) + (((double)c.v[4] + (double)c.v[5]) + ((double)c.v[6] + (double)c.v[7]));
 }
 struct Mean { float mean, rest; };
-__device__ __forceinline__ Mean mean_of(double sum, double inverse)
+// (The quotient is corrected by what it leaves over, so that it is rounded once: the mean of a row of one number is this number, and nothing is left over, which a large
+// number's 2^-53 times rstd would make visible.)
+__device__ __forceinline__ Mean mean_of(double sum, double inverse, double K)
 {
-    const double mean = sum * inverse;
-    const float rounded = (float)mean;
+    const double about = sum * inverse, mean = fma(fma(-K, about, sum), inverse, about);
+    const float rounded = (float)about;
     return {rounded, (float)(mean - (double)rounded)};
 }
 // 0 where the squares' sum is infinite, which it is of finite rows alone (whose rest may have an infinite square too): rows with an infinity or a NaN have NaN among their squares.
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void norm_kernel(Nor
             for (int u = 0; u < HELD; ++u) next[u] = rows8::load_raw(X + std::min(row + step, job.N - 1) * job.ldx, 8 * (lane + u * THREADS), K);
         }
         add_up<THREADS>(sum, part_sum);
-        const Mean m = mean_of(sum[0], inverse);
+        const Mean m = mean_of(sum[0], inverse, (double)K);
         float squares[1] = {0.f};
 #pragma unroll
         for (int u = 0; u < HELD; ++u) {
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(wave_threads(HELD * sizeof(T))) void norm_wave_kern
             sum[0] += sum_of<false>(held[u]);
         }
         add_up<LANES>(sum, static_cast<double (*)[1]>(nullptr));
-        const Mean m = mean_of(sum[0], inverse);
+        const Mean m = mean_of(sum[0], inverse, (double)K);
         const float d_last = last < K ? x_last - m.mean : 0.f;
         float squares[1] = {d_last * d_last};
 #pragma unroll
@@ -304,7 +306,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob job, bo
         sum[0] += s;
     }
     add_up<kLongThreads>(sum, part_sum);
-    const Mean m = mean_of(sum[0], inverse);
+    const Mean m = mean_of(sum[0], inverse, (double)K);
     float squares[1] = {0.f};
     for (int64_t k = 8 * (int64_t)threadIdx.x; k < K; k += 8 * kLongThreads) {
         rows8::load(x_row, k, K, x);

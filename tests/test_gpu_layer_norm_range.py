@@ -97,3 +97,13 @@ def test_gradients_of_rows_whose_squares_are_beyond_32_bits(dtype, need_dX, N, K
         assert g is None or np.all(np.abs(_np(g) - w) <= t)
     if need_dX:
         assert not got[0][(at < 3).cuda()].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K", SIZES + [(9, 1), (2100, 1), (2100, 11), (2100, 333)])
+def test_rows_of_one_number(dtype, N, K):
+    """Whatever the number of columns: what the mean's rounding leaves over is nothing."""
+    values = [1.1, -3e4, 123.25, 1e10, -1.3e20, 3.0 * 2.0 ** 100, -1.1e38, float(torch.finfo(TYPES[dtype]).max)]
+    rows = torch.tensor(values, dtype=torch.float64)[:, None].expand(-1, K).to(TYPES[dtype])
+    gain, offset, at, *out = _forward(rows, N)
+    _no_variance(rows, offset, at, *out)
