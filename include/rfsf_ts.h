@@ -386,10 +386,12 @@ int rfsf_dropout(const rfsf_dropout_mask *mask, const void *X, int32_t bf16, int
  *   gain, offset [K] float32, or NULL: 1, 0
  *   eps finite and above zero, also in 32 bits (RFSF_E_BAD_SETTING)
  *   mask: NULL for no dropout. The backward pass needs the settings of the forward pass, and what offset_on_device holds has to be the same.
- *   mean, rstd [N] float32: written by the forward pass (either may be NULL there), read by the backward pass
+ *   mean, rstd [N] float32: written by the forward pass (either may be NULL there), read by the backward pass, whose z is (X[n] - mean[n]) rstd[n] for the
+ *     numbers that it is given. The forward pass itself works with the mean before it is rounded to 32 bits, so that z of the backward pass is off
+ *     from the forward pass's by up to 2^-24 |mean| rstd: of rows 3e4 deviations from zero by 0.002, and dX and dgain accordingly.
  *   dX [N, ld_dx], or NULL if not wanted; dgain, doffset [K] float32, or both NULL
- * Y may be X and dX may be X or dY (with the same row stride); no other overlap. Columns beyond K are untouched. Statistics and sums are held in 32 bits; the
- * variance is that of numbers less their mean, so that rows far from zero lose nothing. A row with an infinity or a NaN is NaN (where
+ * Y may be X and dX may be X or dY (with the same row stride); no other overlap. Columns beyond K are untouched. The sum of a row is formed in 64 bits (eight bfloat16
+ * numbers of it in 32), its squares' and the gradients' sums in 32. The variance is that of numbers less their mean, so that in the forward pass rows far from zero lose nothing. A row with an infinity or a NaN is NaN (where
  * dropout keeps it), and so is its rstd. Where the sum of the squares of a finite row's differences to its mean is beyond 32 bits (differences of 2^64 / sqrt(K) or
  * so), rstd is 0, the row is its offset, and its dX is 0. Equal calls give equal bits.
  * rfsf_layer_norm_backward_workspace_bytes: scratch for dgain and doffset (without them it may be NULL). with_dx: whether dX is asked for.

@@ -363,7 +363,8 @@ def rfsf_layer_norm_backward(X: torch.Tensor, mean: torch.Tensor, rstd: torch.Te
                              dX: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None, doffset: Optional[torch.Tensor] = None,
                              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """(dX or None, dgain [K] or None, doffset [K] or None): gradients of rfsf_layer_norm with these X, gain and dropout, mean and rstd being what it
-    returned, from the gradient dY of its result. Buffers that are not given are allocated; dX may be X or dY."""
+    returned, from the gradient dY of its result. Buffers that are not given are allocated; dX may be X or dY. (X - mean) rstd is formed from the
+    rounded mean: off by up to 2^-24 |mean| rstd, which only rows far from zero show."""
     ldx = _matrix(X, "X")
     N, K = X.shape
     ldy, ldd = _matrix(dY, "dY", X.dtype, (N, K)), K
